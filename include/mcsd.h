@@ -337,6 +337,117 @@ int mcsd_commit_kv(void* const* k_cache_layers, void* const* v_cache_layers,
                    int n_levels, int B, int H, int N, int D, int L_max, int dtype, void* stream);
 
 /*
+ * Rows for tree attention from a target layer's projections (the input side of Section 2.2; the paper's targets rotate
+ * queries and keys by position, newer ones also normalise every head first).  For every sequence b, token n and head:
+ *     y = x * rsqrt(mean(x^2) + eps) * weight      queries and keys, where a weight is given; values are copied
+ *     angle_i = (seq_lens[b] + depth[n]) * freqs[i],  i = 0 .. rot_dim / 2 - 1, in 64 bits
+ *     (y_a, y_c) -> (y_a cos - y_c sin, y_c cos + y_a sin)   queries and keys; (a, c) = (i, i + rot_dim / 2), or
+ *                                                             (2i, 2i + 1) when `interleaved` is not 0
+ * in fp32, rounded once to dtype, and stored head-major as mcsd_tree_attention takes it.  Elements from rot_dim on are
+ * normalised but not rotated.
+ *
+ *   q_in, k_in, v_in   [dev] dtype, element [b][n][h][d] at b * batch stride + n * token stride + h * D + d: parts of one
+ *                      fused projection, or tensors of their own.  Must not overlap the outputs.
+ *   strides            [host] int64[6]: batch and token stride of q_in, of k_in, of v_in, in elements
+ *   q_weight, k_weight [dev] dtype[D] or NULL = no norm for that side;  eps >= 0
+ *   freqs              [dev] double[rot_dim / 2], radians per position (NULL allowed when rot_dim is 0)
+ *   rot_dim            even, 0 .. D; a multiple of 16 unless interleaved
+ *   seq_lens           [dev] int32[B], position of the first token
+ *   depth              [dev] int32[N] from mcsd_build_mask, or NULL: token n lies n positions on (a prompt, a chain)
+ *   n_active           [dev] int32[B] or NULL = N; rows n >= n_active[b] are neither read nor written
+ *   q_out              [dev] dtype[B][H_q][N][D];  k_out, v_out  [dev] dtype[B][H_kv][N][D]
+ *   D                  64 or 128; N any (B * N < 2^31); dtype MCSD_BF16 or MCSD_F32
+ *
+ * One launch on `stream`, no workspace.  16-byte loads and stores when all pointers and strides allow them.
+ * Errors: MCSD_ERR_NULL, MCSD_ERR_BAD_SHAPE, MCSD_ERR_BAD_DTYPE, MCSD_ERR_CUDA.
+ */
+int mcsd_qk_norm_rope(const void* q_in, const void* k_in, const void* v_in, const int64_t* strides, const void* q_weight,
+                      const void* k_weight, float eps, const double* freqs, int rot_dim, int interleaved,
+                      const int32_t* seq_lens, const int32_t* depth, const int32_t* n_active, void* q_out, void* k_out,
+                      void* v_out, int B, int H_q, int H_kv, int N, int D, int dtype, void* stream);
+
+/*
+ * Prefix cache in 4 bits (the paper keeps its caches in 16; this is for targets whose cache is the larger part of what a
+ * verification step reads).  A cache is [B][H_kv][L_max / 32] pages of MCSD_KV4_PAGE_BYTES(D) bytes, L_max a multiple
+ * of 32, 16-byte aligned; a page holds 32 consecutive rows of keys and values of one head:
+ *
+ *   offset 0      key codes    [D / 32][32 rows][16 bytes], channels 32c .. 32c + 31 of a row in its chunk c
+ *   offset 16 D   value codes  [D][16 bytes], the 32 rows of one channel
+ *   offset 32 D   bf16 key scale[32], key offset[32], value scale[32], value offset[32]
+ *
+ * Value 8w + 2i + h of a chunk (w, i < 4, h < 2) is the nibble at bits 4i + 16h of its 32-bit word w.  Code c of a row
+ * stands for scale * (16 + c) + offset.  A row x is stored with lo, hi = min x, max x, scale = bf16((hi - lo) / 15),
+ * offset = bf16(lo - 16 scale), code = clamp(round_half_even((x - offset) / scale) - 16, 0, 15), or 0 where the scale is 0:
+ * every value comes back within half a step of (hi - lo) / 15 plus the rounding of scale and offset (1/256 of 31 scale + |lo|).
+ * Rows must be finite with a finite range: a row with an infinity comes back as NaN, a NaN as the row's lowest level.
+ */
+#define MCSD_KV4_PAGE_ROWS 32
+#define MCSD_KV4_PAGE_BYTES(D) (32 * (D) + 256)
+
+/* Bytes of a cache; 0 for a shape that is not supported (D 64 or 128, B * H_kv <= 65535, L_max a positive multiple of 32). */
+size_t mcsd_kv4_cache_bytes(int B, int H_kv, int D, int L_max);
+
+/*
+ * Appends rows to a 4-bit cache (a prompt or a part of one): row t < n_new[b] of k and v becomes cache row start[b] + t.
+ * Rows beyond L_max are dropped, sequences with start[b] < 0 are left alone, and so are all other rows of the cache.
+ *
+ *   k, v     [dev] dtype[B][H_kv][T][D], as mcsd_qk_norm_rope writes them
+ *   cache    [dev] in/out;   start  [dev] int32[B];   n_new  [dev] int32[B] or NULL = T
+ *
+ * One launch on `stream`.  Errors: MCSD_ERR_NULL, MCSD_ERR_BAD_SHAPE, MCSD_ERR_BAD_DTYPE, MCSD_ERR_CUDA.
+ */
+int mcsd_append_kv4(const void* k, const void* v, void* cache, const int32_t* start, const int32_t* n_new, int B, int H_kv,
+                    int T, int D, int L_max, int dtype, void* stream);
+
+/*
+ * Rows of 4-bit caches as dense tensors: k[layer][b][h][t] and v[..] = cache row first[b] + t for t < n_rows[b]; zeros for
+ * t >= n_rows[b] and for rows outside the cache.
+ *
+ *   cache_layers  [dev] array of n_layers device pointers;   first  [dev] int32[B];   n_rows  [dev] int32[B] or NULL = T
+ *   k, v          [dev] dtype[n_layers][B][H_kv][T][D] out
+ *
+ * One launch on `stream`.  Errors: as mcsd_append_kv4.
+ */
+int mcsd_read_kv4(const void* const* cache_layers, int n_layers, const int32_t* first, const int32_t* n_rows, int B, int H_kv,
+                  int T, int D, int L_max, int dtype, void* k, void* v, void* stream);
+
+/*
+ * mcsd_commit_kv for 4-bit caches (Fig. 1 step 6): the keys/values of the winning root and of the accepted nodes are
+ * stored as cache rows seq_lens[b], seq_lens[b] + 1, ... of every layer, then seq_lens[b] grows by 1 + accept_len[b].
+ * Rows that would fall beyond L_max are dropped and the length saturates at L_max.
+ *
+ *   cache_layers                    [dev] array of n_layers device pointers to caches (in/out), each 16-byte aligned
+ *   k_tree_layers, v_tree_layers    [dev] arrays of n_layers device pointers, each dtype[B][H_kv][N][D]
+ *   all other arguments             as for mcsd_commit_kv
+ *
+ * Two launches on `stream` for all layers together; no workspace.  Errors: as mcsd_commit_kv.
+ */
+int mcsd_commit_kv4(void* const* cache_layers, const void* const* k_tree_layers, const void* const* v_tree_layers, int n_layers,
+                    int32_t* seq_lens, const int32_t* accept_len, const int32_t* out_nodes, const int32_t* best_root,
+                    int n_levels, int B, int H_kv, int N, int D, int L_max, int dtype, void* stream);
+
+/*
+ * mcsd_tree_attention_gqa with the prefix in a 4-bit cache (Section 2.2): prefix keys and values are what the cache's codes
+ * stand for, the tree's own are rows of dtype as before.  N = 1 is the decoding step of a single token.
+ *
+ *   q, out           [dev] dtype[B][H_q][N][D];   k_tree, v_tree  [dev] dtype[B][H_kv][N][D]
+ *   cache            [dev] 4-bit cache, 16-byte aligned; rows from seq_lens[b] on may hold anything
+ *   seq_lens, n_active, anc, words, softmax_scale   as for mcsd_tree_attention; rows n >= n_active[b] of `out` are not
+ *                    written, those of q, k_tree and v_tree not used.  Active rows of v_tree must be finite.
+ *   workspace        [dev] >= mcsd_tree_attention_kv4_workspace_bytes(...) bytes, 256-byte aligned, zero-filled once; calls
+ *                    that may overlap on the device need distinct workspaces
+ *
+ * Errors and limits: as mcsd_tree_attention_gqa, plus MCSD_ERR_BAD_SHAPE when L_max is not a positive multiple of 32 or the
+ * cache is not 16-byte aligned.  mcsd_tree_attention_path() tells which kernel runs here as well.
+ */
+size_t mcsd_tree_attention_kv4_workspace_bytes(int B, int H_q, int H_kv, int N, int D, int L_max, int dtype);
+
+int mcsd_tree_attention_kv4(const void* q, const void* cache, const void* k_tree, const void* v_tree, void* out,
+                            const int32_t* seq_lens, const int32_t* n_active, const uint64_t* anc, int words, int B, int H_q,
+                            int H_kv, int N, int D, int L_max, float softmax_scale, int dtype, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
  * mcsd_verify_tree with the vocabulary split over several GPUs (Fig. 1 steps 4-6, the procedure of
  * mcsd_verify_tree): rank r holds columns [v0, v0 + Vs) of p and q, the way a tensor-parallel output layer leaves
  * them, so no rank ever gathers a full row.  The four calls below are the per-rank kernels; between them the

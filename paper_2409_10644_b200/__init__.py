@@ -10,6 +10,8 @@ _BINDING_NAMES = (
     "mcsd_verify_tree", "mcsd_verify_tree_logits", "mcsd_sample_roots", "mcsd_verify_tree_static", "mcsd_commit_kv", "layer_pointer_table", "mcsd_verify_tree_workspace_bytes", "mcsd_workspace_status", "verify_node_states", "mcsd_tree_attention_path", "mcsd_tree_attention_plan", "mcsd_selftest_bounded_wait",
     "mcsd_status_string", "mcsd_launch_count", "n_active_from_gamma", "shard_batch", "new_workspace",
     "VocabShard", "mcsd_verify_shard_workspace_bytes",
+    "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "new_kv4_cache", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
+    "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
 )
 
 

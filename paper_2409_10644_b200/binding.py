@@ -27,6 +27,8 @@ _EXPORTS = (
     "mcsd_tree_attention", "mcsd_tree_attention_gqa", "mcsd_workspace_status", "verify_node_states", "mcsd_tree_attention_path", "mcsd_tree_attention_plan", "mcsd_selftest_bounded_wait", "mcsd_verify_tree_workspace_bytes", "mcsd_verify_tree", "mcsd_verify_tree_logits", "mcsd_verify_tree_static", "mcsd_commit_kv", "mcsd_sample_roots",
     "mcsd_sample_roots_logits", "mcsd_verify_shard_workspace_bytes", "mcsd_verify_shard_gather", "mcsd_verify_shard_round",
     "mcsd_verify_shard_select", "mcsd_verify_shard_pick",
+    "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
+    "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
 )
 
 
@@ -92,6 +94,20 @@ def _load() -> ctypes.CDLL:
     lib.mcsd_verify_shard_pick.restype = c_int
     lib.mcsd_verify_shard_pick.argtypes = ([c_void_p] * 3 + [c_int] * 8 + [c_void_p] * 2 +
                                            [c_void_p, c_size_t, c_void_p])
+    lib.mcsd_qk_norm_rope.restype = c_int
+    lib.mcsd_qk_norm_rope.argtypes = ([c_void_p] * 6 + [c_float, c_void_p, c_int, c_int] + [c_void_p] * 6 + [c_int] * 6 + [c_void_p])
+    lib.mcsd_kv4_cache_bytes.restype = c_size_t
+    lib.mcsd_kv4_cache_bytes.argtypes = [c_int] * 4
+    lib.mcsd_append_kv4.restype = c_int
+    lib.mcsd_append_kv4.argtypes = [c_void_p] * 5 + [c_int] * 6 + [c_void_p]
+    lib.mcsd_read_kv4.restype = c_int
+    lib.mcsd_read_kv4.argtypes = [c_void_p, c_int, c_void_p, c_void_p] + [c_int] * 6 + [c_void_p] * 3
+    lib.mcsd_commit_kv4.restype = c_int
+    lib.mcsd_commit_kv4.argtypes = [c_void_p] * 3 + [c_int] + [c_void_p] * 4 + [c_int] * 7 + [c_void_p]
+    lib.mcsd_tree_attention_kv4_workspace_bytes.restype = c_size_t
+    lib.mcsd_tree_attention_kv4_workspace_bytes.argtypes = [c_int] * 7
+    lib.mcsd_tree_attention_kv4.restype = c_int
+    lib.mcsd_tree_attention_kv4.argtypes = [c_void_p] * 8 + [c_int] * 7 + [c_float, c_int, c_void_p, c_size_t, c_void_p]
     return lib
 
 
@@ -470,6 +486,168 @@ def mcsd_commit_kv(k_cache_ptrs, v_cache_ptrs, k_tree_ptrs, v_tree_ptrs, seq_len
                                 _ptr(verify_out["best_root"]), mask.n_levels, B, H, mask.n_nodes, D, L_max, code,
                                 _stream())
     _check(st, "mcsd_commit_kv")
+
+
+# ---------------------------------------------------------------- rows and the 4-bit prefix cache
+
+KV4_PAGE_ROWS = 32
+
+
+def _on_device(dev: torch.device, fn, *args) -> int:
+    """fn(*args, stream) on the tensors' device and torch's current stream there."""
+    if torch.cuda.current_device() == dev.index:
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(dev):
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
+
+
+def _same(t: torch.Tensor, dtype, shape, dev, name: str) -> int:
+    """Address of a contiguous CUDA tensor of this dtype, shape and device."""
+    if t.dtype != dtype or t.device != dev or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of dtype %s on %s" % (name, dtype, dev))
+    if t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    return t.data_ptr()
+
+
+def _maybe(t: Optional[torch.Tensor], dtype, shape, dev, name: str):
+    return None if t is None else _same(t, dtype, shape, dev, name)
+
+
+def _projection(t: torch.Tensor, dtype, dev, name: str):
+    """Address and (batch, token) strides of projection rows [B][N][H][D] whose heads lie next to each other."""
+    if t.dim() != 4 or t.dtype != dtype or t.device != dev or not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor [B][N][H][D] of dtype %s on %s" % (name, dtype, dev))
+    B, N, H, D = t.shape
+    if (t.stride(3) != 1 and D > 1) or (t.stride(2) != D and H > 1):
+        raise ValueError("the heads of %s must lie next to each other (strides %s)" % (name, t.stride()))
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def mcsd_qk_norm_rope(q_in, k_in, v_in, seq_lens, freqs, depth=None, n_active=None, q_weight=None, k_weight=None,
+                      eps: float = 1e-6, interleaved: bool = False, out=None):
+    """Norm of every query and key head, rotation by position, head-major rows (see mcsd.h): returns (q, k, v).
+
+    ``q_in`` [B][N][H_q][D], ``k_in`` and ``v_in`` [B][N][H_kv][D] may be views of one fused projection (any batch and
+    token stride).  ``freqs``: float64 [rot_dim / 2], radians per position, or None for no rotation.  ``depth``: the
+    mask's depths (tree rows) or None (consecutive positions).  ``out``: (q, k, v) to write into."""
+    dt, dev = q_in.dtype, q_in.device
+    code = _dtype_code(q_in)
+    B, N, H, D = q_in.shape
+    H_kv = k_in.shape[2]
+    if k_in.shape != (B, N, H_kv, D) or v_in.shape != (B, N, H_kv, D):
+        raise ValueError("k_in %s and v_in %s do not fit q_in %s" % (tuple(k_in.shape), tuple(v_in.shape), tuple(q_in.shape)))
+    qp, qb, qt = _projection(q_in, dt, dev, "q_in")
+    kp, kb, kt = _projection(k_in, dt, dev, "k_in")
+    vp, vb, vt = _projection(v_in, dt, dev, "v_in")
+    if out is None:
+        out = (torch.empty((B, H, N, D), dtype=dt, device=dev), torch.empty((B, H_kv, N, D), dtype=dt, device=dev),
+               torch.empty((B, H_kv, N, D), dtype=dt, device=dev))
+    q, k, v = out
+    half = 0 if freqs is None else freqs.numel()
+    st = _on_device(dev, lib.mcsd_qk_norm_rope, qp, kp, vp, (ctypes.c_int64 * 6)(qb, qt, kb, kt, vb, vt),
+                    _maybe(q_weight, dt, (D,), dev, "q_weight"), _maybe(k_weight, dt, (D,), dev, "k_weight"), eps,
+                    _maybe(freqs, torch.float64, (half,), dev, "freqs"), 2 * half, int(interleaved),
+                    _same(seq_lens, torch.int32, (B,), dev, "seq_lens"), _maybe(depth, torch.int32, (N,), dev, "depth"),
+                    _maybe(n_active, torch.int32, (B,), dev, "n_active"), _same(q, dt, (B, H, N, D), dev, "out[0]"),
+                    _same(k, dt, (B, H_kv, N, D), dev, "out[1]"), _same(v, dt, (B, H_kv, N, D), dev, "out[2]"), B, H, H_kv, N, D, code)
+    _check(st, "mcsd_qk_norm_rope")
+    return q, k, v
+
+
+def mcsd_kv4_cache_bytes(B, H_kv, D, L_max) -> int:
+    return int(lib.mcsd_kv4_cache_bytes(B, H_kv, D, L_max))
+
+
+def new_kv4_cache(B: int, H_kv: int, L_max: int, D: int, device) -> torch.Tensor:
+    """A zero-filled 4-bit cache uint8 [B][H_kv][pages][page bytes] for at least L_max rows (whole pages of 32)."""
+    pages = -(-int(L_max) // KV4_PAGE_ROWS)
+    if mcsd_kv4_cache_bytes(B, H_kv, D, pages * KV4_PAGE_ROWS) == 0:
+        raise ValueError("no 4-bit cache for B=%d, H_kv=%d, L_max=%d, D=%d" % (B, H_kv, L_max, D))
+    return torch.zeros((B, H_kv, pages, 32 * D + 256), dtype=torch.uint8, device=device)
+
+
+def _kv4_cache(cache: torch.Tensor, B: int, H_kv: int, D: int, dev):
+    """Address and L_max of a 4-bit cache tensor."""
+    pages = cache.shape[2] if cache.dim() == 4 else 0
+    return _same(cache, torch.uint8, (B, H_kv, pages, 32 * D + 256), dev, "cache"), pages * KV4_PAGE_ROWS
+
+
+def mcsd_append_kv4(k, v, cache, start, n_new=None) -> None:
+    """Rows k, v [B][H_kv][T][D] into rows start[b].. of a 4-bit cache (see mcsd.h)."""
+    dt, dev = k.dtype, k.device
+    code = _dtype_code(k)
+    B, H_kv, T, D = k.shape
+    ptr, L_max = _kv4_cache(cache, B, H_kv, D, dev)
+    st = _on_device(dev, lib.mcsd_append_kv4, _same(k, dt, (B, H_kv, T, D), dev, "k"), _same(v, dt, (B, H_kv, T, D), dev, "v"), ptr,
+                    _same(start, torch.int32, (B,), dev, "start"), _maybe(n_new, torch.int32, (B,), dev, "n_new"), B, H_kv, T, D,
+                    L_max, code)
+    _check(st, "mcsd_append_kv4")
+
+
+def mcsd_read_kv4(cache_ptrs, first, rows: int, n_rows, B: int, H_kv: int, D: int, L_max: int, dtype: torch.dtype, out=None):
+    """Rows first[b] .. first[b] + rows - 1 of 4-bit caches as dense (k, v) [n_layers][B][H_kv][rows][D] (see mcsd.h).
+
+    ``cache_ptrs``: layer_pointer_table() of the layers' caches; ``n_rows`` int32 [B] or None: rows past it are zeros."""
+    dev, n_layers = cache_ptrs.device, cache_ptrs.numel()
+    shape = (n_layers, B, H_kv, rows, D)
+    if out is None:
+        out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+    code = _dtype_code(out[0])
+    st = _on_device(dev, lib.mcsd_read_kv4, _same(cache_ptrs, torch.int64, (n_layers,), dev, "cache_ptrs"), n_layers,
+                    _same(first, torch.int32, (B,), dev, "first"), _maybe(n_rows, torch.int32, (B,), dev, "n_rows"), B, H_kv, rows, D,
+                    L_max, code, _same(out[0], dtype, shape, dev, "out[0]"), _same(out[1], dtype, shape, dev, "out[1]"))
+    _check(st, "mcsd_read_kv4")
+    return out
+
+
+def mcsd_commit_kv4(cache_ptrs, k_tree_ptrs, v_tree_ptrs, seq_lens, verify_out, mask: TreeMask, B: int, H_kv: int, D: int,
+                    L_max: int, dtype: torch.dtype) -> None:
+    """Append the accepted tokens' K/V to every layer's 4-bit cache and grow seq_lens (see mcsd.h; pointer tables and
+    ``verify_out`` as for mcsd_commit_kv)."""
+    dev, n_layers = seq_lens.device, cache_ptrs.numel()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("tree rows are bf16 or fp32")
+    ptrs = [_same(t, torch.int64, (n_layers,), dev, name)
+            for t, name in ((cache_ptrs, "cache_ptrs"), (k_tree_ptrs, "k_tree_ptrs"), (v_tree_ptrs, "v_tree_ptrs"))]
+    st = _on_device(dev, lib.mcsd_commit_kv4, *ptrs, n_layers, _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
+                    _same(verify_out["accept_len"], torch.int32, (B,), dev, "accept_len"),
+                    _same(verify_out["out_nodes"], torch.int32, (B, mask.n_levels), dev, "out_nodes"),
+                    _same(verify_out["best_root"], torch.int32, (B,), dev, "best_root"), mask.n_levels, B, H_kv, mask.n_nodes, D,
+                    L_max, MCSD_BF16 if dtype == torch.bfloat16 else MCSD_F32)
+    _check(st, "mcsd_commit_kv4")
+
+
+def mcsd_tree_attention_kv4_workspace_bytes(B, H_q, H_kv, N, D, L_max, dtype_code) -> int:
+    return int(lib.mcsd_tree_attention_kv4_workspace_bytes(B, H_q, H_kv, N, D, L_max, dtype_code))
+
+
+def mcsd_tree_attention_kv4(q, cache, k_tree, v_tree, seq_lens, n_active, mask: TreeMask, out: Optional[torch.Tensor] = None,
+                            softmax_scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """mcsd_tree_attention with the prefix in a 4-bit cache (see mcsd.h; ``cache`` from new_kv4_cache)."""
+    dt, dev = q.dtype, q.device
+    code = _dtype_code(q)
+    B, H, N, D = q.shape
+    H_kv = k_tree.shape[1]
+    if H_kv < 1 or H % H_kv:
+        raise ValueError("q has %d heads, the key/value tensors %d" % (H, H_kv))
+    if mask.n_nodes != N:
+        raise ValueError("mask was built for %d nodes, q has %d" % (mask.n_nodes, N))
+    ptr, L_max = _kv4_cache(cache, B, H_kv, D, dev)
+    if out is None:
+        out = torch.empty_like(q)
+    if softmax_scale is None:
+        softmax_scale = D ** -0.5
+    if workspace is None:
+        workspace = new_workspace(mcsd_tree_attention_kv4_workspace_bytes(B, H, H_kv, N, D, L_max, code), dev)
+    st = _on_device(dev, lib.mcsd_tree_attention_kv4, _same(q, dt, (B, H, N, D), dev, "q"), ptr,
+                    _same(k_tree, dt, (B, H_kv, N, D), dev, "k_tree"), _same(v_tree, dt, (B, H_kv, N, D), dev, "v_tree"),
+                    _same(out, dt, (B, H, N, D), dev, "out"), _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
+                    _maybe(n_active, torch.int32, (B,), dev, "n_active"), _same(mask.anc, torch.int64, (N, mask.words), dev, "mask.anc"),
+                    mask.words, B, H, H_kv, N, D, L_max, softmax_scale, code,
+                    _same(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel())
+    _check(st, "mcsd_tree_attention_kv4")
+    return out
 
 
 def mcsd_verify_shard_workspace_bytes(B, N) -> int:

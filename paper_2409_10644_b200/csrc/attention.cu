@@ -1,6 +1,7 @@
 // C ABI entry point of tree attention (Section 2.2 of the paper): argument checks, workspace carving and
 // the choice between the tcgen05 tensor-core kernel (bf16, head_dim 128) and the CUDA-core kernel.
 #include "attention.cuh"
+#include "kv4.cuh"
 
 namespace mcsd {
 
@@ -30,6 +31,9 @@ extern "C" size_t mcsd_tree_attention_workspace_bytes(int B, int H, int N, int D
     }
     return sizeof(mcsd::WorkspaceHeader) + mcsd::align_up(scratch, 256);
 }
+
+// The 4-bit cache comes in pages of 32 rows.
+static bool whole_pages(int L_max) { return L_max >= mcsd::kPageRows && L_max % mcsd::kPageRows == 0; }
 
 static int run_attention(const void* q, const void* k_cache, const void* v_cache, const void* k_tree, const void* v_tree,
                          void* out, const int32_t* seq_lens, const int32_t* n_active, const uint64_t* anc, int words,
@@ -102,4 +106,29 @@ extern "C" int mcsd_tree_attention_gqa(const void* q, const void* k_cache, const
     if (H_kv < 1 || H_q < H_kv || H_q % H_kv != 0) return MCSD_ERR_BAD_SHAPE;
     return run_attention(q, k_cache, v_cache, k_tree, v_tree, out, seq_lens, n_active, anc, words, B, H_q, H_q / H_kv, N,
                          D, L_max, softmax_scale, dtype, workspace, workspace_bytes, stream);
+}
+
+extern "C" size_t mcsd_tree_attention_kv4_workspace_bytes(int B, int H_q, int H_kv, int N, int D, int L_max, int dtype) {
+    if (check_shape(B, H_q, N, D, L_max, dtype) != MCSD_OK || !whole_pages(L_max)) return 0;
+    if (H_kv < 1 || H_q < H_kv || H_q % H_kv != 0) return 0;
+    const size_t scratch = mcsd::simt_workspace_bytes(B, H_q, N, D, L_max);
+    return sizeof(mcsd::WorkspaceHeader) + mcsd::align_up(scratch, 256);
+}
+
+extern "C" int mcsd_tree_attention_kv4(const void* q, const void* cache, const void* k_tree, const void* v_tree, void* out,
+                                       const int32_t* seq_lens, const int32_t* n_active, const uint64_t* anc, int words, int B,
+                                       int H_q, int H_kv, int N, int D, int L_max, float softmax_scale, int dtype,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !cache || !k_tree || !v_tree || !out || !seq_lens || !anc || !workspace) return MCSD_ERR_NULL;
+    const int st = check_shape(B, H_q, N, D, L_max, dtype);
+    if (st != MCSD_OK) return st;
+    if (H_kv < 1 || H_q < H_kv || H_q % H_kv != 0 || !whole_pages(L_max)) return MCSD_ERR_BAD_SHAPE;
+    if (words < (N + 63) / 64 || words > MCSD_MAX_WORDS) return MCSD_ERR_BAD_SHAPE;
+    if (workspace_bytes < mcsd_tree_attention_kv4_workspace_bytes(B, H_q, H_kv, N, D, L_max, dtype)) return MCSD_ERR_WORKSPACE_TOO_SMALL;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || !mcsd::aligned16(cache)) return MCSD_ERR_BAD_SHAPE;
+
+    mcsd::AttentionArgs a{q, nullptr, nullptr, k_tree, v_tree, out, seq_lens, n_active, anc, words,
+                          B, H_q, N, D, L_max, softmax_scale, dtype, H_q / H_kv, cache};
+    void* scratch = static_cast<char*>(workspace) + sizeof(mcsd::WorkspaceHeader);
+    return mcsd::tree_attention_simt(a, scratch, static_cast<cudaStream_t>(stream));
 }

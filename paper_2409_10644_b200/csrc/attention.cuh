@@ -20,6 +20,7 @@ struct AttentionArgs {
     float scale;
     int dtype;
     int G;                   // query heads per key/value head (1: multi-head attention); key/value tensors have H / G heads
+    const void* kv4 = nullptr;   // the prefix cache as 4-bit pages (kv4.cuh) instead of k_cache and v_cache
 };
 
 // CUDA-core path (fp32, or bf16 shapes the tensor-core kernel does not take)

@@ -8,6 +8,7 @@
 #include <cuda_bf16.h>
 
 #include "attention.cuh"
+#include "kv4.cuh"
 
 namespace mcsd {
 
@@ -46,14 +47,43 @@ template <> struct Vec16<__nv_bfloat16> {
     }
 };
 
-// grid: (splits, query blocks, B * H)
-template <typename T, int D>
+// Rows j0 .. j0 + 31 of a 4-bit prefix cache (one page: tiles start at multiples of 32), those below `rows`, as fp32.
+template <int D>
+__device__ __forceinline__ void load_kv4_tile(const unsigned char* __restrict__ page, int rows, float (*s_k)[D + 1], float (*s_v)[D], int tid) {
+    static_assert(kSimtTile == kPageRows, "a tile is a page");
+    const __nv_bfloat16* sc = reinterpret_cast<const __nv_bfloat16*>(page + kv4_scales_at(D));
+    for (int i = tid; i < kPageRows * D / 8; i += kSimtThreads) {
+        {   // a word of eight channels of one key row
+            const int r = i % kPageRows, w = i / kPageRows;
+            if (r < rows) {
+                const uint32_t x = *reinterpret_cast<const uint32_t*>(page + (size_t)(w >> 2) * (kPageRows * 16) + r * 16 + (w & 3) * 4);
+                const float sv = __bfloat162float(sc[r]), ov = __bfloat162float(sc[kPageRows + r]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s_k[r][8 * w + e] = kv4_value((x >> kv4_bit(e)) & 15u, sv, ov);
+            }
+        }
+        {   // a word of eight rows of one value channel
+            const int d = i % D, w = i / D;
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(page + kv4_values_at(D) + d * 16 + w * 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = 8 * w + e;
+                if (r < rows)
+                    s_v[r][d] = kv4_value((x >> kv4_bit(e)) & 15u, __bfloat162float(sc[2 * kPageRows + r]), __bfloat162float(sc[3 * kPageRows + r]));
+            }
+        }
+    }
+}
+
+// grid: (splits, query blocks, B * H).  KV4: the prefix cache is `pages` (kv4.cuh), k_cache and v_cache are not used.
+template <typename T, int D, bool KV4>
 __global__ void __launch_bounds__(kSimtThreads)
 tree_attention_simt_kernel(const T* __restrict__ q, const T* __restrict__ k_cache, const T* __restrict__ v_cache,
                            const T* __restrict__ k_tree, const T* __restrict__ v_tree, T* __restrict__ out,
                            const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ n_active,
                            const uint64_t* __restrict__ anc, int words, int H, int G, int N, int L_max, float scale,
-                           int splits, float* __restrict__ part_ml, float* __restrict__ part_acc) {
+                           int splits, float* __restrict__ part_ml, float* __restrict__ part_acc,
+                           const unsigned char* __restrict__ pages) {
     constexpr int DL = D / 32;                            // output columns per lane
     __shared__ float s_q[kSimtQBlock][D];
     __shared__ float s_k[kSimtTile][D + 1];
@@ -72,8 +102,9 @@ tree_attention_simt_kernel(const T* __restrict__ q, const T* __restrict__ k_cach
     constexpr int EV = Vec16<T>::E, DV = D / EV;          // elements per 16-byte load, loads per row
     const T* qb = q + (size_t)bh * N * D;
     const size_t bkv = (size_t)b * (H / G) + (bh % H) / G;   // query head h reads key/value head h / G
-    const T* kc = k_cache + bkv * L_max * D;
-    const T* vc = v_cache + bkv * L_max * D;
+    const T* kc = KV4 ? nullptr : k_cache + bkv * L_max * D;
+    const T* vc = KV4 ? nullptr : v_cache + bkv * L_max * D;
+    const int L_dense = KV4 ? 0 : L;                          // prefix rows that are read as rows of T
     const T* kt = k_tree + bkv * N * D;
     const T* vt = v_tree + bkv * N * D;
     // rows are multiples of 16 bytes long, so 128-bit loads need only 16-byte aligned tensors (uniform per launch)
@@ -106,16 +137,21 @@ tree_attention_simt_kernel(const T* __restrict__ q, const T* __restrict__ k_cach
 
     for (int j0 = j_begin; j0 < j_end; j0 += kSimtTile) {
         __syncthreads();
-        if (vec) {
+        if (KV4 && j0 < L)
+            load_kv4_tile<D>(pages + (bkv * (size_t)(L_max / kPageRows) + j0 / kPageRows) * kv4_page_bytes(D), min(L, j_end) - j0, s_k, s_v, tid);
+        if (KV4 && j0 + kSimtTile <= L) {
+            // all rows came from the page
+        } else if (vec) {
             // one 128-bit load of K and one of V per thread and step, converted in registers
             for (int i = tid; i < kSimtTile * DV; i += kSimtThreads) {
                 const int r = i / DV, d = (i % DV) * EV, j = j0 + r;
+                if (KV4 && j < L) continue;
                 float kv[EV], vv[EV];
 #pragma unroll
                 for (int e = 0; e < EV; ++e) { kv[e] = 0.f; vv[e] = 0.f; }
                 if (j < j_end) {
-                    const T* kr = j < L ? kc + (size_t)j * D : kt + (size_t)(j - L) * D;
-                    const T* vr = j < L ? vc + (size_t)j * D : vt + (size_t)(j - L) * D;
+                    const T* kr = j < L_dense ? kc + (size_t)j * D : kt + (size_t)(j - L) * D;
+                    const T* vr = j < L_dense ? vc + (size_t)j * D : vt + (size_t)(j - L) * D;
                     Vec16<T>::load(kr + d, kv);
                     Vec16<T>::load(vr + d, vv);
                 }
@@ -125,9 +161,10 @@ tree_attention_simt_kernel(const T* __restrict__ q, const T* __restrict__ k_cach
         } else {
             for (int i = tid; i < kSimtTile * D; i += kSimtThreads) {
                 const int r = i / D, d = i % D, j = j0 + r;
+                if (KV4 && j < L) continue;
                 float kv = 0.f, vv = 0.f;
                 if (j < j_end) {
-                    if (j < L) { kv = to_f32(kc[(size_t)j * D + d]); vv = to_f32(vc[(size_t)j * D + d]); }
+                    if (j < L_dense) { kv = to_f32(kc[(size_t)j * D + d]); vv = to_f32(vc[(size_t)j * D + d]); }
                     else { kv = to_f32(kt[(size_t)(j - L) * D + d]); vv = to_f32(vt[(size_t)(j - L) * D + d]); }
                 }
                 s_k[r][d] = kv;
@@ -236,7 +273,7 @@ size_t simt_workspace_bytes(int B, int H, int N, int D, int L_max) {
     return align_up(slots * 2 * sizeof(float), 256) + align_up(slots * D * sizeof(float), 256);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool KV4>
 static int launch_simt(const AttentionArgs& a, void* scratch, cudaStream_t stream) {
     const int splits = simt_splits(a.B, a.H, a.N, a.L_max);
     const size_t slots = (size_t)a.B * a.H * splits * a.N;
@@ -244,10 +281,11 @@ static int launch_simt(const AttentionArgs& a, void* scratch, cudaStream_t strea
     float* part_acc = reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up(slots * 2 * sizeof(float), 256));
     const int qblocks = (a.N + kSimtQBlock - 1) / kSimtQBlock;
     dim3 grid(splits, qblocks, a.B * a.H);
-    tree_attention_simt_kernel<T, D><<<grid, kSimtThreads, 0, stream>>>(
+    tree_attention_simt_kernel<T, D, KV4><<<grid, kSimtThreads, 0, stream>>>(
         static_cast<const T*>(a.q), static_cast<const T*>(a.k_cache), static_cast<const T*>(a.v_cache),
         static_cast<const T*>(a.k_tree), static_cast<const T*>(a.v_tree), static_cast<T*>(a.out), a.seq_lens,
-        a.n_active, a.anc, a.words, a.H, a.G, a.N, a.L_max, a.scale, splits, part_ml, part_acc);
+        a.n_active, a.anc, a.words, a.H, a.G, a.N, a.L_max, a.scale, splits, part_ml, part_acc,
+        static_cast<const unsigned char*>(a.kv4));
     MCSD_CUDA_CHECK(cudaGetLastError());
     count_launches(1);
     if (splits > 1) {
@@ -259,12 +297,17 @@ static int launch_simt(const AttentionArgs& a, void* scratch, cudaStream_t strea
     return MCSD_OK;
 }
 
-int tree_attention_simt(const AttentionArgs& a, void* scratch, cudaStream_t stream) {
+template <bool KV4>
+static int launch_simt_by_type(const AttentionArgs& a, void* scratch, cudaStream_t stream) {
     if (a.dtype == MCSD_F32) {
-        return a.D == 64 ? launch_simt<float, 64>(a, scratch, stream) : launch_simt<float, 128>(a, scratch, stream);
+        return a.D == 64 ? launch_simt<float, 64, KV4>(a, scratch, stream) : launch_simt<float, 128, KV4>(a, scratch, stream);
     }
-    return a.D == 64 ? launch_simt<__nv_bfloat16, 64>(a, scratch, stream)
-                     : launch_simt<__nv_bfloat16, 128>(a, scratch, stream);
+    return a.D == 64 ? launch_simt<__nv_bfloat16, 64, KV4>(a, scratch, stream)
+                     : launch_simt<__nv_bfloat16, 128, KV4>(a, scratch, stream);
+}
+
+int tree_attention_simt(const AttentionArgs& a, void* scratch, cudaStream_t stream) {
+    return a.kv4 ? launch_simt_by_type<true>(a, scratch, stream) : launch_simt_by_type<false>(a, scratch, stream);
 }
 
 }  // namespace mcsd
