@@ -111,7 +111,11 @@ extern "C" int mcsd_tree_attention_gqa(const void* q, const void* k_cache, const
 extern "C" size_t mcsd_tree_attention_kv4_workspace_bytes(int B, int H_q, int H_kv, int N, int D, int L_max, int dtype) {
     if (check_shape(B, H_q, N, D, L_max, dtype) != MCSD_OK || !whole_pages(L_max)) return 0;
     if (H_kv < 1 || H_q < H_kv || H_q % H_kv != 0) return 0;
-    const size_t scratch = mcsd::simt_workspace_bytes(B, H_q, N, D, L_max);
+    size_t scratch = mcsd::simt_workspace_bytes(B, H_q, N, D, L_max);
+    if (mcsd::kv4_tc_shape(B, H_q, H_q / H_kv, N, D, L_max, dtype)) {
+        const size_t tc = mcsd::kv4_tc_workspace_bytes(B, H_q, H_q / H_kv, N);
+        if (tc > scratch) scratch = tc;
+    }
     return sizeof(mcsd::WorkspaceHeader) + mcsd::align_up(scratch, 256);
 }
 
@@ -129,6 +133,9 @@ extern "C" int mcsd_tree_attention_kv4(const void* q, const void* cache, const v
 
     mcsd::AttentionArgs a{q, nullptr, nullptr, k_tree, v_tree, out, seq_lens, n_active, anc, words,
                           B, H_q, N, D, L_max, softmax_scale, dtype, H_q / H_kv, cache};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
     void* scratch = static_cast<char*>(workspace) + sizeof(mcsd::WorkspaceHeader);
-    return mcsd::tree_attention_simt(a, scratch, static_cast<cudaStream_t>(stream));
+    if (mcsd::kv4_tc_shape(B, H_q, a.G, N, D, L_max, dtype) && mcsd::aligned16(q) && mcsd::aligned16(k_tree))
+        return mcsd::tree_attention_kv4_tc(a, static_cast<mcsd::WorkspaceHeader*>(workspace), scratch, s);
+    return mcsd::tree_attention_simt(a, scratch, s);
 }

@@ -38,4 +38,9 @@ constexpr int kTcMaxBlocks = 160;                    // thread blocks of a launc
 int tree_attention_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scratch, size_t scratch_bytes,
                       cudaStream_t stream);
 
+// tcgen05 path over a 4-bit cache: bf16, D = 128, the shapes of the tensor-core kernel above
+bool kv4_tc_shape(int B, int H, int G, int N, int D, int L_max, int dtype);
+size_t kv4_tc_workspace_bytes(int B, int H, int G, int N);
+int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scratch, cudaStream_t stream);
+
 }  // namespace mcsd
