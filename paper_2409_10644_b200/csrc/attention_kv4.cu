@@ -1,34 +1,41 @@
 // Tree attention (Section 2.2 of the paper) over a prefix cache held in 4 bits (page layout in kv4.cuh), on the
-// fifth-generation tensor cores of sm_100a: bf16 tree tensors, head_dim 128, 1 to 96 query columns per work item.
+// fifth-generation tensor cores of sm_100a: bf16 tree tensors, head_dim 128, 1 to 64 query columns per work item.
 //
 // The products are set up transposed, the small dimension (query columns) as the MMA N:
-//     S^T[key][query] = K Q^T,     O^T[channel][query] += V^T P^T
+//     S^T[key][query] = K Q^T,     O^T[channel][query] += V^T P^T,     l[query] += 1 P^T
 // and the A operands live in tensor memory, not in shared memory: thread r of the key warps owns key row r of a
 // 128-key tile, thread d of the value warps channel d, and both turn 16-byte pieces of a page (neighbouring threads read
 // neighbouring pieces) into operand columns with a shift and a mask per two values and store them with tcgen05.st.
 //   * Keys stay codes: 16 + code is exact in bf16, so S' = sum (16 + code) q is exact up to fp32 sums, and the row's scale
 //     and offset are applied to the score, where the softmax thread owns the same key row:
 //         score = scale_k S' + offset_k (sum of q).
-//   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values, rounded to bf16.
-// The rows of the tree itself are read as they are: same operand columns, scale 1, offset 0.
+//   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
+//     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
+//     whose values lie well inside fp16's range, which the value warps vote on tile by tile; else bf16.
+// The rows of the tree itself are read as they are (bf16): same operand columns, scale 1, offset 0.
 //
-// What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; the unpacking
-// (about 20 integer and half-precision instructions per eight keys' and eight values' codes) and the exponentials then
-// share the issue slots, so the work is spread over specialised warps:
-//   warps 0-3   keys     page pieces -> operand columns (two buffers)
-//   warps 4-7   values   page pieces -> operand columns
-//   warps 8-15  softmax  two groups that split the query columns; epilogue and merge
-//   warp 16     copies whole pages (1 to 4 of them, contiguous) into a ring with cp.async.bulk
-//   warp 17     issues the MMAs and owns the tensor memory
-//   warps 18-19 bring the queries of the next work item and their sums
+// What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; unpacking
+// and the exponentials then share the issue slots of the schedulers, so the work is spread over specialised warps:
+//   warps 0-3    keys      page pieces -> operand columns
+//   warps 4-7    values    page pieces -> operand columns
+//   warps 8-11   softmax of the even tiles, all columns;  warps 12-15 of the odd ones.  The two groups have their own
+//                references, accumulators and row sums and meet only at the end of a work item: with one group per tile
+//                a tile's chain (scores, vote, exponentials, P^T, products) may take twice the time between two tiles
+//   warp 16      copies whole pages (1 to 4 of them, contiguous) into a ring with cp.async.bulk
+//   warp 17      issues the MMAs and owns the tensor memory
+//   warps 18-19  bring the queries of the next work item and their sums
+// Loops are rolled as far as the latencies allow: the roles share the instruction caches, and with unrolled bodies (a
+// kernel of 180 KB) a tile took three times as long, most of it in waits for instructions.
 //
 // Work: one block per multiprocessor walks a contiguous range of the (sequence, key/value head, query block, tile) space,
 // cut by cost.  A work item that a range boundary cuts is finished by whichever of its blocks comes last (a counter of
-// tiles per item and softmax group; nothing waits): it reads all pieces in block order, so the result does not depend
-// on who that is.  Every wait is bounded; one that runs out raises a flag in the workspace header.
+// tiles per item; nothing waits): it reads all pieces in block order, so the result does not depend on who that is.
+// Every wait is bounded; one that runs out raises a flag in the workspace header.
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
+
+#include <cuda_fp16.h>
 
 #include "attention_tc_common.cuh"
 #include "kv4.cuh"
@@ -42,15 +49,21 @@ constexpr int kPageBytes = kv4_page_bytes(kD);
 constexpr int kStageBytes = 4 * kPageBytes;      // one tile: 128 rows
 constexpr int kValueWarp = 4, kSoftWarp = 8, kCopyWarp = 16, kIssueWarp = 17, kQueryWarp = 18;
 constexpr int kThreads = 640;
-constexpr int kWideQ = 96;                       // query columns of a work item, at most
-constexpr int kStages = 7;
-// Tensor-memory columns: scores twice, O^T, keys twice, and values twice where all that fits in 512.
+constexpr int kWideQ = 64;                       // query columns of a work item, at most
+constexpr int kStages = 6;
+constexpr int kMaxPieces = kMaxCtas;             // of a work item
+// Tensor-memory columns: scores, O^T and row sums of the two softmax groups, then keys and values, twice where it fits,
+// and the ones of the row sums' A operand (bf16, fp16; they are in shared memory where no column is left, and such a
+// product takes 41 cycles instead of 12 at 16 columns, 50 instead of 34 at 64).
 template <int QB>
 struct Columns {
-    static constexpr int wide = (QB + 31) & ~31;
-    static constexpr int S = 0, O = 2 * wide, K = 3 * wide, V = K + 128;
-    static constexpr int value_buffers = V + 128 <= kTmemCols ? 2 : 1;
-    static_assert(V + 64 * value_buffers <= kTmemCols, "tensor memory");
+    static constexpr int S = 0, O = 2 * QB, L = 4 * QB, K = 6 * QB;
+    static constexpr bool ones = K + 128 + 16 <= kTmemCols;
+    static constexpr int key_buffers = K + 256 + 16 <= kTmemCols ? 2 : 1;
+    static constexpr int V = K + 64 * key_buffers;
+    static constexpr int value_buffers = V + 128 + 16 <= kTmemCols ? 2 : 1;
+    static constexpr int One = V + 64 * value_buffers;
+    static_assert(One + (ones ? 16 : 0) <= kTmemCols, "tensor memory");
 };
 
 struct Params {
@@ -63,7 +76,7 @@ struct Params {
     float scale_log2;
     float* part_ml;       // [2 * kMaxCtas][2][kWideQ]
     float* part_o;        // [2 * kMaxCtas][kWideQ][128]
-    int* counters;        // [work items][2] tiles that have been finished; zero between launches
+    int* counters;        // [work items] tiles that have been finished; zero between launches
     WorkspaceHeader* header;
 };
 
@@ -72,7 +85,7 @@ struct Plan {
     long long tiles[kMaxBatchTc + 1], cost[kMaxBatchTc + 1];   // of the sequences before b
     int items[kMaxBatchTc + 1];
     int len[kMaxBatchTc], nodes[kMaxBatchTc];
-    long long range[2];
+    long long first[kMaxCtas + 1];   // first tile of every block
     int blocks;
 };
 
@@ -110,9 +123,9 @@ __device__ __forceinline__ void piece_at(const Plan& pl, const Params& p, long l
     s.L = pl.len[lo];
     s.Nb = pl.nodes[lo];
     const Shape sh = shape_of<QB>(s.L, s.Nb, p.G);
-    const long long r = t - pl.tiles[lo];
-    const int it = (int)(r / sh.T);
-    s.lt = (int)(r - (long long)it * sh.T);
+    const uint32_t r = (uint32_t)(t - pl.tiles[lo]);          // below 2^31 by the limit on the shape
+    const int it = (int)(r / (uint32_t)sh.T);
+    s.lt = (int)r - it * sh.T;
     s.T = sh.T;
     s.Tp = sh.Tp;
     s.item = pl.items[lo] + it;
@@ -140,16 +153,6 @@ __device__ __forceinline__ long long first_tile(const Plan& pl, const Params& p,
     const long long it = off / ci, rem = off - it * ci;
     const long long lt = (rem + w - 1) / w;
     return pl.tiles[lo] + it * sh.T + (lt < sh.T ? lt : sh.T);
-}
-
-// The block that owns a tile: the inverse of first_tile.
-template <int QB>
-__device__ __forceinline__ int block_of(const Plan& pl, const Params& p, int b, long long tile_in_b) {
-    const Shape sh = shape_of<QB>(pl.len[b], pl.nodes[b], p.G);
-    const int w = tile_cost(sh.per_q);
-    const long long it = tile_in_b / sh.T, lt = tile_in_b - it * sh.T;
-    const long long x = pl.cost[b] + it * ((long long)sh.T * w + kItemCost) + lt * w;
-    return (int)(x * pl.blocks / pl.cost[p.B]);
 }
 
 template <int QB>
@@ -196,27 +199,31 @@ __device__ void make_plan(Plan& pl, const Params& p) {
         __syncwarp();
         const long long all = __shfl_sync(0xffffffffu, tb, 31);
         if (tid == 0) pl.blocks = (int)min((long long)gridDim.x, all);
-        __syncwarp();
-        if (tid < 2 && all > 0) pl.range[tid] = first_tile<QB>(pl, p, blockIdx.x + tid);
-        if (tid < 2 && all == 0) pl.range[tid] = 0;
     }
+    __syncthreads();
+    if (tid <= (int)gridDim.x) pl.first[tid] = first_tile<QB>(pl, p, tid);
     __syncthreads();
 }
 
 template <int QB>
 struct Small {
     unsigned long long full[kStages], empty[kStages];
-    unsigned long long k_full[2], s_full[2], v_full[2], pv_done[2], q_full[2], piece_done[2];
-    unsigned long long p_full, drain;
+    unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], q_full[2], piece_done[2], fmt_full[4];
+    unsigned long long drain;
     uint32_t tmem_base;
     int abort_flag;
-    int merge[2];                                     // tiles of the item finished before this block's, by group
+    int merge, merge_pieces;                          // tiles of the item finished before this block's; its pieces
+    int fmt[4];                                       // 1: the tile's values and weights are fp16, 0: bf16
+    int row[2][QB];                                   // rows of q and out of the piece's columns
+    short slots[kMaxPieces];                          // of the pieces that are merged
     alignas(16) float2 kab[4][kTile];                 // scale and offset of a tile's key rows, in score units
+    alignas(16) unsigned short vab[2][2][kTile];      // scales and offsets of a tile's value rows, in the tile's format
     alignas(16) float q_sum[2][QB];
-    alignas(16) float ref[2][QB / 2 + 8];             // running reference of a group's own columns
-    alignas(16) float alpha[2][QB / 2 + 8];
-    alignas(16) float red[2][4][QB / 2 + 8];
+    alignas(16) float nref[2][QB];                    // running references of the two groups, negated
+    alignas(16) float alpha[2][QB];
+    alignas(16) float red[2][4][QB];
     alignas(16) uint64_t anc[MCSD_MAX_NODES * MCSD_MAX_WORDS];
+    alignas(16) unsigned short ones[2][kTile * 16];   // A operand of the row sums: bf16, fp16
     Plan plan;
 };
 
@@ -228,14 +235,27 @@ __device__ __forceinline__ void bulk_load_once(uint32_t dst, const void* src, ui
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy) : "memory");
 }
-// tcgen05.mma with the A operand in tensor memory; see tc_mma_elect for the elected lane
-__device__ __forceinline__ void tc_mma_ta_elect(uint32_t d_tmem, uint32_t a_tmem, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+// One lane of a converged warp, the same one every time: it issues the MMAs and the commits that track them.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// tcgen05.mma by the calling lane, A operand in tensor memory or in shared memory
+__device__ __forceinline__ void mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\t"
-        "elect.sync _|e, 0xffffffff;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d_tmem), "r"(a_tmem), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_sa(uint32_t d_tmem, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void commit(void* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // sixteen consecutive columns of this thread's lane
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -244,31 +264,66 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16])
         ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
           "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
-// codes (2i, 2i + 1) of a word as two bf16 numbers 16 + code
+// codes (2i, 2i + 1) of a word as two numbers 16 + code: bf16 (code in mantissa bits 3..6) or fp16 (bits 6..9)
+template <bool HALF>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) {
+    if (HALF) {
+        const uint32_t x = i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6);
+        return (x & 0x03C003C0u) | 0x4C004C00u;
+    }
     const uint32_t x = i == 0 ? w << 3 : w >> (4 * i - 3);
     return (x & 0x00780078u) | 0x41804180u;
 }
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+template <bool HALF>
+__device__ __forceinline__ uint32_t fma_x2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t d;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    if (HALF) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
-// lo += low half, hi += high half of a bf16 pair, in fp32
-__device__ __forceinline__ void add_pair(float& lo, float& hi, uint32_t v) {
-    asm("{.reg .b16 a, b; mov.b32 {a, b}, %2; add.f32.bf16 %0, a, %0; add.f32.bf16 %1, b, %1;}" : "+f"(lo), "+f"(hi) : "r"(v));
+template <bool HALF>
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
+    uint32_t d;
+    if (HALF) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// two fp32 fused multiply-adds in one instruction
+__device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\t"
+        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// barrier over both softmax groups
+__device__ __forceinline__ bool both_sync_any(bool pred) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.or.pred q, 4, 256, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r) : "r"((uint32_t)pred) : "memory");
+    return r != 0;
+}
+// A row of values may be fp16: no value can leave its range, and neither scale nor values are so small that fp16's fixed
+// spacing below 2^-14 would round them more coarsely than bf16 does.  False for scales that are not finite.
+__device__ __forceinline__ bool fits_half(float scale, float offset) {
+    const float o = fabsf(offset);
+    return 31.f * scale + o <= 32768.f && (scale >= 6.103515625e-5f || (scale == 0.f && (o == 0.f || o >= 6.103515625e-5f)));
 }
 
 template <int QB>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attention_kv4_kernel(const Params p) {
-    constexpr int CPT = QB / 16;                      // 8-column groups of a softmax thread, at most
     using Col = Columns<QB>;
     extern __shared__ unsigned char smem_raw[];
-    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char* smem = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);   // (an offset: the compiler keeps knowing it is shared memory)
     unsigned char* q_buf = smem;                      // two buffers of QB rows: [2 slabs of 64 channels][QB rows][128 bytes], swizzled
-    unsigned char* p_buf = q_buf + 2 * QB * 256;      // P^T: [QB / 8][128 keys][16 bytes]
-    unsigned char* ring = p_buf + QB * 256;
+    unsigned char* p_buf = q_buf + 2 * QB * 256;      // P^T of the two groups: [QB / 8][128 keys][16 bytes]
+    unsigned char* ring = p_buf + 2 * QB * 256;
     Small<QB>* sm = reinterpret_cast<Small<QB>*>(ring + kStages * kStageBytes);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -280,21 +335,25 @@ tree_attention_kv4_kernel(const Params p) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm->k_full[i], 4);
             mbar_init(&sm->s_full[i], 1);
+            mbar_init(&sm->s_free[i], 4);
             mbar_init(&sm->v_full[i], 4);
+            mbar_init(&sm->p_full[i], 4);
             mbar_init(&sm->pv_done[i], 1);
             mbar_init(&sm->q_full[i], 2);
             mbar_init(&sm->piece_done[i], 8);
         }
-        mbar_init(&sm->p_full, 8);
+        for (int i = 0; i < 4; ++i) mbar_init(&sm->fmt_full[i], 4);
         mbar_init(&sm->drain, 1);
         sm->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    for (int i = tid; i < kTile * 16; i += kThreads) { sm->ones[0][i] = 0x3F80; sm->ones[1][i] = 0x3C00; }
+    fence_async_smem();                               // read by the tensor cores through the async proxy
     asm volatile("griddepcontrol.wait;" ::: "memory");
     for (int i = tid; i < p.N * p.words; i += kThreads) sm->anc[i] = p.anc[i];
     make_plan<QB>(sm->plan, p);
     const Plan& pl = sm->plan;
-    const long long t_begin = pl.range[0], t_end = pl.range[1];
+    const long long t_begin = pl.first[blockIdx.x], t_end = pl.first[blockIdx.x + 1];
     if (t_begin >= t_end) return;                     // uniform for the whole block: nothing allocated yet
 
     if (warp == kIssueWarp) {
@@ -343,59 +402,70 @@ tree_attention_kv4_kernel(const Params p) {
         // S^T of tile g + 1 is issued before the products of tile g, across pieces as well
         const uint64_t dq0 = smem_desc(smem_u32(q_buf), 16, 1024, 2);
         const uint64_t dp0 = smem_desc(smem_u32(p_buf), 128, 2048, 0);
-        constexpr uint32_t q_slab = (QB * 128) >> 4, q_next = (QB * 256) >> 4;
+        const uint64_t d1 = smem_desc(smem_u32(sm->ones), 128, 256, 0);
+        constexpr uint32_t q_slab = (QB * 128) >> 4, q_next = (QB * 256) >> 4, p_next = (QB * 256) >> 4, one_next = (kTile * 32) >> 4;
         const uint32_t n_tiles = (uint32_t)(t_end - t_begin);
-        Piece s, o;                                   // of the scores and of the products
-        long long ts = t_begin, to = t_begin;
-        int si = 0, oi = 0;
+        Piece s;                                      // of the scores
+        long long ts = t_begin;
+        int si = 0, oi = 0, o_cnt = 0, o_nq = 0;      // the products are one tile behind: in the same piece or the one before
         uint32_t seg = 0;
-        piece_at<QB>(pl, p, ts, t_end, s);
-        o = s;
-        bool ok = mbar_wait(&sm->q_full[0], 0, abort_flag, hdr, 32);
+        bool ok = true;
+        s.cnt = 0;
         for (uint32_t g = 0; g <= n_tiles && ok; ++g) {
             if (g < n_tiles) {
                 if (si == s.cnt) {
                     ts += s.cnt;
                     piece_at<QB>(pl, p, ts, t_end, s);
                     si = 0;
-                    ++seg;
                     ok = mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 32);
                     if (!ok) break;
+                    ++seg;
                 }
                 const uint32_t buf = g & 1u;
                 ok = mbar_wait(&sm->k_full[buf], (g >> 1) & 1u, abort_flag, hdr, 33);
+                if (ok && g >= 2) ok = mbar_wait(&sm->s_free[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 46);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t idesc = instr_desc((s.Nq + 15) & ~15, 0, 0);
-                const uint64_t dq = dq0 + (seg & 1u) * q_next;
+                if (elect_one()) {
+                    const uint32_t idesc = instr_desc((s.Nq + 15) & ~15, 0, 0);
+                    const uint64_t dq = dq0 + ((seg - 1u) & 1u) * q_next;
+                    const uint32_t d = tmem + Col::S + buf * QB, ka = tmem + Col::K + (Col::key_buffers == 2 ? buf * 64 : 0u);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    tc_mma_ta_elect(tmem + Col::S + buf * Col::wide, tmem + Col::K + buf * 64 + 8 * k,
-                                    dq + (uint32_t)(k >> 2) * q_slab + (uint32_t)(k & 3) * 2u, idesc, k > 0);
-                tc_commit_elect(&sm->s_full[buf]);
+                    for (int k = 0; k < 8; ++k) mma_ta(d, ka + 8 * k, dq + (uint32_t)(k >> 2) * q_slab + (uint32_t)(k & 3) * 2u, idesc, k > 0);
+                    commit(&sm->s_full[buf]);
+                }
+                __syncwarp();
                 ++si;
             }
             if (g >= 1) {
-                const uint32_t h = g - 1u;
-                if (oi == o.cnt) {
-                    to += o.cnt;
-                    piece_at<QB>(pl, p, to, t_end, o);
-                    oi = 0;
-                }
-                ok = mbar_wait(&sm->v_full[h & 1u], (h >> 1) & 1u, abort_flag, hdr, 34);
-                if (!ok) break;
-                ok = mbar_wait(&sm->p_full, h & 1u, abort_flag, hdr, 35);
+                const uint32_t h = g - 1u, hb = h & 1u;
+                ok = mbar_wait(&sm->v_full[hb], (h >> 1) & 1u, abort_flag, hdr, 34);
+                if (ok) ok = mbar_wait(&sm->p_full[hb], (h >> 1) & 1u, abort_flag, hdr, 35);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t idesc = instr_desc((o.Nq + 15) & ~15, 0, 1);
+                if (elect_one()) {
+                    // fp16 operands are format 0 of both operand fields, bf16 is 1
+                    const uint32_t half = sm->fmt[h & 3u];
+                    const uint32_t idesc = instr_desc((o_nq + 15) & ~15, 0, 1) & ~(half ? (1u << 7) | (1u << 10) : 0u);
+                    const uint32_t d = tmem + Col::O + hb * QB, l = tmem + Col::L + hb * QB;
+                    const uint32_t va = tmem + Col::V + (Col::value_buffers == 2 ? hb * 64 : 0u), one = tmem + Col::One + half * 8;
+                    const uint64_t dp = dp0 + hb * p_next, d1h = d1 + half * one_next;
+                    const uint32_t more = oi >= 2;    // a group's first tile of a piece overwrites
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    tc_mma_ta_elect(tmem + Col::O, tmem + Col::V + (Col::value_buffers == 2 ? (h & 1u) * 64 : 0u) + 8 * k, dp0 + (uint32_t)(k * (256 >> 4)), idesc, (oi > 0) | (k > 0));
-                tc_commit_elect(&sm->pv_done[h & 1u]);
+                    for (int k = 0; k < 8; ++k) {
+                        mma_ta(d, va + 8 * k, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
+                        if (Col::ones) mma_ta(l, one, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
+                        else mma_sa(l, d1h, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
+                    }
+                    commit(&sm->pv_done[hb]);
+                }
+                __syncwarp();
                 ++oi;
             }
+            if (oi == o_cnt) { oi = 0; o_cnt = s.cnt; o_nq = s.Nq; }   // the next products belong to the scores' piece
         }
-        tc_commit_elect(&sm->drain);                  // all MMAs have finished before tensor memory is released
+        if (elect_one()) commit(&sm->drain);          // all MMAs have finished before tensor memory is released
+        __syncwarp();
         const long long t0 = clock64();
         while (!mbar_try_wait(&sm->drain, 0) && clock64() - t0 < kSpinCycles) {}
     } else if (warp >= kQueryWarp) {
@@ -415,7 +485,9 @@ tree_attention_kv4_kernel(const Params p) {
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (r < s.Nq) {
                     const int j = s.q0 + r, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
-                    v = *reinterpret_cast<const uint4*>(p.q + (((size_t)s.b * p.Hkv * p.G + h) * p.N + n) * kD + c * 8);
+                    const int row = (s.b * p.Hkv * p.G + h) * p.N + n;          // below 65535 * 192
+                    v = *reinterpret_cast<const uint4*>(p.q + (size_t)row * kD + c * 8);
+                    if (c == 0) sm->row[buf][r] = row;
                 }
                 *reinterpret_cast<uint4*>(dst + r * 128 + (((c & 7) ^ (r & 7)) * 16)) = v;
                 float sum = 0.f;
@@ -433,50 +505,58 @@ tree_attention_kv4_kernel(const Params p) {
         }
     } else if (warp < kValueWarp) {
         // ---- keys: thread r owns key row r of a tile
+        constexpr uint32_t NK = Col::key_buffers;
         const int r = tid;
         const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
+        if (Col::ones) {                              // ordered before the products by the barrier of the first tile's keys
+            uint32_t y[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = e < 8 ? 0x3F803F80u : 0x3C003C00u;
+            tc_st16(lane_addr + Col::One, y);
+        }
         uint32_t g = 0, f = 0;
         bool ok = true;
         for (long long t = t_begin; t < t_end && ok;) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
             for (int i = s.lt; i < s.lt + s.cnt && ok; ++i, ++g) {
-                const uint32_t buf = g & 1u, dst = lane_addr + Col::K + buf * 64;
+                const uint32_t buf = g & 1u, dst = lane_addr + Col::K + (NK == 2 ? buf * 64 : 0u);
                 if (i < s.Tp) {
                     const uint32_t st = f % kStages;
                     ok = mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 37);
                     if (!ok) break;
                     const unsigned char* page = ring + st * kStageBytes + warp * kPageBytes;   // rows 32 warp .. of the tile
-                    uint4 x[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) x[c] = *reinterpret_cast<const uint4*>(page + c * (kPageRows * 16) + lane * 16);
+                    const uint4* piece = reinterpret_cast<const uint4*>(page) + lane;
                     const unsigned short* sc = reinterpret_cast<const unsigned short*>(page + kv4_scales_at(kD));
                     const float a = bf16_bits_to_f32(sc[lane]), b = bf16_bits_to_f32(sc[kPageRows + lane]);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sm->empty[st]);
-                    ++f;
-                    // The buffer is free once the scores of the tile before last are done.  They were issued after the
-                    // softmax warps had finished tile g - 4, whose scales the entry below held.
-                    if (g >= 2) ok = mbar_wait(&sm->s_full[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 38);
+                    uint4 x = piece[0];
+                    // The buffer is free once the scores of the tile that used it are done.  They were issued after the
+                    // softmax warps had taken the scores and the scales of tile g - 4, which the entry below held.
+                    if (g >= NK) ok = mbar_wait(&sm->s_full[(g - NK) & 1u], ((g - NK) >> 1) & 1u, abort_flag, hdr, 38);
                     if (!ok) break;
                     tc_fence_after();
                     sm->kab[g & 3u][r] = make_float2(a * p.scale_log2, b * p.scale_log2);
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                        const uint4 next = piece[((c + 1) & 3) * kPageRows];
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
                         uint32_t y[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = code_pair(w[e >> 2], e & 3);
+                        for (int e = 0; e < 16; ++e) y[e] = code_pair<false>(w[e >> 2], e & 3);
                         tc_st16(dst + 16 * c, y);
+                        x = next;
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm->empty[st]);
+                    ++f;
                 } else {
                     const int n = (i - s.Tp) * kTile + r;
-                    if (g >= 2) ok = mbar_wait(&sm->s_full[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 38);
+                    if (g >= NK) ok = mbar_wait(&sm->s_full[(g - NK) & 1u], ((g - NK) >> 1) & 1u, abort_flag, hdr, 38);
                     if (!ok) break;
                     tc_fence_after();
                     sm->kab[g & 3u][r] = make_float2(p.scale_log2, 0.f);
                     const uint4* row = reinterpret_cast<const uint4*>(p.k_tree + (((size_t)s.b * p.Hkv + s.hk) * p.N + n) * kD);
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t y[16];
 #pragma unroll
@@ -500,52 +580,69 @@ tree_attention_kv4_kernel(const Params p) {
         const int d = tid & 127;
         const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + Col::V;
         uint32_t g = 0, f = 0;
-        bool ok = true;
-        for (long long t = t_begin; t < t_end && ok;) {
+        bool failed = false, gone = false;                    // gone: all threads of the role know that one has failed
+        for (long long t = t_begin; t < t_end && !gone;) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
-            for (int i = s.lt; i < s.lt + s.cnt && ok; ++i, ++g) {
+            for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
                 const uint32_t dst = lane_addr + (NV == 2 ? (g & 1u) * 64 : 0u);
                 const uint32_t st = f % kStages;
-                if (i < s.Tp) ok = mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 39);
+                unsigned short* const va = sm->vab[g & 1u][0];
+                unsigned short* const vb = sm->vab[g & 1u][1];
+                uint32_t a16 = 0, b16 = 0;
+                if (i < s.Tp) {
+                    if (!mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 39)) failed = true;
+                    // Scales of the tile's rows, thread d the row d, rounded to fp16.  Rows past the end of the prefix have
+                    // probability zero but may hold anything, and 0 * NaN would be NaN: their scale and offset are zero.
+                    const unsigned short* sc = reinterpret_cast<const unsigned short*>(ring + st * kStageBytes + (warp & 3) * kPageBytes + kv4_scales_at(kD)) + 2 * kPageRows + lane;
+                    if (d < s.L - i * kTile) { a16 = sc[0]; b16 = sc[kPageRows]; }
+                    va[d] = __half_as_ushort(__float2half_rn(bf16_bits_to_f32(a16)));
+                    vb[d] = __half_as_ushort(__float2half_rn(bf16_bits_to_f32(b16)));
+                }
+                const bool half = !group_sync_any(3, failed || i >= s.Tp || !fits_half(bf16_bits_to_f32(a16), bf16_bits_to_f32(b16)));
+                if (!half) {
+                    va[d] = (unsigned short)a16;
+                    vb[d] = (unsigned short)b16;
+                    gone = group_sync_any(3, failed);
+                    if (gone) break;
+                }
+                if (lane == 0) {
+                    if (warp == kValueWarp) sm->fmt[g & 3u] = half;
+                    mbar_arrive(&sm->fmt_full[g & 3u]);
+                }
                 // the buffer is free once the products of the tile that used it are done
-                if (ok && g >= NV) ok = mbar_wait(&sm->pv_done[(g - NV) & 1u], ((g - NV) >> 1) & 1u, abort_flag, hdr, 40);
-                if (!ok) break;
+                if (g >= NV && !mbar_wait(&sm->pv_done[(g - NV) & 1u], ((g - NV) >> 1) & 1u, abort_flag, hdr, 40)) failed = true;
                 tc_fence_after();
                 if (i < s.Tp) {
-                    const int valid = min(kTile, s.L - i * kTile);
+                    const unsigned char* codes = ring + st * kStageBytes + kv4_values_at(kD) + d * 16;
+                    const uint4* sa = reinterpret_cast<const uint4*>(va);
+                    const uint4* sb = reinterpret_cast<const uint4*>(vb);
+                    auto unpack = [&](auto half_tag) {
+                        constexpr bool HALF = decltype(half_tag)::value;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(codes + c * kPageBytes);
+                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                            uint32_t y[16];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const unsigned char* page = ring + st * kStageBytes + c * kPageBytes;
-                        const uint4 x = *reinterpret_cast<const uint4*>(page + kv4_values_at(kD) + d * 16);
-                        const uint4* sc = reinterpret_cast<const uint4*>(page + kv4_scales_at(kD) + 4 * kPageRows);   // scales, then offsets
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                        uint32_t y[16];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint4 a = sc[j], b = sc[4 + j];
-                            y[4 * j] = fma_bf16x2(code_pair(w[j], 0), a.x, b.x);
-                            y[4 * j + 1] = fma_bf16x2(code_pair(w[j], 1), a.y, b.y);
-                            y[4 * j + 2] = fma_bf16x2(code_pair(w[j], 2), a.z, b.z);
-                            y[4 * j + 3] = fma_bf16x2(code_pair(w[j], 3), a.w, b.w);
-                        }
-                        // rows past the end of the prefix have probability zero, but may hold anything: 0 * NaN would be NaN
-                        if (valid < kTile) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const int n = 32 * c + 2 * e;
-                                y[e] &= (n < valid ? 0xFFFFu : 0u) | (n + 1 < valid ? 0xFFFF0000u : 0u);
+                            for (int j = 0; j < 4; ++j) {
+                                const uint4 a = sa[4 * c + j], b = sb[4 * c + j];
+                                y[4 * j] = fma_x2<HALF>(code_pair<HALF>(w[j], 0), a.x, b.x);
+                                y[4 * j + 1] = fma_x2<HALF>(code_pair<HALF>(w[j], 1), a.y, b.y);
+                                y[4 * j + 2] = fma_x2<HALF>(code_pair<HALF>(w[j], 2), a.z, b.z);
+                                y[4 * j + 3] = fma_x2<HALF>(code_pair<HALF>(w[j], 3), a.w, b.w);
                             }
+                            tc_st16(dst + 16 * c, y);
                         }
-                        tc_st16(dst + 16 * c, y);
-                    }
+                    };
+                    if (half) unpack(std::true_type{}); else unpack(std::false_type{});
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sm->empty[st]);
                     ++f;
                 } else {
                     const int n0 = (i - s.Tp) * kTile, n1 = min(kTile, s.Nb - n0);
                     const unsigned short* col = reinterpret_cast<const unsigned short*>(p.v_tree) + (((size_t)s.b * p.Hkv + s.hk) * p.N + n0) * kD + d;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t y[16];
 #pragma unroll
@@ -565,89 +662,55 @@ tree_attention_kv4_kernel(const Params p) {
             t += s.cnt;
         }
     } else {
-        // ---- softmax, epilogue, merge: group wg has about half of the query columns, thread r key row r
+        // ---- softmax, epilogue, merge: group wg has the tiles with g % 2 == wg, thread r key row r
         const int wg = (warp - kSoftWarp) >> 2, wq = warp & 3, r = tid & 127;
         const int bar_id = 1 + wg;
         const uint32_t lane_addr = tmem + ((uint32_t)(wq * 32) << 16);
-        float* const ref = sm->ref[wg];
-        float* const alph = sm->alpha[wg];
-        uint32_t g = 0, seg = 0;
-        bool failed = false;
+        unsigned char* const p_own = p_buf + wg * (QB * 256) + r * 16;
+        float* const nref = sm->nref[wg];
+        uint32_t g_piece = 0, seg = 0;                           // tiles of this block before the piece
+        bool failed = false, gone = false;                       // gone: all threads know that one has failed
         for (long long t = t_begin; t < t_end; ++seg) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
             const int n8 = (s.Nq + 7) >> 3;
-            const int g0 = wg ? (n8 + 1) / 2 : 0;                // first 8-column group of this group, and how many
-            const int ncg = wg ? n8 / 2 : (n8 + 1) / 2;
-            const int col0 = 8 * g0;
-            const float* qs = &sm->q_sum[seg & 1u][col0];
-            float lsum[CPT][8];
-#pragma unroll
-            for (int j = 0; j < CPT; ++j)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) lsum[j][k] = 0.f;
-            if (r < 8 * ncg) ref[r] = -1e30f;                    // below any score: the first tile sets it
-            if (group_sync_any(bar_id, failed)) { failed = true; break; }
-
-            for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
-                const uint32_t buf = g & 1u;
+            const float* qs = sm->q_sum[seg & 1u];
+            const uint32_t g_end = g_piece + (uint32_t)s.cnt;
+            const uint32_t g_own = g_piece + ((g_piece ^ (uint32_t)wg) & 1u);   // the group's first tile, if below g_end
+            for (uint32_t g = g_own; g < g_end; g += 2) {
+                const int i = s.lt + (int)(g - g_piece);
                 const bool tree = i >= s.Tp;
-                const int row = (tree ? i - s.Tp : i) * kTile + r;
+                const int key = (tree ? i - s.Tp : i) * kTile + r;
                 const bool plain = !tree && (i + 1) * kTile <= s.L;   // every key there and visible to every query
-                unsigned long long cm = 0;                        // columns that see this thread's key
+                unsigned long long cm = 0;                       // columns that see this thread's key
                 if (!plain) {
-                    const int nq = min(s.Nq - col0, 8 * ncg);
                     if (!tree) {
-                        if (row < s.L) cm = (1ull << max(nq, 0)) - 1ull;
-                    } else if (row < s.Nb) {
-                        int n = (s.q0 + col0) / p.G, rest = (s.q0 + col0) - n * p.G;
-                        for (int c = 0; c < nq; ++c) {
-                            cm |= (unsigned long long)((sm->anc[n * p.words + (row >> 6)] >> (row & 63)) & 1ull) << c;
+                        if (key < s.L) cm = ~0ull;
+                    } else if (key < s.Nb) {
+                        int n = s.q0 / p.G, rest = s.q0 - n * p.G;
+                        for (int c = 0; c < s.Nq; ++c) {
+                            cm |= (unsigned long long)((sm->anc[n * p.words + (key >> 6)] >> (key & 63)) & 1ull) << c;
                             if (++rest == p.G) { rest = 0; ++n; }
                         }
                     }
                 }
-                if (!mbar_wait(&sm->s_full[buf], (g >> 1) & 1u, abort_flag, hdr, 41)) failed = true;
+                if (!mbar_wait(&sm->s_full[wg], (g >> 1) & 1u, abort_flag, hdr, 41)) failed = true;
+                if (!mbar_wait(&sm->fmt_full[g & 3u], (g >> 2) & 1u, abort_flag, hdr, 45)) failed = true;
+                // P^T is free once the products of the group's previous tile are done, and the accumulators are current
+                if (g >= 2 && !mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
                 tc_fence_after();
-                const uint32_t s_addr = lane_addr + Col::S + buf * Col::wide + col0;
+                const bool half = sm->fmt[g & 3u], first = g == g_own;
                 const float2 ab = sm->kab[g & 3u][r];
-                uint32_t pk[CPT][4];
-                float dmax = -INFINITY;
-                auto sweep = [&](auto masked_tag) {
-                    constexpr bool MASKED = decltype(masked_tag)::value;
-                    dmax = -INFINITY;
-#pragma unroll
-                    for (int j = 0; j < CPT; ++j) {
-                        if (j < ncg) {
-                            float y[8];
-                            tc_ld8(s_addr + 8 * j, y);
-                            const float4 q0 = *reinterpret_cast<const float4*>(qs + 8 * j), q1 = *reinterpret_cast<const float4*>(qs + 8 * j + 4);
-                            const float4 m0 = *reinterpret_cast<const float4*>(ref + 8 * j), m1 = *reinterpret_cast<const float4*>(ref + 8 * j + 4);
-                            const float qv[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
-                            const float mv[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
-                            tc_wait_ld();
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                y[k] = fmaf(y[k], ab.x, fmaf(qv[k], ab.y, -mv[k]));
-                                if (MASKED) y[k] = ((cm >> (8 * j + k)) & 1ull) ? y[k] : -INFINITY;
-                            }
-                            dmax = fmaxf(dmax, fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7]))));
-#pragma unroll
-                            for (int k = 0; k < 8; k += 2) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(ex2_approx(y[k]), ex2_approx(y[k + 1]));
-                                pk[j][k >> 1] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
-                        }
-                    }
-                };
-                if (plain) sweep(std::false_type{}); else sweep(std::true_type{});
-                // one vote per group: does any score exceed its reference by more than the lazy threshold?
-                if (group_sync_any(bar_id, dmax > kLazyTau || failed)) {
-                    if (group_sync_any(bar_id, failed)) { failed = true; break; }
-                    // exact column maxima of the tile, new references, what was accumulated rescaled
-#pragma unroll
-                    for (int j = 0; j < CPT; ++j) {
-                        if (j < ncg) {
+                const float2 a2 = make_float2(ab.x, ab.x), b2 = make_float2(ab.y, ab.y);
+                const uint32_t s_addr = lane_addr + Col::S + wg * QB;
+                // New references come first in a piece's first tile, and again where a score exceeds its reference by more
+                // than 2^8 after the optimistic sweep below, which is then redone.
+                bool raise = first, raised = false;
+                for (;;) {
+                    if (raise) {
+                        raised = true;
+#pragma unroll 1
+                        for (int j = 0; j < n8; ++j) {
                             float y[8];
                             tc_ld8(s_addr + 8 * j, y);
                             tc_wait_ld();
@@ -660,180 +723,181 @@ tree_attention_kv4_kernel(const Params p) {
                             }
                             if (lane < 8) sm->red[wg][wq][8 * j + lane] = mine;
                         }
-                    }
-                    group_sync_any(bar_id, false);
-                    bool need = false;
-                    if (r < 8 * ncg) {
-                        const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
-                        const float old = ref[r];
-                        float a = 1.f;
-                        if (top > old) {
-                            a = exp2f(old - top);
-                            ref[r] = top;
-                            need = i > s.lt;
+                        group_sync_any(bar_id, false);
+                        if (r < 8 * n8) {
+                            const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
+                            // (a column that has seen no key yet keeps one below any score)
+                            const float old = first ? -1e30f : -nref[r], now = fmaxf(old, top);
+                            nref[r] = -now;
+                            sm->alpha[wg][r] = exp2f(old - now);
                         }
-                        alph[r] = a;
-                    }
-                    const bool rescale = group_sync_any(bar_id, need);
-                    if (rescale) {
-                        if (g > 0 && !mbar_wait(&sm->pv_done[(g - 1u) & 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 42)) failed = true;
-                        tc_fence_after();
-#pragma unroll
-                        for (int j = 0; j < CPT; ++j) {
-                            if (j < ncg) {
+                        group_sync_any(bar_id, false);
+                        if (!first) {
+#pragma unroll 1
+                            for (int j = 0; j < 2 * n8; ++j) {   // accumulators, then row sums
+                                const int jj = j < n8 ? j : j - n8;
+                                const uint32_t at = lane_addr + (j < n8 ? Col::O : Col::L) + wg * QB + 8 * jj;
                                 float o[8];
-                                tc_ld8(lane_addr + Col::O + col0 + 8 * j, o);
+                                tc_ld8(at, o);
                                 tc_wait_ld();
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    o[k] *= alph[8 * j + k];
-                                    lsum[j][k] *= alph[8 * j + k];
+                                for (int k = 0; k < 8; ++k) o[k] *= sm->alpha[wg][8 * jj + k];
+                                tc_st8(at, o);
+                            }
+                            tc_wait_st();
+                        }
+                    }
+                    // scores of this thread's key relative to the references, exponentiated, packed, stored: two column
+                    // groups at a time (one is enough to keep the unit busy only with four times the warps)
+                    float dmax = -INFINITY;
+#pragma unroll 1
+                    for (int j = 0; j < n8; j += 2) {
+                        float y[2][8];
+                        tc_ld8(s_addr + 8 * j, y[0]);
+                        if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y[1]);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (j + h < n8) {
+                                const float* qj = qs + 8 * (j + h);
+                                const float* nj = nref + 8 * (j + h);
+#pragma unroll
+                                for (int k = 0; k < 8; k += 4) {
+                                    const float4 q = *reinterpret_cast<const float4*>(qj + k), m = *reinterpret_cast<const float4*>(nj + k);
+                                    const float2 u = fma_f32x2(make_float2(y[h][k], y[h][k + 1]), a2, fma_f32x2(make_float2(q.x, q.y), b2, make_float2(m.x, m.y)));
+                                    const float2 v = fma_f32x2(make_float2(y[h][k + 2], y[h][k + 3]), a2, fma_f32x2(make_float2(q.z, q.w), b2, make_float2(m.z, m.w)));
+                                    y[h][k] = u.x; y[h][k + 1] = u.y; y[h][k + 2] = v.x; y[h][k + 3] = v.y;
                                 }
-                                tc_st8(lane_addr + Col::O + col0 + 8 * j, o);
+                                if (!plain) {
+                                    const uint32_t bits = (uint32_t)(cm >> (8 * (j + h)));
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) y[h][k] = ((bits >> k) & 1u) ? y[h][k] : -INFINITY;
+                                }
+                                dmax = fmaxf(dmax, fmaxf(fmaxf(fmaxf(y[h][0], y[h][1]), fmaxf(y[h][2], y[h][3])), fmaxf(fmaxf(y[h][4], y[h][5]), fmaxf(y[h][6], y[h][7]))));
+                                uint32_t w[4];
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) y[h][k] = ex2_approx(y[h][k]);
+                                if (half) {
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) w[k] = pack_pair<true>(y[h][2 * k], y[h][2 * k + 1]);
+                                } else {
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) w[k] = pack_pair<false>(y[h][2 * k], y[h][2 * k + 1]);
+                                }
+                                *reinterpret_cast<uint4*>(p_own + (j + h) * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
                             }
                         }
-                        tc_wait_st();
                     }
-                    if (plain) sweep(std::false_type{}); else sweep(std::true_type{});
+                    raise = group_sync_any(bar_id, (dmax > kLazyTau && !raised) || failed);   // one vote of the group
+                    if (!raise) break;
+                    gone = group_sync_any(bar_id, failed);
+                    if (gone) break;
                 }
-                // row sums of the rounded weights, then P^T once the products of the previous tile no longer read it
-#pragma unroll
-                for (int j = 0; j < CPT; ++j)
-                    if (j < ncg) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) add_pair(lsum[j][2 * k], lsum[j][2 * k + 1], pk[j][k]);
-                    }
-                if (g > 0 && !mbar_wait(&sm->pv_done[(g - 1u) & 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
-#pragma unroll
-                for (int j = 0; j < CPT; ++j)
-                    if (j < ncg)
-                        *reinterpret_cast<uint4*>(p_buf + (g0 + j) * 2048 + r * 16) = make_uint4(pk[j][0], pk[j][1], pk[j][2], pk[j][3]);
+                if (gone) break;
+                tc_fence_before();
+                if (lane == 0) mbar_arrive(&sm->s_free[wg]);     // (the vote above came after everybody's last read)
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sm->p_full);
+                if (lane == 0) mbar_arrive(&sm->p_full[wg]);
             }
-            if (group_sync_any(bar_id, failed)) { failed = true; break; }
-
-            // ---- the piece is done: row sums over the 128 key rows, eight columns at a time.  Exchanging halves leaves
-            // lane x with the sum over the warp of column (x >> 2) & 7 (bits 4, 3, 2 of the lane, in this order).
-#pragma unroll
-            for (int j = 0; j < CPT; ++j) {
-                if (j < ncg) {
-                    float v[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = lsum[j][k];
-#pragma unroll
-                    for (int half = 4, bit = 16; half > 0; half >>= 1, bit >>= 1) {
-                        const bool up = lane & bit;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (k < half) {
-                                const float got = __shfl_xor_sync(0xffffffffu, up ? v[k] : v[k + half], bit);
-                                v[k] = (up ? v[k + half] : v[k]) + got;
-                            }
-                        }
-                    }
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 2);
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
-                    if ((lane & 3) == 0) sm->red[wg][wq][8 * j + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1)] = v[0];
-                }
+            // ---- the piece is done when the last products of both groups are
+            if (!gone && g_own < g_end) {
+                const uint32_t last = g_end - 1u - ((g_end - 1u - g_own) & 1u);
+                if (!mbar_wait(&sm->pv_done[wg], (last >> 1) & 1u, abort_flag, hdr, 44)) failed = true;
             }
-            if (!mbar_wait(&sm->pv_done[(g - 1u) & 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 44)) failed = true;
+            if (both_sync_any(failed || gone)) break;
             tc_fence_after();
-            if (group_sync_any(bar_id, failed)) { failed = true; break; }
             const bool whole = s.cnt == s.T;
             const int slot = 2 * (int)blockIdx.x + (t > t_begin ? 1 : 0);
-            if (r < 8 * ncg) {
-                const float l = (sm->red[wg][0][r] + sm->red[wg][1][r]) + (sm->red[wg][2][r] + sm->red[wg][3][r]);
-                if (whole) {
-                    alph[r] = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-                } else if (col0 + r < s.Nq) {
-                    p.part_ml[((size_t)slot * 2 + 0) * kWideQ + col0 + r] = ref[r];
-                    p.part_ml[((size_t)slot * 2 + 1) * kWideQ + col0 + r] = l;
-                }
-            }
-            group_sync_any(bar_id, false);
-            // rows of `out` of the group's columns: query j = q0 + column is head j % G, node j / G
-            auto put = [&](int c, float v) {
-                const int j = s.q0 + c, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
-                p.out[(((size_t)s.b * p.Hkv * p.G + h) * p.N + n) * kD + r] = __float2bfloat16_rn(v);
-            };
+            const bool has0 = s.cnt > 1 || !(g_piece & 1u), has1 = s.cnt > 1 || (g_piece & 1u);   // groups with a tile in the piece
+            const int* rows = sm->row[seg & 1u];
+            // the groups split the columns; thread r has channel r of both accumulators
+            const int j0 = wg ? (n8 + 1) / 2 : 0, j1 = wg ? n8 : (n8 + 1) / 2;
+#pragma unroll 1
+            for (int j = j0; j < j1; ++j) {
+                float o0[8], o1[8], l0[8], l1[8];
+                tc_ld8(lane_addr + Col::O + 8 * j, o0);
+                tc_ld8(lane_addr + Col::O + QB + 8 * j, o1);
+                tc_ld8(lane_addr + Col::L + 8 * j, l0);
+                tc_ld8(lane_addr + Col::L + QB + 8 * j, l1);
+                tc_wait_ld();
 #pragma unroll
-            for (int j = 0; j < CPT; ++j) {
-                if (j < ncg) {
-                    float o[8];
-                    tc_ld8(lane_addr + Col::O + col0 + 8 * j, o);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int c = col0 + 8 * j + k;
-                        if (c < s.Nq) {
-                            if (whole) put(c, o[k] * alph[8 * j + k]);
-                            else p.part_o[((size_t)slot * kWideQ + c) * kD + r] = o[k];
+                for (int k = 0; k < 8; ++k) {
+                    const int c = 8 * j + k;
+                    if (c < s.Nq) {
+                        const float m0 = has0 ? -sm->nref[0][c] : -1e30f, m1 = has1 ? -sm->nref[1][c] : -1e30f, M = fmaxf(m0, m1);
+                        const float w0 = ex2_approx(m0 - M), w1 = ex2_approx(m1 - M);
+                        const float o = (has0 ? o0[k] * w0 : 0.f) + (has1 ? o1[k] * w1 : 0.f);
+                        const float l = (has0 ? l0[k] * w0 : 0.f) + (has1 ? l1[k] * w1 : 0.f);
+                        if (whole) {
+                            p.out[(size_t)rows[c] * kD + r] = __float2bfloat16_rn(l != 0.f ? o / l : 0.f);
+                        } else {
+                            p.part_o[((size_t)slot * kWideQ + c) * kD + r] = o;
+                            if (r == 0) {
+                                p.part_ml[((size_t)slot * 2 + 0) * kWideQ + c] = M;
+                                p.part_ml[((size_t)slot * 2 + 1) * kWideQ + c] = l;
+                            }
                         }
                     }
                 }
             }
             if (!whole) {
-                // the group that finishes an item's last tile merges its columns of all pieces
+                // the block that finishes an item's last tile merges all pieces
                 __threadfence();
-                group_sync_any(bar_id, false);
-                if (r == 0) sm->merge[wg] = atomicAdd(&p.counters[2 * s.item + wg], s.cnt);
-                group_sync_any(bar_id, false);
-                if (sm->merge[wg] + s.cnt == s.T) {
+                both_sync_any(false);
+                const long long first = pl.tiles[s.b] + (long long)(s.item - pl.items[s.b]) * s.T;   // the item's first tile
+                if (tid == kSoftWarp * 32) sm->merge = atomicAdd(&p.counters[s.item], s.cnt);
+                // every block's piece of this item: its slot, or -1
+                const int c = tid - kSoftWarp * 32;
+                if (c < pl.blocks) {
+                    const long long a = pl.first[c], b = pl.first[c + 1];
+                    sm->slots[c] = max(a, first) < min(b, first + s.T) ? (short)(2 * c + (a < first ? 1 : 0)) : (short)-1;
+                }
+                both_sync_any(false);
+                if (sm->merge + s.cnt == s.T) {
                     __threadfence();
-                    const long long it0 = (long long)(s.item - pl.items[s.b]) * s.T;     // the item's first tile, in its sequence
-                    const int c0 = block_of<QB>(pl, p, s.b, it0), c1 = block_of<QB>(pl, p, s.b, it0 + s.T - 1);
-                    const long long first = pl.tiles[s.b] + it0;
-                    // slot of block c's piece of this item, or -1
-                    auto slot_of = [&](int c) -> int {
-                        const long long a = first_tile<QB>(pl, p, c), b = first_tile<QB>(pl, p, c + 1);
-                        if (max(a, first) >= min(b, first + s.T)) return -1;
-                        return 2 * c + (a < first ? 1 : 0);
-                    };
-                    if (r < 8 * ncg && col0 + r < s.Nq) {
-                        float M = -INFINITY, l = 0.f;
-                        for (int c = c0; c <= c1; ++c) {
-                            const int sl = slot_of(c);
-                            if (sl >= 0) M = fmaxf(M, __ldcg(&p.part_ml[((size_t)sl * 2) * kWideQ + col0 + r]));
-                        }
-                        for (int c = c0; c <= c1; ++c) {
-                            const int sl = slot_of(c);
-                            if (sl >= 0)
-                                l += exp2f(__ldcg(&p.part_ml[((size_t)sl * 2) * kWideQ + col0 + r]) - M) *
-                                     __ldcg(&p.part_ml[((size_t)sl * 2 + 1) * kWideQ + col0 + r]);
-                        }
-                        ref[r] = M;
-                        alph[r] = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-                    }
-                    group_sync_any(bar_id, false);
+                    // the item's pieces lie in consecutive blocks, this one among them
+                    int c0 = blockIdx.x, c1 = blockIdx.x + 1;
+                    while (c0 > 0 && pl.first[c0] > first) --c0;
+                    while (c1 < pl.blocks && pl.first[c1] < first + s.T) ++c1;
 #pragma unroll 1
-                    for (int j = 0; j < ncg; ++j) {
-                        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                        for (int c = c0; c <= c1; ++c) {
-                            const int sl = slot_of(c);
+                    for (int j = j0; j < j1; ++j) {
+                        float M[8], l[8], o[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) { M[k] = -INFINITY; l[k] = 0.f; o[k] = 0.f; }
+#pragma unroll 1
+                        for (int x = c0; x < c1; ++x) {
+                            const int sl = sm->slots[x];
                             if (sl < 0) continue;
+                            const float* ml = p.part_ml + (size_t)sl * 2 * kWideQ + 8 * j;
+                            const float* po = p.part_o + ((size_t)sl * kWideQ + 8 * j) * kD + r;
+                            float mx[8], lx[8], ox[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (8 * j + k < s.Nq) { mx[k] = __ldcg(ml + k); lx[k] = __ldcg(ml + kWideQ + k); ox[k] = __ldcg(po + k * kD); }
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                const int q = col0 + 8 * j + k;
-                                if (q < s.Nq)
-                                    acc[k] = fmaf(exp2f(__ldcg(&p.part_ml[((size_t)sl * 2) * kWideQ + q]) - ref[8 * j + k]),
-                                                  __ldcg(&p.part_o[((size_t)sl * kWideQ + q) * kD + r]), acc[k]);
+                                if (8 * j + k < s.Nq) {
+                                    const float m = fmaxf(M[k], mx[k]), w0 = ex2_approx(M[k] - m), w1 = ex2_approx(mx[k] - m);
+                                    l[k] = l[k] * w0 + lx[k] * w1;
+                                    o[k] = o[k] * w0 + ox[k] * w1;
+                                    M[k] = m;
+                                }
                             }
                         }
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            if (col0 + 8 * j + k < s.Nq) put(col0 + 8 * j + k, acc[k] * alph[8 * j + k]);
+                            if (8 * j + k < s.Nq) p.out[(size_t)rows[8 * j + k] * kD + r] = __float2bfloat16_rn(l[k] != 0.f ? o[k] / l[k] : 0.f);
                     }
-                    if (r == 0) p.counters[2 * s.item + wg] = 0;
-                    group_sync_any(bar_id, false);               // the references are read by all
+                    if (tid == kSoftWarp * 32) p.counters[s.item] = 0;
                 }
             }
             tc_fence_before();
-            __syncwarp();
+            both_sync_any(false);                                // references, rows and accumulators have been read
             if (lane == 0) mbar_arrive(&sm->piece_done[seg & 1u]);
             t += s.cnt;
+            g_piece = g_end;
         }
     }
 
@@ -850,12 +914,12 @@ tree_attention_kv4_kernel(const Params p) {
 int columns_for(int nq) {
     const int blocks = (nq + kWideQ - 1) / kWideQ;
     const int per = ((nq + blocks - 1) / blocks + 7) & ~7;
-    return per <= 16 ? 16 : per <= 32 ? 32 : per <= 48 ? 48 : per <= 64 ? 64 : kWideQ;
+    return per <= 16 ? 16 : per <= 32 ? 32 : per <= 48 ? 48 : kWideQ;
 }
 
 template <int QB>
 int launch(const Params& p, int grid, cudaStream_t stream) {
-    constexpr size_t smem_bytes = 1024 + 3 * QB * 256 + (size_t)kStages * kStageBytes + sizeof(Small<QB>);
+    constexpr size_t smem_bytes = 1024 + 4 * QB * 256 + (size_t)kStages * kStageBytes + sizeof(Small<QB>);
     static_assert(smem_bytes <= kSmemLimit, "ring and buffers fit the block's shared memory");
     static std::mutex mu;                                        // the opt-in to large shared memory is per device
     static bool done[64] = {};
@@ -888,11 +952,15 @@ constexpr size_t kOBytes = (size_t)2 * kMaxCtas * kWideQ * kD * sizeof(float);
 
 }  // namespace
 
-bool kv4_tc_shape(int B, int H, int G, int N, int D, int L_max, int dtype) { return tc_shape_supported(B, H, G, N, D, L_max, dtype); }
+// The shapes of the tensor-core kernel over dense caches, as long as the tiles of one sequence can be counted in 31 bits.
+bool kv4_tc_shape(int B, int H, int G, int N, int D, int L_max, int dtype) {
+    const long long blocks_q = ((long long)G * N + kWideQ - 1) / kWideQ;
+    return tc_shape_supported(B, H, G, N, D, L_max, dtype) && (H / G) * blocks_q * ((long long)L_max / kTile + 4) < (1LL << 31);
+}
 
 size_t kv4_tc_workspace_bytes(int B, int H, int G, int N) {
-    const size_t blocks_q = ((size_t)G * N + kWideQ - 1) / kWideQ * 2;   // narrower launches cut finer, by less than two
-    return kMlBytes + kOBytes + align_up((size_t)B * (H / G) * blocks_q * 2 * sizeof(int), 256);
+    const size_t blocks_q = ((size_t)G * N + kWideQ - 1) / kWideQ;
+    return kMlBytes + kOBytes + align_up((size_t)B * (H / G) * blocks_q * sizeof(int), 256);
 }
 
 int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scratch, cudaStream_t stream) {
@@ -924,7 +992,6 @@ int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void*
         case 16: return launch<16>(p, grid, stream);
         case 32: return launch<32>(p, grid, stream);
         case 48: return launch<48>(p, grid, stream);
-        case 64: return launch<64>(p, grid, stream);
         default: return launch<kWideQ>(p, grid, stream);
     }
 }
