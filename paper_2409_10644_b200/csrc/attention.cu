@@ -135,7 +135,8 @@ extern "C" int mcsd_tree_attention_kv4(const void* q, const void* cache, const v
                           B, H_q, N, D, L_max, softmax_scale, dtype, H_q / H_kv, cache};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     void* scratch = static_cast<char*>(workspace) + sizeof(mcsd::WorkspaceHeader);
-    if (mcsd::kv4_tc_shape(B, H_q, a.G, N, D, L_max, dtype) && mcsd::aligned16(q) && mcsd::aligned16(k_tree))
+    if (mcsd::kv4_tc_shape(B, H_q, a.G, N, D, L_max, dtype) && mcsd::aligned16(q) && mcsd::aligned16(k_tree) &&
+        mcsd::aligned16(out))
         return mcsd::tree_attention_kv4_tc(a, static_cast<mcsd::WorkspaceHeader*>(workspace), scratch, s);
     return mcsd::tree_attention_simt(a, scratch, s);
 }

@@ -2,28 +2,30 @@
 // fifth-generation tensor cores of sm_100a: bf16 tree tensors, head_dim 128, 1 to 64 query columns per work item.
 //
 // The products are set up transposed, the small dimension (query columns) as the MMA N:
-//     S^T[key][query] = K Q^T,     O^T[channel][query] += V^T P^T,     l[query] += 1 P^T
-// and the A operands live in tensor memory, not in shared memory: thread r of the key warps owns key row r of a
+//     S^T[key][query] = K Q^T,     O^T[channel][query] += V^T P^T,     l[query] += P 1
+// and the A operands of the first two live in tensor memory, not in shared memory: thread r of the key warps owns key row r of a
 // 128-key tile, thread d of the value warps channel d, and both turn 16-byte pieces of a page (neighbouring threads read
 // neighbouring pieces) into operand columns with a shift and a mask per two values and store them with tcgen05.st.
-//   * Keys stay codes: 16 + code is exact in bf16, so S' = sum (16 + code) q is exact up to fp32 sums, and the row's scale
-//     and offset are applied to the score, where the softmax thread owns the same key row:
-//         score = scale_k S' + offset_k (sum of q).
+//   * Keys stay codes: the byte c (0..15) is c 2^-9 in e4m3 (its two lowest binades have the same spacing), so eight codes
+//     become operands with two masks and a shift.  Queries are split into two e4m3 parts, high and low, on a scale common to the
+//     work item: together they hold the eight bits of a bf16 number down to 2^-18 of the item's largest.  The sums are exact up
+//     to fp32, and the row's scale and offset are applied to the score, where the softmax thread owns the same key row:
+//         score = scale_k (sum of code q) + (16 scale_k + offset_k) (sum of q).
 //   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
 //     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
 //     whose values lie well inside fp16's range, which the value warps vote on tile by tile; else bf16.
-// The rows of the tree itself are read as they are (bf16): same operand columns, scale 1, offset 0.
+// The rows of the tree itself are read as they are (bf16, against the bf16 queries): scale 1, offset 0.
 //
 // What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; unpacking
 // and the exponentials then share the issue slots of the schedulers, so the work is spread over specialised warps:
-//   warps 0-3    keys      page pieces -> operand columns
-//   warps 4-7    values    page pieces -> operand columns
-//   warps 8-11   softmax of the even tiles, all columns;  warps 12-15 of the odd ones.  The two groups have their own
-//                references, accumulators and row sums and meet only at the end of a work item: with one group per tile
-//                a tile's chain (scores, vote, exponentials, P^T, products) may take twice the time between two tiles
-//   warp 16      copies whole pages (1 to 4 of them, contiguous) into a ring with cp.async.bulk
-//   warp 17      issues the MMAs and owns the tensor memory
-//   warps 18-19  bring the queries of the next work item and their sums
+//   warps 0-3    keys      page pieces -> operand columns, and the scales of the value rows
+//   warps 4-11   values    page pieces -> operand columns; warps 4-7 the even tiles, 8-11 the odd ones
+//   warps 12-19  softmax   warps 12-15 the even tiles, 16-19 the odd ones.  The two groups have their own references,
+//                accumulators and row sums and meet only at the end of a work item: a tile's chain (scores, exponentials, vote,
+//                P^T, products) may take twice the time between two tiles
+//   warp 20      copies whole pages (1 to 4 of them, contiguous) into a ring with cp.async.bulk
+//   warps 21, 22 issue the MMAs of the scores and of the products
+//   warp 23      brings the queries of the next work item and their sums
 // Loops are rolled as far as the latencies allow: the roles share the instruction caches, and with unrolled bodies (a
 // kernel of 180 KB) a tile took three times as long, most of it in waits for instructions.
 //
@@ -47,23 +49,17 @@ namespace {
 constexpr int kD = 128;
 constexpr int kPageBytes = kv4_page_bytes(kD);
 constexpr int kStageBytes = 4 * kPageBytes;      // one tile: 128 rows
-constexpr int kValueWarp = 4, kSoftWarp = 8, kCopyWarp = 16, kIssueWarp = 17, kQueryWarp = 18;
-constexpr int kThreads = 640;
+constexpr int kValueWarp = 4, kSoftWarp = 12, kSides = 1, kCopyWarp = 12 + 8 * kSides, kScoreWarp = kCopyWarp + 1, kProductWarp = kCopyWarp + 2, kQueryWarp = kCopyWarp + 3;
+constexpr int kThreads = 32 * (kQueryWarp + 1), kSoftThreads = 256 * kSides;
 constexpr int kWideQ = 64;                       // query columns of a work item, at most
-constexpr int kStages = 6;
-constexpr int kMaxPieces = kMaxCtas;             // of a work item
-// Tensor-memory columns: scores, O^T and row sums of the two softmax groups, then keys and values, twice where it fits,
-// and the ones of the row sums' A operand (bf16, fp16; they are in shared memory where no column is left, and such a
-// product takes 41 cycles instead of 12 at 16 columns, 50 instead of 34 at 64).
+template <int QB> constexpr int kStages = QB > 48 ? 5 : 6;
+// Tensor-memory columns: scores, O^T and row sums of the two softmax groups (the sums with a query per lane and sixteen identical
+// columns, of which the first counts), keys (two buffers of codes; a tile of tree rows takes
+// both), values.
 template <int QB>
 struct Columns {
-    static constexpr int S = 0, O = 2 * QB, L = 4 * QB, K = 6 * QB;
-    static constexpr bool ones = K + 128 + 16 <= kTmemCols;
-    static constexpr int key_buffers = K + 256 + 16 <= kTmemCols ? 2 : 1;
-    static constexpr int V = K + 64 * key_buffers;
-    static constexpr int value_buffers = V + 128 + 16 <= kTmemCols ? 2 : 1;
-    static constexpr int One = V + 64 * value_buffers;
-    static_assert(One + (ones ? 16 : 0) <= kTmemCols, "tensor memory");
+    static constexpr int S = 0, O = 2 * QB, L = 4 * QB, K = L + 32, V = K + 64;
+    static_assert(V + 128 <= kTmemCols, "tensor memory");
 };
 
 struct Params {
@@ -140,7 +136,8 @@ template <int QB>
 __device__ __forceinline__ long long first_tile(const Plan& pl, const Params& p, int c) {
     const long long total = pl.cost[p.B];
     if (c >= pl.blocks) return pl.tiles[p.B];
-    const long long x = (total * c + pl.blocks - 1) / pl.blocks;
+    const long long xc = total * c + pl.blocks - 1;           // (a 64-bit division takes a thousand cycles)
+    const long long x = (unsigned long long)xc >> 32 ? xc / pl.blocks : (long long)((uint32_t)xc / (uint32_t)pl.blocks);
     int lo = 0, hi = p.B;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -150,8 +147,9 @@ __device__ __forceinline__ long long first_tile(const Plan& pl, const Params& p,
     if (sh.T == 0) return pl.tiles[p.B];
     const int w = tile_cost(sh.per_q);
     const long long ci = (long long)sh.T * w + kItemCost, off = x - pl.cost[lo];
-    const long long it = off / ci, rem = off - it * ci;
-    const long long lt = (rem + w - 1) / w;
+    const long long it = (unsigned long long)off >> 32 || ci >> 32 ? off / ci : (long long)((uint32_t)off / (uint32_t)ci);
+    const long long rem = off - it * ci;                      // below T * w + the item's cost, T below 2^23
+    const int lt = (int)(((uint32_t)rem + (uint32_t)w - 1u) / (uint32_t)w);
     return pl.tiles[lo] + it * sh.T + (lt < sh.T ? lt : sh.T);
 }
 
@@ -207,23 +205,28 @@ __device__ void make_plan(Plan& pl, const Params& p) {
 
 template <int QB>
 struct Small {
-    unsigned long long full[kStages], empty[kStages];
-    unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], q_full[2], piece_done[2], fmt_full[4];
+    unsigned long long full[kStages<QB>], empty[kStages<QB>];
+    unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], q_full[2], piece_done[2], scales_full[8];
     unsigned long long drain;
     uint32_t tmem_base;
     int abort_flag;
-    int merge, merge_pieces;                          // tiles of the item finished before this block's; its pieces
-    int fmt[4];                                       // 1: the tile's values and weights are fp16, 0: bf16
+    struct Merge {                                    // a cut work item, first or last of this block
+        int before, cnt, T, hk, b, q0, Nq;            // tiles finished before this block's cnt, of T
+        long long first;                              // the item's first tile
+    } merge[2];
+    int q_max;                                        // largest |query| of the first piece, as bits
+    float q_factor[2];                                // brings sums over codes to score units
+    int fmt[8];                                       // 1: the tile's values and weights are fp16, 0: bf16
     int row[2][QB];                                   // rows of q and out of the piece's columns
-    short slots[kMaxPieces];                          // of the pieces that are merged
     alignas(16) float2 kab[4][kTile];                 // scale and offset of a tile's key rows, in score units
-    alignas(16) unsigned short vab[2][2][kTile];      // scales and offsets of a tile's value rows, in the tile's format
+    alignas(16) unsigned short vab[8][2][kTile];      // scales and offsets of a tile's value rows, in the tile's format
     alignas(16) float q_sum[2][QB];
     alignas(16) float nref[2][QB];                    // running references of the two groups, negated
-    alignas(16) float alpha[2][QB];
+    alignas(16) float alpha[2][QB];                   // rescale factors of the two groups; at the end of a piece their weights
     alignas(16) float red[2][4][QB];
     alignas(16) uint64_t anc[MCSD_MAX_NODES * MCSD_MAX_WORDS];
-    alignas(16) unsigned short ones[2][kTile * 16];   // A operand of the row sums: bf16, fp16
+    alignas(128) unsigned short ones[2][256];         // B operand of the row sums: bf16, fp16
+    Piece piece[2];                                   // of the queries in the two buffers
     Plan plan;
 };
 
@@ -264,15 +267,39 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t (&v)[16])
         ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
           "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
+__device__ __forceinline__ void mma_ta8(uint32_t d_tmem, uint32_t a_tmem, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// two numbers to e4m3 (b in the upper byte) and back
+__device__ __forceinline__ uint32_t to_e4m3x2(float a, float b) {
+    unsigned short d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(b), "f"(a));
+    return d;
+}
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)v));
+    const __half2 x = *reinterpret_cast<const __half2*>(&h);
+    return __half22float2(x);
+}
+// (x & mask) | base, as the one instruction it is (left to itself the compiler makes it two)
+__device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(x), "r"(mask), "r"(base));
+    return d;
+}
 // codes (2i, 2i + 1) of a word as two numbers 16 + code: bf16 (code in mantissa bits 3..6) or fp16 (bits 6..9)
 template <bool HALF>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w, int i) {
     if (HALF) {
         const uint32_t x = i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6);
-        return (x & 0x03C003C0u) | 0x4C004C00u;
+        return and_or(x, 0x03C003C0u, 0x4C004C00u);
     }
     const uint32_t x = i == 0 ? w << 3 : w >> (4 * i - 3);
-    return (x & 0x00780078u) | 0x41804180u;
+    return and_or(x, 0x00780078u, 0x41804180u);
 }
 template <bool HALF>
 __device__ __forceinline__ uint32_t fma_x2(uint32_t a, uint32_t b, uint32_t c) {
@@ -281,12 +308,16 @@ __device__ __forceinline__ uint32_t fma_x2(uint32_t a, uint32_t b, uint32_t c) {
     else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
+// eight weights as four pairs
 template <bool HALF>
-__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {
-    uint32_t d;
-    if (HALF) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
+__device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (HALF) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[2 * k + 1]), "f"(y[2 * k]));
+        else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[2 * k + 1]), "f"(y[2 * k]));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // two fp32 fused multiply-adds in one instruction
 __device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
@@ -297,15 +328,15 @@ __device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
-// barrier over both softmax groups
-__device__ __forceinline__ bool both_sync_any(bool pred) {
+// barrier over all softmax warps
+__device__ __forceinline__ bool soft_sync_any(bool pred) {
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.u32 p, %1, 0;\n\t"
-        "bar.red.or.pred q, 4, 256, p;\n\t"
+        "bar.red.or.pred q, 7, %2, p;\n\t"
         "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(r) : "r"((uint32_t)pred) : "memory");
+        : "=r"(r) : "r"((uint32_t)pred), "n"(kSoftThreads) : "memory");
     return r != 0;
 }
 // A row of values may be fp16: no value can leave its range, and neither scale nor values are so small that fp16's fixed
@@ -315,57 +346,133 @@ __device__ __forceinline__ bool fits_half(float scale, float offset) {
     return 31.f * scale + o <= 32768.f && (scale >= 6.103515625e-5f || (scale == 0.f && (o == 0.f || o >= 6.103515625e-5f)));
 }
 
+// Queries of a piece, sixteen lanes per row, lane c channels 8c .. 8c + 7.  In two steps, since the second needs the largest
+// of them all.  Operand layouts: rows of 128 bytes with the 16-byte pieces of a row exchanged by row % 8; bf16 in two
+// slabs of 64 channels, the e4m3 parts (high, low) behind them.  Codes come out of a word in the order 0 4 1 5 2 6 3 7, so the
+// e4m3 channels are stored in that order.  Rows from the last query on are zeros.  Stacked query j of a key/value head
+// is head j % G of its group, node j / G.
+template <int QB>
+__device__ __forceinline__ float load_query(Small<QB>* sm, unsigned char* q_buf, const Params& p, const Piece& s, uint32_t buf, int r, int c) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < s.Nq) {
+        const int j = s.q0 + r, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
+        const int row = (s.b * p.Hkv * p.G + h) * p.N + n;          // below 65535 * 192
+        v = *reinterpret_cast<const uint4*>(p.q + (size_t)row * kD + c * 8);
+        if (c == 0) sm->row[buf][r] = row;
+    }
+    *reinterpret_cast<uint4*>(q_buf + buf * (QB * 512) + (c >> 3) * (QB * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16)) = v;
+    float sum = 0.f, top = 0.f;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xFFFF0000u);
+        sum += a + b;
+        top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+    }
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+    if (c == 0) sm->q_sum[buf][r] = sum;
+    return top;
+}
+// the power of two that brings the largest query to 128 .. 256 (e4m3 ends at 448)
+__device__ __forceinline__ float query_scale(float top) {
+    const int e = (int)(__float_as_uint(top) >> 23);               // of a number that is not negative
+    return top > 0.f && e < 255 ? __uint_as_float((uint32_t)(min(max(127 + 7 - (e - 127), 27), 227)) << 23) : 1.f;
+}
+template <int QB>
+__device__ __forceinline__ void split_query(unsigned char* q_buf, uint32_t buf, float scale, int r, int c) {
+    const uint4 v = *reinterpret_cast<const uint4*>(q_buf + buf * (QB * 512) + (c >> 3) * (QB * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16) * scale;
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) * scale;
+    }
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                                    // channels 0 4 1 5, then 2 6 3 7
+        const float a = x[2 * i], b = x[2 * i + 4], d = x[2 * i + 1], e = x[2 * i + 5];
+        const uint32_t h0 = to_e4m3x2(a, b), h1 = to_e4m3x2(d, e);
+        const float2 f0 = from_e4m3x2(h0), f1 = from_e4m3x2(h1);
+        hi[i] = h0 | (h1 << 16);
+        lo[i] = to_e4m3x2(a - f0.x, b - f0.y) | (to_e4m3x2(d - f1.x, e - f1.y) << 16);
+    }
+    unsigned char* at = q_buf + buf * (QB * 512) + QB * 256 + r * 128 + (((c >> 1) ^ (r & 7)) * 16) + (c & 1) * 8;
+    *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
+    *reinterpret_cast<uint2*>(at + QB * 128) = make_uint2(lo[0], lo[1]);
+}
+
 template <int QB>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attention_kv4_kernel(const Params p) {
     using Col = Columns<QB>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);   // (an offset: the compiler keeps knowing it is shared memory)
-    unsigned char* q_buf = smem;                      // two buffers of QB rows: [2 slabs of 64 channels][QB rows][128 bytes], swizzled
-    unsigned char* p_buf = q_buf + 2 * QB * 256;      // P^T of the two groups: [QB / 8][128 keys][16 bytes]
+    unsigned char* q_buf = smem;                      // two buffers of QB rows: [2 bf16 slabs, high, low][QB rows][128 bytes]
+    unsigned char* p_buf = q_buf + 2 * QB * 512;      // P^T of the two groups: [QB / 8][128 keys][16 bytes]
     unsigned char* ring = p_buf + 2 * QB * 256;
-    Small<QB>* sm = reinterpret_cast<Small<QB>*>(ring + kStages * kStageBytes);
+    Small<QB>* sm = reinterpret_cast<Small<QB>*>(ring + kStages<QB> * kStageBytes);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- set-up; what comes before the wait touches no global memory and overlaps the tail of the preceding kernel
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 8); }
+        for (int i = 0; i < kStages<QB>; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 8); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm->k_full[i], 4);
             mbar_init(&sm->s_full[i], 1);
-            mbar_init(&sm->s_free[i], 4);
+            mbar_init(&sm->s_free[i], 4 * kSides);
             mbar_init(&sm->v_full[i], 4);
-            mbar_init(&sm->p_full[i], 4);
+            mbar_init(&sm->p_full[i], 4 * kSides);
             mbar_init(&sm->pv_done[i], 1);
-            mbar_init(&sm->q_full[i], 2);
-            mbar_init(&sm->piece_done[i], 8);
+            mbar_init(&sm->q_full[i], 1);
+            mbar_init(&sm->piece_done[i], kSoftThreads / 32);
         }
-        for (int i = 0; i < 4; ++i) mbar_init(&sm->fmt_full[i], 4);
-        mbar_init(&sm->drain, 1);
+        for (int i = 0; i < 8; ++i) mbar_init(&sm->scales_full[i], 4);
+        mbar_init(&sm->drain, 2);
         sm->abort_flag = 0;
+        sm->q_max = 0;
+        sm->merge[0].T = sm->merge[1].T = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int i = tid; i < kTile * 16; i += kThreads) { sm->ones[0][i] = 0x3F80; sm->ones[1][i] = 0x3C00; }
+    if (tid < 256) { sm->ones[0][tid] = 0x3F80; sm->ones[1][tid] = 0x3C00; }
     fence_async_smem();                               // read by the tensor cores through the async proxy
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int i = tid; i < p.N * p.words; i += kThreads) sm->anc[i] = p.anc[i];
+    for (int i = tid - kMaxBatchTc; i >= 0 && i < p.N * p.words; i += kThreads - kMaxBatchTc) sm->anc[i] = p.anc[i];
     make_plan<QB>(sm->plan, p);
     const Plan& pl = sm->plan;
     const long long t_begin = pl.first[blockIdx.x], t_end = pl.first[blockIdx.x + 1];
     if (t_begin >= t_end) return;                     // uniform for the whole block: nothing allocated yet
 
-    if (warp == kIssueWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(kTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = *(volatile uint32_t*)&sm->tmem_base;
     WorkspaceHeader* const hdr = p.header;
     int* const abort_flag = &sm->abort_flag;
+    uint32_t tmem = 0;
+    if (warp != kCopyWarp) {                          // whose first loads are on their way meanwhile
+        if (warp == kScoreWarp) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm->tmem_base)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+        // the first piece's queries, by everybody
+        Piece s;
+        piece_at<QB>(pl, p, t_begin, t_end, s);
+        const int r0 = warp > kCopyWarp ? (tid >> 4) - 2 : tid >> 4, c = tid & 15, rows = (s.Nq + 15) & ~15;
+        constexpr int at_once = (kThreads - 32) / 16;
+        float top = 0.f;
+        for (int r = r0; r < rows; r += at_once) top = fmaxf(top, load_query<QB>(sm, q_buf, p, s, 0, r, c));
+        top = warp_max_f32(top);
+        if (lane == 0) atomicMax(&sm->q_max, __float_as_int(top));
+        tc_fence_before();
+        asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+        tc_fence_after();
+        tmem = *(volatile uint32_t*)&sm->tmem_base;
+        const float scale = query_scale(__int_as_float(sm->q_max));
+        for (int r = r0; r < rows; r += at_once) split_query<QB>(q_buf, 0, scale, r, c);
+        if (tid == 0) { sm->q_factor[0] = 512.f / scale; sm->piece[0] = s; }
+        fence_async_smem();
+        asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+    }
 
     // Tiles of this block are numbered g = 0, 1, ... across its pieces; f counts those that come through the ring.
     if (warp == kCopyWarp) {
@@ -379,8 +486,8 @@ tree_attention_kv4_kernel(const Params p) {
                 piece_at<QB>(pl, p, t, t_end, s);
                 const unsigned char* head = p.cache + ((size_t)s.b * p.Hkv + s.hk) * p.pages * kPageBytes;
                 for (int i = s.lt; i < min(s.lt + s.cnt, s.Tp) && ok; ++i, ++f) {
-                    const uint32_t st = f % kStages;
-                    if (f >= kStages) ok = mbar_wait(&sm->empty[st], (f / kStages - 1u) & 1u, abort_flag, hdr, 31);
+                    const uint32_t st = f % kStages<QB>;
+                    if (f >= kStages<QB>) ok = mbar_wait(&sm->empty[st], (f / kStages<QB> - 1u) & 1u, abort_flag, hdr, 31);
                     if (!ok) break;
                     const uint32_t bytes = (uint32_t)(min(kTile, s.L - i * kTile) + kPageRows - 1) / kPageRows * kPageBytes;
                     mbar_expect_tx(&sm->full[st], bytes);
@@ -392,168 +499,193 @@ tree_attention_kv4_kernel(const Params p) {
                 t += s.cnt;
             }
             if (!ok) {                                // gave up: let the copies already issued land before the block exits
-                for (uint32_t x = f > kStages ? f - kStages : 0; x < f; ++x) {
+                for (uint32_t x = f > kStages<QB> ? f - kStages<QB> : 0; x < f; ++x) {
                     const long long t0 = clock64();
-                    while (!mbar_try_wait(&sm->full[x % kStages], (x / kStages) & 1u) && clock64() - t0 < kSpinCycles / 8) {}
+                    while (!mbar_try_wait(&sm->full[x % kStages<QB>], (x / kStages<QB>) & 1u) && clock64() - t0 < kSpinCycles / 8) {}
                 }
             }
         }
-    } else if (warp == kIssueWarp) {
-        // S^T of tile g + 1 is issued before the products of tile g, across pieces as well
+    } else if (warp == kScoreWarp) {
         const uint64_t dq0 = smem_desc(smem_u32(q_buf), 16, 1024, 2);
-        const uint64_t dp0 = smem_desc(smem_u32(p_buf), 128, 2048, 0);
-        const uint64_t d1 = smem_desc(smem_u32(sm->ones), 128, 256, 0);
-        constexpr uint32_t q_slab = (QB * 128) >> 4, q_next = (QB * 256) >> 4, p_next = (QB * 256) >> 4, one_next = (kTile * 32) >> 4;
-        const uint32_t n_tiles = (uint32_t)(t_end - t_begin);
-        Piece s;                                      // of the scores
-        long long ts = t_begin;
-        int si = 0, oi = 0, o_cnt = 0, o_nq = 0;      // the products are one tile behind: in the same piece or the one before
-        uint32_t seg = 0;
+        constexpr uint32_t q_slab = (QB * 128) >> 4, q_next = (QB * 512) >> 4;
+        uint32_t g = 0, seg = 0;
         bool ok = true;
-        s.cnt = 0;
-        for (uint32_t g = 0; g <= n_tiles && ok; ++g) {
-            if (g < n_tiles) {
-                if (si == s.cnt) {
-                    ts += s.cnt;
-                    piece_at<QB>(pl, p, ts, t_end, s);
-                    si = 0;
-                    ok = mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 32);
-                    if (!ok) break;
-                    ++seg;
-                }
+        for (long long t = t_begin; t < t_end && ok; ++seg) {
+            Piece s;
+            piece_at<QB>(pl, p, t, t_end, s);
+            ok = mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 32);
+            const uint32_t idesc = instr_desc((s.Nq + 15) & ~15, 0, 0), idesc8 = idesc & ~((1u << 7) | (1u << 10));   // e4m3 is format 0
+            const uint64_t dq = dq0 + (seg & 1u) * q_next;
+            for (int i = s.lt; i < s.lt + s.cnt && ok; ++i, ++g) {
                 const uint32_t buf = g & 1u;
                 ok = mbar_wait(&sm->k_full[buf], (g >> 1) & 1u, abort_flag, hdr, 33);
                 if (ok && g >= 2) ok = mbar_wait(&sm->s_free[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 46);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t idesc = instr_desc((s.Nq + 15) & ~15, 0, 0);
-                    const uint64_t dq = dq0 + ((seg - 1u) & 1u) * q_next;
-                    const uint32_t d = tmem + Col::S + buf * QB, ka = tmem + Col::K + (Col::key_buffers == 2 ? buf * 64 : 0u);
+                    const uint32_t d = tmem + Col::S + buf * QB;
+                    if (i < s.Tp) {                   // 32 channels per MMA: high parts, then low parts
+                        const uint32_t ka = tmem + Col::K + buf * 32;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) mma_ta(d, ka + 8 * k, dq + (uint32_t)(k >> 2) * q_slab + (uint32_t)(k & 3) * 2u, idesc, k > 0);
+                        for (int k = 0; k < 8; ++k)
+                            mma_ta8(d, ka + 8 * (k & 3), dq + (uint32_t)(2 + (k >> 2)) * q_slab + (uint32_t)(k & 3) * 2u, idesc8, k > 0);
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < 8; ++k)
+                            mma_ta(d, tmem + Col::K + 8 * k, dq + (uint32_t)(k >> 2) * q_slab + (uint32_t)(k & 3) * 2u, idesc, k > 0);
+                    }
                     commit(&sm->s_full[buf]);
                 }
                 __syncwarp();
-                ++si;
             }
-            if (g >= 1) {
-                const uint32_t h = g - 1u, hb = h & 1u;
-                ok = mbar_wait(&sm->v_full[hb], (h >> 1) & 1u, abort_flag, hdr, 34);
-                if (ok) ok = mbar_wait(&sm->p_full[hb], (h >> 1) & 1u, abort_flag, hdr, 35);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
-                    // fp16 operands are format 0 of both operand fields, bf16 is 1
-                    const uint32_t half = sm->fmt[h & 3u];
-                    const uint32_t idesc = instr_desc((o_nq + 15) & ~15, 0, 1) & ~(half ? (1u << 7) | (1u << 10) : 0u);
-                    const uint32_t d = tmem + Col::O + hb * QB, l = tmem + Col::L + hb * QB;
-                    const uint32_t va = tmem + Col::V + (Col::value_buffers == 2 ? hb * 64 : 0u), one = tmem + Col::One + half * 8;
-                    const uint64_t dp = dp0 + hb * p_next, d1h = d1 + half * one_next;
-                    const uint32_t more = oi >= 2;    // a group's first tile of a piece overwrites
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        mma_ta(d, va + 8 * k, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
-                        if (Col::ones) mma_ta(l, one, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
-                        else mma_sa(l, d1h, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
-                    }
-                    commit(&sm->pv_done[hb]);
-                }
-                __syncwarp();
-                ++oi;
-            }
-            if (oi == o_cnt) { oi = 0; o_cnt = s.cnt; o_nq = s.Nq; }   // the next products belong to the scores' piece
+            t += s.cnt;
         }
         if (elect_one()) commit(&sm->drain);          // all MMAs have finished before tensor memory is released
         __syncwarp();
         const long long t0 = clock64();
         while (!mbar_try_wait(&sm->drain, 0) && clock64() - t0 < kSpinCycles) {}
-    } else if (warp >= kQueryWarp) {
-        // Queries of the next piece: sixteen lanes per row, 16 bytes each, into the swizzled operand layout; rows past the
-        // last query are zeros.  Stacked query j of a key/value head is head j % G of its group, node j / G.
-        const int sub = lane >> 4, c = lane & 15;
-        uint32_t seg = 0;
-        for (long long t = t_begin; t < t_end; ++seg) {
-            Piece s;
-            piece_at<QB>(pl, p, t, t_end, s);
-            const uint32_t buf = seg & 1u;
-            if (seg >= 2 && !mbar_wait(&sm->piece_done[buf], ((seg - 2u) >> 1) & 1u, abort_flag, hdr, 36)) break;
-            const int rows = (s.Nq + 15) & ~15;
-            unsigned char* dst = q_buf + buf * (QB * 256) + (c >> 3) * (QB * 128);
-#pragma unroll 4
-            for (int r = (warp - kQueryWarp) * 2 + sub; r < rows; r += 4) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (r < s.Nq) {
-                    const int j = s.q0 + r, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
-                    const int row = (s.b * p.Hkv * p.G + h) * p.N + n;          // below 65535 * 192
-                    v = *reinterpret_cast<const uint4*>(p.q + (size_t)row * kD + c * 8);
-                    if (c == 0) sm->row[buf][r] = row;
-                }
-                *reinterpret_cast<uint4*>(dst + r * 128 + (((c & 7) ^ (r & 7)) * 16)) = v;
-                float sum = 0.f;
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum += __uint_as_float(w[i] << 16) + __uint_as_float(w[i] & 0xFFFF0000u);
-#pragma unroll
-                for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-                if (c == 0) sm->q_sum[buf][r] = sum;
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm->q_full[buf]);
-            t += s.cnt;
-        }
-    } else if (warp < kValueWarp) {
-        // ---- keys: thread r owns key row r of a tile
-        constexpr uint32_t NK = Col::key_buffers;
-        const int r = tid;
-        const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
-        if (Col::ones) {                              // ordered before the products by the barrier of the first tile's keys
-            uint32_t y[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = e < 8 ? 0x3F803F80u : 0x3C003C00u;
-            tc_st16(lane_addr + Col::One, y);
-        }
-        uint32_t g = 0, f = 0;
+    } else if (warp == kProductWarp) {
+        const uint64_t dp0 = smem_desc(smem_u32(p_buf), 128, 2048, 0);
+        const uint64_t d1 = smem_desc(smem_u32(sm->ones), 128, 256, 0);
+        constexpr uint32_t p_next = (QB * 256) >> 4, one_next = 512 >> 4;
+        const uint32_t idesc_lb = instr_desc(16, 1, 0);
+        uint32_t g = 0;
         bool ok = true;
         for (long long t = t_begin; t < t_end && ok;) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
-            for (int i = s.lt; i < s.lt + s.cnt && ok; ++i, ++g) {
-                const uint32_t buf = g & 1u, dst = lane_addr + Col::K + (NK == 2 ? buf * 64 : 0u);
+            const uint32_t idesc_b = instr_desc((s.Nq + 15) & ~15, 0, 1);
+            for (int i = 0; i < s.cnt; ++i, ++g) {
+                const uint32_t hb = g & 1u;
+                ok = mbar_wait(&sm->v_full[hb], (g >> 1) & 1u, abort_flag, hdr, 34);
+                if (ok) ok = mbar_wait(&sm->p_full[hb], (g >> 1) & 1u, abort_flag, hdr, 35);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    // fp16 operands are format 0 of both operand fields, bf16 is 1
+                    const uint32_t half = sm->fmt[g & 7u];
+                    const uint32_t fp16 = ~(half ? (1u << 7) | (1u << 10) : 0u), idesc = idesc_b & fp16, idesc_l = idesc_lb & fp16;
+                    const uint32_t d = tmem + Col::O + hb * QB, l = tmem + Col::L + hb * 16, va = tmem + Col::V + hb * 64;
+                    const uint64_t dp = dp0 + hb * p_next, d1h = d1 + half * one_next;
+                    const uint32_t more = i >= 2;     // a group's first tile of a piece overwrites
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        mma_ta(d, va + 8 * k, dp + (uint32_t)(k * (256 >> 4)), idesc, more | (uint32_t)(k > 0));
+                        // (P^T read as the A operand, queries on the lanes; lanes past the last query hold nothing of use)
+                        mma_sa(l, dp + (uint32_t)(k * (256 >> 4)), d1h, idesc_l, more | (uint32_t)(k > 0));
+                    }
+                    commit(&sm->pv_done[hb]);
+                }
+                __syncwarp();
+            }
+            t += s.cnt;
+        }
+        if (elect_one()) commit(&sm->drain);
+        __syncwarp();
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&sm->drain, 0) && clock64() - t0 < kSpinCycles) {}
+    } else if (warp == kQueryWarp) {
+        // queries of the next piece (the first one's are there), two rows at a time; and, a while after a piece of a cut item is
+        // done, the count of the item's tiles (who brings the last ones merges, see the end of the kernel)
+        const int sub = lane >> 4, c = lane & 15;
+        uint32_t seg = 0;
+        bool ok = true;
+        auto finish = [&](uint32_t done) {                    // piece number `done`, the last or the one before
+            ok = mbar_wait(&sm->piece_done[done & 1u], (done >> 1) & 1u, abort_flag, hdr, 36);
+            const Piece& s = sm->piece[done & 1u];
+            if (ok && lane == 0 && s.cnt != s.T) {
+                auto& m = sm->merge[done > 0 ? 1 : 0];
+                m.b = s.b; m.hk = s.hk; m.q0 = s.q0; m.Nq = s.Nq; m.T = s.T; m.cnt = s.cnt;
+                m.first = pl.tiles[s.b] + (long long)(s.item - pl.items[s.b]) * s.T;
+                __threadfence();
+                m.before = atomicAdd(&p.counters[s.item], s.cnt);
+                if (m.before + s.cnt == s.T) p.counters[s.item] = 0;
+            }
+            __syncwarp();
+        };
+        for (long long t = t_begin; t < t_end && ok; ++seg) {
+            Piece s;
+            piece_at<QB>(pl, p, t, t_end, s);
+            const uint32_t buf = seg & 1u;
+            if (seg > 0) {
+                if (seg >= 2) finish(seg - 2u);
+                if (!ok) break;
+                const int rows = (s.Nq + 15) & ~15;
+                float top = 0.f;
+#pragma unroll 4
+                for (int r = sub; r < rows; r += 2) top = fmaxf(top, load_query<QB>(sm, q_buf, p, s, buf, r, c));
+                const float scale = query_scale(warp_max_f32(top));
+#pragma unroll 2
+                for (int r = sub; r < rows; r += 2) split_query<QB>(q_buf, buf, scale, r, c);
+                if (lane == 0) { sm->q_factor[buf] = 512.f / scale; sm->piece[buf] = s; }
+                fence_async_smem();
+                __syncwarp();
+            }
+            if (lane == 0) mbar_arrive(&sm->q_full[buf]);
+            t += s.cnt;
+        }
+        if (ok && seg >= 2) finish(seg - 2u);
+        if (ok) finish(seg - 1u);
+    } else if (warp < kValueWarp) {
+        // ---- keys: thread r owns key row r of a tile
+        const int r = tid;
+        const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
+        uint32_t g = 0, f = 0;
+        bool bad = false, gone = false, wide = false;         // wide: the previous tile took both buffers
+        for (long long t = t_begin; t < t_end && !gone;) {
+            Piece s;
+            piece_at<QB>(pl, p, t, t_end, s);
+            for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
+                const uint32_t buf = g & 1u;
+                const uint32_t st = f % kStages<QB>;
+                if (i < s.Tp) bad |= !mbar_wait(&sm->full[st], (f / kStages<QB>) & 1u, abort_flag, hdr, 37);
+                // Scales of the tile's value rows, thread r the row r, rounded to fp16.  Rows past the end of the prefix have
+                // probability zero but may hold anything, and 0 * NaN would be NaN: their scale and offset are zero.
+                const unsigned char* page = ring + st * kStageBytes + warp * kPageBytes;   // rows 32 warp .. of the tile
+                const unsigned short* sc = reinterpret_cast<const unsigned short*>(page + kv4_scales_at(kD)) + lane;
+                uint32_t a16 = 0, b16 = 0;
+                if (i < s.Tp && r < s.L - i * kTile) { a16 = sc[2 * kPageRows]; b16 = sc[3 * kPageRows]; }
+                const float va = bf16_bits_to_f32(a16), vb = bf16_bits_to_f32(b16);
+                const bool odd = group_sync_any(8, bad || i >= s.Tp || !fits_half(va, vb));   // not fp16
+                if (odd) {
+                    gone = group_sync_any(8, bad);
+                    if (gone) break;
+                }
+                // (The entry of tile g - 8.  The scores of tile g - 3 are done; so softmax had stored the weights of tile g - 5, for which it
+                // waited for the products of tile g - 7, and those of tile g - 8 came before.)
+                sm->vab[g & 7u][0][r] = odd ? (unsigned short)a16 : __half_as_ushort(__float2half_rn(va));
+                sm->vab[g & 7u][1][r] = odd ? (unsigned short)b16 : __half_as_ushort(__float2half_rn(vb));
+                if (r == 0) sm->fmt[g & 7u] = !odd;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm->scales_full[g & 7u]);
+                // A buffer is free once the scores of the tile that used it are done: the tile before last, and the last one
+                // too where either of the two takes both buffers.  They were issued after the softmax warps had taken
+                // the scores and the scales of tile g - 4, whose entry is rewritten below.
+                if (g >= 2) bad |= !mbar_wait(&sm->s_full[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 38);
+                if (g >= 1 && (wide || i >= s.Tp)) bad |= !mbar_wait(&sm->s_full[buf ^ 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 47);
+                tc_fence_after();
+                wide = i >= s.Tp;
                 if (i < s.Tp) {
-                    const uint32_t st = f % kStages;
-                    ok = mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 37);
-                    if (!ok) break;
-                    const unsigned char* page = ring + st * kStageBytes + warp * kPageBytes;   // rows 32 warp .. of the tile
                     const uint4* piece = reinterpret_cast<const uint4*>(page) + lane;
-                    const unsigned short* sc = reinterpret_cast<const unsigned short*>(page + kv4_scales_at(kD));
-                    const float a = bf16_bits_to_f32(sc[lane]), b = bf16_bits_to_f32(sc[kPageRows + lane]);
-                    uint4 x = piece[0];
-                    // The buffer is free once the scores of the tile that used it are done.  They were issued after the
-                    // softmax warps had taken the scores and the scales of tile g - 4, which the entry below held.
-                    if (g >= NK) ok = mbar_wait(&sm->s_full[(g - NK) & 1u], ((g - NK) >> 1) & 1u, abort_flag, hdr, 38);
-                    if (!ok) break;
-                    tc_fence_after();
-                    sm->kab[g & 3u][r] = make_float2(a * p.scale_log2, b * p.scale_log2);
+                    const float a = bf16_bits_to_f32(sc[0]), b = bf16_bits_to_f32(sc[kPageRows]);
+                    sm->kab[g & 3u][r] = make_float2(a * p.scale_log2, fmaf(16.f, a, b) * p.scale_log2);
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        const uint4 next = piece[((c + 1) & 3) * kPageRows];
-                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    for (int c = 0; c < 2; ++c) {
+                        const uint4 x0 = piece[2 * c * kPageRows], x1 = piece[(2 * c + 1) * kPageRows];
+                        const uint32_t w[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
                         uint32_t y[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = code_pair<false>(w[e >> 2], e & 3);
-                        tc_st16(dst + 16 * c, y);
-                        x = next;
+                        for (int e = 0; e < 8; ++e) {
+                            y[2 * e] = w[e] & 0x0F0F0F0Fu;
+                            y[2 * e + 1] = (w[e] >> 4) & 0x0F0F0F0Fu;
+                        }
+                        tc_st16(lane_addr + Col::K + buf * 32 + 16 * c, y);
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sm->empty[st]);
                     ++f;
                 } else {
                     const int n = (i - s.Tp) * kTile + r;
-                    if (g >= NK) ok = mbar_wait(&sm->s_full[(g - NK) & 1u], ((g - NK) >> 1) & 1u, abort_flag, hdr, 38);
-                    if (!ok) break;
-                    tc_fence_after();
                     sm->kab[g & 3u][r] = make_float2(p.scale_log2, 0.f);
                     const uint4* row = reinterpret_cast<const uint4*>(p.k_tree + (((size_t)s.b * p.Hkv + s.hk) * p.N + n) * kD);
 #pragma unroll 1
@@ -564,7 +696,7 @@ tree_attention_kv4_kernel(const Params p) {
                             const uint4 v = n < s.Nb ? row[4 * c + e] : make_uint4(0, 0, 0, 0);
                             y[4 * e] = v.x; y[4 * e + 1] = v.y; y[4 * e + 2] = v.z; y[4 * e + 3] = v.w;
                         }
-                        tc_st16(dst + 16 * c, y);
+                        tc_st16(lane_addr + Col::K + 16 * c, y);
                     }
                 }
                 tc_wait_st();
@@ -576,47 +708,33 @@ tree_attention_kv4_kernel(const Params p) {
         }
     } else if (warp < kSoftWarp) {
         // ---- values: thread d owns channel d
-        constexpr uint32_t NV = Col::value_buffers;
         const int d = tid & 127;
+        const uint32_t vg = (uint32_t)(warp - kValueWarp) >> 2;   // takes the tiles with g % 2 == vg
         const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + Col::V;
         uint32_t g = 0, f = 0;
-        bool failed = false, gone = false;                    // gone: all threads of the role know that one has failed
-        for (long long t = t_begin; t < t_end && !gone;) {
+        bool ok = true;
+        for (long long t = t_begin; t < t_end && ok;) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
             for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
-                const uint32_t dst = lane_addr + (NV == 2 ? (g & 1u) * 64 : 0u);
-                const uint32_t st = f % kStages;
-                unsigned short* const va = sm->vab[g & 1u][0];
-                unsigned short* const vb = sm->vab[g & 1u][1];
-                uint32_t a16 = 0, b16 = 0;
-                if (i < s.Tp) {
-                    if (!mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 39)) failed = true;
-                    // Scales of the tile's rows, thread d the row d, rounded to fp16.  Rows past the end of the prefix have
-                    // probability zero but may hold anything, and 0 * NaN would be NaN: their scale and offset are zero.
-                    const unsigned short* sc = reinterpret_cast<const unsigned short*>(ring + st * kStageBytes + (warp & 3) * kPageBytes + kv4_scales_at(kD)) + 2 * kPageRows + lane;
-                    if (d < s.L - i * kTile) { a16 = sc[0]; b16 = sc[kPageRows]; }
-                    va[d] = __half_as_ushort(__float2half_rn(bf16_bits_to_f32(a16)));
-                    vb[d] = __half_as_ushort(__float2half_rn(bf16_bits_to_f32(b16)));
+                if ((g & 1u) != vg) {
+                    if (i < s.Tp) ++f;
+                    continue;
                 }
-                const bool half = !group_sync_any(3, failed || i >= s.Tp || !fits_half(bf16_bits_to_f32(a16), bf16_bits_to_f32(b16)));
-                if (!half) {
-                    va[d] = (unsigned short)a16;
-                    vb[d] = (unsigned short)b16;
-                    gone = group_sync_any(3, failed);
-                    if (gone) break;
-                }
-                if (lane == 0) {
-                    if (warp == kValueWarp) sm->fmt[g & 3u] = half;
-                    mbar_arrive(&sm->fmt_full[g & 3u]);
-                }
+                const uint32_t dst = lane_addr + (g & 1u) * 64;
+                const uint32_t st = f % kStages<QB>;
+                // (the key warps have seen the tile arrive before they announce its scales)
+                ok = mbar_wait(&sm->scales_full[g & 7u], (g >> 3) & 1u, abort_flag, hdr, 39);
                 // the buffer is free once the products of the tile that used it are done
-                if (g >= NV && !mbar_wait(&sm->pv_done[(g - NV) & 1u], ((g - NV) >> 1) & 1u, abort_flag, hdr, 40)) failed = true;
+                if (ok && g >= 2) ok = mbar_wait(&sm->pv_done[vg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 40);
+                if (!ok) break;
                 tc_fence_after();
                 if (i < s.Tp) {
+                    if (!mbar_try_wait(&sm->full[st], (f / kStages<QB>) & 1u)) { ok = false; break; }   // (has completed)
+                    const bool half = sm->fmt[g & 7u];
                     const unsigned char* codes = ring + st * kStageBytes + kv4_values_at(kD) + d * 16;
-                    const uint4* sa = reinterpret_cast<const uint4*>(va);
-                    const uint4* sb = reinterpret_cast<const uint4*>(vb);
+                    const uint4* sa = reinterpret_cast<const uint4*>(sm->vab[g & 7u][0]);
+                    const uint4* sb = reinterpret_cast<const uint4*>(sm->vab[g & 7u][1]);
                     auto unpack = [&](auto half_tag) {
                         constexpr bool HALF = decltype(half_tag)::value;
 #pragma unroll 1
@@ -662,18 +780,23 @@ tree_attention_kv4_kernel(const Params p) {
             t += s.cnt;
         }
     } else {
-        // ---- softmax, epilogue, merge: group wg has the tiles with g % 2 == wg, thread r key row r
-        const int wg = (warp - kSoftWarp) >> 2, wq = warp & 3, r = tid & 127;
-        const int bar_id = 1 + wg;
+        // ---- softmax, epilogue: group wg has the tiles with g % 2 == wg, thread r key row r
+        const int quarter = (warp - kSoftWarp) >> 2, wg = quarter / kSides, side = quarter % kSides, wq = warp & 3, r = tid & 127;
+        const int bar_id = 1 + quarter;
         const uint32_t lane_addr = tmem + ((uint32_t)(wq * 32) << 16);
+        const uint32_t s_addr = lane_addr + Col::S + wg * QB;
         unsigned char* const p_own = p_buf + wg * (QB * 256) + r * 16;
         float* const nref = sm->nref[wg];
+        float* const alph = sm->alpha[wg];
         uint32_t g_piece = 0, seg = 0;                           // tiles of this block before the piece
         bool failed = false, gone = false;                       // gone: all threads know that one has failed
         for (long long t = t_begin; t < t_end; ++seg) {
-            Piece s;
-            piece_at<QB>(pl, p, t, t_end, s);
+            if (!mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 48)) failed = true;
+            const Piece s = sm->piece[seg & 1u];
+            if (soft_sync_any(failed)) break;                    // (all leave or none)
             const int n8 = (s.Nq + 7) >> 3;
+            const int per_side = (n8 + kSides - 1) / kSides, j_lo = side * per_side, j_hi = min(n8, j_lo + per_side);
+            const bool own_col = r >= 8 * j_lo && r < 8 * j_hi;  // thread r keeps column r's reference
             const float* qs = sm->q_sum[seg & 1u];
             const uint32_t g_end = g_piece + (uint32_t)s.cnt;
             const uint32_t g_own = g_piece + ((g_piece ^ (uint32_t)wg) & 1u);   // the group's first tile, if below g_end
@@ -687,30 +810,49 @@ tree_attention_kv4_kernel(const Params p) {
                     if (!tree) {
                         if (key < s.L) cm = ~0ull;
                     } else if (key < s.Nb) {
-                        int n = s.q0 / p.G, rest = s.q0 - n * p.G;
-                        for (int c = 0; c < s.Nq; ++c) {
+                        int n = (s.q0 + 8 * j_lo) / p.G, rest = s.q0 + 8 * j_lo - n * p.G;
+                        for (int c = 8 * j_lo; c < min(s.Nq, 8 * j_hi); ++c) {
                             cm |= (unsigned long long)((sm->anc[n * p.words + (key >> 6)] >> (key & 63)) & 1ull) << c;
                             if (++rest == p.G) { rest = 0; ++n; }
                         }
                     }
                 }
                 if (!mbar_wait(&sm->s_full[wg], (g >> 1) & 1u, abort_flag, hdr, 41)) failed = true;
-                if (!mbar_wait(&sm->fmt_full[g & 3u], (g >> 2) & 1u, abort_flag, hdr, 45)) failed = true;
-                // P^T is free once the products of the group's previous tile are done, and the accumulators are current
-                if (g >= 2 && !mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
                 tc_fence_after();
-                const bool half = sm->fmt[g & 3u], first = g == g_own;
-                const float2 ab = sm->kab[g & 3u][r];
+                const uint32_t half = sm->fmt[g & 7u];
+                const bool first = g == g_own;
+                float2 ab = sm->kab[g & 3u][r];
+                if (!tree) ab.x *= sm->q_factor[seg & 1u];
                 const float2 a2 = make_float2(ab.x, ab.x), b2 = make_float2(ab.y, ab.y);
-                const uint32_t s_addr = lane_addr + Col::S + wg * QB;
-                // New references come first in a piece's first tile, and again where a score exceeds its reference by more
-                // than 2^8 after the optimistic sweep below, which is then redone.
-                bool raise = first, raised = false;
+                // The first references of a piece: the largest of four keys' scores (one per warp) plus 3.  Any reference that
+                // no score exceeds by more than 2^8 and that is not far above the largest gives the same result; one that
+                // is exceeded is raised below.  A tile with a mask takes exact column maxima instead.
+                if (first && plain) {
+#pragma unroll 1
+                    for (int j = j_lo; j < j_hi; ++j) {
+                        float y[8];
+                        tc_ld8(s_addr + 8 * j, y);
+                        tc_wait_ld();
+                        if (lane == 0) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) sm->red[wg][wq][8 * j + k] = fmaf(y[k], ab.x, qs[8 * j + k] * ab.y);
+                        }
+                    }
+                    group_sync_any(bar_id, false);
+                    if (own_col) {
+                        const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
+                        nref[r] = -fmaxf(top + 3.f, -1e30f);
+                    }
+                    group_sync_any(bar_id, false);
+                }
+                // Then an optimistic sweep; where a score exceeds its reference by more than 2^8, new references and the same
+                // again.
+                bool raise = first && !plain, raised = false;
                 for (;;) {
                     if (raise) {
                         raised = true;
 #pragma unroll 1
-                        for (int j = 0; j < n8; ++j) {
+                        for (int j = j_lo; j < j_hi; ++j) {
                             float y[8];
                             tc_ld8(s_addr + 8 * j, y);
                             tc_wait_ld();
@@ -724,177 +866,167 @@ tree_attention_kv4_kernel(const Params p) {
                             if (lane < 8) sm->red[wg][wq][8 * j + lane] = mine;
                         }
                         group_sync_any(bar_id, false);
-                        if (r < 8 * n8) {
+                        if (own_col) {
                             const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
                             // (a column that has seen no key yet keeps one below any score)
                             const float old = first ? -1e30f : -nref[r], now = fmaxf(old, top);
                             nref[r] = -now;
-                            sm->alpha[wg][r] = exp2f(old - now);
+                            alph[r] = exp2f(old - now);
                         }
                         group_sync_any(bar_id, false);
                         if (!first) {
+                            // (the accumulators are current once the products of the group's previous tile are done)
+                            if (!mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 42)) failed = true;
+                            tc_fence_after();
 #pragma unroll 1
-                            for (int j = 0; j < 2 * n8; ++j) {   // accumulators, then row sums
-                                const int jj = j < n8 ? j : j - n8;
-                                const uint32_t at = lane_addr + (j < n8 ? Col::O : Col::L) + wg * QB + 8 * jj;
+                            for (int j = j_lo; j < j_hi; ++j) {
                                 float o[8];
-                                tc_ld8(at, o);
+                                tc_ld8(lane_addr + Col::O + wg * QB + 8 * j, o);
                                 tc_wait_ld();
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) o[k] *= sm->alpha[wg][8 * jj + k];
-                                tc_st8(at, o);
+                                for (int k = 0; k < 8; ++k) o[k] *= alph[8 * j + k];
+                                tc_st8(lane_addr + Col::O + wg * QB + 8 * j, o);
                             }
+                            const float l = tc_ld1(lane_addr + Col::L + wg * 16 + side);   // of query r
+                            tc_wait_ld();
+                            tc_st1(lane_addr + Col::L + wg * 16 + side, own_col ? l * alph[r] : l);
                             tc_wait_st();
                         }
                     }
-                    // scores of this thread's key relative to the references, exponentiated, packed, stored: two column
-                    // groups at a time (one is enough to keep the unit busy only with four times the warps)
+                    // scores of this thread's key relative to the references, exponentiated, packed, stored
                     float dmax = -INFINITY;
+                    // P^T may be written once the products of the group's previous tile are done (they are, nearly always)
+                    auto p_free = [&]() {
+                        if (g >= 2 && !mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
+                    };
+                    auto scores = [&](float (&y)[8], int j) {
+#pragma unroll
+                        for (int k = 0; k < 8; k += 4) {
+                            const float4 q = *reinterpret_cast<const float4*>(qs + 8 * j + k), m = *reinterpret_cast<const float4*>(nref + 8 * j + k);
+                            const float2 u = fma_f32x2(make_float2(y[k], y[k + 1]), a2, fma_f32x2(make_float2(q.x, q.y), b2, make_float2(m.x, m.y)));
+                            const float2 v = fma_f32x2(make_float2(y[k + 2], y[k + 3]), a2, fma_f32x2(make_float2(q.z, q.w), b2, make_float2(m.z, m.w)));
+                            y[k] = u.x; y[k + 1] = u.y; y[k + 2] = v.x; y[k + 3] = v.y;
+                        }
+                    };
+                    if (plain && half) {                         // nearly all tiles
 #pragma unroll 1
-                    for (int j = 0; j < n8; j += 2) {
-                        float y[2][8];
-                        tc_ld8(s_addr + 8 * j, y[0]);
-                        if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y[1]);
-                        tc_wait_ld();
+                        for (int j = j_lo; j < j_hi; j += 2) {   // two column groups side by side
+                            const bool two = j + 1 < j_hi;
+                            float y[2][8];
+                            tc_ld8(s_addr + 8 * j, y[0]);
+                            if (two) tc_ld8(s_addr + 8 * j + 8, y[1]);
+                            if (j == j_lo) p_free();
+                            tc_wait_ld();
+                            scores(y[0], j);
+                            if (two) scores(y[1], j + 1);
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            if (j + h < n8) {
-                                const float* qj = qs + 8 * (j + h);
-                                const float* nj = nref + 8 * (j + h);
-#pragma unroll
-                                for (int k = 0; k < 8; k += 4) {
-                                    const float4 q = *reinterpret_cast<const float4*>(qj + k), m = *reinterpret_cast<const float4*>(nj + k);
-                                    const float2 u = fma_f32x2(make_float2(y[h][k], y[h][k + 1]), a2, fma_f32x2(make_float2(q.x, q.y), b2, make_float2(m.x, m.y)));
-                                    const float2 v = fma_f32x2(make_float2(y[h][k + 2], y[h][k + 3]), a2, fma_f32x2(make_float2(q.z, q.w), b2, make_float2(m.z, m.w)));
-                                    y[h][k] = u.x; y[h][k + 1] = u.y; y[h][k + 2] = v.x; y[h][k + 3] = v.y;
-                                }
-                                if (!plain) {
-                                    const uint32_t bits = (uint32_t)(cm >> (8 * (j + h)));
-#pragma unroll
-                                    for (int k = 0; k < 8; ++k) y[h][k] = ((bits >> k) & 1u) ? y[h][k] : -INFINITY;
-                                }
-                                dmax = fmaxf(dmax, fmaxf(fmaxf(fmaxf(y[h][0], y[h][1]), fmaxf(y[h][2], y[h][3])), fmaxf(fmaxf(y[h][4], y[h][5]), fmaxf(y[h][6], y[h][7]))));
-                                uint32_t w[4];
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) y[h][k] = ex2_approx(y[h][k]);
-                                if (half) {
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) w[k] = pack_pair<true>(y[h][2 * k], y[h][2 * k + 1]);
-                                } else {
-#pragma unroll
-                                    for (int k = 0; k < 4; ++k) w[k] = pack_pair<false>(y[h][2 * k], y[h][2 * k + 1]);
-                                }
-                                *reinterpret_cast<uint4*>(p_own + (j + h) * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int k = 0; k < 8; k += 2) {
+                                dmax = fmaxf(dmax, fmaxf(y[0][k], y[0][k + 1]));
+                                y[0][k] = ex2_approx(y[0][k]);
+                                y[0][k + 1] = ex2_approx(y[0][k + 1]);
                             }
+                            if (two) {
+#pragma unroll
+                                for (int k = 0; k < 8; k += 2) {
+                                    dmax = fmaxf(dmax, fmaxf(y[1][k], y[1][k + 1]));
+                                    y[1][k] = ex2_approx(y[1][k]);
+                                    y[1][k + 1] = ex2_approx(y[1][k + 1]);
+                                }
+                                *reinterpret_cast<uint4*>(p_own + (j + 1) * 2048) = pack8<true>(y[1]);
+                            }
+                            *reinterpret_cast<uint4*>(p_own + j * 2048) = pack8<true>(y[0]);
+                        }
+                    } else {                                     // masks, bf16
+                        p_free();
+#pragma unroll 1
+                        for (int j = j_lo; j < j_hi; ++j) {
+                            const uint32_t bits = plain ? 0xFFu : (uint32_t)(cm >> (8 * j));
+                            float y[8];
+                            tc_ld8(s_addr + 8 * j, y);
+                            tc_wait_ld();
+                            scores(y, j);
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                y[k] = ((bits >> k) & 1u) ? y[k] : -INFINITY;
+                                dmax = fmaxf(dmax, y[k]);
+                                y[k] = ex2_approx(y[k]);
+                            }
+                            *reinterpret_cast<uint4*>(p_own + j * 2048) = half ? pack8<true>(y) : pack8<false>(y);
                         }
                     }
-                    raise = group_sync_any(bar_id, (dmax > kLazyTau && !raised) || failed);   // one vote of the group
+                    raise = group_sync_any(bar_id, (dmax > kLazyTau && !raised) || failed);   // one vote of the four warps
                     if (!raise) break;
                     gone = group_sync_any(bar_id, failed);
                     if (gone) break;
                 }
                 if (gone) break;
                 tc_fence_before();
-                if (lane == 0) mbar_arrive(&sm->s_free[wg]);     // (the vote above came after everybody's last read)
+                if (lane == 0) mbar_arrive(&sm->s_free[wg]);     // (the vote came after everybody's last read)
                 fence_async_smem();
-                tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm->p_full[wg]);
             }
             // ---- the piece is done when the last products of both groups are
-            if (!gone && g_own < g_end) {
+            if (wq == 0 && !gone && g_own < g_end) {
                 const uint32_t last = g_end - 1u - ((g_end - 1u - g_own) & 1u);
                 if (!mbar_wait(&sm->pv_done[wg], (last >> 1) & 1u, abort_flag, hdr, 44)) failed = true;
             }
-            if (both_sync_any(failed || gone)) break;
+            if (soft_sync_any(failed || gone)) break;
             tc_fence_after();
             const bool whole = s.cnt == s.T;
             const int slot = 2 * (int)blockIdx.x + (t > t_begin ? 1 : 0);
             const bool has0 = s.cnt > 1 || !(g_piece & 1u), has1 = s.cnt > 1 || (g_piece & 1u);   // groups with a tile in the piece
             const int* rows = sm->row[seg & 1u];
-            // the groups split the columns; thread r has channel r of both accumulators
-            const int j0 = wg ? (n8 + 1) / 2 : 0, j1 = wg ? n8 : (n8 + 1) / 2;
+            // weights of the groups' accumulators, one thread per column (the sums of query r lie in lane r)
+            if (quarter == 0 && wq < (QB + 31) / 32) {
+                float l[2][kSides];
+#pragma unroll
+                for (int x = 0; x < 2 * kSides; ++x) l[x / kSides][x % kSides] = tc_ld1(lane_addr + Col::L + (x / kSides) * 16 + x % kSides);
+                tc_wait_ld();
+                if (r < 8 * n8) {
+                    // (the copy that the column's warps kept)
+                    const float l0 = kSides == 2 && r >= 8 * per_side ? l[0][kSides - 1] : l[0][0], l1 = kSides == 2 && r >= 8 * per_side ? l[1][kSides - 1] : l[1][0];
+                    const float m0 = has0 ? -sm->nref[0][r] : -1e30f, m1 = has1 ? -sm->nref[1][r] : -1e30f, M = fmaxf(m0, m1);
+                    float w0 = has0 ? exp2f(m0 - M) : 0.f, w1 = has1 ? exp2f(m1 - M) : 0.f;
+                    const float sum = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
+                    if (whole) {
+                        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+                        w0 *= inv;
+                        w1 *= inv;
+                    } else {
+                        p.part_ml[((size_t)slot * 2 + 0) * kWideQ + r] = M;
+                        p.part_ml[((size_t)slot * 2 + 1) * kWideQ + r] = sum;
+                    }
+                    sm->alpha[0][r] = w0;
+                    sm->alpha[1][r] = w1;
+                }
+            }
+            soft_sync_any(false);
+            // every other column group for each group of warps; thread r has channel r of both accumulators
 #pragma unroll 1
-            for (int j = j0; j < j1; ++j) {
-                float o0[8], o1[8], l0[8], l1[8];
-                tc_ld8(lane_addr + Col::O + 8 * j, o0);
-                tc_ld8(lane_addr + Col::O + QB + 8 * j, o1);
-                tc_ld8(lane_addr + Col::L + 8 * j, l0);
-                tc_ld8(lane_addr + Col::L + QB + 8 * j, l1);
+            for (int j = quarter; j < n8; j += 2 * kSides) {
+                float o[8], o1[8];
+                if (has0) tc_ld8(lane_addr + Col::O + 8 * j, o);
+                if (has1) tc_ld8(lane_addr + Col::O + QB + 8 * j, o1);
                 tc_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const int c = 8 * j + k;
-                    if (c < s.Nq) {
-                        const float m0 = has0 ? -sm->nref[0][c] : -1e30f, m1 = has1 ? -sm->nref[1][c] : -1e30f, M = fmaxf(m0, m1);
-                        const float w0 = ex2_approx(m0 - M), w1 = ex2_approx(m1 - M);
-                        const float o = (has0 ? o0[k] * w0 : 0.f) + (has1 ? o1[k] * w1 : 0.f);
-                        const float l = (has0 ? l0[k] * w0 : 0.f) + (has1 ? l1[k] * w1 : 0.f);
-                        if (whole) {
-                            p.out[(size_t)rows[c] * kD + r] = __float2bfloat16_rn(l != 0.f ? o / l : 0.f);
-                        } else {
-                            p.part_o[((size_t)slot * kWideQ + c) * kD + r] = o;
-                            if (r == 0) {
-                                p.part_ml[((size_t)slot * 2 + 0) * kWideQ + c] = M;
-                                p.part_ml[((size_t)slot * 2 + 1) * kWideQ + c] = l;
-                            }
-                        }
-                    }
+                    const float x = has0 ? o[k] * sm->alpha[0][8 * j + k] : 0.f;
+                    o[k] = has1 ? fmaf(o1[k], sm->alpha[1][8 * j + k], x) : x;
+                }
+                if (whole) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (8 * j + k < s.Nq) p.out[(size_t)rows[8 * j + k] * kD + r] = __float2bfloat16_rn(o[k]);
+                } else {
+                    float* po = p.part_o + ((size_t)slot * kWideQ + 8 * j) * kD + r;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) po[k * kD] = o[k];
                 }
             }
-            if (!whole) {
-                // the block that finishes an item's last tile merges all pieces
-                __threadfence();
-                both_sync_any(false);
-                const long long first = pl.tiles[s.b] + (long long)(s.item - pl.items[s.b]) * s.T;   // the item's first tile
-                if (tid == kSoftWarp * 32) sm->merge = atomicAdd(&p.counters[s.item], s.cnt);
-                // every block's piece of this item: its slot, or -1
-                const int c = tid - kSoftWarp * 32;
-                if (c < pl.blocks) {
-                    const long long a = pl.first[c], b = pl.first[c + 1];
-                    sm->slots[c] = max(a, first) < min(b, first + s.T) ? (short)(2 * c + (a < first ? 1 : 0)) : (short)-1;
-                }
-                both_sync_any(false);
-                if (sm->merge + s.cnt == s.T) {
-                    __threadfence();
-                    // the item's pieces lie in consecutive blocks, this one among them
-                    int c0 = blockIdx.x, c1 = blockIdx.x + 1;
-                    while (c0 > 0 && pl.first[c0] > first) --c0;
-                    while (c1 < pl.blocks && pl.first[c1] < first + s.T) ++c1;
-#pragma unroll 1
-                    for (int j = j0; j < j1; ++j) {
-                        float M[8], l[8], o[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) { M[k] = -INFINITY; l[k] = 0.f; o[k] = 0.f; }
-#pragma unroll 1
-                        for (int x = c0; x < c1; ++x) {
-                            const int sl = sm->slots[x];
-                            if (sl < 0) continue;
-                            const float* ml = p.part_ml + (size_t)sl * 2 * kWideQ + 8 * j;
-                            const float* po = p.part_o + ((size_t)sl * kWideQ + 8 * j) * kD + r;
-                            float mx[8], lx[8], ox[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (8 * j + k < s.Nq) { mx[k] = __ldcg(ml + k); lx[k] = __ldcg(ml + kWideQ + k); ox[k] = __ldcg(po + k * kD); }
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                if (8 * j + k < s.Nq) {
-                                    const float m = fmaxf(M[k], mx[k]), w0 = ex2_approx(M[k] - m), w1 = ex2_approx(mx[k] - m);
-                                    l[k] = l[k] * w0 + lx[k] * w1;
-                                    o[k] = o[k] * w0 + ox[k] * w1;
-                                    M[k] = m;
-                                }
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            if (8 * j + k < s.Nq) p.out[(size_t)rows[8 * j + k] * kD + r] = __float2bfloat16_rn(l[k] != 0.f ? o[k] / l[k] : 0.f);
-                    }
-                    if (tid == kSoftWarp * 32) p.counters[s.item] = 0;
-                }
-            }
+            if (!whole) __threadfence();
             tc_fence_before();
-            both_sync_any(false);                                // references, rows and accumulators have been read
+            soft_sync_any(false);                                // references, rows and accumulators have been read
             if (lane == 0) mbar_arrive(&sm->piece_done[seg & 1u]);
             t += s.cnt;
             g_piece = g_end;
@@ -904,9 +1036,56 @@ tree_attention_kv4_kernel(const Params p) {
     // ---- tear-down
     tc_fence_before();
     __syncthreads();
-    if (warp == kIssueWarp) {
+    if (warp == kScoreWarp) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+    // ---- cut items that this block finished: four warps per column group, thread r channel r, pieces in block order
+    if (sm->abort_flag) return;
+#pragma unroll 1
+    for (int x = 0; x < 2 * (QB / 8); ++x) {
+        const auto& m = sm->merge[x & 1];
+        const int j = x >> 1, r = tid & 127;
+        if (j % (kThreads / 128) != tid >> 7 || m.T == 0 || m.before + m.cnt != m.T || 8 * j >= m.Nq) continue;
+        __threadfence();
+        // the pieces lie in consecutive blocks, this one among them
+        int c0 = blockIdx.x, c1 = blockIdx.x + 1;
+        while (c0 > 0 && pl.first[c0] > m.first) --c0;
+        while (c1 < pl.blocks && pl.first[c1] < m.first + m.T) ++c1;
+        float M[8], l[8], o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { M[k] = -INFINITY; l[k] = 0.f; o[k] = 0.f; }
+#pragma unroll 2
+        for (int c = c0; c < c1; ++c) {
+            const long long a = pl.first[c];
+            if (a == pl.first[c + 1]) continue;                  // a block without tiles
+            const int sl = 2 * c + (a < m.first ? 1 : 0);
+            const float* ml = p.part_ml + (size_t)sl * 2 * kWideQ + 8 * j;
+            const float* po = p.part_o + ((size_t)sl * kWideQ + 8 * j) * kD + r;
+            float mx[8], lx[8], ox[8];
+#pragma unroll
+            for (int k = 0; k < 8; k += 4) {
+                const float4 a4 = __ldcg(reinterpret_cast<const float4*>(ml + k)), b4 = __ldcg(reinterpret_cast<const float4*>(ml + kWideQ + k));
+                mx[k] = a4.x; mx[k + 1] = a4.y; mx[k + 2] = a4.z; mx[k + 3] = a4.w;
+                lx[k] = b4.x; lx[k + 1] = b4.y; lx[k + 2] = b4.z; lx[k + 3] = b4.w;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ox[k] = __ldcg(po + k * kD);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float top = fmaxf(M[k], mx[k]), w0 = ex2_approx(M[k] - top), w1 = ex2_approx(mx[k] - top);
+                l[k] = l[k] * w0 + lx[k] * w1;
+                o[k] = o[k] * w0 + ox[k] * w1;
+                M[k] = top;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (8 * j + k < m.Nq) {
+                const int q = m.q0 + 8 * j + k, n = q / p.G, h = m.hk * p.G + (q - n * p.G);
+                p.out[(((size_t)m.b * p.Hkv * p.G + h) * p.N + n) * kD + r] = __float2bfloat16_rn(l[k] != 0.f ? o[k] * __frcp_rn(l[k]) : 0.f);
+            }
+        }
     }
 }
 
@@ -919,7 +1098,7 @@ int columns_for(int nq) {
 
 template <int QB>
 int launch(const Params& p, int grid, cudaStream_t stream) {
-    constexpr size_t smem_bytes = 1024 + 4 * QB * 256 + (size_t)kStages * kStageBytes + sizeof(Small<QB>);
+    constexpr size_t smem_bytes = 1024 + 6 * QB * 256 + (size_t)kStages<QB> * kStageBytes + sizeof(Small<QB>);
     static_assert(smem_bytes <= kSmemLimit, "ring and buffers fit the block's shared memory");
     static std::mutex mu;                                        // the opt-in to large shared memory is per device
     static bool done[64] = {};
