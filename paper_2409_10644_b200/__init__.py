@@ -18,7 +18,8 @@ _BINDING_NAMES = (
 def __getattr__(name):
     if name in _BINDING_NAMES:
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)      # found directly from the second use on
+        return value
     raise AttributeError(name)
 
 

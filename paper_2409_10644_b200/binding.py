@@ -493,35 +493,43 @@ def mcsd_commit_kv(k_cache_ptrs, v_cache_ptrs, k_tree_ptrs, v_tree_ptrs, seq_len
 KV4_PAGE_ROWS = 32
 
 
-def _on_device(dev: torch.device, fn, *args) -> int:
+# These calls take a few microseconds on the GPU for one token, so the checks before them are written for few interpreter
+# steps: `dev` is a device index, a CPU tensor's is -1.
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _on_device(dev: int, fn, *args) -> int:
     """fn(*args, stream) on the tensors' device and torch's current stream there."""
-    if torch.cuda.current_device() == dev.index:
-        return fn(*args, torch.cuda.current_stream().cuda_stream)
+    if dev < 0:
+        raise ValueError("tensors must be on a CUDA device")
+    if torch.cuda.current_device() == dev:
+        return fn(*args, _raw_stream(dev))
     with torch.cuda.device(dev):
-        return fn(*args, torch.cuda.current_stream().cuda_stream)
+        return fn(*args, _raw_stream(dev))
 
 
-def _same(t: torch.Tensor, dtype, shape, dev, name: str) -> int:
+def _same(t: torch.Tensor, dtype, shape, dev: int, name: str) -> int:
     """Address of a contiguous CUDA tensor of this dtype, shape and device."""
-    if t.dtype != dtype or t.device != dev or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor of dtype %s on %s" % (name, dtype, dev))
+    if t.dtype is not dtype or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of dtype %s on device %d" % (name, dtype, dev))
     if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     return t.data_ptr()
 
 
-def _maybe(t: Optional[torch.Tensor], dtype, shape, dev, name: str):
+def _maybe(t: Optional[torch.Tensor], dtype, shape, dev: int, name: str):
     return None if t is None else _same(t, dtype, shape, dev, name)
 
 
-def _projection(t: torch.Tensor, dtype, dev, name: str):
+def _projection(t: torch.Tensor, dtype, dev: int, name: str):
     """Address and (batch, token) strides of projection rows [B][N][H][D] whose heads lie next to each other."""
-    if t.dim() != 4 or t.dtype != dtype or t.device != dev or not t.is_cuda:
-        raise ValueError("%s must be a CUDA tensor [B][N][H][D] of dtype %s on %s" % (name, dtype, dev))
-    B, N, H, D = t.shape
-    if (t.stride(3) != 1 and D > 1) or (t.stride(2) != D and H > 1):
+    if t.dtype is not dtype or t.get_device() != dev or dev < 0:
+        raise ValueError("%s must be a CUDA tensor [B][N][H][D] of dtype %s on device %d" % (name, dtype, dev))
+    sb, sn, sh, sd = t.stride()
+    if (sd != 1 and t.shape[3] > 1) or (sh != t.shape[3] and t.shape[2] > 1):
         raise ValueError("the heads of %s must lie next to each other (strides %s)" % (name, t.stride()))
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), sb, sn
 
 
 def mcsd_qk_norm_rope(q_in, k_in, v_in, seq_lens, freqs, depth=None, n_active=None, q_weight=None, k_weight=None,
@@ -531,7 +539,7 @@ def mcsd_qk_norm_rope(q_in, k_in, v_in, seq_lens, freqs, depth=None, n_active=No
     ``q_in`` [B][N][H_q][D], ``k_in`` and ``v_in`` [B][N][H_kv][D] may be views of one fused projection (any batch and
     token stride).  ``freqs``: float64 [rot_dim / 2], radians per position, or None for no rotation.  ``depth``: the
     mask's depths (tree rows) or None (consecutive positions).  ``out``: (q, k, v) to write into."""
-    dt, dev = q_in.dtype, q_in.device
+    dt, dev = q_in.dtype, q_in.get_device()
     code = _dtype_code(q_in)
     B, N, H, D = q_in.shape
     H_kv = k_in.shape[2]
@@ -541,8 +549,8 @@ def mcsd_qk_norm_rope(q_in, k_in, v_in, seq_lens, freqs, depth=None, n_active=No
     kp, kb, kt = _projection(k_in, dt, dev, "k_in")
     vp, vb, vt = _projection(v_in, dt, dev, "v_in")
     if out is None:
-        out = (torch.empty((B, H, N, D), dtype=dt, device=dev), torch.empty((B, H_kv, N, D), dtype=dt, device=dev),
-               torch.empty((B, H_kv, N, D), dtype=dt, device=dev))
+        out = (torch.empty((B, H, N, D), dtype=dt, device=q_in.device), torch.empty((B, H_kv, N, D), dtype=dt, device=q_in.device),
+               torch.empty((B, H_kv, N, D), dtype=dt, device=q_in.device))
     q, k, v = out
     half = 0 if freqs is None else freqs.numel()
     st = _on_device(dev, lib.mcsd_qk_norm_rope, qp, kp, vp, (ctypes.c_int64 * 6)(qb, qt, kb, kt, vb, vt),
@@ -575,7 +583,7 @@ def _kv4_cache(cache: torch.Tensor, B: int, H_kv: int, D: int, dev):
 
 def mcsd_append_kv4(k, v, cache, start, n_new=None) -> None:
     """Rows k, v [B][H_kv][T][D] into rows start[b].. of a 4-bit cache (see mcsd.h)."""
-    dt, dev = k.dtype, k.device
+    dt, dev = k.dtype, k.get_device()
     code = _dtype_code(k)
     B, H_kv, T, D = k.shape
     ptr, L_max = _kv4_cache(cache, B, H_kv, D, dev)
@@ -589,10 +597,10 @@ def mcsd_read_kv4(cache_ptrs, first, rows: int, n_rows, B: int, H_kv: int, D: in
     """Rows first[b] .. first[b] + rows - 1 of 4-bit caches as dense (k, v) [n_layers][B][H_kv][rows][D] (see mcsd.h).
 
     ``cache_ptrs``: layer_pointer_table() of the layers' caches; ``n_rows`` int32 [B] or None: rows past it are zeros."""
-    dev, n_layers = cache_ptrs.device, cache_ptrs.numel()
+    dev, n_layers = cache_ptrs.get_device(), cache_ptrs.numel()
     shape = (n_layers, B, H_kv, rows, D)
     if out is None:
-        out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+        out = (torch.empty(shape, dtype=dtype, device=cache_ptrs.device), torch.empty(shape, dtype=dtype, device=cache_ptrs.device))
     code = _dtype_code(out[0])
     st = _on_device(dev, lib.mcsd_read_kv4, _same(cache_ptrs, torch.int64, (n_layers,), dev, "cache_ptrs"), n_layers,
                     _same(first, torch.int32, (B,), dev, "first"), _maybe(n_rows, torch.int32, (B,), dev, "n_rows"), B, H_kv, rows, D,
@@ -605,7 +613,7 @@ def mcsd_commit_kv4(cache_ptrs, k_tree_ptrs, v_tree_ptrs, seq_lens, verify_out, 
                     L_max: int, dtype: torch.dtype) -> None:
     """Append the accepted tokens' K/V to every layer's 4-bit cache and grow seq_lens (see mcsd.h; pointer tables and
     ``verify_out`` as for mcsd_commit_kv)."""
-    dev, n_layers = seq_lens.device, cache_ptrs.numel()
+    dev, n_layers = seq_lens.get_device(), cache_ptrs.numel()
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("tree rows are bf16 or fp32")
     ptrs = [_same(t, torch.int64, (n_layers,), dev, name)
@@ -625,7 +633,7 @@ def mcsd_tree_attention_kv4_workspace_bytes(B, H_q, H_kv, N, D, L_max, dtype_cod
 def mcsd_tree_attention_kv4(q, cache, k_tree, v_tree, seq_lens, n_active, mask: TreeMask, out: Optional[torch.Tensor] = None,
                             softmax_scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """mcsd_tree_attention with the prefix in a 4-bit cache (see mcsd.h; ``cache`` from new_kv4_cache)."""
-    dt, dev = q.dtype, q.device
+    dt, dev = q.dtype, q.get_device()
     code = _dtype_code(q)
     B, H, N, D = q.shape
     H_kv = k_tree.shape[1]
@@ -639,7 +647,7 @@ def mcsd_tree_attention_kv4(q, cache, k_tree, v_tree, seq_lens, n_active, mask: 
     if softmax_scale is None:
         softmax_scale = D ** -0.5
     if workspace is None:
-        workspace = new_workspace(mcsd_tree_attention_kv4_workspace_bytes(B, H, H_kv, N, D, L_max, code), dev)
+        workspace = new_workspace(mcsd_tree_attention_kv4_workspace_bytes(B, H, H_kv, N, D, L_max, code), q.device)
     st = _on_device(dev, lib.mcsd_tree_attention_kv4, _same(q, dt, (B, H, N, D), dev, "q"), ptr,
                     _same(k_tree, dt, (B, H_kv, N, D), dev, "k_tree"), _same(v_tree, dt, (B, H_kv, N, D), dev, "v_tree"),
                     _same(out, dt, (B, H, N, D), dev, "out"), _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
