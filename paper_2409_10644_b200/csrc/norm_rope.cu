@@ -8,9 +8,9 @@
 // Every element is read once and written once, so memory bounds it (launch latency for single tokens).  A group of
 // D / 8 lanes holds one head, eight consecutive elements per lane: 16-byte loads and stores for bf16, the sum of squares
 // by shuffles inside the group, and for pairs that lie half a rotation apart the other element from the lane that has
-// it.  The angles of a token are the same for all heads: one block works on one token, its first threads reduce
+// it.  The angles of a token are the same for all heads: a block works on one or a few whole tokens, its threads first reduce
 // position * freq / 2 pi to a fraction of a turn in 64 bits (a far position has no bits left for the angle in 32) and
-// leave sine and cosine in shared memory while the head rows are on their way.
+// leave sine and cosine in shared memory while the first head rows are on their way.
 #include "norm_rope.cuh"
 
 namespace mcsd {
@@ -71,77 +71,95 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
     }
 }
 
-// grid: (B * N, head splits).  VEC: every row starts on a 16-byte boundary.
-template <typename T, int D, bool VEC>
-__global__ void __launch_bounds__(kRopeThreads)
+// grid: (groups of TOK tokens, head splits).  VEC: every row starts on a 16-byte boundary.
+template <typename T, int D, bool VEC, int TOK>
+__global__ void __launch_bounds__(kRopeThreads, 3)
 qk_norm_rope_kernel(const NormRopeArgs a) {
     constexpr int LPH = D / 8;                                // lanes per head
     constexpr int HPB = kRopeThreads / LPH;                   // heads of a block at a time
-    constexpr int U = 4;                                      // of them whose loads are in flight together
-    __shared__ float2 s_cs[D / 2];
+    constexpr int U = 3;                                      // of them whose loads are in flight together
+    __shared__ float2 s_cs[TOK][D / 2];
     const int tid = threadIdx.x, c = tid % LPH;
-    const int b = blockIdx.x / a.N, n = blockIdx.x % a.N;
-    if (a.n_active && n >= a.n_active[b]) return;
     const int half = a.rot_dim >> 1;
-    const int H_all = a.H_q + 2 * a.H_kv;
-    const int step = HPB * gridDim.y;
+    const int H_all = a.H_q + 2 * a.H_kv, H_qk = a.H_q + a.H_kv;
+    const long long token0 = (long long)blockIdx.x * TOK, tokens = (long long)a.B * a.N;
+    // The rows of the block in the order (token, head), `per` heads to a token; this thread takes every HPB-th.
+    const int per = (H_all + gridDim.y - 1) / gridDim.y, h_lo = blockIdx.y * per;
+    const int rows = per * TOK;
 
-    // head h of the row: queries, then keys, then values
-    auto source = [&](int h) -> const T* {
-        if (h < a.H_q) return static_cast<const T*>(a.q_in) + b * a.q_batch + n * a.q_token + (long long)h * D;
-        if (h < a.H_q + a.H_kv) return static_cast<const T*>(a.k_in) + b * a.k_batch + n * a.k_token + (long long)(h - a.H_q) * D;
-        return static_cast<const T*>(a.v_in) + b * a.v_batch + n * a.v_token + (long long)(h - a.H_q - a.H_kv) * D;
-    };
-    auto target = [&](int h) -> T* {
+    struct Row { const T* from; T* to; int h, tok; };          // h < 0: nothing there
+    auto row_at = [&](int i) -> Row {
+        Row x;
+        x.tok = TOK == 1 ? 0 : i / per;
+        x.h = h_lo + i - x.tok * per;
+        const long long token = token0 + x.tok;
+        if (i >= rows || x.h >= H_all || token >= tokens) { x.h = -1; return x; }
+        const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
+        if (a.n_active && n >= a.n_active[b]) { x.h = -1; return x; }
         const size_t N = a.N;
-        if (h < a.H_q) return static_cast<T*>(a.q_out) + (((size_t)b * a.H_q + h) * N + n) * D;
-        if (h < a.H_q + a.H_kv) return static_cast<T*>(a.k_out) + (((size_t)b * a.H_kv + (h - a.H_q)) * N + n) * D;
-        return static_cast<T*>(a.v_out) + (((size_t)b * a.H_kv + (h - a.H_q - a.H_kv)) * N + n) * D;
+        if (x.h < a.H_q) {
+            x.from = static_cast<const T*>(a.q_in) + b * a.q_batch + n * a.q_token + (long long)x.h * D;
+            x.to = static_cast<T*>(a.q_out) + (((size_t)b * a.H_q + x.h) * N + n) * D;
+        } else if (x.h < H_qk) {
+            x.from = static_cast<const T*>(a.k_in) + b * a.k_batch + n * a.k_token + (long long)(x.h - a.H_q) * D;
+            x.to = static_cast<T*>(a.k_out) + (((size_t)b * a.H_kv + (x.h - a.H_q)) * N + n) * D;
+        } else {
+            x.from = static_cast<const T*>(a.v_in) + b * a.v_batch + n * a.v_token + (long long)(x.h - H_qk) * D;
+            x.to = static_cast<T*>(a.v_out) + (((size_t)b * a.H_kv + (x.h - H_qk)) * N + n) * D;
+        }
+        return x;
     };
 
-    const int h_first = blockIdx.y * HPB + tid / LPH;
     float x[U][8];
-    auto fetch = [&](int h0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (h0 + u * step < H_all) load8<T, VEC>(source(h0 + u * step) + 8 * c, x[u]);
-    };
-    fetch(h_first);
-    if (tid < half) {
-        const long long pos = (long long)a.seq_lens[b] + (a.depth ? a.depth[n] : n);
-        double turn = (double)pos * a.freqs[tid] * 0.15915494309189533577;      // 1 / (2 pi)
-        turn -= rint(turn);
-        float sn, cs;
-        sincospif(2.0f * (float)turn, &sn, &cs);
-        s_cs[tid] = make_float2(cs, sn);
-    }
-    float wq[8], wk[8];
-    if (a.q_weight) load8<T, VEC>(static_cast<const T*>(a.q_weight) + 8 * c, wq);
-    if (a.k_weight) load8<T, VEC>(static_cast<const T*>(a.k_weight) + 8 * c, wk);
-    __syncthreads();
-    // the loop runs alike for all lanes of a warp (shuffles), whatever heads they hold
-    for (int h0 = h_first; h0 - h_first < H_all; h0 += U * step) {
-        if (h0 != h_first) fetch(h0);
+    Row at[U];
+    auto fetch = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * step;
-            const bool mine = h < H_all, is_q = h < a.H_q, is_k = mine && !is_q && h < a.H_q + a.H_kv;
+            at[u] = row_at(i0 + u * HPB);
+            if (at[u].h >= 0) load8<T, VEC>(at[u].from + 8 * c, x[u]);
+        }
+    };
+    const int i_first = tid / LPH;
+    fetch(i_first);
+    for (int i = tid; i < TOK * half; i += kRopeThreads) {
+        const int tok = i / half, j = i - tok * half;
+        const long long token = token0 + tok;
+        if (token < tokens) {
+            const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
+            const long long pos = (long long)a.seq_lens[b] + (a.depth ? a.depth[n] : n);
+            double turn = (double)pos * a.freqs[j] * 0.15915494309189533577;    // 1 / (2 pi)
+            turn -= rint(turn);
+            float sn, cs;
+            sincospif(2.0f * (float)turn, &sn, &cs);
+            s_cs[tok][j] = make_float2(cs, sn);
+        }
+    }
+    __syncthreads();
+    // the loop runs alike for all lanes of a warp (shuffles), whatever heads they hold
+    for (int i0 = 0; i0 < rows; i0 += U * HPB) {
+        if (i0 > 0) fetch(i0 + i_first);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = at[u].h;
+            const bool is_q = h >= 0 && h < a.H_q, is_k = h >= a.H_q && h < H_qk;
+            const float2* const cs_of = s_cs[at[u].tok < TOK ? at[u].tok : 0];
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = mine ? x[u][e] : 0.f;
-            float sum = 0.f;
+            for (int e = 0; e < 8; ++e) y[e] = h >= 0 ? x[u][e] : 0.f;
+            if (a.q_weight || a.k_weight) {
+                float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+                for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
 #pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float inv = rsqrtf(sum * (1.0f / D) + a.eps);
-            if (is_q && a.q_weight) {
+                for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                const float inv = rsqrtf(sum * (1.0f / D) + a.eps);
+                const void* const weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+                if (weight) {
+                    float w[8];
+                    load8<T, VEC>(static_cast<const T*>(weight) + 8 * c, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] *= inv * wq[e];
-            }
-            if (is_k && a.k_weight) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] *= inv * wk[e];
+                    for (int e = 0; e < 8; ++e) y[e] *= inv * w[e];
+                }
             }
             if (a.interleaved) {
                 if (is_q || is_k) {
@@ -149,14 +167,14 @@ qk_norm_rope_kernel(const NormRopeArgs a) {
                     for (int e = 0; e < 8; e += 2) {
                         const int i = 4 * c + e / 2;
                         if (i < half) {
-                            const float2 cs = s_cs[i];
+                            const float2 cs = cs_of[i];
                             const float y0 = y[e], y1 = y[e + 1];
                             y[e] = y0 * cs.x - y1 * cs.y;
                             y[e + 1] = y1 * cs.x + y0 * cs.y;
                         }
                     }
                 }
-            } else {
+            } else if (half > 0) {
                 // element i pairs with i + half, which lies half / 8 lanes further on (half is a multiple of 8)
                 const int apart = half >> 3;
                 const bool low = c < apart, high = !low && c < 2 * apart;
@@ -167,12 +185,12 @@ qk_norm_rope_kernel(const NormRopeArgs a) {
                 if ((is_q || is_k) && (low || high)) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float2 cs = s_cs[8 * (low ? c : c - apart) + e];
+                        const float2 cs = cs_of[8 * (low ? c : c - apart) + e];
                         y[e] = low ? y[e] * cs.x - z[e] * cs.y : y[e] * cs.x + z[e] * cs.y;
                     }
                 }
             }
-            if (mine) store8<T, VEC>(target(h) + 8 * c, y);
+            if (h >= 0) store8<T, VEC>(at[u].to + 8 * c, y);
         }
     }
 }
@@ -182,13 +200,14 @@ static int launch(const NormRopeArgs& a, bool vec, cudaStream_t stream) {
     constexpr int HPB = kRopeThreads / (D / 8);
     const int H_all = a.H_q + 2 * a.H_kv;
     const long long tokens = (long long)a.B * a.N;
-    // With few tokens the heads of a token go to several blocks (each repeats the token's angles); with many, one block
-    // takes all heads of its token.
-    int splits = 1;
-    if (tokens < 296) splits = (H_all + HPB - 1) / HPB;
-    const dim3 grid((unsigned)tokens, (unsigned)splits);
-    if (vec) qk_norm_rope_kernel<T, D, true><<<grid, kRopeThreads, 0, stream>>>(a);
-    else qk_norm_rope_kernel<T, D, false><<<grid, kRopeThreads, 0, stream>>>(a);
+    // With few tokens the heads of a token go to several blocks (each repeats the token's angles); with many, a block takes
+    // four whole tokens, whose angles keep all its threads busy once.
+    const bool many = tokens >= 4 * 296;
+    const dim3 grid((unsigned)(many ? (tokens + 3) / 4 : tokens), (unsigned)(tokens < 296 ? (H_all + HPB - 1) / HPB : 1));
+    if (many && vec) qk_norm_rope_kernel<T, D, true, 4><<<grid, kRopeThreads, 0, stream>>>(a);
+    else if (many) qk_norm_rope_kernel<T, D, false, 4><<<grid, kRopeThreads, 0, stream>>>(a);
+    else if (vec) qk_norm_rope_kernel<T, D, true, 1><<<grid, kRopeThreads, 0, stream>>>(a);
+    else qk_norm_rope_kernel<T, D, false, 1><<<grid, kRopeThreads, 0, stream>>>(a);
     MCSD_CUDA_CHECK(cudaGetLastError());
     count_launches(1);
     return MCSD_OK;
