@@ -6,11 +6,14 @@
 // The offset is rounded to nearest: it moves the levels by at most 2^-9 |o|, a fraction of a step for rows whose
 // range is not small against their magnitude, and no more than the rounding of bf16 rows themselves otherwise.
 //
-// All three move bytes and little else.  A thread block owns a whole page while it writes: two rows share a byte of the
-// value codes, so a page that is written in part is read, merged and written back by the one thread that owns a
-// channel; no two blocks of a call touch the same page.
+// All three move bytes and little else, so what bounds them is memory, and the instructions per element while they store.
+// A warp turns eight rows, the ones that share the 32-bit words of the value codes, into codes: their loads are in flight
+// together, the scales and offsets of all of them are computed at once (one lane per row), and every code is added to its
+// words as it is made.  Two rows share a byte of the value codes: one warp owns all of its words, and where only some of
+// the rows are written it merges with what is there; no two warps of a call touch the same word.
 #include <type_traits>
 
+#include "f32x2.cuh"
 #include "kv4.cuh"
 
 namespace mcsd {
@@ -29,208 +32,278 @@ __device__ __forceinline__ float warp_max(float v) {
     return r;
 }
 
-// The type that decides between two codes.  For bf16 rows x - o is a short number and fp32 division cannot turn a value
-// next to the middle of two levels into the middle itself; fp32 rows have all 24 bits, so they are decided in 64.
-template <typename T> struct Decide { using type = float; };
-template <> struct Decide<float> { using type = double; };
-
-__device__ __forceinline__ float div_ieee(float a, float b) { return __fdiv_rn(a, b); }
-__device__ __forceinline__ double div_ieee(double a, double b) { return __ddiv_rn(a, b); }
-__device__ __forceinline__ double round_even(double a) { return rint(a); }
-__device__ __forceinline__ float round_even(float a) { return rintf(a); }
 __device__ __forceinline__ __nv_bfloat16 to_bf16(float a) { return __float2bfloat16_rn(a); }
 __device__ __forceinline__ __nv_bfloat16 to_bf16(double a) { return __float2bfloat16_rn((float)a); }   // by way of fp32 in both forms
 
-// E consecutive elements as fp32; VEC: the address is a multiple of their size
-template <int E, bool VEC> __device__ __forceinline__ void load_row(const float* p, float (&x)[E]) {
-    if (VEC && E == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        x[0] = v.x; x[1] = v.y; x[E - 2] = v.z; x[E - 1] = v.w;
-    } else if (VEC) {
-        const float2 v = *reinterpret_cast<const float2*>(p);
-        x[0] = v.x; x[1] = v.y;
-    } else {
+// E consecutive elements as they lie in memory; VEC: the address is a multiple of their size.  get() gives a neighbouring pair.
+template <typename T, int E> struct Piece;
+template <int E> struct Piece<float, E> {
+    float x[E];
+    template <bool VEC> __device__ __forceinline__ void load(const float* p) {
+        if (VEC && E == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p);
+            x[0] = v.x; x[1] = v.y; x[E - 2] = v.z; x[E - 1] = v.w;
+        } else if (VEC) {
+            const float2 v = *reinterpret_cast<const float2*>(p);
+            x[0] = v.x; x[1] = v.y;
+        } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = p[e];
+            for (int e = 0; e < E; ++e) x[e] = p[e];
+        }
     }
-}
-template <int E, bool VEC> __device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&x)[E]) {
-    if (VEC) {
-        uint32_t w[E / 2];
-        if (E == 4) {
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
+    }
+    __device__ __forceinline__ float2 get(int e) const { return make_float2(x[e], x[e + 1]); }
+};
+template <int E> struct Piece<__nv_bfloat16, E> {
+    uint32_t w[E / 2];
+    template <bool VEC> __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        if (VEC && E == 4) {
             const uint2 v = *reinterpret_cast<const uint2*>(p);
             w[0] = v.x; w[E / 2 - 1] = v.y;
-        } else {
+        } else if (VEC) {
             w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) w[e] = u[2 * e] | ((uint32_t)u[2 * e + 1] << 16);
         }
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = __bfloat162float(p[e]);
     }
-}
-
-// Codes of the E channels of one lane (a warp holds a row); returns the row's scale and offset.
-template <typename T, int E>
-__device__ __forceinline__ void quantise_row(const float (&x)[E], uint32_t (&code)[E], __nv_bfloat16& scale, __nv_bfloat16& offset) {
-    using F = typename Decide<T>::type;
-    float lo = x[0], hi = x[0];
+    __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int e = 1; e < E; ++e) { lo = fminf(lo, x[e]); hi = fmaxf(hi, x[e]); }
-    lo = warp_min(lo) + 0.f;                                  // rows of zeros: one bit pattern whatever their signs
-    hi = warp_max(hi) + 0.f;
-    scale = to_bf16(div_ieee((F)hi - (F)lo, (F)15));
-    const F s = (F)__bfloat162float(scale);
-    offset = to_bf16((F)lo - (F)16 * s);                      // 16 s is exact: the difference is rounded once either way
-    const F o = (F)__bfloat162float(offset);
-    if (sizeof(F) == 4 && (float)s > 1e-30f && (float)s < 1e30f) {
-        // The quotient by the row's reciprocal, corrected once by its own remainder (which the fused multiply-add gives without
-        // rounding): a value in the middle between two levels comes out as that middle, and no other value does.  Clamped
-        // to 16..31, the sum with 1.5 2^23 rounds it to the nearest whole number, ties to even, whose low four bits are the code.
-        const float r = 1.0f / (float)s;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = x[e] - (float)o, q0 = d * r, q = fmaf(fmaf(-q0, (float)s, d), r, q0);
-            code[e] = __float_as_uint(fminf(fmaxf(q, 16.f), 31.f) + 12582912.f) & 15u;      // (a NaN counts as 16)
-        }
-        return;
+        for (int e = 0; e < E / 2; ++e) w[e] = 0u;
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const F t = round_even(div_ieee((F)x[e] - o, s));
-        // comparisons are false for NaN (rows that are not finite): code 0
-        const F c = t > (F)16 ? (t < (F)31 ? t : (F)31) : (F)16;
-        code[e] = s > (F)0 ? (uint32_t)(int)c - 16u : 0u;
+    __device__ __forceinline__ float2 get(int e) const {
+        return make_float2(__uint_as_float(w[e / 2] << 16), __uint_as_float(w[e / 2] & 0xFFFF0000u));
     }
-}
-
-template <int D>
-struct PageSmem {
-    alignas(16) unsigned char codes[kPageRows][D];   // value codes by row, one byte each
-    uint32_t present;                         // rows of the page that are written
 };
 
-// Writes rows r0 .. r1 - 1 of a page; row_of(values, r) gives the source of page row r, or NULL to leave the row alone.
-// Called by all threads of the block.
-template <typename T, int D, bool VEC, typename RowOf>
-__device__ __forceinline__ void store_page(unsigned char* page, int r0, int r1, PageSmem<D>& sm, RowOf row_of) {
-    constexpr int E = D / 32;                                 // channels per lane
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    __nv_bfloat16* scales = reinterpret_cast<__nv_bfloat16*>(page + kv4_scales_at(D));
-    if (tid == 0) sm.present = 0;
-    // what a page that is written in part keeps; on its way while the rows are made
-    uint4* const dst = reinterpret_cast<uint4*>(page + kv4_values_at(D) + (tid < D ? tid : 0) * 16);
-    const bool part = r0 > 0 || r1 < kPageRows;
-    uint4 old = part && r0 < r1 ? *dst : make_uint4(0, 0, 0, 0);
-    __syncthreads();
-#pragma unroll 4
-    for (int r = r0 + warp; r < r1; r += kStoreWarps) {
-        const T* ks = row_of(false, r);
-        const T* vs = row_of(true, r);
-        if (ks == nullptr || vs == nullptr) continue;         // uniform in the warp
-        float xk[E], xv[E];
-        load_row<E, VEC>(ks + lane * E, xk);
-        load_row<E, VEC>(vs + lane * E, xv);
-        uint32_t ck[E], cv[E];
-        __nv_bfloat16 sk, ok, sv, ov;
-        quantise_row<T, E>(xk, ck, sk, ok);
-        quantise_row<T, E>(xv, cv, sv, ov);
-        // keys: the 8 / E lanes of a word put their nibbles together
-        uint32_t word = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) word |= ck[e] << kv4_bit((lane * E + e) & 7);
-#pragma unroll
-        for (int o = 1; o < 8 / E; o <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, o);
-        const int w = lane * E / 8;                           // word of the row
-        if ((lane * E) % 8 == 0)
-            *reinterpret_cast<uint32_t*>(page + (size_t)(w >> 2) * (kPageRows * 16) + r * 16 + (w & 3) * 4) = word;
-        if (E == 4) *reinterpret_cast<uint32_t*>(&sm.codes[r][lane * E]) = cv[0] | (cv[1] << 8) | (cv[E - 2] << 16) | (cv[E - 1] << 24);
-        else *reinterpret_cast<unsigned short*>(&sm.codes[r][lane * E]) = (unsigned short)(cv[0] | (cv[1] << 8));
-        if (lane == 0) {
-            scales[r] = sk;
-            scales[kPageRows + r] = ok;
-            scales[2 * kPageRows + r] = sv;
-            scales[3 * kPageRows + r] = ov;
-            atomicOr(&sm.present, 1u << r);
-        }
-    }
-    __syncthreads();
-    const uint32_t present = sm.present;
-    if (tid < D && present != 0) {
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (present == 0xFFFFFFFFu) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w[j] |= (uint32_t)sm.codes[8 * j + e][tid] << kv4_bit(e);
+// What a row's codes are made from.  The quotient (x - o) / s is the product with the reciprocal of s, corrected once by its
+// own remainder, which the fused multiply-add gives without rounding.  s has 8 significant bits, so no quotient is so
+// close to the middle of two neighbouring numbers that this could round it otherwise than a division does: a value in
+// the middle between two levels comes out as that middle, and no other value does.  bf16 rows are decided in 32 bits; fp32 rows,
+// whose x - o has more bits than that, in 64.  s = 0, infinite or NaN gives 0 or NaN here, and a NaN counts as code 0.
+//
+// code_bits() returns kCodeBase + code: the quotient, clamped to 16 .. 31, plus 1.5 2^23 is rounded to the nearest whole
+// number, ties to even, and its low bits are that number.
+constexpr uint32_t kCodeBase = 0x4B400010u;
+template <typename T> struct RowScale;
+template <> struct RowScale<__nv_bfloat16> {
+    using F = float;
+    float2 minus_o, minus_s, r;
+    __device__ __forceinline__ RowScale(float s, float o, float inv) : minus_o(make_float2(-o, -o)), minus_s(make_float2(-s, -s)), r(make_float2(inv, inv)) {}
+    // Outside this range products with the reciprocal could lose bits or overflow, and the division is made instead.
+    __device__ __forceinline__ static bool plain(float s) { return !(s > 0.f && s <= 1e-30f) && !(s >= 1e30f && s <= 3.4e38f); }
+    __device__ __forceinline__ static float inverse(float s) { return s > 0.f ? 1.0f / s : 0.f; }
+    template <bool PLAIN>
+    __device__ __forceinline__ void code_bits(float2 x, uint32_t& c0, uint32_t& c1) const {
+        const float2 d = add_f32x2(x, minus_o);
+        float2 q;
+        if (PLAIN) {
+            const float2 q0 = mul_f32x2(d, r);
+            q = fma_f32x2(fma_f32x2(q0, minus_s, d), r, q0);
         } else {
-            if (!part) old = *dst;                            // a whole page of which a row is left out (a malformed node)
-            const uint32_t keep[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int r = 8 * j + e;
-                    w[j] |= (present >> r) & 1u ? (uint32_t)sm.codes[r][tid] << kv4_bit(e) : keep[j] & (0xFu << kv4_bit(e));
-                }
+            q = make_float2(minus_s.x < 0.f ? __fdiv_rn(d.x, -minus_s.x) : 0.f, minus_s.y < 0.f ? __fdiv_rn(d.y, -minus_s.y) : 0.f);
         }
-        *dst = make_uint4(w[0], w[1], w[2], w[3]);
+        q = add_f32x2(make_float2(fminf(fmaxf(q.x, 16.f), 31.f), fminf(fmaxf(q.y, 16.f), 31.f)), make_float2(12582912.f, 12582912.f));
+        c0 = __float_as_uint(q.x);
+        c1 = __float_as_uint(q.y);
     }
-    __syncthreads();                                          // the codes may be overwritten
+};
+template <> struct RowScale<float> {
+    using F = double;
+    double s, o, r;
+    __device__ __forceinline__ RowScale(float s_, float o_, float) : s(s_), o(o_), r(s_ > 0.f ? 1.0 / (double)s_ : 0.0) {}
+    __device__ __forceinline__ static bool plain(float) { return true; }           // no fp32 number is near the limits of 64 bits
+    __device__ __forceinline__ static float inverse(float) { return 0.f; }
+    __device__ __forceinline__ uint32_t one(float x) const {
+        const double d = (double)x - o, q0 = d * r, q = fma(fma(-q0, s, d), r, q0);
+        return (uint32_t)__double2loint(fmin(fmax(q, 16.0), 31.0) + 6755399441055744.0) - 16u + kCodeBase;    // 1.5 2^52, likewise
+    }
+    template <bool PLAIN>
+    __device__ __forceinline__ void code_bits(float2 x, uint32_t& c0, uint32_t& c1) const { c0 = one(x.x); c1 = one(x.y); }
+};
+
+constexpr int kGroup = 8;                                     // rows that share the words of the value codes
+
+// Makes the codes of rows 8g .. 8g + 7 of a page as far as `present` has their bit; one whole warp.  k_row(r), v_row(r) give the
+// sources.  Key codes, scales and offsets go to the page, the words of the value codes (channels E lane ..) to vw, 0 in
+// the nibbles of absent rows.
+template <typename T, int D, bool VEC, typename KRow, typename VRow>
+__device__ __forceinline__ void make_group(unsigned char* page, int g, uint32_t present, KRow k_row, VRow v_row, uint32_t (&vw)[D / 32]) {
+    constexpr int E = D / 32;                                 // channels per lane
+    using F = typename RowScale<T>::F;
+    const int lane = threadIdx.x & 31;
+    Piece<T, E> x[2][kGroup];
+#pragma unroll
+    for (int r = 0; r < kGroup; ++r) {
+        x[0][r].zero();
+        x[1][r].zero();
+        if ((present >> r) & 1u) {
+            x[0][r].template load<VEC>(k_row(r) + lane * E);
+            x[1][r].template load<VEC>(v_row(r) + lane * E);
+        }
+    }
+    // lane r keeps the range of key row r, lane 8 + r that of value row r
+    float lo_mine = 0.f, hi_mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * kGroup; ++i) {
+        const Piece<T, E>& p = x[i / kGroup][i % kGroup];
+        float2 lo = p.get(0), hi = lo;
+        if (E == 4) {
+            const float2 z = p.get(E - 2);
+            lo = make_float2(fminf(lo.x, z.x), fminf(lo.y, z.y));
+            hi = make_float2(fmaxf(hi.x, z.x), fmaxf(hi.y, z.y));
+        }
+        const float l = warp_min(fminf(lo.x, lo.y)), h = warp_max(fmaxf(hi.x, hi.y));
+        if (lane == i) { lo_mine = l; hi_mine = h; }
+    }
+    lo_mine += 0.f;                                           // rows of zeros: one bit pattern whatever their signs
+    hi_mine += 0.f;
+    const __nv_bfloat16 scale = to_bf16(((F)hi_mine - (F)lo_mine) / (F)15);
+    const F s_mine = (F)__bfloat162float(scale);
+    const __nv_bfloat16 offset = to_bf16((F)lo_mine - (F)16 * s_mine);      // 16 s is exact: the difference is rounded once either way
+    const float s32 = __bfloat162float(scale), o32 = __bfloat162float(offset), inv = RowScale<T>::inverse(s32);
+    if (lane < 2 * kGroup && ((present >> (lane % kGroup)) & 1u)) {
+        __nv_bfloat16* const at = reinterpret_cast<__nv_bfloat16*>(page + kv4_scales_at(D)) + (lane / kGroup) * 2 * kPageRows + g * kGroup + lane % kGroup;
+        at[0] = scale;
+        at[kPageRows] = offset;
+    }
+    const bool plain = __all_sync(0xffffffffu, RowScale<T>::plain(s32));
+
+    uint32_t kw[kGroup], sum[E];
+    constexpr uint32_t kAll = 0x11111111u * kCodeBase;        // what the bases of eight codes add up to, modulo 2^32
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = 0u - kAll;
+    auto codes = [&](auto plain_t) {
+        constexpr bool kPlain = decltype(plain_t)::value;
+#pragma unroll
+        for (int r = 0; r < kGroup; ++r) {
+            const RowScale<T> key(__shfl_sync(0xffffffffu, s32, r), __shfl_sync(0xffffffffu, o32, r), __shfl_sync(0xffffffffu, inv, r));
+            kw[r] = 0u;
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                uint32_t c0, c1;
+                key.template code_bits<kPlain>(x[0][r].get(e), c0, c1);
+                kw[r] += ((c0 - kCodeBase) << kv4_bit(e)) + ((c1 - kCodeBase) << kv4_bit(e + 1));
+            }
+            const RowScale<T> val(__shfl_sync(0xffffffffu, s32, kGroup + r), __shfl_sync(0xffffffffu, o32, kGroup + r), __shfl_sync(0xffffffffu, inv, kGroup + r));
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                uint32_t c0, c1;
+                val.template code_bits<kPlain>(x[1][r].get(e), c0, c1);
+                sum[e] += c0 << kv4_bit(r);
+                sum[e + 1] += c1 << kv4_bit(r);
+            }
+        }
+    };
+    if (plain) codes(std::true_type{});
+    else codes(std::false_type{});
+#pragma unroll
+    for (int e = 0; e < E; ++e) vw[e] = sum[e];               // (absent rows are rows of zeros: code 0)
+    // The words of the key codes: the lanes of a word (2 or 4) put their nibbles together, even lanes for one row of a pair
+    // of rows and odd lanes for the other.
+    const int word = lane * E / 8, shift = lane * E % 8 * 2;  // elements lane E .. start at bit 2 (lane E mod 8)
+#pragma unroll
+    for (int r = 0; r < kGroup; r += 2) {
+        const uint32_t w0 = kw[r] << shift, w1 = kw[r + 1] << shift;
+        uint32_t w = (lane & 1 ? w1 : w0) | __shfl_xor_sync(0xffffffffu, lane & 1 ? w0 : w1, 1);
+        if (E == 2) w |= __shfl_xor_sync(0xffffffffu, w, 2);
+        const int row = r + (lane & 1);
+        if (((present >> row) & 1u) && (E == 4 || (lane & 2) == 0))
+            *reinterpret_cast<uint32_t*>(page + (word >> 2) * (kPageRows * 16) + (g * kGroup + row) * 16 + (word & 3) * 4) = w;
+    }
 }
 
-// grid: (pages that T rows can touch, B * H)
+// the nibbles of a word of value codes that belong to the rows of `present` (8 bits)
+__device__ __forceinline__ uint32_t nibbles_of(uint32_t present) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int r = 0; r < kGroup; ++r) m |= ((present >> r) & 1u) * (0xFu << kv4_bit(r));
+    return m;
+}
+
+// grid: (pages that T rows can touch, B * H); warp g makes rows 8g .. 8g + 7 of the page
 template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kStoreThreads)
 append_kv4_kernel(const T* __restrict__ k, const T* __restrict__ v, unsigned char* __restrict__ cache,
                   const int32_t* __restrict__ start, const int32_t* __restrict__ n_new, int H, int T_rows, int pages) {
-    __shared__ PageSmem<D> sm;
-    const int bh = blockIdx.y, b = bh / H;
+    constexpr int E = D / 32;
+    static_assert(kStoreWarps * kGroup == kPageRows, "one warp per group of rows");
+    __shared__ alignas(16) uint32_t s_words[kStoreWarps][D];
+    const int bh = blockIdx.y, b = bh / H, tid = threadIdx.x, lane = tid & 31, g = tid >> 5;
     const int first = start[b], n = n_new ? min(max(n_new[b], 0), T_rows) : T_rows;
     if (first < 0) return;
     const long long page = (long long)(first / kPageRows) + blockIdx.x;
     const long long row0 = page * kPageRows;                  // cache row of the page's row 0
     if (page >= pages || row0 >= (long long)first + n) return;
     const int r0 = (int)max((long long)first - row0, 0LL), r1 = (int)min((long long)first + n - row0, (long long)kPageRows);
-    const size_t src = (size_t)bh * T_rows;
-    store_page<T, D, VEC>(cache + ((size_t)bh * pages + page) * kv4_page_bytes(D), r0, r1, sm, [&](bool values, int r) {
-        return (values ? v : k) + (src + (size_t)(row0 + r - first)) * D;
-    });
+    if (r0 >= r1) return;                                     // nothing to append, in the middle of a page
+    unsigned char* const at = cache + ((size_t)bh * pages + page) * kv4_page_bytes(D);
+    uint4* const dst = reinterpret_cast<uint4*>(at + kv4_values_at(D) + (tid < D ? tid : 0) * 16);
+    uint4 old = make_uint4(0, 0, 0, 0);
+    if (r0 > 0 || r1 < kPageRows) old = *dst;                 // what a page that is written in part keeps
+    const uint32_t rows = (uint32_t)((1ULL << r1) - (1ULL << r0)), present = (rows >> (g * kGroup)) & 0xFFu;
+    const long long src = (long long)bh * T_rows + (row0 + g * kGroup - first);   // row of k and v of the group's row 0
+    uint32_t vw[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) vw[e] = 0u;
+    if (present != 0u)
+        make_group<T, D, VEC>(at, g, present, [&](int r) { return k + (src + r) * D; }, [&](int r) { return v + (src + r) * D; }, vw);
+    if (E == 4) *reinterpret_cast<uint4*>(&s_words[g][lane * E]) = make_uint4(vw[0], vw[1], vw[E - 2], vw[E - 1]);
+    else *reinterpret_cast<uint2*>(&s_words[g][lane * E]) = make_uint2(vw[0], vw[1]);
+    __syncthreads();
+    if (tid < D) {
+        const uint32_t o[4] = {old.x, old.y, old.z, old.w};
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = s_words[j][tid] | (o[j] & ~nibbles_of((rows >> (j * kGroup)) & 0xFFu));
+        *dst = make_uint4(w[0], w[1], w[2], w[3]);
+    }
 }
 
-// grid: (B * H, n_layers)
+// One warp per (layer, sequence, head): the rows it commits lie in one group or a few.
 template <typename T, int D>
 __global__ void __launch_bounds__(kStoreThreads)
 commit_kv4_kernel(void* const* __restrict__ cache_layers, const void* const* __restrict__ k_tree_layers,
                   const void* const* __restrict__ v_tree_layers, const int32_t* __restrict__ seq_lens,
                   const int32_t* __restrict__ accept_len, const int32_t* __restrict__ out_nodes,
-                  const int32_t* __restrict__ best_root, int n_levels, int H, int N, int pages) {
-    __shared__ PageSmem<D> sm;
-    const int bh = blockIdx.x, b = bh / H, layer = blockIdx.y;
+                  const int32_t* __restrict__ best_root, int n_levels, int BH, int H, int N, int pages) {
+    constexpr int E = D / 32;
+    const int bh = blockIdx.x * kStoreWarps + (threadIdx.x >> 5), b = bh / H, layer = blockIdx.y, lane = threadIdx.x & 31;
+    if (bh >= BH) return;
     const int L_max = pages * kPageRows;
     const int L = min(max(seq_lens[b], 0), L_max);
     const int acc = min(max(accept_len[b], 0), n_levels);
     const int end = min(L + 1 + acc, L_max);                  // rows beyond the cache are dropped
-    const T* kt = static_cast<const T*>(k_tree_layers[layer]) + (size_t)bh * N * D;
-    const T* vt = static_cast<const T*>(v_tree_layers[layer]) + (size_t)bh * N * D;
-    unsigned char* head = static_cast<unsigned char*>(cache_layers[layer]) + (size_t)bh * pages * kv4_page_bytes(D);
+    const T* const kt = static_cast<const T*>(k_tree_layers[layer]) + (size_t)bh * N * D;
+    const T* const vt = static_cast<const T*>(v_tree_layers[layer]) + (size_t)bh * N * D;
+    unsigned char* const head = static_cast<unsigned char*>(cache_layers[layer]) + (size_t)bh * pages * kv4_page_bytes(D);
     // (the pointers come from a table on the device, so their alignment is only known here)
     const bool vec = ((reinterpret_cast<uintptr_t>(kt) | reinterpret_cast<uintptr_t>(vt)) & 15u) == 0;
-    for (int page = L / kPageRows; page * kPageRows < end; ++page) {
-        const int row0 = page * kPageRows;
-        auto row_of = [&](bool values, int r) -> const T* {
-            const int i = row0 + r - L;                       // 0: the winning root, else accepted node i - 1
-            const int node = i == 0 ? best_root[b] : out_nodes[(size_t)b * n_levels + (i - 1)];
-            if (node < 0 || node >= N) return nullptr;        // malformed verify output: leave the row alone
-            return (values ? vt : kt) + (size_t)node * D;
-        };
-        unsigned char* const at = head + (size_t)page * kv4_page_bytes(D);
-        if (vec) store_page<T, D, true>(at, max(L - row0, 0), min(end - row0, kPageRows), sm, row_of);
-        else store_page<T, D, false>(at, max(L - row0, 0), min(end - row0, kPageRows), sm, row_of);
+    for (int row0 = L / kGroup * kGroup; row0 < end; row0 += kGroup) {
+        unsigned char* const at = head + (size_t)(row0 / kPageRows) * kv4_page_bytes(D);
+        const int g = row0 % kPageRows / kGroup;
+        // lane r: the tree node of row row0 + r (the winning root first, then the accepted nodes)
+        int node = -1;
+        const int row = row0 + lane;
+        if (lane < kGroup && row >= L && row < end) node = row == L ? best_root[b] : out_nodes[(size_t)b * n_levels + (row - L - 1)];
+        if (node >= N) node = -1;                             // malformed verify output: leave the row alone
+        const uint32_t present = __ballot_sync(0xffffffffu, node >= 0);
+        if (present == 0u) continue;
+        uint32_t old[E], vw[E];
+        uint32_t* const dst = reinterpret_cast<uint32_t*>(at + kv4_values_at(D) + lane * E * 16 + g * 4);
+#pragma unroll
+        for (int e = 0; e < E; ++e) old[e] = present == 0xFFu ? 0u : dst[e * 4];
+        auto k_row = [&](int r) { return kt + (size_t)__shfl_sync(0xffffffffu, node, r) * D; };
+        auto v_row = [&](int r) { return vt + (size_t)__shfl_sync(0xffffffffu, node, r) * D; };
+        if (vec) make_group<T, D, true>(at, g, present, k_row, v_row, vw);
+        else make_group<T, D, false>(at, g, present, k_row, v_row, vw);
+        const uint32_t keep = ~nibbles_of(present);
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[e * 4] = vw[e] | (old[e] & keep);
     }
 }
 
@@ -267,7 +340,7 @@ template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(kStoreThreads)
 read_kv4_kernel(const void* const* __restrict__ cache_layers, const int32_t* __restrict__ first_rows, const int32_t* __restrict__ n_rows,
                 int H, int T_rows, int pages, T* __restrict__ k, T* __restrict__ v) {
-    __shared__ PageSmem<D> sm;
+    __shared__ alignas(16) unsigned char s_codes[kPageRows][D];   // value codes by row, one byte each
     const int bh = blockIdx.y, b = bh / H, layer = blockIdx.z, tid = threadIdx.x;
     const long long first = first_rows[b];
     const int n = n_rows ? min(max(n_rows[b], 0), T_rows) : T_rows;
@@ -283,7 +356,7 @@ read_kv4_kernel(const void* const* __restrict__ cache_layers, const int32_t* __r
         const uint4 x = *reinterpret_cast<const uint4*>(at + kv4_values_at(D) + tid * 16);
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int r = 0; r < kPageRows; ++r) sm.codes[r][tid] = (unsigned char)((w[r >> 3] >> kv4_bit(r & 7)) & 15u);
+        for (int r = 0; r < kPageRows; ++r) s_codes[r][tid] = (unsigned char)((w[r >> 3] >> kv4_bit(r & 7)) & 15u);
     }
     __syncthreads();
     for (int i = tid; i < (r1 - r0) * (D / 8); i += kStoreThreads) {
@@ -294,7 +367,7 @@ read_kv4_kernel(const void* const* __restrict__ cache_layers, const int32_t* __r
         for (int e = 0; e < 8; ++e) xk[e] = xv[e] = 0.f;
         if (there && t < n) {
             const uint32_t w = *reinterpret_cast<const uint32_t*>(at + (size_t)(c >> 2) * (kPageRows * 16) + r * 16 + (c & 3) * 4);
-            const uint2 u = *reinterpret_cast<const uint2*>(&sm.codes[r][8 * c]);
+            const uint2 u = *reinterpret_cast<const uint2*>(&s_codes[r][8 * c]);
             const float ks = __bfloat162float(sc[r]), ko = __bfloat162float(sc[kPageRows + r]);
             const float vs = __bfloat162float(sc[2 * kPageRows + r]), vo = __bfloat162float(sc[3 * kPageRows + r]);
 #pragma unroll
@@ -393,8 +466,8 @@ extern "C" int mcsd_commit_kv4(void* const* cache_layers, const void* const* k_t
     return by_type(dtype, D, [&](auto t, auto d) {
         using T_ = decltype(t);
         constexpr int D_ = decltype(d)::value;
-        commit_kv4_kernel<T_, D_><<<dim3((unsigned)(B * H), (unsigned)n_layers), kStoreThreads, 0, s>>>(
-            cache_layers, k_tree_layers, v_tree_layers, seq_lens, accept_len, out_nodes, best_root, n_levels, H, N, L_max / kPageRows);
+        commit_kv4_kernel<T_, D_><<<dim3((unsigned)((B * H + kStoreWarps - 1) / kStoreWarps), (unsigned)n_layers), kStoreThreads, 0, s>>>(
+            cache_layers, k_tree_layers, v_tree_layers, seq_lens, accept_len, out_nodes, best_root, n_levels, B * H, H, N, L_max / kPageRows);
         MCSD_CUDA_CHECK(cudaGetLastError());
         grow_lens_kernel<<<(B + 127) / 128, 128, 0, s>>>(seq_lens, accept_len, n_levels, B, L_max);
         MCSD_CUDA_CHECK(cudaGetLastError());

@@ -5,192 +5,188 @@
 //   y = x * rsqrt(mean(x^2) + eps) * w          (skipped without a weight)
 //   angle = position * freq[i];   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin)   for every rotated pair (a, b)
 //
-// Every element is read once and written once, so memory bounds it (launch latency for single tokens).  A group of
-// D / 8 lanes holds one head, eight consecutive elements per lane: 16-byte loads and stores for bf16, the sum of squares
-// by shuffles inside the group, and for pairs that lie half a rotation apart the other element from the lane that has
-// it.  The angles of a token are the same for all heads: a block works on one or a few whole tokens, its threads first reduce
-// position * freq / 2 pi to a fraction of a turn in 64 bits (a far position has no bits left for the angle in 32) and
-// leave sine and cosine in shared memory while the first head rows are on their way.
+// Every element is read once and written once, so memory bounds it (launch latency for single tokens).  To come near that
+// bound the instructions per element have to be few: D / 8 lanes hold one head, and a lane takes four elements and the
+// four they are rotated with, so that no pair crosses lanes (only the sum of squares does); it keeps one token's sines
+// and cosines in registers for all the heads it works on, and the weights for all its rows; the arithmetic goes by two.
+// The angles are reduced as position * freq / 2 pi to a fraction of a turn in 64 bits (a far position has no bits left
+// for the angle in 32) by all threads of a block while the first rows are on their way.
+#include "f32x2.cuh"
 #include "norm_rope.cuh"
 
 namespace mcsd {
 
 constexpr int kRopeThreads = 256;
 
-template <typename T> struct Row8;
-template <> struct Row8<__nv_bfloat16> {
-    __device__ __forceinline__ static void load(const __nv_bfloat16* p, float (&x)[8]) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+// four consecutive elements as they lie in memory; VEC: aligned to their size
+template <typename T> struct Quad;
+template <> struct Quad<__nv_bfloat16> {
+    uint2 w;
+    template <bool VEC> __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        if (VEC) {
+            w = *reinterpret_cast<const uint2*>(p);
+        } else {
+            const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+            w = make_uint2(u[0] | ((uint32_t)u[1] << 16), u[2] | ((uint32_t)u[3] << 16));
         }
     }
-    __device__ __forceinline__ static void store(__nv_bfloat16* p, const float (&x)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    template <bool VEC> __device__ __forceinline__ void store(__nv_bfloat16* p) const {
+        if (VEC) {
+            *reinterpret_cast<uint2*>(p) = w;
+        } else {
+            unsigned short* u = reinterpret_cast<unsigned short*>(p);
+            u[0] = (unsigned short)w.x; u[1] = (unsigned short)(w.x >> 16); u[2] = (unsigned short)w.y; u[3] = (unsigned short)(w.y >> 16);
         }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ __forceinline__ static float one(__nv_bfloat16 v) { return __bfloat162float(v); }
-    __device__ __forceinline__ static __nv_bfloat16 back(float v) { return __float2bfloat16_rn(v); }
+    __device__ __forceinline__ void ones() { w = make_uint2(0x3F803F80u, 0x3F803F80u); }
+    __device__ __forceinline__ void zero() { w = make_uint2(0u, 0u); }
+    __device__ __forceinline__ float2 lo() const { return make_float2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u)); }
+    __device__ __forceinline__ float2 hi() const { return make_float2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)); }
+    __device__ __forceinline__ void set(float2 a, float2 b) {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y), y = __floats2bfloat162_rn(b.x, b.y);
+        w = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+    }
 };
-template <> struct Row8<float> {
-    __device__ __forceinline__ static void load(const float* p, float (&x)[8]) {
-        const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+template <> struct Quad<float> {
+    float4 w;
+    template <bool VEC> __device__ __forceinline__ void load(const float* p) {
+        if (VEC) w = *reinterpret_cast<const float4*>(p);
+        else w = make_float4(p[0], p[1], p[2], p[3]);
     }
-    __device__ __forceinline__ static void store(float* p, const float (&x)[8]) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    template <bool VEC> __device__ __forceinline__ void store(float* p) const {
+        if (VEC) {
+            *reinterpret_cast<float4*>(p) = w;
+        } else {
+            p[0] = w.x; p[1] = w.y; p[2] = w.z; p[3] = w.w;
+        }
     }
-    __device__ __forceinline__ static float one(float v) { return v; }
-    __device__ __forceinline__ static float back(float v) { return v; }
+    __device__ __forceinline__ void ones() { w = make_float4(1.f, 1.f, 1.f, 1.f); }
+    __device__ __forceinline__ void zero() { w = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ float2 lo() const { return make_float2(w.x, w.y); }
+    __device__ __forceinline__ float2 hi() const { return make_float2(w.z, w.w); }
+    __device__ __forceinline__ void set(float2 a, float2 b) { w = make_float4(a.x, a.y, b.x, b.y); }
 };
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
-    if (VEC) {
-        Row8<T>::load(p, x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = Row8<T>::one(p[e]);
-    }
-}
-template <typename T, bool VEC>
-__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
-    if (VEC) {
-        Row8<T>::store(p, x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = Row8<T>::back(x[e]);
-    }
-}
 
 // grid: (groups of TOK tokens, head splits).  VEC: every row starts on a 16-byte boundary.
 template <typename T, int D, bool VEC, int TOK>
-__global__ void __launch_bounds__(kRopeThreads, 3)
+__global__ void __launch_bounds__(kRopeThreads)
 qk_norm_rope_kernel(const NormRopeArgs a) {
     constexpr int LPH = D / 8;                                // lanes per head
-    constexpr int HPB = kRopeThreads / LPH;                   // heads of a block at a time
-    constexpr int U = 3;                                      // of them whose loads are in flight together
-    __shared__ float2 s_cs[TOK][D / 2];
-    const int tid = threadIdx.x, c = tid % LPH;
+    constexpr int GPT = kRopeThreads / LPH / TOK;             // heads of one token at a time
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;                 // rows of a lane whose loads are in flight together
+    __shared__ float4 s_cos[TOK][LPH], s_sin[TOK][LPH];
+    const int tid = threadIdx.x, c = tid % LPH, group = tid / LPH, tok = group / GPT;
     const int half = a.rot_dim >> 1;
     const int H_all = a.H_q + 2 * a.H_kv, H_qk = a.H_q + a.H_kv;
     const long long token0 = (long long)blockIdx.x * TOK, tokens = (long long)a.B * a.N;
-    // The rows of the block in the order (token, head), `per` heads to a token; this thread takes every HPB-th.
-    const int per = (H_all + gridDim.y - 1) / gridDim.y, h_lo = blockIdx.y * per;
-    const int rows = per * TOK;
+    const int per = (H_all + gridDim.y - 1) / gridDim.y, h_first = blockIdx.y * per + group % GPT;
+    const long long token = min(token0 + tok, tokens - 1);
+    const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
+    int h_end = min((int)(blockIdx.y + 1) * per, H_all);
+    if (token0 + tok >= tokens || (a.n_active && n >= a.n_active[b])) h_end = 0;    // the same for all lanes of a warp
 
-    struct Row { const T* from; T* to; int h, tok; };          // h < 0: nothing there
-    auto row_at = [&](int i) -> Row {
-        Row x;
-        x.tok = TOK == 1 ? 0 : i / per;
-        x.h = h_lo + i - x.tok * per;
-        const long long token = token0 + x.tok;
-        if (i >= rows || x.h >= H_all || token >= tokens) { x.h = -1; return x; }
-        const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
-        if (a.n_active && n >= a.n_active[b]) { x.h = -1; return x; }
-        const size_t N = a.N;
-        if (x.h < a.H_q) {
-            x.from = static_cast<const T*>(a.q_in) + b * a.q_batch + n * a.q_token + (long long)x.h * D;
-            x.to = static_cast<T*>(a.q_out) + (((size_t)b * a.H_q + x.h) * N + n) * D;
-        } else if (x.h < H_qk) {
-            x.from = static_cast<const T*>(a.k_in) + b * a.k_batch + n * a.k_token + (long long)(x.h - a.H_q) * D;
-            x.to = static_cast<T*>(a.k_out) + (((size_t)b * a.H_kv + (x.h - a.H_q)) * N + n) * D;
-        } else {
-            x.from = static_cast<const T*>(a.v_in) + b * a.v_batch + n * a.v_token + (long long)(x.h - H_qk) * D;
-            x.to = static_cast<T*>(a.v_out) + (((size_t)b * a.H_kv + (x.h - H_qk)) * N + n) * D;
+    // Where this lane's two quads lie in a row.  Neighbours are pairs: eight elements in a row.  Pairs half a rotation apart:
+    // elements 4c .. 4c + 3 and their partners; what is not rotated lies behind, and is split down its middle.
+    const int off_a = a.interleaved ? 8 * c : 4 * c < half ? 4 * c : 4 * c + half;
+    const int off_b = a.interleaved ? 8 * c + 4 : 4 * c < half ? 4 * c + half : 4 * c + D / 2;
+
+    const T* const q_in = static_cast<const T*>(a.q_in) + b * a.q_batch + n * a.q_token;
+    const T* const k_in = static_cast<const T*>(a.k_in) + b * a.k_batch + n * a.k_token;
+    const T* const v_in = static_cast<const T*>(a.v_in) + b * a.v_batch + n * a.v_token;
+    Quad<T> xa[U], xb[U];
+    auto fetch = [&](int h, int u) {
+        xa[u].zero();
+        xb[u].zero();
+        if (h < h_end) {
+            const T* const from = h < a.H_q ? q_in + (long long)h * D : h < H_qk ? k_in + (long long)(h - a.H_q) * D : v_in + (long long)(h - H_qk) * D;
+            xa[u].template load<VEC>(from + off_a);
+            xb[u].template load<VEC>(from + off_b);
         }
-        return x;
     };
-
-    float x[U][8];
-    Row at[U];
-    auto fetch = [&](int i0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            at[u] = row_at(i0 + u * HPB);
-            if (at[u].h >= 0) load8<T, VEC>(at[u].from + 8 * c, x[u]);
-        }
-    };
-    const int i_first = tid / LPH;
-    fetch(i_first);
+    for (int u = 0; u < U; ++u) fetch(h_first + u * GPT, u);
+    Quad<T> wqa, wqb, wka, wkb;
+    wqa.ones(); wqb.ones(); wka.ones(); wkb.ones();
+    if (a.q_weight) {
+        wqa.template load<VEC>(static_cast<const T*>(a.q_weight) + off_a);
+        wqb.template load<VEC>(static_cast<const T*>(a.q_weight) + off_b);
+    }
+    if (a.k_weight) {
+        wka.template load<VEC>(static_cast<const T*>(a.k_weight) + off_a);
+        wkb.template load<VEC>(static_cast<const T*>(a.k_weight) + off_b);
+    }
     for (int i = tid; i < TOK * half; i += kRopeThreads) {
-        const int tok = i / half, j = i - tok * half;
-        const long long token = token0 + tok;
-        if (token < tokens) {
-            const int b = (int)(token / a.N), n = (int)(token - (long long)b * a.N);
-            const long long pos = (long long)a.seq_lens[b] + (a.depth ? a.depth[n] : n);
+        const int t = i / half, j = i - t * half;
+        if (token0 + t < tokens) {
+            const int tb = (int)((token0 + t) / a.N), tn = (int)(token0 + t - (long long)tb * a.N);
+            const long long pos = (long long)a.seq_lens[tb] + (a.depth ? a.depth[tn] : tn);
             double turn = (double)pos * a.freqs[j] * 0.15915494309189533577;    // 1 / (2 pi)
             turn -= rint(turn);
             float sn, cs;
             sincospif(2.0f * (float)turn, &sn, &cs);
-            s_cs[tok][j] = make_float2(cs, sn);
+            reinterpret_cast<float*>(s_cos[t])[j] = cs;
+            reinterpret_cast<float*>(s_sin[t])[j] = sn;
         }
     }
     __syncthreads();
+    const float4 cs = s_cos[tok][c], sn = s_sin[tok][c];      // of pairs 4c .. 4c + 3; not set, and not used, from `half` on
+    const size_t N = a.N;
+    T* const q_out = static_cast<T*>(a.q_out) + ((size_t)b * a.H_q * N + n) * D;
+    T* const k_out = static_cast<T*>(a.k_out) + ((size_t)b * a.H_kv * N + n) * D;
+    T* const v_out = static_cast<T*>(a.v_out) + ((size_t)b * a.H_kv * N + n) * D;
+    const bool norms = a.q_weight || a.k_weight;
     // the loop runs alike for all lanes of a warp (shuffles), whatever heads they hold
-    for (int i0 = 0; i0 < rows; i0 += U * HPB) {
-        if (i0 > 0) fetch(i0 + i_first);
+    for (int h0 = h_first; h0 - h_first < per; h0 += U * GPT) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = at[u].h;
-            const bool is_q = h >= 0 && h < a.H_q, is_k = h >= a.H_q && h < H_qk;
-            const float2* const cs_of = s_cs[at[u].tok < TOK ? at[u].tok : 0];
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = h >= 0 ? x[u][e] : 0.f;
-            if (a.q_weight || a.k_weight) {
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(y[e], y[e], sum);
+            const int h = h0 + u * GPT;
+            const bool is_q = h < a.H_q, is_v = h >= H_qk;
+            Quad<T> ya = xa[u], yb = xb[u];
+            float2 a0 = ya.lo(), a1 = ya.hi(), b0 = yb.lo(), b1 = yb.hi();
+            const Quad<T> va = ya, vb = yb;                   // values pass through unchanged
+            fetch(h + U * GPT, u);
+            if (norms) {
+                float2 sq = mul_f32x2(a0, a0);
+                sq = fma_f32x2(a1, a1, sq);
+                sq = fma_f32x2(b0, b0, sq);
+                sq = fma_f32x2(b1, b1, sq);
+                float sum = sq.x + sq.y;
 #pragma unroll
                 for (int o = LPH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const float inv = rsqrtf(sum * (1.0f / D) + a.eps);
-                const void* const weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
-                if (weight) {
-                    float w[8];
-                    load8<T, VEC>(static_cast<const T*>(weight) + 8 * c, w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= inv * w[e];
-                }
+                const float inv = (is_q ? a.q_weight : a.k_weight) ? rsqrtf(sum * (1.0f / D) + a.eps) : 1.0f;
+                const float2 inv2 = make_float2(inv, inv);
+                Quad<T> wa = wqa, wb = wqb;
+                if (!is_q) { wa = wka; wb = wkb; }
+                a0 = mul_f32x2(a0, mul_f32x2(wa.lo(), inv2));
+                a1 = mul_f32x2(a1, mul_f32x2(wa.hi(), inv2));
+                b0 = mul_f32x2(b0, mul_f32x2(wb.lo(), inv2));
+                b1 = mul_f32x2(b1, mul_f32x2(wb.hi(), inv2));
             }
             if (a.interleaved) {
-                if (is_q || is_k) {
-#pragma unroll
-                    for (int e = 0; e < 8; e += 2) {
-                        const int i = 4 * c + e / 2;
-                        if (i < half) {
-                            const float2 cs = cs_of[i];
-                            const float y0 = y[e], y1 = y[e + 1];
-                            y[e] = y0 * cs.x - y1 * cs.y;
-                            y[e + 1] = y1 * cs.x + y0 * cs.y;
-                        }
-                    }
-                }
-            } else if (half > 0) {
-                // element i pairs with i + half, which lies half / 8 lanes further on (half is a multiple of 8)
-                const int apart = half >> 3;
-                const bool low = c < apart, high = !low && c < 2 * apart;
-                const int from = (tid & 31) + (low ? apart : high ? -apart : 0);
-                float z[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = __shfl_sync(0xffffffffu, y[e], from);
-                if ((is_q || is_k) && (low || high)) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float2 cs = cs_of[8 * (low ? c : c - apart) + e];
-                        y[e] = low ? y[e] * cs.x - z[e] * cs.y : y[e] * cs.x + z[e] * cs.y;
-                    }
-                }
+                auto turn = [&](float2& y, int pair, float co, float si) {
+                    if (pair < half) y = make_float2(y.x * co - y.y * si, y.y * co + y.x * si);
+                };
+                turn(a0, 4 * c, cs.x, sn.x);
+                turn(a1, 4 * c + 1, cs.y, sn.y);
+                turn(b0, 4 * c + 2, cs.z, sn.z);
+                turn(b1, 4 * c + 3, cs.w, sn.w);
+            } else if (4 * c < half) {                        // half is a multiple of 8
+                const float2 c0 = make_float2(cs.x, cs.y), c1 = make_float2(cs.z, cs.w), s0 = make_float2(sn.x, sn.y), s1 = make_float2(sn.z, sn.w);
+                const float2 m0 = make_float2(-sn.x, -sn.y), m1 = make_float2(-sn.z, -sn.w);
+                const float2 x0 = a0, x1 = a1;
+                a0 = fma_f32x2(b0, m0, mul_f32x2(x0, c0));
+                a1 = fma_f32x2(b1, m1, mul_f32x2(x1, c1));
+                b0 = fma_f32x2(x0, s0, mul_f32x2(b0, c0));
+                b1 = fma_f32x2(x1, s1, mul_f32x2(b1, c1));
             }
-            if (h >= 0) store8<T, VEC>(at[u].to + 8 * c, y);
+            ya.set(a0, a1);
+            yb.set(b0, b1);
+            if (is_v) { ya = va; yb = vb; }
+            if (h < h_end) {
+                T* const to = is_q ? q_out + (size_t)h * N * D : !is_v ? k_out + (size_t)(h - a.H_q) * N * D : v_out + (size_t)(h - H_qk) * N * D;
+                ya.template store<VEC>(to + off_a);
+                yb.template store<VEC>(to + off_b);
+            }
         }
     }
 }
@@ -204,10 +200,9 @@ static int launch(const NormRopeArgs& a, bool vec, cudaStream_t stream) {
     // four whole tokens, whose angles keep all its threads busy once.
     const bool many = tokens >= 4 * 296;
     const dim3 grid((unsigned)(many ? (tokens + 3) / 4 : tokens), (unsigned)(tokens < 296 ? (H_all + HPB - 1) / HPB : 1));
-    if (many && vec) qk_norm_rope_kernel<T, D, true, 4><<<grid, kRopeThreads, 0, stream>>>(a);
-    else if (many) qk_norm_rope_kernel<T, D, false, 4><<<grid, kRopeThreads, 0, stream>>>(a);
-    else if (vec) qk_norm_rope_kernel<T, D, true, 1><<<grid, kRopeThreads, 0, stream>>>(a);
-    else qk_norm_rope_kernel<T, D, false, 1><<<grid, kRopeThreads, 0, stream>>>(a);
+    if (!vec) qk_norm_rope_kernel<T, D, false, 1><<<dim3((unsigned)tokens, grid.y), kRopeThreads, 0, stream>>>(a);
+    else if (many) qk_norm_rope_kernel<T, D, true, 4><<<grid, kRopeThreads, 0, stream>>>(a);
+    else qk_norm_rope_kernel<T, D, true, 1><<<grid, kRopeThreads, 0, stream>>>(a);
     MCSD_CUDA_CHECK(cudaGetLastError());
     count_launches(1);
     return MCSD_OK;
