@@ -130,8 +130,9 @@ constexpr int kGroup = 8;                                     // rows that share
 
 // Makes the codes of rows 8g .. 8g + 7 of a page as far as `present` has their bit; one whole warp.  k_row(r), v_row(r) give the
 // sources.  Key codes, scales and offsets go to the page, the words of the value codes (channels E lane ..) to vw, 0 in
-// the nibbles of absent rows.
-template <typename T, int D, bool VEC, typename KRow, typename VRow>
+// the nibbles of absent rows.  SPARSE: few rows are expected, and the instructions for absent ones are branched over, else they
+// are made as rows of zeros.
+template <typename T, int D, bool VEC, bool SPARSE, typename KRow, typename VRow>
 __device__ __forceinline__ void make_group(unsigned char* page, int g, uint32_t present, KRow k_row, VRow v_row, uint32_t (&vw)[D / 32]) {
     constexpr int E = D / 32;                                 // channels per lane
     using F = typename RowScale<T>::F;
@@ -150,6 +151,7 @@ __device__ __forceinline__ void make_group(unsigned char* page, int g, uint32_t 
     float lo_mine = 0.f, hi_mine = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * kGroup; ++i) {
+        if (SPARSE && ((present >> (i % kGroup)) & 1u) == 0u) continue;
         const Piece<T, E>& p = x[i / kGroup][i % kGroup];
         float2 lo = p.get(0), hi = lo;
         if (E == 4) {
@@ -176,13 +178,14 @@ __device__ __forceinline__ void make_group(unsigned char* page, int g, uint32_t 
     uint32_t kw[kGroup], sum[E];
     constexpr uint32_t kAll = 0x11111111u * kCodeBase;        // what the bases of eight codes add up to, modulo 2^32
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0u - kAll;
+    for (int e = 0; e < E; ++e) sum[e] = SPARSE ? 0u : 0u - kAll;
     auto codes = [&](auto plain_t) {
         constexpr bool kPlain = decltype(plain_t)::value;
 #pragma unroll
         for (int r = 0; r < kGroup; ++r) {
-            const RowScale<T> key(__shfl_sync(0xffffffffu, s32, r), __shfl_sync(0xffffffffu, o32, r), __shfl_sync(0xffffffffu, inv, r));
             kw[r] = 0u;
+            if (SPARSE && ((present >> r) & 1u) == 0u) continue;
+            const RowScale<T> key(__shfl_sync(0xffffffffu, s32, r), __shfl_sync(0xffffffffu, o32, r), __shfl_sync(0xffffffffu, inv, r));
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
                 uint32_t c0, c1;
@@ -194,20 +197,21 @@ __device__ __forceinline__ void make_group(unsigned char* page, int g, uint32_t 
             for (int e = 0; e < E; e += 2) {
                 uint32_t c0, c1;
                 val.template code_bits<kPlain>(x[1][r].get(e), c0, c1);
-                sum[e] += c0 << kv4_bit(r);
-                sum[e + 1] += c1 << kv4_bit(r);
+                sum[e] += (SPARSE ? c0 - kCodeBase : c0) << kv4_bit(r);
+                sum[e + 1] += (SPARSE ? c1 - kCodeBase : c1) << kv4_bit(r);
             }
         }
     };
     if (plain) codes(std::true_type{});
     else codes(std::false_type{});
 #pragma unroll
-    for (int e = 0; e < E; ++e) vw[e] = sum[e];               // (absent rows are rows of zeros: code 0)
+    for (int e = 0; e < E; ++e) vw[e] = sum[e];               // (rows of zeros have code 0)
     // The words of the key codes: the lanes of a word (2 or 4) put their nibbles together, even lanes for one row of a pair
     // of rows and odd lanes for the other.
     const int word = lane * E / 8, shift = lane * E % 8 * 2;  // elements lane E .. start at bit 2 (lane E mod 8)
 #pragma unroll
     for (int r = 0; r < kGroup; r += 2) {
+        if (SPARSE && ((present >> r) & 3u) == 0u) continue;
         const uint32_t w0 = kw[r] << shift, w1 = kw[r + 1] << shift;
         uint32_t w = (lane & 1 ? w1 : w0) | __shfl_xor_sync(0xffffffffu, lane & 1 ? w0 : w1, 1);
         if (E == 2) w |= __shfl_xor_sync(0xffffffffu, w, 2);
@@ -251,7 +255,7 @@ append_kv4_kernel(const T* __restrict__ k, const T* __restrict__ v, unsigned cha
 #pragma unroll
     for (int e = 0; e < E; ++e) vw[e] = 0u;
     if (present != 0u)
-        make_group<T, D, VEC>(at, g, present, [&](int r) { return k + (src + r) * D; }, [&](int r) { return v + (src + r) * D; }, vw);
+        make_group<T, D, VEC, false>(at, g, present, [&](int r) { return k + (src + r) * D; }, [&](int r) { return v + (src + r) * D; }, vw);
     if (E == 4) *reinterpret_cast<uint4*>(&s_words[g][lane * E]) = make_uint4(vw[0], vw[1], vw[E - 2], vw[E - 1]);
     else *reinterpret_cast<uint2*>(&s_words[g][lane * E]) = make_uint2(vw[0], vw[1]);
     __syncthreads();
@@ -299,8 +303,8 @@ commit_kv4_kernel(void* const* __restrict__ cache_layers, const void* const* __r
         for (int e = 0; e < E; ++e) old[e] = present == 0xFFu ? 0u : dst[e * 4];
         auto k_row = [&](int r) { return kt + (size_t)__shfl_sync(0xffffffffu, node, r) * D; };
         auto v_row = [&](int r) { return vt + (size_t)__shfl_sync(0xffffffffu, node, r) * D; };
-        if (vec) make_group<T, D, true>(at, g, present, k_row, v_row, vw);
-        else make_group<T, D, false>(at, g, present, k_row, v_row, vw);
+        if (vec) make_group<T, D, true, true>(at, g, present, k_row, v_row, vw);
+        else make_group<T, D, false, true>(at, g, present, k_row, v_row, vw);
         const uint32_t keep = ~nibbles_of(present);
 #pragma unroll
         for (int e = 0; e < E; ++e) dst[e * 4] = vw[e] | (old[e] & keep);
@@ -350,31 +354,47 @@ read_kv4_kernel(const void* const* __restrict__ cache_layers, const int32_t* __r
     if (r0 >= r1) return;
     const bool there = page >= 0 && page < pages;
     const unsigned char* at = static_cast<const unsigned char*>(cache_layers[layer]) + ((size_t)bh * pages + (there ? page : 0)) * kv4_page_bytes(D);
-    const __nv_bfloat16* sc = reinterpret_cast<const __nv_bfloat16*>(at + kv4_scales_at(D));
+    const unsigned short* const sc = reinterpret_cast<const unsigned short*>(at + kv4_scales_at(D));
     const size_t out0 = ((size_t)layer * gridDim.y + bh) * T_rows;
-    if (there && tid < D) {
-        const uint4 x = *reinterpret_cast<const uint4*>(at + kv4_values_at(D) + tid * 16);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    // all that the block reads is on its way before the first of it is used
+    constexpr int U = kPageRows * (D / 8) / kStoreThreads;    // pieces of eight channels per thread
+    const int pieces = (r1 - r0) * (D / 8);
+    uint4 vals = make_uint4(0, 0, 0, 0);
+    if (there && tid < D) vals = *reinterpret_cast<const uint4*>(at + kv4_values_at(D) + tid * 16);
+    uint32_t keys[U], k_scale[U], v_scale[U];                 // scale in the low half, offset in the high half
 #pragma unroll
-        for (int r = 0; r < kPageRows; ++r) s_codes[r][tid] = (unsigned char)((w[r >> 3] >> kv4_bit(r & 7)) & 15u);
+    for (int u = 0; u < U; ++u) {
+        const int i = tid + u * kStoreThreads, r = r0 + i / (D / 8), c = i % (D / 8);
+        keys[u] = k_scale[u] = v_scale[u] = 0u;               // rows that are not there read as zero
+        if (there && i < pieces && (int)(row0 + r - first) < n) {
+            keys[u] = *reinterpret_cast<const uint32_t*>(at + (c >> 2) * (kPageRows * 16) + r * 16 + (c & 3) * 4);
+            k_scale[u] = sc[r] | ((uint32_t)sc[kPageRows + r] << 16);
+            v_scale[u] = sc[2 * kPageRows + r] | ((uint32_t)sc[3 * kPageRows + r] << 16);
+        }
+    }
+    if (tid < D) {
+        const uint32_t w[4] = {vals.x, vals.y, vals.z, vals.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (8 * j + 8 <= r0 || 8 * j >= r1) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s_codes[8 * j + e][tid] = (unsigned char)((w[j] >> kv4_bit(e)) & 15u);
+        }
     }
     __syncthreads();
-    for (int i = tid; i < (r1 - r0) * (D / 8); i += kStoreThreads) {
-        const int r = r0 + i / (D / 8), c = i % (D / 8);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = tid + u * kStoreThreads, r = r0 + i / (D / 8), c = i % (D / 8);
+        if (i >= pieces) break;
         const int t = (int)(row0 + r - first);
+        const uint2 codes = *reinterpret_cast<const uint2*>(&s_codes[r][8 * c]);
+        const float ks = bf16_bits_to_f32(k_scale[u] & 0xFFFFu), ko = __uint_as_float(k_scale[u] & 0xFFFF0000u);
+        const float vs = bf16_bits_to_f32(v_scale[u] & 0xFFFFu), vo = __uint_as_float(v_scale[u] & 0xFFFF0000u);
         float xk[8], xv[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) xk[e] = xv[e] = 0.f;
-        if (there && t < n) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(at + (size_t)(c >> 2) * (kPageRows * 16) + r * 16 + (c & 3) * 4);
-            const uint2 u = *reinterpret_cast<const uint2*>(&s_codes[r][8 * c]);
-            const float ks = __bfloat162float(sc[r]), ko = __bfloat162float(sc[kPageRows + r]);
-            const float vs = __bfloat162float(sc[2 * kPageRows + r]), vo = __bfloat162float(sc[3 * kPageRows + r]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                xk[e] = kv4_value((w >> kv4_bit(e)) & 15u, ks, ko);
-                xv[e] = kv4_value(((e < 4 ? u.x : u.y) >> (8 * (e & 3))) & 15u, vs, vo);
-            }
+        for (int e = 0; e < 8; ++e) {
+            xk[e] = kv4_value((keys[u] >> kv4_bit(e)) & 15u, ks, ko);
+            xv[e] = kv4_value(((e < 4 ? codes.x : codes.y) >> (8 * (e & 3))) & 15u, vs, vo);
         }
         T* const dk = k + (out0 + t) * D + 8 * c;
         T* const dv = v + (out0 + t) * D + 8 * c;
