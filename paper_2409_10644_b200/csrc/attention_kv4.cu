@@ -899,42 +899,33 @@ tree_attention_kv4_kernel(const Params p) {
                     auto p_free = [&]() {
                         if (g >= 2 && !mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
                     };
-                    auto scores = [&](float (&y)[8], int j) {
+                    auto scores = [&](float (&y)[8], float (&x)[8], int j) {
 #pragma unroll
                         for (int k = 0; k < 8; k += 4) {
                             const float4 q = *reinterpret_cast<const float4*>(qs + 8 * j + k), m = *reinterpret_cast<const float4*>(nref + 8 * j + k);
                             const float2 u = fma_f32x2(make_float2(y[k], y[k + 1]), a2, fma_f32x2(make_float2(q.x, q.y), b2, make_float2(m.x, m.y)));
                             const float2 v = fma_f32x2(make_float2(y[k + 2], y[k + 3]), a2, fma_f32x2(make_float2(q.z, q.w), b2, make_float2(m.z, m.w)));
-                            y[k] = u.x; y[k + 1] = u.y; y[k + 2] = v.x; y[k + 3] = v.y;
+                            x[k] = u.x; x[k + 1] = u.y; x[k + 2] = v.x; x[k + 3] = v.y;
                         }
                     };
                     if (plain && half) {                         // nearly all tiles
+                        // (the next column group is on its way as soon as this one is out of the load's registers)
+                        float y[8];
+                        tc_ld8(s_addr + 8 * j_lo, y);
+                        p_free();
 #pragma unroll 1
-                        for (int j = j_lo; j < j_hi; j += 2) {   // two column groups side by side
-                            const bool two = j + 1 < j_hi;
-                            float y[2][8];
-                            tc_ld8(s_addr + 8 * j, y[0]);
-                            if (two) tc_ld8(s_addr + 8 * j + 8, y[1]);
-                            if (j == j_lo) p_free();
+                        for (int j = j_lo; j < j_hi; ++j) {
+                            float x[8];
                             tc_wait_ld();
-                            scores(y[0], j);
-                            if (two) scores(y[1], j + 1);
+                            scores(y, x, j);
+                            if (j + 1 < j_hi) tc_ld8(s_addr + 8 * j + 8, y);
 #pragma unroll
                             for (int k = 0; k < 8; k += 2) {
-                                dmax = fmaxf(dmax, fmaxf(y[0][k], y[0][k + 1]));
-                                y[0][k] = ex2_approx(y[0][k]);
-                                y[0][k + 1] = ex2_approx(y[0][k + 1]);
+                                dmax = fmaxf(dmax, fmaxf(x[k], x[k + 1]));
+                                x[k] = ex2_approx(x[k]);
+                                x[k + 1] = ex2_approx(x[k + 1]);
                             }
-                            if (two) {
-#pragma unroll
-                                for (int k = 0; k < 8; k += 2) {
-                                    dmax = fmaxf(dmax, fmaxf(y[1][k], y[1][k + 1]));
-                                    y[1][k] = ex2_approx(y[1][k]);
-                                    y[1][k + 1] = ex2_approx(y[1][k + 1]);
-                                }
-                                *reinterpret_cast<uint4*>(p_own + (j + 1) * 2048) = pack8<true>(y[1]);
-                            }
-                            *reinterpret_cast<uint4*>(p_own + j * 2048) = pack8<true>(y[0]);
+                            *reinterpret_cast<uint4*>(p_own + j * 2048) = pack8<true>(x);
                         }
                     } else {                                     // masks, bf16
                         p_free();
@@ -944,7 +935,7 @@ tree_attention_kv4_kernel(const Params p) {
                             float y[8];
                             tc_ld8(s_addr + 8 * j, y);
                             tc_wait_ld();
-                            scores(y, j);
+                            scores(y, y, j);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
                                 y[k] = ((bits >> k) & 1u) ? y[k] : -INFINITY;
