@@ -13,7 +13,7 @@
 //         score = scale_k (sum of code q) + (16 scale_k + offset_k) (sum of q).
 //   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
 //     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
-//     whose values lie well inside fp16's range, which the value warps vote on tile by tile; else bf16.
+//     whose values lie well inside fp16's range, which the key warps vote on tile by tile; else bf16.
 // The rows of the tree itself are read as they are (bf16, against the bf16 queries): scale 1, offset 0.
 //
 // What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; unpacking
@@ -40,6 +40,7 @@
 #include <cuda_fp16.h>
 
 #include "attention_tc_common.cuh"
+#include "f32x2.cuh"
 #include "kv4.cuh"
 
 namespace mcsd {
@@ -49,8 +50,8 @@ namespace {
 constexpr int kD = 128;
 constexpr int kPageBytes = kv4_page_bytes(kD);
 constexpr int kStageBytes = 4 * kPageBytes;      // one tile: 128 rows
-constexpr int kValueWarp = 4, kSoftWarp = 12, kSides = 1, kCopyWarp = 12 + 8 * kSides, kScoreWarp = kCopyWarp + 1, kProductWarp = kCopyWarp + 2, kQueryWarp = kCopyWarp + 3;
-constexpr int kThreads = 32 * (kQueryWarp + 1), kSoftThreads = 256 * kSides;
+constexpr int kValueWarp = 4, kSoftWarp = 12, kCopyWarp = 20, kScoreWarp = 21, kProductWarp = 22, kQueryWarp = 23;
+constexpr int kThreads = 32 * (kQueryWarp + 1), kSoftThreads = 256;
 constexpr int kWideQ = 64;                       // query columns of a work item, at most
 template <int QB> constexpr int kStages = QB > 48 ? 5 : 6;
 // Tensor-memory columns: scores, O^T and row sums of the two softmax groups (the sums with a query per lane and sixteen identical
@@ -319,15 +320,6 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// two fp32 fused multiply-adds in one instruction
-__device__ __forceinline__ float2 fma_f32x2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n\t.reg .b64 x, y, z, w;\n\t"
-        "mov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
 // barrier over all softmax warps
 __device__ __forceinline__ bool soft_sync_any(bool pred) {
     uint32_t r;
@@ -423,9 +415,9 @@ tree_attention_kv4_kernel(const Params p) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm->k_full[i], 4);
             mbar_init(&sm->s_full[i], 1);
-            mbar_init(&sm->s_free[i], 4 * kSides);
+            mbar_init(&sm->s_free[i], 4);
             mbar_init(&sm->v_full[i], 4);
-            mbar_init(&sm->p_full[i], 4 * kSides);
+            mbar_init(&sm->p_full[i], 4);
             mbar_init(&sm->pv_done[i], 1);
             mbar_init(&sm->q_full[i], 1);
             mbar_init(&sm->piece_done[i], kSoftThreads / 32);
@@ -781,8 +773,7 @@ tree_attention_kv4_kernel(const Params p) {
         }
     } else {
         // ---- softmax, epilogue: group wg has the tiles with g % 2 == wg, thread r key row r
-        const int quarter = (warp - kSoftWarp) >> 2, wg = quarter / kSides, side = quarter % kSides, wq = warp & 3, r = tid & 127;
-        const int bar_id = 1 + quarter;
+        const int wg = (warp - kSoftWarp) >> 2, wq = warp & 3, r = tid & 127, bar_id = 1 + wg;
         const uint32_t lane_addr = tmem + ((uint32_t)(wq * 32) << 16);
         const uint32_t s_addr = lane_addr + Col::S + wg * QB;
         unsigned char* const p_own = p_buf + wg * (QB * 256) + r * 16;
@@ -795,8 +786,7 @@ tree_attention_kv4_kernel(const Params p) {
             const Piece s = sm->piece[seg & 1u];
             if (soft_sync_any(failed)) break;                    // (all leave or none)
             const int n8 = (s.Nq + 7) >> 3;
-            const int per_side = (n8 + kSides - 1) / kSides, j_lo = side * per_side, j_hi = min(n8, j_lo + per_side);
-            const bool own_col = r >= 8 * j_lo && r < 8 * j_hi;  // thread r keeps column r's reference
+            const bool own_col = r < 8 * n8;                     // thread r keeps column r's reference
             const float* qs = sm->q_sum[seg & 1u];
             const uint32_t g_end = g_piece + (uint32_t)s.cnt;
             const uint32_t g_own = g_piece + ((g_piece ^ (uint32_t)wg) & 1u);   // the group's first tile, if below g_end
@@ -810,8 +800,8 @@ tree_attention_kv4_kernel(const Params p) {
                     if (!tree) {
                         if (key < s.L) cm = ~0ull;
                     } else if (key < s.Nb) {
-                        int n = (s.q0 + 8 * j_lo) / p.G, rest = s.q0 + 8 * j_lo - n * p.G;
-                        for (int c = 8 * j_lo; c < min(s.Nq, 8 * j_hi); ++c) {
+                        int n = s.q0 / p.G, rest = s.q0 - n * p.G;
+                        for (int c = 0; c < s.Nq; ++c) {
                             cm |= (unsigned long long)((sm->anc[n * p.words + (key >> 6)] >> (key & 63)) & 1ull) << c;
                             if (++rest == p.G) { rest = 0; ++n; }
                         }
@@ -829,7 +819,7 @@ tree_attention_kv4_kernel(const Params p) {
                 // is exceeded is raised below.  A tile with a mask takes exact column maxima instead.
                 if (first && plain) {
 #pragma unroll 1
-                    for (int j = j_lo; j < j_hi; ++j) {
+                    for (int j = 0; j < n8; ++j) {
                         float y[8];
                         tc_ld8(s_addr + 8 * j, y);
                         tc_wait_ld();
@@ -852,7 +842,7 @@ tree_attention_kv4_kernel(const Params p) {
                     if (raise) {
                         raised = true;
 #pragma unroll 1
-                        for (int j = j_lo; j < j_hi; ++j) {
+                        for (int j = 0; j < n8; ++j) {
                             float y[8];
                             tc_ld8(s_addr + 8 * j, y);
                             tc_wait_ld();
@@ -879,7 +869,7 @@ tree_attention_kv4_kernel(const Params p) {
                             if (!mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 42)) failed = true;
                             tc_fence_after();
 #pragma unroll 1
-                            for (int j = j_lo; j < j_hi; ++j) {
+                            for (int j = 0; j < n8; ++j) {
                                 float o[8];
                                 tc_ld8(lane_addr + Col::O + wg * QB + 8 * j, o);
                                 tc_wait_ld();
@@ -887,9 +877,9 @@ tree_attention_kv4_kernel(const Params p) {
                                 for (int k = 0; k < 8; ++k) o[k] *= alph[8 * j + k];
                                 tc_st8(lane_addr + Col::O + wg * QB + 8 * j, o);
                             }
-                            const float l = tc_ld1(lane_addr + Col::L + wg * 16 + side);   // of query r
+                            const float l = tc_ld1(lane_addr + Col::L + wg * 16);   // of query r
                             tc_wait_ld();
-                            tc_st1(lane_addr + Col::L + wg * 16 + side, own_col ? l * alph[r] : l);
+                            tc_st1(lane_addr + Col::L + wg * 16, own_col ? l * alph[r] : l);
                             tc_wait_st();
                         }
                     }
@@ -911,14 +901,14 @@ tree_attention_kv4_kernel(const Params p) {
                     if (plain && half) {                         // nearly all tiles
                         // (the next column group is on its way as soon as this one is out of the load's registers)
                         float y[8];
-                        tc_ld8(s_addr + 8 * j_lo, y);
+                        tc_ld8(s_addr, y);
                         p_free();
 #pragma unroll 1
-                        for (int j = j_lo; j < j_hi; ++j) {
+                        for (int j = 0; j < n8; ++j) {
                             float x[8];
                             tc_wait_ld();
                             scores(y, x, j);
-                            if (j + 1 < j_hi) tc_ld8(s_addr + 8 * j + 8, y);
+                            if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y);
 #pragma unroll
                             for (int k = 0; k < 8; k += 2) {
                                 dmax = fmaxf(dmax, fmaxf(x[k], x[k + 1]));
@@ -930,7 +920,7 @@ tree_attention_kv4_kernel(const Params p) {
                     } else {                                     // masks, bf16
                         p_free();
 #pragma unroll 1
-                        for (int j = j_lo; j < j_hi; ++j) {
+                        for (int j = 0; j < n8; ++j) {
                             const uint32_t bits = plain ? 0xFFu : (uint32_t)(cm >> (8 * j));
                             float y[8];
                             tc_ld8(s_addr + 8 * j, y);
@@ -969,14 +959,10 @@ tree_attention_kv4_kernel(const Params p) {
             const bool has0 = s.cnt > 1 || !(g_piece & 1u), has1 = s.cnt > 1 || (g_piece & 1u);   // groups with a tile in the piece
             const int* rows = sm->row[seg & 1u];
             // weights of the groups' accumulators, one thread per column (the sums of query r lie in lane r)
-            if (quarter == 0 && wq < (QB + 31) / 32) {
-                float l[2][kSides];
-#pragma unroll
-                for (int x = 0; x < 2 * kSides; ++x) l[x / kSides][x % kSides] = tc_ld1(lane_addr + Col::L + (x / kSides) * 16 + x % kSides);
+            if (wg == 0 && wq < (QB + 31) / 32) {
+                const float l0 = tc_ld1(lane_addr + Col::L), l1 = tc_ld1(lane_addr + Col::L + 16);
                 tc_wait_ld();
                 if (r < 8 * n8) {
-                    // (the copy that the column's warps kept)
-                    const float l0 = kSides == 2 && r >= 8 * per_side ? l[0][kSides - 1] : l[0][0], l1 = kSides == 2 && r >= 8 * per_side ? l[1][kSides - 1] : l[1][0];
                     const float m0 = has0 ? -sm->nref[0][r] : -1e30f, m1 = has1 ? -sm->nref[1][r] : -1e30f, M = fmaxf(m0, m1);
                     float w0 = has0 ? exp2f(m0 - M) : 0.f, w1 = has1 ? exp2f(m1 - M) : 0.f;
                     const float sum = (has0 ? l0 * w0 : 0.f) + (has1 ? l1 * w1 : 0.f);
@@ -995,7 +981,7 @@ tree_attention_kv4_kernel(const Params p) {
             soft_sync_any(false);
             // every other column group for each group of warps; thread r has channel r of both accumulators
 #pragma unroll 1
-            for (int j = quarter; j < n8; j += 2 * kSides) {
+            for (int j = wg; j < n8; j += 2) {
                 float o[8], o1[8];
                 if (has0) tc_ld8(lane_addr + Col::O + 8 * j, o);
                 if (has1) tc_ld8(lane_addr + Col::O + QB + 8 * j, o1);
