@@ -218,7 +218,7 @@ struct Small {
     int q_max;                                        // largest |query| of the first piece, as bits
     float q_factor[2];                                // brings sums over codes to score units
     int fmt[8];                                       // 1: the tile's values and weights are fp16, 0: bf16
-    int row[2][QB];                                   // rows of q and out of the piece's columns
+    alignas(16) int row[2][QB];                                   // rows of q and out of the piece's columns
     alignas(16) float2 kab[4][kTile];                 // scale and offset of a tile's key rows, in score units
     alignas(16) unsigned short vab[8][2][kTile];      // scales and offsets of a tile's value rows, in the tile's format
     alignas(16) float q_sum[2][QB];
@@ -822,10 +822,12 @@ tree_attention_kv4_kernel(const Params p) {
                     for (int j = 0; j < n8; ++j) {
                         float y[8];
                         tc_ld8(s_addr + 8 * j, y);
+                        const float4 q0 = *reinterpret_cast<const float4*>(qs + 8 * j), q1 = *reinterpret_cast<const float4*>(qs + 8 * j + 4);
                         tc_wait_ld();
                         if (lane == 0) {
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) sm->red[wg][wq][8 * j + k] = fmaf(y[k], ab.x, qs[8 * j + k] * ab.y);
+                            float4* const to = reinterpret_cast<float4*>(&sm->red[wg][wq][8 * j]);
+                            to[0] = make_float4(fmaf(y[0], ab.x, q0.x * ab.y), fmaf(y[1], ab.x, q0.y * ab.y), fmaf(y[2], ab.x, q0.z * ab.y), fmaf(y[3], ab.x, q0.w * ab.y));
+                            to[1] = make_float4(fmaf(y[4], ab.x, q1.x * ab.y), fmaf(y[5], ab.x, q1.y * ab.y), fmaf(y[6], ab.x, q1.z * ab.y), fmaf(y[7], ab.x, q1.w * ab.y));
                         }
                     }
                     group_sync_any(bar_id, false);
@@ -985,16 +987,25 @@ tree_attention_kv4_kernel(const Params p) {
                 float o[8], o1[8];
                 if (has0) tc_ld8(lane_addr + Col::O + 8 * j, o);
                 if (has1) tc_ld8(lane_addr + Col::O + QB + 8 * j, o1);
+                float w0[8], w1[8];
+                int row[8];
+#pragma unroll
+                for (int k = 0; k < 8; k += 4) {
+                    *reinterpret_cast<float4*>(w0 + k) = *reinterpret_cast<const float4*>(&sm->alpha[0][8 * j + k]);
+                    *reinterpret_cast<float4*>(w1 + k) = *reinterpret_cast<const float4*>(&sm->alpha[1][8 * j + k]);
+                    *reinterpret_cast<int4*>(row + k) = *reinterpret_cast<const int4*>(rows + 8 * j + k);
+                }
                 tc_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float x = has0 ? o[k] * sm->alpha[0][8 * j + k] : 0.f;
-                    o[k] = has1 ? fmaf(o1[k], sm->alpha[1][8 * j + k], x) : x;
+                    const float x = has0 ? o[k] * w0[k] : 0.f;
+                    o[k] = has1 ? fmaf(o1[k], w1[k], x) : x;
                 }
                 if (whole) {
+                    __nv_bfloat16* const out = p.out + r;
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        if (8 * j + k < s.Nq) p.out[(size_t)rows[8 * j + k] * kD + r] = __float2bfloat16_rn(o[k]);
+                        if (8 * j + k < s.Nq) out[(size_t)(uint32_t)row[k] * kD] = __float2bfloat16_rn(o[k]);
                 } else {
                     float* po = p.part_o + ((size_t)slot * kWideQ + 8 * j) * kD + r;
 #pragma unroll
