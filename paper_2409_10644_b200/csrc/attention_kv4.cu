@@ -86,9 +86,12 @@ struct Plan {
     int blocks;
 };
 
-// Cost of a tile with nq query columns and of a work item on top of its tiles.
-__host__ __device__ __forceinline__ int tile_cost(int nq) { return 32 + nq / 2; }
-constexpr int kItemCost = 64;
+// Cost of a tile with nq query columns (unpacking bounds it up to 16 columns, the exponentials beyond: about 29 cycles per unit)
+// and of a work item on top of its tiles: its first references, the tree rows read as they are, its end.  Measured on 32
+// ragged sequences with 8 to 160 nodes / the 45-node trees / 8 long single tokens: 361 / 156 / 67 us with 200, 350 / 155 / 69 us
+// with 400, 398 / 157 / 67 us with 100.
+__host__ __device__ __forceinline__ int tile_cost(int nq) { return nq < 16 ? 40 : 24 + nq; }
+constexpr int kItemCost = 256;
 
 struct Shape {            // of the work items of one sequence
     int Tp, T, blocks_q, per_q, total_q;
@@ -239,6 +242,14 @@ __device__ __forceinline__ void bulk_load_once(uint32_t dst, const void* src, ui
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy) : "memory");
 }
+// (from the 16-byte boundary at or below src: values of the tree may start anywhere)
+__device__ __forceinline__ void prefetch_l2(const void* src, uint32_t bytes) {
+    src = reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15);
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy16_async(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
 // One lane of a converged warp, the same one every time: it issues the MMAs and the commits that track them.
 __device__ __forceinline__ bool elect_one() {
     uint32_t r;
@@ -320,6 +331,17 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// 32 x 32 bits, a row per lane: exchanges rows and columns
+__device__ __forceinline__ uint32_t transpose_bits(uint32_t x, int lane) {
+    uint32_t m = 0x0000FFFFu;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+        const uint32_t y = __shfl_xor_sync(0xffffffffu, x, s);
+        x = lane & s ? (x & ~m) | ((y >> s) & m) : (x & m) | ((y & m) << s);
+        m ^= m << (s >> 1);
+    }
+    return x;
+}
 // barrier over all softmax warps
 __device__ __forceinline__ bool soft_sync_any(bool pred) {
     uint32_t r;
@@ -343,28 +365,42 @@ __device__ __forceinline__ bool fits_half(float scale, float offset) {
 // slabs of 64 channels, the e4m3 parts (high, low) behind them.  Codes come out of a word in the order 0 4 1 5 2 6 3 7, so the
 // e4m3 channels are stored in that order.  Rows from the last query on are zeros.  Stacked query j of a key/value head
 // is head j % G of its group, node j / G.
+__device__ __forceinline__ int query_row(const Params& p, const Piece& s, int r) {   // row of q and out; below 65535 * 192
+    const int j = s.q0 + r, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
+    return (s.b * p.Hkv * p.G + h) * p.N + n;
+}
+template <int QB>
+__device__ __forceinline__ unsigned char* query_piece(unsigned char* q_buf, uint32_t buf, int r, int c) {   // of the bf16 form
+    return q_buf + buf * (QB * 512) + (c >> 3) * (QB * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16);
+}
+// The row's sum, kept; returns the largest magnitude of the lane's channels.
+template <int QB>
+__device__ __forceinline__ float sum_query(Small<QB>* sm, uint32_t buf, int r, int c, uint4 v) {
+    float2 sum = make_float2(0.f, 0.f);
+    float top = 0.f;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        sum = add_f32x2(sum, x);
+        top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
+    }
+    float all = sum.x + sum.y;
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) all += __shfl_xor_sync(0xffffffffu, all, x);
+    if (c == 0) sm->q_sum[buf][r] = all;
+    return top;
+}
 template <int QB>
 __device__ __forceinline__ float load_query(Small<QB>* sm, unsigned char* q_buf, const Params& p, const Piece& s, uint32_t buf, int r, int c) {
     uint4 v = make_uint4(0, 0, 0, 0);
     if (r < s.Nq) {
-        const int j = s.q0 + r, n = j / p.G, h = s.hk * p.G + (j - n * p.G);
-        const int row = (s.b * p.Hkv * p.G + h) * p.N + n;          // below 65535 * 192
+        const int row = query_row(p, s, r);
         v = *reinterpret_cast<const uint4*>(p.q + (size_t)row * kD + c * 8);
         if (c == 0) sm->row[buf][r] = row;
     }
-    *reinterpret_cast<uint4*>(q_buf + buf * (QB * 512) + (c >> 3) * (QB * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16)) = v;
-    float sum = 0.f, top = 0.f;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = __uint_as_float(w[i] << 16), b = __uint_as_float(w[i] & 0xFFFF0000u);
-        sum += a + b;
-        top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
-    }
-#pragma unroll
-    for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-    if (c == 0) sm->q_sum[buf][r] = sum;
-    return top;
+    *reinterpret_cast<uint4*>(query_piece<QB>(q_buf, buf, r, c)) = v;
+    return sum_query<QB>(sm, buf, r, c, v);
 }
 // the power of two that brings the largest query to 128 .. 256 (e4m3 ends at 448)
 __device__ __forceinline__ float query_scale(float top) {
@@ -373,7 +409,7 @@ __device__ __forceinline__ float query_scale(float top) {
 }
 template <int QB>
 __device__ __forceinline__ void split_query(unsigned char* q_buf, uint32_t buf, float scale, int r, int c) {
-    const uint4 v = *reinterpret_cast<const uint4*>(q_buf + buf * (QB * 512) + (c >> 3) * (QB * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16));
+    const uint4 v = *reinterpret_cast<const uint4*>(query_piece<QB>(q_buf, buf, r, c));
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     float x[8];
 #pragma unroll
@@ -477,6 +513,11 @@ tree_attention_kv4_kernel(const Params p) {
                 Piece s;
                 piece_at<QB>(pl, p, t, t_end, s);
                 const unsigned char* head = p.cache + ((size_t)s.b * p.Hkv + s.hk) * p.pages * kPageBytes;
+                if (s.lt + s.cnt > s.Tp && s.Nb > 0) {              // the rows of the tree, into L2 long before they are read
+                    const size_t row = ((size_t)s.b * p.Hkv + s.hk) * p.N * kD;
+                    prefetch_l2(p.k_tree + row, (uint32_t)s.Nb * kD * 2);
+                    prefetch_l2(p.v_tree + row, (uint32_t)s.Nb * kD * 2);
+                }
                 for (int i = s.lt; i < min(s.lt + s.cnt, s.Tp) && ok; ++i, ++f) {
                     const uint32_t st = f % kStages<QB>;
                     if (f >= kStages<QB>) ok = mbar_wait(&sm->empty[st], (f / kStages<QB> - 1u) & 1u, abort_flag, hdr, 31);
@@ -603,9 +644,19 @@ tree_attention_kv4_kernel(const Params p) {
                 if (seg >= 2) finish(seg - 2u);
                 if (!ok) break;
                 const int rows = (s.Nq + 15) & ~15;
+                for (int r = lane; r < s.Nq; r += 32) sm->row[buf][r] = query_row(p, s, r);
+                __syncwarp();
+                // all rows are on their way at once: a short work item has little time to hide this behind
+                for (int r = sub; r < rows; r += 2) {
+                    unsigned char* const to = query_piece<QB>(q_buf, buf, r, c);
+                    if (r < s.Nq) copy16_async(to, p.q + (size_t)(uint32_t)sm->row[buf][r] * kD + c * 8);
+                    else *reinterpret_cast<uint4*>(to) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");       // (a lane reads below what it has copied itself)
                 float top = 0.f;
 #pragma unroll 4
-                for (int r = sub; r < rows; r += 2) top = fmaxf(top, load_query<QB>(sm, q_buf, p, s, buf, r, c));
+                for (int r = sub; r < rows; r += 2)
+                    top = fmaxf(top, sum_query<QB>(sm, buf, r, c, *reinterpret_cast<const uint4*>(query_piece<QB>(q_buf, buf, r, c))));
                 const float scale = query_scale(warp_max_f32(top));
 #pragma unroll 2
                 for (int r = sub; r < rows; r += 2) split_query<QB>(q_buf, buf, scale, r, c);
@@ -799,12 +850,17 @@ tree_attention_kv4_kernel(const Params p) {
                 if (!plain) {
                     if (!tree) {
                         if (key < s.L) cm = ~0ull;
-                    } else if (key < s.Nb) {
-                        int n = s.q0 / p.G, rest = s.q0 - n * p.G;
-                        for (int c = 0; c < s.Nq; ++c) {
-                            cm |= (unsigned long long)((sm->anc[n * p.words + (key >> 6)] >> (key & 63)) & 1ull) << c;
-                            if (++rest == p.G) { rest = 0; ++n; }
+                    } else {
+                        const int key0 = (i - s.Tp) * kTile + wq * 32;   // the warp's first key
+                        const uint32_t* const anc32 = reinterpret_cast<const uint32_t*>(sm->anc) + (key0 >> 5);
+                        uint32_t m[2];
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {            // lane c: which of the warp's keys column 32 x + c sees
+                            const int c = 32 * x + lane;
+                            m[x] = c < s.Nq && key0 < s.Nb ? anc32[(s.q0 + c) / p.G * (2 * p.words)] : 0u;
+                            m[x] = transpose_bits(m[x], lane);   // lane r: which of those columns see key r
                         }
+                        cm = key < s.Nb ? m[0] | ((unsigned long long)m[1] << 32) : 0ull;
                     }
                 }
                 if (!mbar_wait(&sm->s_full[wg], (g >> 1) & 1u, abort_flag, hdr, 41)) failed = true;
@@ -920,21 +976,23 @@ tree_attention_kv4_kernel(const Params p) {
                             *reinterpret_cast<uint4*>(p_own + j * 2048) = pack8<true>(x);
                         }
                     } else {                                     // masks, bf16
+                        float y[8];
+                        tc_ld8(s_addr, y);
                         p_free();
 #pragma unroll 1
                         for (int j = 0; j < n8; ++j) {
                             const uint32_t bits = plain ? 0xFFu : (uint32_t)(cm >> (8 * j));
-                            float y[8];
-                            tc_ld8(s_addr + 8 * j, y);
+                            float x[8];
                             tc_wait_ld();
-                            scores(y, y, j);
+                            scores(y, x, j);
+                            if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                y[k] = ((bits >> k) & 1u) ? y[k] : -INFINITY;
-                                dmax = fmaxf(dmax, y[k]);
-                                y[k] = ex2_approx(y[k]);
+                                x[k] = ((bits >> k) & 1u) ? x[k] : -INFINITY;
+                                dmax = fmaxf(dmax, x[k]);
+                                x[k] = ex2_approx(x[k]);
                             }
-                            *reinterpret_cast<uint4*>(p_own + j * 2048) = half ? pack8<true>(y) : pack8<false>(y);
+                            *reinterpret_cast<uint4*>(p_own + j * 2048) = half ? pack8<true>(x) : pack8<false>(x);
                         }
                     }
                     raise = group_sync_any(bar_id, (dmax > kLazyTau && !raised) || failed);   // one vote of the four warps
