@@ -438,7 +438,9 @@ int mcsd_commit_kv4(void* const* cache_layers, const void* const* k_tree_layers,
  *                    that may overlap on the device need distinct workspaces
  *
  * Errors and limits: as mcsd_tree_attention_gqa, plus MCSD_ERR_BAD_SHAPE when L_max is not a positive multiple of 32 or the
- * cache is not 16-byte aligned.  mcsd_tree_attention_path() tells which kernel runs here as well.
+ * cache is not 16-byte aligned.  The tensor-core kernel takes the shapes that mcsd_tree_attention_path() reports, with q, k_tree
+ * and out 16-byte aligned and fewer than 2^31 (key/value head, query block, 128-key tile) triples per sequence; the
+ * CUDA-core kernel takes the others.
  */
 size_t mcsd_tree_attention_kv4_workspace_bytes(int B, int H_q, int H_kv, int N, int D, int L_max, int dtype);
 
