@@ -61,7 +61,7 @@ constexpr int kStageBytes = 4 * kPageBytes;      // one tile: 128 rows
 constexpr int kValueWarp = 4, kSoftWarp = 12, kCopyWarp = 20, kScoreWarp = 21, kProductWarp = 22, kQueryWarp = 23;
 constexpr int kThreads = 32 * (kQueryWarp + 1), kSoftThreads = 256;
 constexpr int kWideQ = 64;                       // query columns of a work item, at most
-constexpr int kStages = 5;                       // tiles of codes in the ring
+template <int QB> constexpr int kStages = QB > 16 ? 5 : 6;   // tiles of codes in the ring: what fits
 // Tensor-memory columns: scores, O^T and row sums of the two softmax groups (the sums with a query per lane and sixteen identical
 // columns, of which the first counts), keys (two buffers of codes; a tile of tree rows takes
 // both), values.
@@ -217,7 +217,7 @@ __device__ void make_plan(Plan& pl, const Params& p) {
 
 template <int QB>
 struct Small {
-    unsigned long long full[kStages], empty[kStages];
+    unsigned long long full[kStages<QB>], empty[kStages<QB>];
     unsigned long long k_full[2], s_full[2], s_free[2], v_full[2], p_full[2], pv_done[2], q_full[2], piece_done[2], scales_full[8];
     unsigned long long drain;
     uint32_t tmem_base;
@@ -448,14 +448,14 @@ tree_attention_kv4_kernel(const Params p) {
     unsigned char* q_buf = smem;                      // two buffers of QB rows: [2 bf16 slabs, high, low][QB rows][128 bytes]
     unsigned char* p_buf = q_buf + 2 * QB * 512;      // P^T of the two groups: [QB / 8][128 keys][16 bytes]
     unsigned char* ring = p_buf + 2 * QB * 256;
-    Small<QB>* sm = reinterpret_cast<Small<QB>*>(ring + kStages * kStageBytes);
+    Small<QB>* sm = reinterpret_cast<Small<QB>*>(ring + kStages<QB> * kStageBytes);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // ---- set-up; what comes before the wait touches no global memory and overlaps the tail of the preceding kernel
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (tid == 0) {
-        for (int i = 0; i < kStages; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 8); }
+        for (int i = 0; i < kStages<QB>; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 8); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm->k_full[i], 4);
             mbar_init(&sm->s_full[i], 1);
@@ -527,8 +527,8 @@ tree_attention_kv4_kernel(const Params p) {
                     prefetch_l2(p.v_tree + row, (uint32_t)s.Nb * kD * 2);
                 }
                 for (int i = s.lt; i < min(s.lt + s.cnt, s.Tp) && ok; ++i, ++f) {
-                    const uint32_t st = f % kStages;
-                    if (f >= kStages) ok = mbar_wait(&sm->empty[st], (f / kStages - 1u) & 1u, abort_flag, hdr, 31);
+                    const uint32_t st = f % kStages<QB>;
+                    if (f >= kStages<QB>) ok = mbar_wait(&sm->empty[st], (f / kStages<QB> - 1u) & 1u, abort_flag, hdr, 31);
                     if (!ok) break;
                     const uint32_t bytes = (uint32_t)(min(kTile, s.L - i * kTile) + kPageRows - 1) / kPageRows * kPageBytes;
                     mbar_expect_tx(&sm->full[st], bytes);
@@ -540,9 +540,9 @@ tree_attention_kv4_kernel(const Params p) {
                 t += s.cnt;
             }
             if (!ok) {                                // gave up: let the copies already issued land before the block exits
-                for (uint32_t x = f > kStages ? f - kStages : 0; x < f; ++x) {
+                for (uint32_t x = f > kStages<QB> ? f - kStages<QB> : 0; x < f; ++x) {
                     const long long t0 = clock64();
-                    while (!mbar_try_wait(&sm->full[x % kStages], (x / kStages) & 1u) && clock64() - t0 < kSpinCycles / 8) {}
+                    while (!mbar_try_wait(&sm->full[x % kStages<QB>], (x / kStages<QB>) & 1u) && clock64() - t0 < kSpinCycles / 8) {}
                 }
             }
         }
@@ -688,8 +688,8 @@ tree_attention_kv4_kernel(const Params p) {
             piece_at<QB>(pl, p, t, t_end, s);
             for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
                 const uint32_t buf = g & 1u;
-                const uint32_t st = f % kStages;
-                if (i < s.Tp) bad |= !mbar_wait(&sm->full[st], (f / kStages) & 1u, abort_flag, hdr, 37);
+                const uint32_t st = f % kStages<QB>;
+                if (i < s.Tp) bad |= !mbar_wait(&sm->full[st], (f / kStages<QB>) & 1u, abort_flag, hdr, 37);
                 // Scales of the tile's value rows, thread r the row r, rounded to fp16.  Rows past the end of the prefix have
                 // probability zero but may hold anything, and 0 * NaN would be NaN: their scale and offset are zero.
                 const unsigned char* page = ring + st * kStageBytes + warp * kPageBytes;   // rows 32 warp .. of the tile
@@ -773,7 +773,7 @@ tree_attention_kv4_kernel(const Params p) {
                     continue;
                 }
                 const uint32_t dst = lane_addr + (g & 1u) * 64;
-                const uint32_t st = f % kStages;
+                const uint32_t st = f % kStages<QB>;
                 // (the key warps have seen the tile arrive before they announce its scales)
                 ok = mbar_wait(&sm->scales_full[g & 7u], (g >> 3) & 1u, abort_flag, hdr, 39);
                 // the buffer is free once the products of the tile that used it are done
@@ -781,7 +781,7 @@ tree_attention_kv4_kernel(const Params p) {
                 if (!ok) break;
                 tc_fence_after();
                 if (i < s.Tp) {
-                    if (!mbar_try_wait(&sm->full[st], (f / kStages) & 1u)) { ok = false; break; }   // (has completed)
+                    if (!mbar_try_wait(&sm->full[st], (f / kStages<QB>) & 1u)) { ok = false; break; }   // (has completed)
                     const bool half = sm->fmt[g & 7u];
                     const unsigned char* codes = ring + st * kStageBytes + kv4_values_at(kD) + d * 16;
                     const uint4* sa = reinterpret_cast<const uint4*>(sm->vab[g & 7u][0]);
@@ -1145,7 +1145,7 @@ tree_attention_kv4_kernel(const Params p) {
 
 template <int QB>
 int launch(const Params& p, int grid, cudaStream_t stream) {
-    constexpr size_t smem_bytes = 1024 + 6 * QB * 256 + (size_t)kStages * kStageBytes + sizeof(Small<QB>);
+    constexpr size_t smem_bytes = 1024 + 6 * QB * 256 + (size_t)kStages<QB> * kStageBytes + sizeof(Small<QB>);
     static_assert(smem_bytes <= kSmemLimit, "ring and buffers fit the block's shared memory");
     static std::mutex mu;                                        // the opt-in to large shared memory is per device
     static bool done[64] = {};
@@ -1214,8 +1214,9 @@ int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void*
     p.counters = reinterpret_cast<int*>(static_cast<char*>(scratch) + kMlBytes + kOBytes);
     p.header = header;
     const int grid = std::min(sms, kMaxCtas);
-    // (Buffers for 16 or 48 columns where no work item has more, with a sixth page in flight, measured the same: 65.9 and 65.7 us
-    // for 8 x 32001 single tokens, 156.2 and 155.3 us for 45-node trees.)
+    // Few query columns (single tokens): the smaller kernel starts and merges faster, 15.2 against 16.1 us for one token after 1001
+    // rows, 66 us either way for 8 x 32001 (with room for a sixth tile; 67 without).  Another one for 48 columns brought nothing (155 and 156 us for 45-node trees).
+    if (a.N * a.G <= 16) return launch<16>(p, grid, stream);
     return launch<kWideQ>(p, grid, stream);
 }
 
