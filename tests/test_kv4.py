@@ -513,3 +513,41 @@ def test_generation_steps_over_a_4_bit_cache(m, dtype, D):
             assert np.array_equal(caches[i].cpu().numpy(), want[i])
         lens_h = new
         assert np.array_equal(lens.cpu().numpy(), lens_h)
+
+
+def _off_by_one(t):
+    """The same contiguous tensor one element further on in memory."""
+    x = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)[1:].view(t.shape)
+    return x.copy_(t)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_off_16_byte_boundaries(m, dtype, D):
+    rng = np.random.default_rng(D)
+    B, H, pages, T = 2, 2, 3, 50
+    k, v = _rows(rng, (B, H, T, D), dtype), _rows(rng, (B, H, T, D), dtype)
+    start = torch.tensor([3, 40], dtype=torch.int32, device="cuda")
+    caches = [torch.from_numpy(_noise_cache(np.random.default_rng(5), B, H, pages, D)).cuda() for _ in range(2)]
+    m.mcsd_append_kv4(k, v, caches[0], start)
+    m.mcsd_append_kv4(_off_by_one(k), _off_by_one(v), caches[1], start)
+    assert torch.equal(caches[0], caches[1])
+    ptrs = m.layer_pointer_table([caches[0]])
+    want = m.mcsd_read_kv4(ptrs, start, T, None, B, H, D, pages * 32, dtype)
+    out = tuple(_off_by_one(torch.full_like(x, 7)) for x in want)
+    m.mcsd_read_kv4(ptrs, start, T, None, B, H, D, pages * 32, dtype, out=out)
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+@pytest.mark.gpu
+def test_attention_with_values_of_the_tree_off_16_byte_boundaries(m):
+    rng = np.random.default_rng(11)
+    parent = parent_array(*TREES["forest"])
+    lens = [200, 33]
+    q, cache, _, kt, vt = _problem(m, rng, torch.bfloat16, 2, 2, 2, 128, parent, lens, None)
+    tm = m.mcsd_build_mask(parent)
+    L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = _attend(m, q, cache, kt, vt, L, None, tm)
+    got = _attend(m, q, cache, kt, _off_by_one(vt), L, None, tm)
+    assert torch.equal(got, want)                            # the same kernel, the same order of sums

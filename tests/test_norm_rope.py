@@ -159,3 +159,11 @@ def test_another_stream_and_a_captured_call(m):
     for a, b, c, d in zip(want, other, out, moved):
         assert torch.equal(a, b) and torch.equal(c, d)
     assert not torch.equal(want[0], moved[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_many_tokens_over_sequence_boundaries(m, dtype, interleaved):
+    for D, rot, sliced in ((64, 64, True), (128, 32, True), (128, 128, False)):
+        _case(m, dtype, 3, 401, 3, 2, D, rot, interleaved, 3, 777, None, sliced, "fused", D + rot)
