@@ -20,6 +20,8 @@
  *     or free device memory: kernels that need scratch take a caller-supplied workspace whose size the
  *     matching *_workspace_bytes() query returns.  A workspace is 256-byte aligned and must be zero-filled
  *     once before its first use (its first 256 bytes hold a sticky status word, see mcsd_workspace_status).
+ *     The calls of mcsd_tree_attention, mcsd_tree_attention_gqa and mcsd_tree_attention_kv4, of any shapes and types, may
+ *     use one workspace in turn.  A workspace of the verify calls is for one B and N, and not for attention.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Calls only enqueue
  *     work on that stream and never synchronise, except where stated.
  *   - Nodes of the tree are in level (BFS) order: parent[n] < n, depth non-decreasing in n, children of a
@@ -108,8 +110,8 @@ int mcsd_build_mask(const int32_t* parent_host, int n_nodes,
  *                           D == 128, all tensors are 16-byte aligned and the shape is one that
  *                           mcsd_tree_attention_path() reports as MCSD_PATH_TENSOR_CORE);  MCSD_F32: fp32 throughout
  *   workspace               [dev] scratch of at least mcsd_tree_attention_workspace_bytes(...) bytes; holds
- *                           split-KV partial results and the status word.  Calls that may overlap on the
- *                           device need distinct workspaces.
+ *                           split-KV partial results, counters of finished pieces and the status word.  Calls that may
+ *                           overlap on the device need distinct workspaces.
  *
  * Split-KV: the keys of one (b, h) may be processed by several thread blocks, each producing an
  * unnormalised partial (running maximum, sum, weighted values); a combine pass merges them.
@@ -204,7 +206,8 @@ int mcsd_tree_attention_gqa(const void* q, const void* k_cache, const void* v_ca
 
 /*
  * Reads the status word that kernels of mcsd_tree_attention / mcsd_verify_tree leave in `workspace`.
- * The word is sticky: kernels only ever set it, the caller clears it by zero-filling the first 256 bytes.
+ * The word is sticky: kernels only ever set it.  After MCSD_ERR_TIMEOUT the caller zero-fills the whole workspace before it
+ * is used again (the call that gave up leaves its counters part-counted).
  * Synchronises `stream`.  Returns MCSD_OK, MCSD_ERR_TIMEOUT (a bounded wait ran out; outputs of that call
  * are invalid) or MCSD_ERR_CUDA.
  */

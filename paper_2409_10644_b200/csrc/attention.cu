@@ -29,7 +29,7 @@ extern "C" size_t mcsd_tree_attention_workspace_bytes(int B, int H, int N, int D
         const size_t tc = mcsd::tc_workspace_bytes(B, H, N, D, L_max);
         if (tc > scratch) scratch = tc;
     }
-    return sizeof(mcsd::WorkspaceHeader) + mcsd::align_up(scratch, 256);
+    return sizeof(mcsd::AttentionWorkspace) + mcsd::align_up(scratch, 256);
 }
 
 // The 4-bit cache comes in pages of 32 rows.
@@ -52,10 +52,10 @@ static int run_attention(const void* q, const void* k_cache, const void* v_cache
     mcsd::AttentionArgs a{q, k_cache, v_cache, k_tree, v_tree, out, seq_lens, n_active, anc, words,
                           B, H, N, D, L_max, softmax_scale, dtype, G};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    auto* header = static_cast<mcsd::WorkspaceHeader*>(workspace);
-    void* scratch = static_cast<char*>(workspace) + sizeof(mcsd::WorkspaceHeader);
-    const size_t scratch_bytes = workspace_bytes - sizeof(mcsd::WorkspaceHeader);
-    if (mcsd::use_tc(a)) return mcsd::tree_attention_tc(a, header, scratch, scratch_bytes, s);
+    auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
+    void* scratch = ws + 1;
+    const size_t scratch_bytes = workspace_bytes - sizeof(mcsd::AttentionWorkspace);
+    if (mcsd::use_tc(a)) return mcsd::tree_attention_tc(a, ws, scratch, scratch_bytes, s);
     return mcsd::tree_attention_simt(a, scratch, s);
 }
 
@@ -113,10 +113,10 @@ extern "C" size_t mcsd_tree_attention_kv4_workspace_bytes(int B, int H_q, int H_
     if (H_kv < 1 || H_q < H_kv || H_q % H_kv != 0) return 0;
     size_t scratch = mcsd::simt_workspace_bytes(B, H_q, N, D, L_max);
     if (mcsd::kv4_tc_shape(B, H_q, H_q / H_kv, N, D, L_max, dtype)) {
-        const size_t tc = mcsd::kv4_tc_workspace_bytes(B, H_q, H_q / H_kv, N);
+        const size_t tc = mcsd::kv4_tc_workspace_bytes();
         if (tc > scratch) scratch = tc;
     }
-    return sizeof(mcsd::WorkspaceHeader) + mcsd::align_up(scratch, 256);
+    return sizeof(mcsd::AttentionWorkspace) + mcsd::align_up(scratch, 256);
 }
 
 extern "C" int mcsd_tree_attention_kv4(const void* q, const void* cache, const void* k_tree, const void* v_tree, void* out,
@@ -134,9 +134,10 @@ extern "C" int mcsd_tree_attention_kv4(const void* q, const void* cache, const v
     mcsd::AttentionArgs a{q, nullptr, nullptr, k_tree, v_tree, out, seq_lens, n_active, anc, words,
                           B, H_q, N, D, L_max, softmax_scale, dtype, H_q / H_kv, cache};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    void* scratch = static_cast<char*>(workspace) + sizeof(mcsd::WorkspaceHeader);
+    auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
+    void* scratch = ws + 1;
     if (mcsd::kv4_tc_shape(B, H_q, a.G, N, D, L_max, dtype) && mcsd::aligned16(q) && mcsd::aligned16(k_tree) &&
         mcsd::aligned16(out))
-        return mcsd::tree_attention_kv4_tc(a, static_cast<mcsd::WorkspaceHeader*>(workspace), scratch, s);
+        return mcsd::tree_attention_kv4_tc(a, ws, scratch, s);
     return mcsd::tree_attention_simt(a, scratch, s);
 }

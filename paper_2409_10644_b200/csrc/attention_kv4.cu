@@ -81,7 +81,7 @@ struct Params {
     float scale_log2;
     float* part_ml;       // [2 * kMaxCtas][2][kWideQ]
     float* part_o;        // [2 * kMaxCtas][kWideQ][128]
-    int* counters;        // [work items] tiles that have been finished; zero between launches
+    int* counters;        // [blocks][kCountersPerBlock], the first: finished tiles of the cut work item that the block starts; zero between launches
     WorkspaceHeader* header;
 };
 
@@ -224,6 +224,7 @@ struct Small {
     int abort_flag;
     struct Merge {                                    // a cut work item, first or last of this block
         int before, cnt, T, hk, b, q0, Nq;            // tiles finished before this block's cnt, of T
+        int block0;                                   // the block that has the item's first tile
         long long first;                              // the item's first tile
     } merge[2];
     int q_max;                                        // largest |query| of the first piece, as bits
@@ -638,9 +639,19 @@ tree_attention_kv4_kernel(const Params p) {
                 auto& m = sm->merge[done > 0 ? 1 : 0];
                 m.b = s.b; m.hk = s.hk; m.q0 = s.q0; m.Nq = s.Nq; m.T = s.T; m.cnt = s.cnt;
                 m.first = pl.tiles[s.b] + (long long)(s.item - pl.items[s.b]) * s.T;
+                int lo = blockIdx.x;
+                if (s.lt > 0) {                               // the last block that does not start behind the item's first tile
+                    lo = 0;
+                    for (int hi = blockIdx.x; hi - lo > 1;) {
+                        const int mid = (lo + hi) >> 1;
+                        if (pl.first[mid] <= m.first) lo = mid; else hi = mid;
+                    }
+                }
+                m.block0 = lo;
+                int* const counter = p.counters + lo * kCountersPerBlock;
                 __threadfence();
-                m.before = atomicAdd(&p.counters[s.item], s.cnt);
-                if (m.before + s.cnt == s.T) p.counters[s.item] = 0;
+                m.before = atomicAdd(counter, s.cnt);
+                if (m.before + s.cnt == s.T) *counter = 0;
             }
             __syncwarp();
         };
@@ -1102,9 +1113,9 @@ tree_attention_kv4_kernel(const Params p) {
         const int j = x >> 1, r = tid & 127;
         if (j % (kThreads / 128) != tid >> 7 || m.T == 0 || m.before + m.cnt != m.T || 8 * j >= m.Nq) continue;
         __threadfence();
-        // the pieces lie in consecutive blocks, this one among them
-        int c0 = blockIdx.x, c1 = blockIdx.x + 1;
-        while (c0 > 0 && pl.first[c0] > m.first) --c0;
+        // the pieces lie in consecutive blocks from block0 on, this one among them
+        const int c0 = m.block0;
+        int c1 = blockIdx.x + 1;
         while (c1 < pl.blocks && pl.first[c1] < m.first + m.T) ++c1;
         float M[8], l[8], o[8];
 #pragma unroll
@@ -1184,12 +1195,9 @@ bool kv4_tc_shape(int B, int H, int G, int N, int D, int L_max, int dtype) {
     return tc_shape_supported(B, H, G, N, D, L_max, dtype) && (H / G) * blocks_q * ((long long)L_max / kTile + 4) < (1LL << 31);
 }
 
-size_t kv4_tc_workspace_bytes(int B, int H, int G, int N) {
-    const size_t blocks_q = ((size_t)G * N + kWideQ - 1) / kWideQ;
-    return kMlBytes + kOBytes + align_up((size_t)B * (H / G) * blocks_q * sizeof(int), 256);
-}
+size_t kv4_tc_workspace_bytes() { return kMlBytes + kOBytes; }
 
-int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scratch, cudaStream_t stream) {
+int tree_attention_kv4_tc(const AttentionArgs& a, AttentionWorkspace* workspace, void* scratch, cudaStream_t stream) {
     static thread_local int sms_dev = -1, sms = 0;
     int dev = 0;
     MCSD_CUDA_CHECK(cudaGetDevice(&dev));
@@ -1211,8 +1219,8 @@ int tree_attention_kv4_tc(const AttentionArgs& a, WorkspaceHeader* header, void*
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.part_ml = static_cast<float*>(scratch);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + kMlBytes);
-    p.counters = reinterpret_cast<int*>(static_cast<char*>(scratch) + kMlBytes + kOBytes);
-    p.header = header;
+    p.counters = workspace->counters;
+    p.header = &workspace->header;
     const int grid = std::min(sms, kMaxCtas);
     // Few query columns (single tokens): the smaller kernel starts and merges faster, 15.2 against 16.1 us for one token after 1001
     // rows, 66 us either way for 8 x 32001 (with room for a sixth tile; 67 without).  Another one for 48 columns brought nothing (155 and 156 us for 45-node trees).

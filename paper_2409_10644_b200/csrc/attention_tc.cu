@@ -732,7 +732,7 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
                 if (t1 > t_end && t0 >= t_begin) {
                     np1 = min(block_of_tile<QB>(ix, p, t1 - 1, G, total_w) - cta, kMaxParts - 1);
                     // one counter per softmax group of the writing blocks; np1 arrivals each
-                    int* counter = p.counters + ((size_t)(sp.b * p.H + sp.h) * 2 + sp.qb) * 4;
+                    int* counter = p.counters + cta * kCountersPerBlock;
                     const long long t_start = clock64();
                     for (int gq = 0; gq < kGroups; ++gq) {
                         while (*(volatile int*)(counter + gq) < np1) {
@@ -775,10 +775,11 @@ tree_attention_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_
             Segment sf;
             locate<QB>(ix, p, t_begin, sf);
             if (sf.lt > 0) {
+                const int owner = block_of_tile<QB>(ix, p, t_begin - sf.lt, G, total_w);   // the block that starts the item
                 asm volatile("bar.sync %0, %1;" ::"n"(kGroups + 4), "n"(128 * kGroups + 32) : "memory");
                 __threadfence();
                 if (lane < kGroups && !*(volatile int*)abort_flag)
-                    atomicAdd(p.counters + ((size_t)(sf.b * p.H + sf.h) * 2 + sf.qb) * 4 + lane, 1);
+                    atomicAdd(p.counters + owner * kCountersPerBlock + lane, 1);
             }
         }
     }
@@ -1075,7 +1076,7 @@ bool tc_supported(const AttentionArgs& a) {
 size_t tc_workspace_bytes(int, int, int N, int, int) {
     if (N > MCSD_MAX_NODES) return 0;
     return align_up((size_t)2 * kMaxCtas * 2 * kMaxQ * sizeof(float), 256) +
-           align_up((size_t)2 * kMaxCtas * kMaxQ * 128 * sizeof(float), 256) + (size_t)65536 * 2 * 4 * sizeof(int);
+           align_up((size_t)2 * kMaxCtas * kMaxQ * 128 * sizeof(float), 256);
 }
 
 template <int NCH>
@@ -1106,7 +1107,7 @@ static int launch_tc(const TcLaunch& l, cudaStream_t stream) {
     return MCSD_OK;
 }
 
-int tree_attention_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scratch, size_t scratch_bytes,
+int tree_attention_tc(const AttentionArgs& a, AttentionWorkspace* workspace, void* scratch, size_t scratch_bytes,
                       cudaStream_t stream) {
     if (scratch_bytes < tc_workspace_bytes(a.B, a.H, a.N, a.D, a.L_max)) return MCSD_ERR_WORKSPACE_TOO_SMALL;
     const int S = tc_stack_for(a.G, a.N);       // query heads per work unit
@@ -1153,8 +1154,8 @@ int tree_attention_tc(const AttentionArgs& a, WorkspaceHeader* header, void* scr
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.part_ml = static_cast<float*>(scratch);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(scratch) + align_up((size_t)2 * kMaxCtas * 2 * kMaxQ * sizeof(float), 256));
-    p.counters = reinterpret_cast<int*>(reinterpret_cast<char*>(p.part_o) + align_up((size_t)2 * kMaxCtas * kMaxQ * 128 * sizeof(float), 256));
-    p.header = header;
+    p.counters = workspace->counters;
+    p.header = &workspace->header;
     p.n_slots = kSlots;
     p.npadq = npadq;
 

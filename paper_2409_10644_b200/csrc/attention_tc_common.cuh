@@ -17,7 +17,7 @@ constexpr int kMaxSlots = 6;
 constexpr int kMaxBatchTc = 256;
 constexpr int kTmemCols = 512;
 constexpr float kLazyTau = 8.0f;              // raise the reference maximum only beyond 2^8
-constexpr int kMaxCtas = 160;                 // partial slots are provisioned for this many thread blocks
+constexpr int kMaxCtas = kTcMaxBlocks;        // partial slots are provisioned for this many thread blocks
 constexpr int kMaxParts = kMaxCtas;           // a work item is cut into at most one piece per thread block
 constexpr int kMaxQ = 160;                    // queries per work item in the widest instantiation (stride of the partials)
 constexpr long long kSpinCycles = 4000000000LL;   // about two seconds
@@ -49,7 +49,7 @@ struct TcParams {
     float scale_log2;
     float* part_ml;      // [2 * kMaxCtas][2][kMaxQ]
     float* part_o;       // [2 * kMaxCtas][kMaxQ][128]
-    int* counters;       // [B * H][query block][softmax group] arrivals per split work item; zero between launches
+    int* counters;       // [block][softmax group] arrivals at the split work item the block starts; zero between launches
     WorkspaceHeader* header;
     int n_slots;
     int npadq;           // rows of the Q box = 16 * (template chunk count)
