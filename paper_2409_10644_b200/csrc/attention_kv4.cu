@@ -13,7 +13,8 @@
 //         score = scale_k (sum of code q) + (16 scale_k + offset_k) (sum of q).
 //   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
 //     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
-//     whose values lie well inside fp16's range, which the key warps vote on tile by tile; else bf16.
+//     whose values and weights both lie well inside fp16's range, which the key warps vote on for the values and the softmax
+//     group for the weights; else both are bf16 (8 bits, as in the kernel over dense caches).
 // The rows of the tree itself are read as they are (bf16, against the bf16 queries): scale 1, offset 0.
 //
 // What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; unpacking
@@ -100,6 +101,11 @@ struct Plan {
 // with 400, 398 / 157 / 67 us with 100.
 __host__ __device__ __forceinline__ int tile_cost(int nq) { return nq < 16 ? 40 : 24 + nq; }
 constexpr int kItemCost = 256;
+
+// Weights are 2^(score - reference).  A reference is taken 2^kFirstLog below the score it comes from and raised when a weight
+// passes 2^kTopLog; fp16 keeps the relative precision of what lies between 2^kLowLog and 2^kTopLog.  A lower first reference
+// leaves more room for small weights and is raised more often: 160 us for the 45-node trees with 4 to 6, 166 with 8, 180 with 10.
+constexpr float kFirstLog = 5.f, kTopLog = 15.f, kLowLog = -14.f;
 
 struct Shape {            // of the work items of one sequence
     int Tp, T, blocks_q, per_q, total_q;
@@ -339,6 +345,37 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
         else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(y[2 * k + 1]), "f"(y[2 * k]));
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// the largest and the smallest of three
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Turns fp16 values into bf16 where they lie: 64 columns of this thread's lane.  (Rarely used, and kept out of the tile loop.)
+__device__ __noinline__ void values_to_bf16(uint32_t taddr) {
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+        float y[8];
+        tc_ld8(taddr + 8 * c, y);
+        tc_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t w = __float_as_uint(y[k]);
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            uint32_t b;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(b) : "f"(v.y), "f"(v.x));
+            y[k] = __uint_as_float(b);
+        }
+        tc_st8(taddr + 8 * c, y);
+    }
+    tc_wait_st();
 }
 // 32 x 32 bits, a row per lane: exchanges rows and columns
 __device__ __forceinline__ uint32_t transpose_bits(uint32_t x, int lane) {
@@ -860,6 +897,7 @@ tree_attention_kv4_kernel(const Params p) {
             const float* qs = sm->q_sum[seg & 1u];
             const uint32_t g_end = g_piece + (uint32_t)s.cnt;
             const uint32_t g_own = g_piece + ((g_piece ^ (uint32_t)wg) & 1u);   // the group's first tile, if below g_end
+            bool deep = false;                                   // has met weights too small for fp16
             for (uint32_t g = g_own; g < g_end; g += 2) {
                 const int i = s.lt + (int)(g - g_piece);
                 const bool tree = i >= s.Tp;
@@ -884,14 +922,15 @@ tree_attention_kv4_kernel(const Params p) {
                 }
                 if (!mbar_wait(&sm->s_full[wg], (g >> 1) & 1u, abort_flag, hdr, 41)) failed = true;
                 tc_fence_after();
-                const uint32_t half = sm->fmt[g & 7u];
+                bool half = sm->fmt[g & 7u] && !deep;
                 const bool first = g == g_own;
                 float2 ab = sm->kab[g & 3u][r];
                 if (!tree) ab.x *= sm->q_factor[seg & 1u];
                 const float2 a2 = make_float2(ab.x, ab.x), b2 = make_float2(ab.y, ab.y);
-                // The first references of a piece: the largest of four keys' scores (one per warp) plus 3.  Any reference that
-                // no score exceeds by more than 2^8 and that is not far above the largest gives the same result; one that
-                // is exceeded is raised below.  A tile with a mask takes exact column maxima instead.
+                // The first references of a piece come from the largest of four keys' scores (one per warp).  Any reference gives
+                // the same result as long as the weights keep their precision; one that is exceeded too far is raised
+                // below, and weights that are too small for fp16 make the tile, and the rest of the piece, bf16.  A tile with
+                // a mask takes exact column maxima instead.
                 if (first && plain) {
 #pragma unroll 1
                     for (int j = 0; j < n8; ++j) {
@@ -908,12 +947,13 @@ tree_attention_kv4_kernel(const Params p) {
                     group_sync_any(bar_id, false);
                     if (own_col) {
                         const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
-                        nref[r] = -fmaxf(top + 3.f, -1e30f);
+                        nref[r] = -fmaxf(top - kFirstLog, -1e30f);
                     }
                     group_sync_any(bar_id, false);
                 }
-                // Then an optimistic sweep; where a score exceeds its reference by more than 2^8, new references and the same
-                // again.
+                // Then an optimistic sweep; where a score exceeds its reference by more than 2^kTopLog, new references and the
+                // same again; where weights are too small for fp16, the same again in bf16.  (Such weights are nothing
+                // beside a key that outweighs them all, but all there is to the result where that key's value is zero.)
                 bool raise = first && !plain, raised = false;
                 for (;;) {
                     if (raise) {
@@ -936,7 +976,7 @@ tree_attention_kv4_kernel(const Params p) {
                         if (own_col) {
                             const float top = fmaxf(fmaxf(sm->red[wg][0][r], sm->red[wg][1][r]), fmaxf(sm->red[wg][2][r], sm->red[wg][3][r]));
                             // (a column that has seen no key yet keeps one below any score)
-                            const float old = first ? -1e30f : -nref[r], now = fmaxf(old, top);
+                            const float old = first ? -1e30f : -nref[r], now = fmaxf(old, top - kFirstLog);
                             nref[r] = -now;
                             alph[r] = exp2f(old - now);
                         }
@@ -961,7 +1001,7 @@ tree_attention_kv4_kernel(const Params p) {
                         }
                     }
                     // scores of this thread's key relative to the references, exponentiated, packed, stored
-                    float dmax = -INFINITY;
+                    float dmax = -INFINITY, dmin = INFINITY;
                     // P^T may be written once the products of the group's previous tile are done (they are, nearly always)
                     auto p_free = [&]() {
                         if (g >= 2 && !mbar_wait(&sm->pv_done[wg], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 43)) failed = true;
@@ -988,7 +1028,8 @@ tree_attention_kv4_kernel(const Params p) {
                             if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y);
 #pragma unroll
                             for (int k = 0; k < 8; k += 2) {
-                                dmax = fmaxf(dmax, fmaxf(x[k], x[k + 1]));
+                                dmax = max3(dmax, x[k], x[k + 1]);
+                                dmin = min3(dmin, x[k], x[k + 1]);
                                 x[k] = ex2_approx(x[k]);
                                 x[k + 1] = ex2_approx(x[k + 1]);
                             }
@@ -1007,19 +1048,32 @@ tree_attention_kv4_kernel(const Params p) {
                             if (j + 1 < n8) tc_ld8(s_addr + 8 * j + 8, y);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                x[k] = ((bits >> k) & 1u) ? x[k] : -INFINITY;
+                                const bool seen = (bits >> k) & 1u;
+                                dmin = fminf(dmin, seen ? x[k] : INFINITY);
+                                x[k] = seen ? x[k] : -INFINITY;
                                 dmax = fmaxf(dmax, x[k]);
                                 x[k] = ex2_approx(x[k]);
                             }
                             *reinterpret_cast<uint4*>(p_own + j * 2048) = half ? pack8<true>(x) : pack8<false>(x);
                         }
                     }
-                    raise = group_sync_any(bar_id, (dmax > kLazyTau && !raised) || failed);   // one vote of the four warps
-                    if (!raise) break;
+                    const bool over = dmax > kTopLog && !raised;
+                    if (!group_sync_any(bar_id, over || (half && dmin < kLowLog) || failed)) break;   // one vote of the four warps
                     gone = group_sync_any(bar_id, failed);
                     if (gone) break;
+                    raise = group_sync_any(bar_id, over);
+                    if (!raise) {
+                        deep = true;
+                        half = false;
+                    }
                 }
                 if (gone) break;
+                if (deep && sm->fmt[g & 7u]) {
+                    // the value warps have stored fp16 and wait for the products, the products wait for this group
+                    if (!mbar_wait(&sm->v_full[wg], (g >> 1) & 1u, abort_flag, hdr, 50)) failed = true;
+                    values_to_bf16(lane_addr + Col::V + wg * 64);
+                    if (r == 0) sm->fmt[g & 7u] = 0;             // (everybody in the group has read it)
+                }
                 tc_fence_before();
                 if (lane == 0) mbar_arrive(&sm->s_free[wg]);     // (the vote came after everybody's last read)
                 fence_async_smem();

@@ -1,9 +1,13 @@
-"""Attention over the 4-bit cache where one call could disturb another: a workspace that several kernels use in turn."""
+"""Attention over the 4-bit cache where one call or key could disturb another: a workspace that several kernels use in turn, a
+key that outweighs the others by far."""
 import numpy as np
 import pytest
 import torch
 
 from mcsd_inputs import parent_array
+from oracle import kv4_oracle as kv4
+from oracle import mcsd_oracle as orc
+from tests.helpers import to_np
 from tests.test_kv4 import TREES, _attend, _check_attention, _off_by_one, _problem, m  # noqa: F401  (m: the fixture)
 
 
@@ -73,3 +77,60 @@ def test_a_workspace_full_of_another_calls_scratch(m, tree):  # noqa: F811
             _attend(m, q, cache, q, q, _i32([128] * 36), None, tw, ws)
             got = call(ws)
             assert torch.equal(got.nan_to_num(7), want.nan_to_num(7)) and not torch.isnan(got[0]).any()
+
+
+# ---------------------------------------------------------------------------------------------- one key outweighs the others
+
+def _stored_cache(m, k, v):
+    """A 4-bit cache of rows k, v [B][H][T][D] and its bytes."""
+    B, H, T, D = k.shape
+    cache = m.new_kv4_cache(B, H, T, D, "cuda")
+    m.mcsd_append_kv4(k, v, cache, _i32([0] * B))
+    return cache, cache.cpu().numpy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tree", ["token", "static", "forest"])
+@pytest.mark.parametrize("sink", [0, 70, 700])
+@pytest.mark.parametrize("nats", [10.0, 14.0, 16.0, 22.0, 40.0, 60.0])
+def test_keys_far_below_a_dominant_one(m, tree, sink, nats):  # noqa: F811
+    """One key (the first of all, or one that no first guess of the row's maximum looks at) outweighs all others by up to e^60, and its
+    value is zero, so the result is what the others give: their weights have to keep their relative precision.
+
+    Tolerance per element, u = 2^-8 half a step of bf16 (no product is made of coarser numbers): the result's rounding,
+    u |ref|; values, u A with A = sum w |v|; weights, in the products and in the row's sum, 2 u A, since the dominant weight
+    is a power of two times its fp32 value in both; the fp32 parts as in _check_attention, whose bounds on scores hold here too."""
+    rng = np.random.default_rng(int(nats) + sink)
+    parent = parent_array(*TREES[tree])
+    N, B, H, D, T = len(parent), 2, 20, 128, 992
+    tm, lens = m.mcsd_build_mask(parent), [960, 933]
+    way = rng.choice([-1.0, 1.0], size=D)
+    q = way + 0.05 * rng.normal(size=(B, H, N, D))
+    k = 0.3 * rng.normal(size=(B, H, T, D))
+    v = 1.0 + 0.3 * rng.normal(size=(B, H, T, D))
+    k[:, :, sink] = way * nats / D ** 0.5                    # score: nats, give or take
+    v[:, :, sink] = 0
+    kt, vt = 0.3 * rng.normal(size=(B, H, N, D)), 1.0 + 0.3 * rng.normal(size=(B, H, N, D))
+    cuda = lambda x, t: torch.from_numpy(x).to("cuda", t)  # noqa: E731
+    cache, cache_h = _stored_cache(m, cuda(k, torch.float32), cuda(v, torch.float32))
+    q, kt, vt = (cuda(x, torch.bfloat16) for x in (q, kt, vt))
+    out = to_np(_attend(m, q, cache, kt, vt, _i32(lens), None, tm)).astype(np.float64)
+
+    kc, vc = kv4.read_rows(cache_h, D)
+    assert (vc[:, :, sink] == 0).all()
+    qh, kh, vh = (to_np(x).astype(np.float64) for x in (q, kt, vt))
+    see, u = orc.dense_mask(parent), 2.0 ** -8
+    for b in range(B):
+        for g in range(H):
+            keys, vals = np.concatenate([kc[b, g, :lens[b]], kh[b, g]]), np.concatenate([vc[b, g, :lens[b]], vh[b, g]])
+            z = qh[b, g] @ keys.T * D ** -0.5
+            z[:, lens[b]:][~see] = -np.inf
+            w = np.exp(z - z.max(-1, keepdims=True))
+            assert (z.argmax(-1) == sink).all()
+            w /= w.sum(-1, keepdims=True)
+            ref, A = w @ vals, w @ np.abs(vals)
+            S = (np.abs(qh[b, g]) @ (2 * np.abs(keys).max(-1)[:, None] * np.ones((1, D))).T * D ** -0.5).max(-1, keepdims=True)
+            weight = 2 * (2 * (D + 4) * 2.0 ** -23 * S + 2.0 ** -21) + (lens[b] + N + 8) * 2.0 ** -23
+            tol = u * np.abs(ref) + 3 * u * A + weight * A
+            err = np.abs(out[b, g] - ref)
+            assert (err <= tol).all(), (b, g, (err / tol).max(), (err / np.abs(ref)).max())
