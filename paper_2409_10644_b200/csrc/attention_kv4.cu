@@ -7,9 +7,14 @@
 // 128-key tile, thread d of the value warps channel d, and both turn 16-byte pieces of a page (neighbouring threads read
 // neighbouring pieces) into operand columns with a shift and a mask per two values and store them with tcgen05.st.
 //   * Keys stay codes: the byte c (0..15) is c 2^-9 in e4m3 (its two lowest binades have the same spacing), so eight codes
-//     become operands with two masks and a shift.  Queries are split into two e4m3 parts, high and low, on a scale common to the
-//     work item: together they hold the eight bits of a bf16 number down to 2^-18 of the item's largest.  The sums are exact up
-//     to fp32, and the row's scale and offset are applied to the score, where the softmax thread owns the same key row:
+//     become operands with two masks and a shift.  Queries are split into two e4m3 parts, high and low, on a power of two common to
+//     the work item that brings its largest to 128 .. 256: together they hold all eight bits of a bf16 number down to 2^-9 of
+//     the largest, and what is smaller to within 2^-17 of the largest.  That is 2^-14 of a row's own largest or less while no
+//     row's largest lies further than a factor of 8 below the item's.  Where one does, so that a row would suffer from its
+//     neighbours, the item's codes become bf16 numbers 16 + c against the bf16 queries (no rounding; the keys of a tile
+//     then take both buffers, as the tree's do: 180 us against 159 for the 45-node trees, 91 against 67 for long single tokens,
+//     467 against 375 for the forests).  The sums are exact up to fp32, and the row's scale and offset are applied to
+//     the score, where the softmax thread owns the same key row:
 //         score = scale_k (sum of code q) + (16 scale_k + offset_k) (sum of q).
 //   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
 //     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
@@ -235,6 +240,7 @@ struct Small {
     } merge[2];
     int q_max;                                        // largest |query| of the first piece, as bits
     float q_factor[2];                                // brings sums over codes to score units
+    int q_split[2];                                   // 1: the e4m3 parts are used, 0: the bf16 form
     int fmt[8];                                       // 1: the tile's values and weights are fp16, 0: bf16
     alignas(16) int row[2][QB];                                   // rows of q and out of the piece's columns
     alignas(16) float2 kab[4][kTile];                 // scale and offset of a tile's key rows, in score units
@@ -312,6 +318,17 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t v) {
     const __half2 x = *reinterpret_cast<const __half2*>(&h);
     return __half22float2(x);
 }
+// the largest and the smallest of three
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 // (x & mask) | base, as the one instruction it is (left to itself the compiler makes it two)
 __device__ __forceinline__ uint32_t and_or(uint32_t x, uint32_t mask, uint32_t base) {
     uint32_t d;
@@ -346,16 +363,18 @@ __device__ __forceinline__ uint4 pack8(const float (&y)[8]) {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// the largest and the smallest of three
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-__device__ __forceinline__ float min3(float a, float b, float c) {
-    float d;
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
+// A key row's codes (its 16-byte pieces lie a page's rows apart) as bf16 numbers 16 + code in 64 columns of this thread's lane.
+// (Rarely used, and kept out of the tile loop.)
+__device__ __noinline__ void keys_to_bf16(const uint4* piece, uint32_t taddr) {
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        const uint4 x = piece[c * kPageRows];
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t y[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) y[e] = code_pair<false>(w[e >> 2], e & 3);
+        tc_st16(taddr + 16 * c, y);
+    }
 }
 // Turns fp16 values into bf16 where they lie: 64 columns of this thread's lane.  (Rarely used, and kept out of the tile loop.)
 __device__ __noinline__ void values_to_bf16(uint32_t taddr) {
@@ -451,10 +470,13 @@ __device__ __forceinline__ float load_query(Small<QB>* sm, unsigned char* q_buf,
 // the power of two that brings the largest query to 128 .. 256 (e4m3 ends at 448)
 __device__ __forceinline__ float query_scale(float top) {
     const int e = (int)(__float_as_uint(top) >> 23);               // of a number that is not negative
-    return top > 0.f && e < 255 ? __uint_as_float((uint32_t)(min(max(127 + 7 - (e - 127), 27), 227)) << 23) : 1.f;
+    return top > 0.f ? __uint_as_float((uint32_t)(min(max(127 + 7 - (e - 127), 10), 254)) << 23) : 1.f;
 }
+constexpr float kLeastTop = 16.f;                                  // of a row, next to the item's 128 .. 256
+constexpr float kMostTop = 0x1p120f;                               // of an item, so that the power of two and its inverse are finite
+// Returns 0 if the row's largest element is too far below the item's.
 template <int QB>
-__device__ __forceinline__ void split_query(unsigned char* q_buf, uint32_t buf, float scale, int r, int c) {
+__device__ __forceinline__ uint32_t split_query(unsigned char* q_buf, uint32_t buf, float scale, int r, int c) {
     const uint4 v = *reinterpret_cast<const uint4*>(query_piece<QB>(q_buf, buf, r, c));
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     float x[8];
@@ -475,6 +497,24 @@ __device__ __forceinline__ void split_query(unsigned char* q_buf, uint32_t buf, 
     unsigned char* at = q_buf + buf * (QB * 512) + QB * 256 + r * 128 + (((c >> 1) ^ (r & 7)) * 16) + (c & 1) * 8;
     *reinterpret_cast<uint2*>(at) = make_uint2(hi[0], hi[1]);
     *reinterpret_cast<uint2*>(at + QB * 128) = make_uint2(lo[0], lo[1]);
+    const float top = max3(max3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2])), max3(fabsf(x[3]), fabsf(x[4]), fabsf(x[5])), fmaxf(fabsf(x[6]), fabsf(x[7])));
+    return __ballot_sync(0xffffffffu, top >= kLeastTop) & (0xFFFFu << (threadIdx.x & 16u));
+}
+// the largest finite magnitude of the lane's channels of rows r, r + step, ... (rarely used)
+template <int QB>
+__device__ __noinline__ float finite_top(unsigned char* q_buf, uint32_t buf, int r, int rows, int step, int c) {
+    uint32_t top = 0;
+#pragma unroll 1
+    for (; r < rows; r += step) {
+        const uint4 v = *reinterpret_cast<const uint4*>(query_piece<QB>(q_buf, buf, r, c));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = (w[i] << 16) & 0x7FFF0000u, b = w[i] & 0x7FFF0000u;
+            top = max(top, max(a < 0x7F800000u ? a : 0u, b < 0x7F800000u ? b : 0u));
+        }
+    }
+    return __uint_as_float(top);
 }
 
 template <int QB>
@@ -508,6 +548,7 @@ tree_attention_kv4_kernel(const Params p) {
         mbar_init(&sm->drain, 2);
         sm->abort_flag = 0;
         sm->q_max = 0;
+        sm->q_split[0] = 1;
         sm->merge[0].T = sm->merge[1].T = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -541,11 +582,24 @@ tree_attention_kv4_kernel(const Params p) {
         asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
         tc_fence_after();
         tmem = *(volatile uint32_t*)&sm->tmem_base;
-        const float scale = query_scale(__int_as_float(sm->q_max));
-        for (int r = r0; r < rows; r += at_once) split_query<QB>(q_buf, 0, scale, r, c);
+        top = __int_as_float(sm->q_max);
+        if (!(top < INFINITY)) {                      // an infinite element says nothing about the others
+            asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+            if (tid == 0) sm->q_max = 0;
+            asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+            top = warp_max_f32(finite_top<QB>(q_buf, 0, r0, rows, at_once, c));
+            if (lane == 0) atomicMax(&sm->q_max, __float_as_int(top));
+            asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+            top = __int_as_float(sm->q_max);
+        }
+        const float scale = query_scale(top);
+        bool fine = top < kMostTop;
+        for (int r = r0; r < rows; r += at_once) fine &= split_query<QB>(q_buf, 0, scale, r, c) != 0u || r >= s.Nq || top == 0.f;
+        if (!fine) sm->q_split[0] = 0;
         if (tid == 0) { sm->q_factor[0] = 512.f / scale; sm->piece[0] = s; }
         fence_async_smem();
         asm volatile("bar.sync 9, %0;" ::"n"(kThreads - 32) : "memory");
+        if (!sm->q_split[0]) sm->q_factor[0] = 1.f;   // (by every thread that reads it)
     }
 
     // Tiles of this block are numbered g = 0, 1, ... across its pieces; f counts those that come through the ring.
@@ -595,6 +649,7 @@ tree_attention_kv4_kernel(const Params p) {
             ok = mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 32);
             const uint32_t idesc = instr_desc((s.Nq + 15) & ~15, 0, 0), idesc8 = idesc & ~((1u << 7) | (1u << 10));   // e4m3 is format 0
             const uint64_t dq = dq0 + (seg & 1u) * q_next;
+            const int narrow = sm->q_split[seg & 1u] ? s.Tp : 0;
             for (int i = s.lt; i < s.lt + s.cnt && ok; ++i, ++g) {
                 const uint32_t buf = g & 1u;
                 ok = mbar_wait(&sm->k_full[buf], (g >> 1) & 1u, abort_flag, hdr, 33);
@@ -603,7 +658,7 @@ tree_attention_kv4_kernel(const Params p) {
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t d = tmem + Col::S + buf * QB;
-                    if (i < s.Tp) {                   // 32 channels per MMA: high parts, then low parts
+                    if (i < narrow) {                 // 32 channels per MMA: high parts, then low parts
                         const uint32_t ka = tmem + Col::K + buf * 32;
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
@@ -713,10 +768,20 @@ tree_attention_kv4_kernel(const Params p) {
 #pragma unroll 4
                 for (int r = sub; r < rows; r += 2)
                     top = fmaxf(top, sum_query<QB>(sm, buf, r, c, *reinterpret_cast<const uint4*>(query_piece<QB>(q_buf, buf, r, c))));
-                const float scale = query_scale(warp_max_f32(top));
+                top = warp_max_f32(top);
+                if (!(top < INFINITY)) {
+                    top = warp_max_f32(finite_top<QB>(q_buf, buf, sub, rows, 2, c));
+                }
+                const float scale = query_scale(top);
+                bool fine = top < kMostTop;
 #pragma unroll 2
-                for (int r = sub; r < rows; r += 2) split_query<QB>(q_buf, buf, scale, r, c);
-                if (lane == 0) { sm->q_factor[buf] = 512.f / scale; sm->piece[buf] = s; }
+                for (int r = sub; r < rows; r += 2) fine &= split_query<QB>(q_buf, buf, scale, r, c) != 0u || r >= s.Nq || top == 0.f;
+                fine = __all_sync(0xffffffffu, fine);
+                if (lane == 0) {
+                    sm->q_factor[buf] = fine ? 512.f / scale : 1.f;
+                    sm->q_split[buf] = fine;
+                    sm->piece[buf] = s;
+                }
                 fence_async_smem();
                 __syncwarp();
             }
@@ -729,11 +794,14 @@ tree_attention_kv4_kernel(const Params p) {
         // ---- keys: thread r owns key row r of a tile
         const int r = tid;
         const uint32_t lane_addr = tmem + ((uint32_t)(warp * 32) << 16);
-        uint32_t g = 0, f = 0;
+        uint32_t g = 0, f = 0, seg = 0;
         bool bad = false, gone = false, wide = false;         // wide: the previous tile took both buffers
-        for (long long t = t_begin; t < t_end && !gone;) {
+        for (long long t = t_begin; t < t_end && !gone; ++seg) {
             Piece s;
             piece_at<QB>(pl, p, t, t_end, s);
+            // (the first piece's queries are there since the set-up)
+            if (seg > 0) bad |= !mbar_wait(&sm->q_full[seg & 1u], (seg >> 1) & 1u, abort_flag, hdr, 51);
+            const int narrow = sm->q_split[seg & 1u] ? s.Tp : 0;   // tiles from here on take both buffers
             for (int i = s.lt; i < s.lt + s.cnt; ++i, ++g) {
                 const uint32_t buf = g & 1u;
                 const uint32_t st = f % kStages<QB>;
@@ -761,10 +829,10 @@ tree_attention_kv4_kernel(const Params p) {
                 // too where either of the two takes both buffers.  They were issued after the softmax warps had taken
                 // the scores and the scales of tile g - 4, whose entry is rewritten below.
                 if (g >= 2) bad |= !mbar_wait(&sm->s_full[buf], ((g - 2u) >> 1) & 1u, abort_flag, hdr, 38);
-                if (g >= 1 && (wide || i >= s.Tp)) bad |= !mbar_wait(&sm->s_full[buf ^ 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 47);
+                if (g >= 1 && (wide || i >= narrow)) bad |= !mbar_wait(&sm->s_full[buf ^ 1u], ((g - 1u) >> 1) & 1u, abort_flag, hdr, 47);
                 tc_fence_after();
-                wide = i >= s.Tp;
-                if (i < s.Tp) {
+                wide = i >= narrow;
+                if (i < narrow) {
                     const uint4* piece = reinterpret_cast<const uint4*>(page) + lane;
                     const float a = bf16_bits_to_f32(sc[0]), b = bf16_bits_to_f32(sc[kPageRows]);
                     sm->kab[g & 3u][r] = make_float2(a * p.scale_log2, fmaf(16.f, a, b) * p.scale_log2);
@@ -780,6 +848,12 @@ tree_attention_kv4_kernel(const Params p) {
                         }
                         tc_st16(lane_addr + Col::K + buf * 32 + 16 * c, y);
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm->empty[st]);
+                    ++f;
+                } else if (i < s.Tp) {
+                    sm->kab[g & 3u][r] = make_float2(bf16_bits_to_f32(sc[0]) * p.scale_log2, bf16_bits_to_f32(sc[kPageRows]) * p.scale_log2);
+                    keys_to_bf16(reinterpret_cast<const uint4*>(page) + lane, lane_addr + Col::K);
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sm->empty[st]);
                     ++f;

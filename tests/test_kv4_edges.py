@@ -1,5 +1,5 @@
-"""Attention over the 4-bit cache where one call or key could disturb another: a workspace that several kernels use in turn, a
-key that outweighs the others by far."""
+"""Attention over the 4-bit cache where one call, row or key could disturb another: a workspace that several kernels use in
+turn, a key that outweighs the others by far, queries of very different size side by side."""
 import numpy as np
 import pytest
 import torch
@@ -134,3 +134,83 @@ def test_keys_far_below_a_dominant_one(m, tree, sink, nats):  # noqa: F811
             tol = u * np.abs(ref) + 3 * u * A + weight * A
             err = np.abs(out[b, g] - ref)
             assert (err <= tol).all(), (b, g, (err / tol).max(), (err / np.abs(ref)).max())
+
+
+# ---------------------------------------------------------------------------------------------- queries of different size
+
+def _row_errors(out, q, cache_h, kt, vt, lens, parent, rows):
+    """Largest error over its bound for the named query rows (head, node), each against the definition for that row alone.
+
+    u = 2^-8.  Result, values and weights are rounded to at most u each (weights in the products and in their sum: 2 u A).  A
+    score is off by the fp32 sums, 2 (D + 4) 2^-23 S as in _check_attention, and by the split of the row's queries: at
+    most 2^-14 of the row's own largest element, against codes of at most 15 steps."""
+    B, H, N, D = q.shape
+    G, u, scale = H // kt.shape[1], 2.0 ** -8, D ** -0.5
+    kc, vc = kv4.read_rows(cache_h, D)
+    sc = (np.ascontiguousarray(cache_h[..., 32 * D:]).view(np.uint16).astype(np.uint32) << 16).view(np.float32)
+    sc = np.abs(sc.astype(np.float64)).reshape(B, H // G, -1, 4, 32)
+    qh, kh, vh, o = (to_np(x).astype(np.float64) for x in (q, kt, vt, out))
+    worst = 0.0
+    for b in range(B):
+        n = lens[b]
+        for h, r in rows:
+            g = h // G
+            see = orc.dense_mask(parent)[r]
+            keys, vals = np.concatenate([kc[b, g, :n], kh[b, g][see]]), np.concatenate([vc[b, g, :n], vh[b, g][see]])
+            steps, offs = sc[b, g, :, 0].reshape(-1)[:n], sc[b, g, :, 1].reshape(-1)[:n]
+            x = qh[b, h, r]
+            z = keys @ x * scale
+            w = np.exp(z - z.max())
+            w /= w.sum()
+            ref, A = w @ vals, w @ np.abs(vals)
+            S = scale * max((np.abs(x).sum() * (31 * steps + offs)).max(), (np.abs(kh[b, g][see]) @ np.abs(x)).max())
+            split = 2.0 ** -14 * np.abs(x).max() * scale * 15 * D * steps.max()
+            weight = 2 * (2 * (D + 4) * 2.0 ** -23 * S + split + 2.0 ** -21) + (n + N + 8) * 2.0 ** -23
+            tol = u * np.abs(ref) + 3 * u * A + weight * A
+            assert np.isfinite(o[b, h, r]).all(), (b, h, r)
+            worst = max(worst, (np.abs(o[b, h, r] - ref) / tol).max())
+    return worst
+
+
+def _scaled_keys(m, cache, kt, T, factor):
+    """The cache's first T rows with their keys times factor, its bytes, and the tree's keys likewise."""
+    B, H, N, D = kt.shape
+    k, v = m.mcsd_read_kv4(m.layer_pointer_table([cache]), _i32([0] * B), T, None, B, H, D, cache.shape[2] * 32, torch.float32)
+    cache, cache_h = _stored_cache(m, k[0] * factor, v[0])
+    return cache, cache_h, kt * factor
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tree,Hq,Hkv", [("token", 8, 1), ("static", 2, 2), ("binary", 8, 2), ("forest", 1, 1)])
+@pytest.mark.parametrize("power", [-16, -12, -8, -4, -2, 10, 16])
+def test_rows_of_very_different_size_in_one_work_item(m, tree, Hq, Hkv, power):  # noqa: F811
+    """Every other query row (node and head) is 2^power times the others: each row's error is bounded by its own size."""
+    rng = np.random.default_rng(40 + power)
+    parent = parent_array(*TREES[tree])
+    lens = [500, 300]
+    q, cache, cache_h, kt, vt = _problem(m, rng, torch.bfloat16, 2, Hq, Hkv, 128, parent, lens, None)
+    rows = [(h, r) for h in range(Hq) for r in range(len(parent))]
+    for h, r in rows:
+        if (h + r) % 2:
+            q[:, h, r] *= 2.0 ** power
+    if power < 0:                                            # scores of the small rows are of order one all the same
+        cache, cache_h, kt = _scaled_keys(m, cache, kt, 512, 2.0 ** -power)
+    out = _attend(m, q, cache, kt, vt, _i32(lens), None, m.mcsd_build_mask(parent))
+    assert _row_errors(out, q, cache_h, kt, vt, lens, parent, rows) <= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("tree,Hq,Hkv", [("token", 8, 1), ("static", 2, 2), ("binary", 8, 2)])
+@pytest.mark.parametrize("size", [2.0 ** -6, 2.0 ** 11])
+def test_a_row_that_is_not_finite_leaves_the_others_alone(m, tree, Hq, Hkv, bad, size):  # noqa: F811
+    rng = np.random.default_rng(50)
+    parent = parent_array(*TREES[tree])
+    lens = [700, 129]
+    q, cache, cache_h, kt, vt = _problem(m, rng, torch.bfloat16, 2, Hq, Hkv, 128, parent, lens, None)
+    cache, cache_h, kt = _scaled_keys(m, cache, kt, 704, 1 / size)
+    q *= size
+    q[:, 0, 0, 5] = bad
+    rows = [(h, r) for h in range(Hq) for r in range(len(parent)) if (h, r) != (0, 0)]
+    out = _attend(m, q, cache, kt, vt, _i32(lens), None, m.mcsd_build_mask(parent))
+    assert _row_errors(out, q, cache_h, kt, vt, lens, parent, rows) <= 1
