@@ -382,7 +382,8 @@ int mcsd_qk_norm_rope(const void* q_in, const void* k_in, const void* v_in, cons
  * stands for scale * (16 + c) + offset.  A row x is stored with lo, hi = min x, max x, scale = bf16((hi - lo) / 15),
  * offset = bf16(lo - 16 scale), code = clamp(round_half_even((x - offset) / scale) - 16, 0, 15), or 0 where the scale is 0:
  * every value comes back within half a step of (hi - lo) / 15 plus the rounding of scale and offset (1/256 of 31 scale + |lo|).
- * Rows must be finite with a finite range: a row with an infinity comes back as NaN, a NaN as the row's lowest level.
+ * Elements must be finite and below 2^125 in magnitude, so that scale and offset are finite: a row with an infinity comes back as
+ * NaN, a NaN as the row's lowest level.
  */
 #define MCSD_KV4_PAGE_ROWS 32
 #define MCSD_KV4_PAGE_BYTES(D) (32 * (D) + 256)

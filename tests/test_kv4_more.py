@@ -15,6 +15,41 @@ def _i32(a):
     return None if a is None else torch.tensor(a, dtype=torch.int32, device="cuda")
 
 
+def _largest_rows(D, dtype):
+    """Rows that reach the largest magnitude the cache takes, on both sides, on one side, and once."""
+    rng = np.random.default_rng(D)
+    top = 2.0 ** 125 * (1 - 2.0 ** -8)                       # a bf16 number
+    x = rng.uniform(-1, 1, size=(4, D)) * top
+    x[1] = np.abs(x[1])
+    x[2] = -top + 2.0 ** 110 * rng.uniform(size=D)
+    x[3] *= 2.0 ** -60
+    x[:, 5], x[0, 9] = top, -top
+    return torch.from_numpy(x).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_oracle_holds_rows_up_to_the_stated_size(dtype, D):
+    """Half a step of (hi - lo) / 15 plus the rounding of scale and offset, 2^-8 of 31 scale + |lo|."""
+    for x in to_np(_largest_rows(D, dtype)).astype(np.float64):
+        _, s, o, _, _ = kv4.quantise_row(x)
+        assert np.isfinite([s, o]).all()
+        assert np.abs(kv4.stored_row(x) - x).max() <= 0.5 * (x.max() - x.min()) / 15 + 2.0 ** -8 * (31 * s + np.abs(x.min()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_up_to_the_stated_size(m, dtype, D):  # noqa: F811
+    x = _largest_rows(D, dtype).view(1, 1, 4, D).cuda()
+    cache = m.new_kv4_cache(1, 1, 32, D, "cuda")
+    m.mcsd_append_kv4(x, x, cache, _i32([0]))
+    want = np.zeros((1, 1, 1, 32 * D + 256), dtype=np.uint8)
+    for t, row in enumerate(to_np(x)[0, 0]):
+        kv4.write_row(want, 0, 0, t, row, row)
+    assert np.array_equal(cache.cpu().numpy(), want)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("D", [64, 128])
