@@ -903,7 +903,13 @@ tree_attention_kv4_kernel(const Params p) {
                 if (!ok) break;
                 tc_fence_after();
                 if (i < s.Tp) {
-                    if (!mbar_try_wait(&sm->full[st], (f / kStages<QB>) & 1u)) { ok = false; break; }   // (has completed)
+                    if (!mbar_try_wait(&sm->full[st], (f / kStages<QB>) & 1u)) {                  // (has completed)
+                        *(volatile int*)abort_flag = 1;
+                        hdr->detail = 52;
+                        hdr->status = MCSD_ERR_TIMEOUT;
+                        ok = false;
+                        break;
+                    }
                     const bool half = sm->fmt[g & 7u];
                     const unsigned char* codes = ring + st * kStageBytes + kv4_values_at(kD) + d * 16;
                     const uint4* sa = reinterpret_cast<const uint4*>(sm->vab[g & 7u][0]);
