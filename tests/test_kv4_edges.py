@@ -168,7 +168,8 @@ def _row_errors(out, q, cache_h, kt, vt, lens, parent, rows):
             weight = 2 * (2 * (D + 4) * 2.0 ** -23 * S + split + 2.0 ** -21) + (n + N + 8) * 2.0 ** -23
             tol = u * np.abs(ref) + 3 * u * A + weight * A
             assert np.isfinite(o[b, h, r]).all(), (b, h, r)
-            worst = max(worst, (np.abs(o[b, h, r] - ref) / tol).max())
+            err = np.abs(o[b, h, r] - ref)
+            worst = max(worst, np.divide(err, tol, out=np.where(err > 0, np.inf, 0.0), where=tol > 0).max())
     return worst
 
 
