@@ -12,14 +12,16 @@
 //     the largest, and what is smaller to within 2^-17 of the largest.  That is 2^-14 of a row's own largest or less while no
 //     row's largest lies further than a factor of 8 below the item's.  Where one does, so that a row would suffer from its
 //     neighbours, the item's codes become bf16 numbers 16 + c against the bf16 queries (no rounding; the keys of a tile
-//     then take both buffers, as the tree's do: 180 us against 159 for the 45-node trees, 91 against 67 for long single tokens,
-//     467 against 375 for the forests).  The sums are exact up to fp32, and the row's scale and offset are applied to
+//     then take both buffers, as the tree's do: 180 us against 160 for the 45-node trees, 92 against 68 for long single tokens,
+//     467 against 348 for the forests).  The sums are exact up to fp32, and the row's scale and offset are applied to
 //     the score, where the softmax thread owns the same key row:
 //         score = scale_k (sum of code q) + (16 scale_k + offset_k) (sum of q).
 //   * Values become scale_v (16 + code) + offset_v, one packed fused multiply-add per two values.  They and the weights
 //     that multiply them are fp16 (11 bits: an order of magnitude below the rounding of the bf16 result) in every tile
 //     whose values and weights both lie well inside fp16's range, which the key warps vote on for the values and the softmax
-//     group for the weights; else both are bf16 (8 bits, as in the kernel over dense caches).
+//     group for the weights; else both are bf16 (8 bits, as in the kernel over dense caches).  A tile whose weights say so late
+//     has its values converted in tensor memory: 235 us against 160 for the 45-node trees, 84 against 68 for long single tokens,
+//     with scores three times as large (a standard deviation of 4 nats).
 // The rows of the tree itself are read as they are (bf16, against the bf16 queries): scale 1, offset 0.
 //
 // What bounds it: 136 bytes per key and head against 512 in bf16 move the floor of a launch down by 3.8; unpacking
@@ -40,11 +42,12 @@
 // tiles per item; nothing waits): it reads all pieces in block order, so the result does not depend on who that is.
 // Every wait is bounded; one that runs out raises a flag in the workspace header.
 //
-// Measured (whole calls back to back): 16 sequences of 4096 rows, 32 heads, 45-node trees: 156 us, 2.0 TB/s (the bytes alone take
-// 47 us at the copy rate); 8 sequences up to 32001 rows, 8 key/value heads, one token: 66 us, 2.5 TB/s (25 us); 32 ragged
-// sequences with 8 to 160 nodes, one to three query blocks each: 354 us (58 us).  Per tile of 128 keys and 45 queries about 2000
-// cycles pass, in which the schedulers issue 4800 instructions (60 % of their slots); the longest role is the softmax, with
-// 2700 cycles for the exponentials of a tile and 4000 from one of a group's tiles to its next.  Tried and slower: both halves of a
+// Measured (whole calls back to back): 16 sequences of 4096 rows, 32 heads, 45-node trees: 160 us, 1.9 TB/s (the bytes alone take
+// 47 us at the copy rate); 8 sequences up to 32001 rows, 8 key/value heads, one token: 68 us, 2.4 TB/s (25 us); 32 ragged
+// sequences with 8 to 160 nodes, one to three query blocks each: 349 us (58 us).  Against the kernel over dense bf16 caches
+// (events, cold cache): 169 / 75 / 352 us here, 179 / 116 / 286 us there, so with many nodes the cache's size is the gain, not
+// the time.  Counters: 52 % of the issue slots used with six warps per scheduler on the trees (19 % of the memory's rate), 49 % on
+// the long tokens (27 %); the warps wait for one another's barriers, and for instructions.  Tried and slower: both halves of a
 // tile's columns on groups of their own (28 and more warps, 64 registers), a second buffer for P^T, longer unrolled loops; and
 // warp-level matrix instructions on operands unpacked into registers (324 us for the 45-node trees).
 #include <algorithm>
@@ -101,11 +104,11 @@ struct Plan {
 };
 
 // Cost of a tile with nq query columns (unpacking bounds it up to 16 columns, the exponentials beyond: about 29 cycles per unit)
-// and of a work item on top of its tiles: its first references, the tree rows read as they are, its end.  Measured on 32
-// ragged sequences with 8 to 160 nodes / the 45-node trees / 8 long single tokens: 361 / 156 / 67 us with 200, 350 / 155 / 69 us
-// with 400, 398 / 157 / 67 us with 100.
+// and of a work item on top of its tiles: its queries, first references, the tree rows read as they are, its end.  Measured on
+// 32 ragged sequences with 8 to 160 nodes / the 45-node trees / 8 long single tokens: 349 / 160 / 68 us with 400, 377 / 161 / 67
+// with 256, 393 / 162 / 66 with 200, 430 / 163 / 66 with 100.
 __host__ __device__ __forceinline__ int tile_cost(int nq) { return nq < 16 ? 40 : 24 + nq; }
-constexpr int kItemCost = 256;
+constexpr int kItemCost = 400;
 
 // Weights are 2^(score - reference).  A reference is taken 2^kFirstLog below the score it comes from and raised when a weight
 // passes 2^kTopLog; fp16 keeps the relative precision of what lies between 2^kLowLog and 2^kTopLog.  A lower first reference
@@ -1356,8 +1359,8 @@ int tree_attention_kv4_tc(const AttentionArgs& a, AttentionWorkspace* workspace,
     p.counters = workspace->counters;
     p.header = &workspace->header;
     const int grid = std::min(sms, kMaxCtas);
-    // Few query columns (single tokens): the smaller kernel starts and merges faster, 15.2 against 16.1 us for one token after 1001
-    // rows, 66 us either way for 8 x 32001 (with room for a sixth tile; 67 without).  Another one for 48 columns brought nothing (155 and 156 us for 45-node trees).
+    // Few query columns (single tokens): the smaller kernel starts and merges faster, 15.6 against 16.4 us for one token after 1001
+    // rows, 67 us either way for 8 x 32001 (with room for a sixth tile).  Another one for 48 columns brought nothing.
     if (a.N * a.G <= 16) return launch<16>(p, grid, stream);
     return launch<kWideQ>(p, grid, stream);
 }
