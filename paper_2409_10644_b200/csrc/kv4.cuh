@@ -7,8 +7,9 @@
 //
 // In the 16 bytes of a chunk, value 8w + 2i + h (w, i = 0..3, h = 0, 1) is the nibble at bits 4i + 16h of 32-bit word w,
 // so that one shift and one mask give two neighbouring values in the two halves of a register.  A row's code c
-// (0..15) stands for scale * (16 + c) + offset: 16 + c is a bf16 number whose mantissa bits 3..6 are c, so a code
-// becomes an operand by masking it into the bf16 pattern of 16, without a conversion.
+// (0..15) stands for scale * (16 + c) + offset: 16 + c is a bf16 or fp16 number of whose mantissa the code is four bits, so
+// value codes become numbers by masking them into the pattern of 16, without a conversion.  Key codes mostly go to the
+// tensor cores as bytes: c is c 2^-9 in e4m3.
 //
 // Keys are stored by row and values by channel because that is how the two products of attention consume them with
 // 128 keys (S^T = K Q^T) or 128 channels (O^T = V^T P^T) on the rows of the tensor-core operand; in both, the 16-byte

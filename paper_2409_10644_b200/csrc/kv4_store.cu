@@ -6,16 +6,17 @@
 // The offset is rounded to nearest: it moves the levels by at most 2^-9 |o|, a fraction of a step for rows whose
 // range is not small against their magnitude, and no more than the rounding of bf16 rows themselves otherwise.
 //
-// All three move bytes and little else, so what bounds them is memory, and the instructions per element while they store.
+// All three move bytes and little else; what bounds them is how many instructions they spend on an element.
 // A warp turns eight rows, the ones that share the 32-bit words of the value codes, into codes: their loads are in flight
 // together, the scales and offsets of all of them are computed at once (one lane per row), and every code is added to its
 // words as it is made.  Two rows share a byte of the value codes: one warp owns all of its words, and where only some of
 // the rows are written it merges with what is there; no two warps of a call touch the same word.
 //
-// Measured with heads of 128 in bf16: 8191 rows of 32 heads appended in 52 us (170 MB, 3.3 TB/s; the instructions that make
-// codes bound it) and read back in 35 us (4.9 TB/s); rows accepted by 16 sequences in 32 layers of 32 heads committed in
-// 37 us (44 us without the branches over absent rows, which a page that is written whole does not want): a chain of
-// three dependent loads for every one of 16384 heads, and half a page of traffic for a few rows, bound it.
+// Measured with heads of 128 in bf16: 8191 rows of 32 heads appended in 52 us (170 MB, 3.3 TB/s; 69 % of the issue slots at 4.7
+// warps per scheduler) and read back in 35 us (4.9 TB/s; 64 % at 8.9); rows accepted by 16 sequences in 32 layers of 32 heads
+// committed in 37 us (44 us without the branches over absent rows, which a page that is written whole does not want; 37 % of
+// the slots, most of the rest waiting for a chain of three dependent loads for every one of 16384 heads) and read back
+// in 35 us (71 %, in 32768 blocks, of which half find nothing to do).  Whole 32-byte sectors would let both go in 15 us.
 #include <type_traits>
 
 #include "f32x2.cuh"

@@ -12,8 +12,10 @@
 // The angles are reduced as position * freq / 2 pi to a fraction of a turn in 64 bits (a far position has no bits left
 // for the angle in 32) by all threads of a block while the first rows are on their way.
 //
-// Measured: 8191 tokens of 48 heads of 128, norm and half rotated, bf16: 47 us, 4.3 TB/s of the 201 MB that have to move;
-// 16 x 45 tokens of 96 heads: 10.2 us, 3.5 TB/s; a single token 4.6 us, of which most is the launch.
+// Measured: 8191 tokens of 48 heads of 128, norm and half rotated, bf16: 47 us, 4.3 TB/s of the 201 MB that have to move, with
+// 69 % of the issue slots used by 5.5 warps per scheduler (77 registers: three blocks on a multiprocessor), so instructions
+// bound it, not loads; 16 x 45 tokens of 96 heads: 10.2 us, 3.5 TB/s, 720 blocks where 444 run at a time, which
+// spend much of their time at the barrier behind the angles; a single token 4.6 us, of which most is the launch.
 #include "f32x2.cuh"
 #include "norm_rope.cuh"
 
@@ -197,10 +199,10 @@ qk_norm_rope_kernel(const NormRopeArgs a) {
 template <typename T, int D>
 static int launch(const NormRopeArgs& a, bool vec, cudaStream_t stream) {
     const long long tokens = (long long)a.B * a.N;
-    // One block per token while that leaves no multiprocessor idle; with more tokens than they hold at a time (two blocks each,
-    // twice over) a block takes four, whose angles keep all its threads busy once.  8191 tokens: 47 us against 70 us with a
-    // block each; 720 tokens: 12.4 us with a block each against 14.1 us by fours.
-    const bool many = tokens >= 4 * 296;
+    // One block per token while there are few; from 1184 tokens on (eight for each of the 148 multiprocessors, which hold three
+    // blocks each) a block takes four, whose angles keep all its threads busy once.  8191 tokens: 47 us against 70 us with
+    // a block each; 720 tokens: 12.4 us with a block each against 14.1 us by fours.
+    const bool many = tokens >= 8 * 148;
     if (!vec) qk_norm_rope_kernel<T, D, false, 1><<<(unsigned)tokens, kRopeThreads, 0, stream>>>(a);
     else if (many) qk_norm_rope_kernel<T, D, true, 4><<<(unsigned)((tokens + 3) / 4), kRopeThreads, 0, stream>>>(a);
     else qk_norm_rope_kernel<T, D, true, 1><<<(unsigned)tokens, kRopeThreads, 0, stream>>>(a);
