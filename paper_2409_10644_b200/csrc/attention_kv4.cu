@@ -1154,8 +1154,10 @@ tree_attention_kv4_kernel(const Params p) {
                 if (deep && sm->fmt[g & 7u]) {
                     // the value warps have stored fp16 and wait for the products, the products wait for this group
                     if (!mbar_wait(&sm->v_full[wg], (g >> 1) & 1u, abort_flag, hdr, 50)) failed = true;
+                    __syncwarp();
                     values_to_bf16(lane_addr + Col::V + wg * 64);
-                    if (r == 0) sm->fmt[g & 7u] = 0;             // (everybody in the group has read it)
+                    group_sync_any(bar_id, false);               // everybody in the group has read the format
+                    if (r == 0) sm->fmt[g & 7u] = 0;
                 }
                 tc_fence_before();
                 if (lane == 0) mbar_arrive(&sm->s_free[wg]);     // (the vote came after everybody's last read)

@@ -162,3 +162,32 @@ def test_prefix_products_keep_eleven_bits(m, tree, Hq, Hkv, L):  # noqa: F811
         tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * (2 * pre + np.abs(ref)) + 2.0 ** -8 * (2 * own + tree_share * np.abs(ref)) + weight * (pre + own)
         err = np.abs(out[0, h] - ref)
         assert (err <= tol).all(), (h, (err / tol).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["usual", "peaked", "a dominant key", "rows of different size"])
+@pytest.mark.parametrize("tree,B,Hq,Hkv,L", [("token", 2, 8, 2, 9000), ("static", 4, 8, 8, 1500), ("forest", 6, 4, 4, 700)])
+def test_repeated_calls_are_equal_to_the_bit(m, kind, tree, B, Hq, Hkv, L):  # noqa: F811
+    """Whichever form a tile takes (fp16 or bf16 weights, split or bf16 queries), timing has no part in it."""
+    g = torch.Generator("cuda").manual_seed(L)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    parent = parent_array(*TREES[tree])
+    N = len(parent)
+    k, q = rnd(B, Hkv, L, 128), rnd(B, Hq, N, 128)
+    if kind == "peaked":
+        q *= 6
+    elif kind == "a dominant key":
+        q = q * 0.3 + 1
+        k[:, :, L // 3] = 20 / 128 ** 0.5
+    elif kind == "rows of different size":
+        q[:, ::2, ::3] *= 2.0 ** -9
+    cache = m.new_kv4_cache(B, Hkv, L, 128, "cuda")
+    m.mcsd_append_kv4(k, rnd(B, Hkv, L, 128), cache, _i32([0] * B))
+    q, kt, vt = (x.to(torch.bfloat16) for x in (q, rnd(B, Hkv, N, 128), rnd(B, Hkv, N, 128)))
+    tm, lens = m.mcsd_build_mask(parent), _i32([L - 37 * b for b in range(B)])
+    want = _attend(m, q, cache, kt, vt, lens, None, tm)
+    ws = m.new_workspace(m.mcsd_tree_attention_kv4_workspace_bytes(B, Hq, Hkv, N, 128, cache.shape[2] * 32, m.MCSD_BF16), "cuda")
+    outs = [torch.empty_like(q) for _ in range(30)]
+    for out in outs:                                         # back to back
+        m.mcsd_tree_attention_kv4(q, cache, kt, vt, lens, None, tm, out=out, workspace=ws)
+    assert all(torch.equal(out, want) for out in outs) and torch.isfinite(want).all()
