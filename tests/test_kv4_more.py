@@ -191,3 +191,25 @@ def test_repeated_calls_are_equal_to_the_bit(m, kind, tree, B, Hq, Hkv, L):  # n
     for out in outs:                                         # back to back
         m.mcsd_tree_attention_kv4(q, cache, kt, vt, lens, None, tm, out=out, workspace=ws)
     assert all(torch.equal(out, want) for out in outs) and torch.isfinite(want).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.1, 0.01, 0.5])
+@pytest.mark.parametrize("zeros", ["none", "some rows", "all rows"])
+def test_scales_and_rows_of_zeros_on_both_kernels(m, scale, zeros):  # noqa: F811
+    """Any softmax scale, queries of zeros alone and beside others; bounds as for the random launches, the scores' part for
+    scores of up to a hundred (2 (D + 4) 2^-23 S twice, with S below 400: 2^-5 in a weight; none for scales up to a tenth)."""
+    g = torch.Generator("cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    parent = parent_array(*TREES["static"])
+    N, B, Hq, Hkv, L = len(parent), 2, 4, 2, 600
+    q = rnd(B, Hq, N, 128)
+    if zeros != "none":
+        q[:, :, ::2 if zeros == "some rows" else 1] = 0
+    cache = m.new_kv4_cache(B, Hkv, L, 128, "cuda")
+    m.mcsd_append_kv4(rnd(B, Hkv, L, 128), 1 + 0.2 * rnd(B, Hkv, L, 128), cache, _i32([0] * B))
+    q, kt, vt = (x.to(torch.bfloat16) for x in (q, rnd(B, Hkv, N, 128), 1 + 0.2 * rnd(B, Hkv, N, 128)))
+    tm, lens = m.mcsd_build_mask(parent), _i32([L, 129])
+    got, want = (m.mcsd_tree_attention_kv4(x, cache, kt, vt, lens, None, tm, softmax_scale=scale).double() for x in (q, _off_by_one(q)))
+    bound = 5 * 2.0 ** -8 * 1.1 + 2.0 ** -12 + (2.0 ** -5 if scale > 0.1 else 0)
+    assert torch.isfinite(got).all() and ((got - want).abs() <= bound * want.abs()).all()
