@@ -20,7 +20,7 @@
  *     or free device memory: kernels that need scratch take a caller-supplied workspace whose size the
  *     matching *_workspace_bytes() query returns.  A workspace is 256-byte aligned and must be zero-filled
  *     once before its first use (its first 256 bytes hold a sticky status word, see mcsd_workspace_status).
- *     The calls of mcsd_tree_attention, mcsd_tree_attention_gqa and mcsd_tree_attention_kv4, of any shapes and types, may
+ *     The calls of mcsd_tree_attention, mcsd_tree_attention_gqa, _kv4 and _latent, of any shapes and types, may
  *     use one workspace in turn.  A workspace of the verify calls is for one B and N, and not for attention.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the legacy default stream).  Calls only enqueue
  *     work on that stream and never synchronise, except where stated.
@@ -452,6 +452,108 @@ int mcsd_tree_attention_kv4(const void* q, const void* cache, const void* k_tree
                             const int32_t* seq_lens, const int32_t* n_active, const uint64_t* anc, int words, int B, int H_q,
                             int H_kv, int N, int D, int L_max, float softmax_scale, int dtype, void* workspace,
                             size_t workspace_bytes, void* stream);
+
+/*
+ * Operators for a target whose layers keep one shared latent row a token instead of keys and values per head (the paper's
+ * targets keep them per head; Section 2.2 defines the attention).  A row has rank + rot values: `rank` latent ones, which are
+ * key and value at once, and `rot` rotated by position, which are key only.  The queries come multiplied into the latent space
+ * (the absorbed form): rank + rot values a head, the scores being plain products with the rows, and the output has rank values
+ * a head, still to be multiplied by the layer's value projection.
+ *   cache   dtype[B][L_max][rank + rot];   tree rows   dtype[B][N][rank + rot];   q   dtype[B][H][N][rank + rot]
+ *   rank    a multiple of 32, 32 .. 512;   rot   a multiple of 16, 0 .. 128;   dtype   MCSD_BF16 or MCSD_F32
+ *
+ * mcsd_latent_rows makes rows and the rotated part of the queries from a layer's projections.  For sequence b, token n, head h:
+ *     rows[b][row_start[b] + n][:rank] = x * rsqrt(mean(x^2) + eps) * weight,  x = latent_in[b][n][:rank]   (x without a weight)
+ *     rows[b][row_start[b] + n][rank:] = latent_in[b][n][rank:] rotated
+ *     q[b][h][n][rank:]                = q_in[b][n][h][:] rotated;  q[b][h][n][:rank] is left alone
+ *     angle_i = (seq_lens[b] + depth[n]) * freqs[i], i = 0 .. rot / 2 - 1, in 64 bits;  pairs (i, i + rot / 2), or
+ *     (2i, 2i + 1) when `interleaved` is not 0;  (y_a, y_c) -> (y_a cos - y_c sin, y_c cos + y_a sin)
+ * in fp32, rounded once to dtype.  Frequencies scaled for long contexts are the caller's.
+ *
+ *   latent_in  [dev] dtype, element [b][n][d] at b * strides[0] + n * strides[1] + d;  q_in  [dev] dtype, element
+ *              [b][n][h][d] at b * strides[2] + n * strides[3] + h * strides[4] + d.  Must not overlap the outputs.
+ *   strides    [host] int64[5], in elements
+ *   weight     [dev] dtype[rank] or NULL;   eps >= 0;   freqs  [dev] double[rot / 2] (NULL allowed when rot is 0)
+ *   seq_lens   [dev] int32[B], position of the first token;   depth  [dev] int32[N] or NULL: token n lies n positions on
+ *   n_active   [dev] int32[B] or NULL = N; tokens n >= n_active[b] are neither read nor written
+ *   row_start  [dev] int32[B] or NULL = 0;  rows  [dev] dtype[B][L_rows][rank + rot] out or NULL: the tree's rows (L_rows = N),
+ *              or the cache itself (L_rows = L_max, row_start the tokens it holds).  Rows outside 0 .. L_rows - 1 are dropped.
+ *   q          [dev] dtype[B][H][N][rank + rot] in/out or NULL;  not both NULL
+ *
+ * One launch on `stream`, no workspace; 16-byte loads and stores where pointers and strides allow them.
+ * Errors: MCSD_ERR_NULL, MCSD_ERR_BAD_SHAPE (B > 65535, H > 65535, B * N >= 2^31, widths), MCSD_ERR_BAD_DTYPE, MCSD_ERR_CUDA.
+ */
+int mcsd_latent_rows(const void* latent_in, const void* q_in, const int64_t* strides, const void* weight, float eps,
+                     const double* freqs, int interleaved, const int32_t* seq_lens, const int32_t* depth,
+                     const int32_t* n_active, const int32_t* row_start, void* rows, int L_rows, void* q, int B, int H, int N,
+                     int rank, int rot, int dtype, void* stream);
+
+/*
+ * Tree attention over a latent cache, absorbed form (Section 2.2 with one key/value row for all heads): for every sequence b,
+ * head h and active node n
+ *     out[b][h][n] = sum_j softmax_j(softmax_scale * <q[b][h][n], row_j>) row_j[:rank]
+ * over the prefix rows j = 0 .. seq_lens[b] - 1 of the cache and the tree rows j with bit j set in anc[n].  N = 1 is the
+ * decoding step of a single token.  Rows n >= n_active[b] of `out` are not written, those of q and tree not used; cache rows
+ * from seq_lens[b] on may hold anything.  A node that sees no row at all (a mask row of zeros and an empty prefix) gets zeros.
+ * Elements of the rows in use must be finite.  fp32 softmax and sums; with bf16 the softmax weights are rounded to bf16 for
+ * the product with the rows (their sum is not), with fp32 nothing is rounded.
+ *
+ *   q [dev] dtype[B][H][N][rank + rot];  cache [dev] dtype[B][L_max][rank + rot] (NULL allowed when L_max is 0);
+ *   tree [dev] dtype[B][N][rank + rot];  out [dev] dtype[B][H][N][rank]
+ *   seq_lens, n_active, anc, words   as for mcsd_tree_attention;   L_max <= 2^30;  B * H <= 65535
+ *   workspace   [dev] >= mcsd_tree_attention_latent_workspace_bytes(...) bytes, 256-byte aligned, zero-filled once; may be the
+ *               workspace of the other attention calls; calls that may overlap on the device need distinct ones
+ *
+ * Errors: as mcsd_tree_attention.
+ */
+size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype);
+
+int mcsd_tree_attention_latent(const void* q, const void* cache, const void* tree, void* out, const int32_t* seq_lens,
+                               const int32_t* n_active, const uint64_t* anc, int words, int B, int H, int N, int rank, int rot,
+                               int L_max, float softmax_scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * mcsd_commit_kv for latent caches (Fig. 1 step 6): the rows of the winning root and of the accepted nodes are copied to cache
+ * rows seq_lens[b], seq_lens[b] + 1, ... of every layer, then seq_lens[b] grows by 1 + accept_len[b].  Rows that would fall
+ * beyond L_max are dropped and the length saturates at L_max.
+ *
+ *   cache_layers  [dev] array of n_layers device pointers, each dtype[B][L_max][width] (in/out)
+ *   tree_layers   [dev] array of n_layers device pointers, each dtype[B][N][width]
+ *   width         rank + rot: a multiple of 16, 32 .. 640;   all other arguments as for mcsd_commit_kv
+ *
+ * One launch on `stream` for all layers together; no workspace.  Errors: as mcsd_commit_kv.
+ */
+int mcsd_commit_latent(void* const* cache_layers, const void* const* tree_layers, int n_layers, int32_t* seq_lens,
+                       const int32_t* accept_len, const int32_t* out_nodes, const int32_t* best_root, int n_levels, int B, int N,
+                       int width, int L_max, int dtype, void* stream);
+
+/*
+ * Candidates from next-token logits under temperature, top-k, top-p and min-p (Fig. 1 step 1: the children of a node are
+ * independent draws from the draft's distribution after it).  The probabilities that it hands out are what mcsd_verify_tree
+ * takes as q for the draft's rows, and, called on the target's logits with the same filters, as p.  For every row, with
+ * weights w_i = exp((l_i - max l) / temperature) and the order "larger logit, then lower id":
+ *     top_k   keeps the first top_k tokens (off when <= 0 or >= V)
+ *     top_p   keeps the shortest beginning of those whose weight is at least top_p of theirs, one token at least (off when
+ *             >= 1 or NaN)
+ *     min_p   keeps those with w_i >= min_p (off when <= 0 or NaN; at most 1)
+ *     probs[i] = w_i / sum of what is kept, 0 elsewhere
+ *     tokens[j] = the smallest id t with (sum of w over kept ids <= t) > u[j] * (sum of what is kept);  K independent draws
+ * temperature <= 0 (or NaN) keeps the largest logit alone, the lowest id among equal ones.  Logits that are NaN or -infinity
+ * are never kept; a row that holds nothing else gives tokens of -1 and probabilities of 0.
+ *
+ *   logits       [dev] dtype, row r at r * row_stride elements, V each (MCSD_F32, or MCSD_BF16 widened exactly)
+ *   temperature, top_p, min_p  [dev] float[rows], top_k  [dev] int32[rows]: a value a row; NULL = 1, or that filter off
+ *   u            [dev] float[rows][K] uniforms in [0, 1);   tokens  [dev] int32[rows][K] out, or NULL (u is then not read)
+ *   probs        [dev] float[rows][V] out, or NULL;  not both NULL
+ *   V            1 .. 262144;  K  1 .. 1024 (any, when tokens is NULL);  rows  1 .. 2^24
+ *
+ * Weights are fp32 and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of
+ * sums: equal inputs give equal outputs, to the bit.  One launch on `stream`, no workspace.
+ * Errors: MCSD_ERR_NULL, MCSD_ERR_BAD_SHAPE, MCSD_ERR_BAD_DTYPE, MCSD_ERR_CUDA.
+ */
+int mcsd_sample_candidates(const void* logits, long long row_stride, int dtype, int rows, int V, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int K, int32_t* tokens,
+                           float* probs, void* stream);
 
 /*
  * mcsd_verify_tree with the vocabulary split over several GPUs (Fig. 1 steps 4-6, the procedure of

@@ -29,6 +29,8 @@ _EXPORTS = (
     "mcsd_verify_shard_select", "mcsd_verify_shard_pick",
     "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
     "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
+    "mcsd_latent_rows", "mcsd_tree_attention_latent_workspace_bytes", "mcsd_tree_attention_latent", "mcsd_commit_latent",
+    "mcsd_sample_candidates",
 )
 
 
@@ -108,6 +110,16 @@ def _load() -> ctypes.CDLL:
     lib.mcsd_tree_attention_kv4_workspace_bytes.argtypes = [c_int] * 7
     lib.mcsd_tree_attention_kv4.restype = c_int
     lib.mcsd_tree_attention_kv4.argtypes = [c_void_p] * 8 + [c_int] * 7 + [c_float, c_int, c_void_p, c_size_t, c_void_p]
+    lib.mcsd_latent_rows.restype = c_int
+    lib.mcsd_latent_rows.argtypes = [c_void_p] * 4 + [c_float, c_void_p, c_int] + [c_void_p] * 5 + [c_int, c_void_p] + [c_int] * 6 + [c_void_p]
+    lib.mcsd_tree_attention_latent_workspace_bytes.restype = c_size_t
+    lib.mcsd_tree_attention_latent_workspace_bytes.argtypes = [c_int] * 7
+    lib.mcsd_tree_attention_latent.restype = c_int
+    lib.mcsd_tree_attention_latent.argtypes = [c_void_p] * 7 + [c_int] * 7 + [c_float, c_int, c_void_p, c_size_t, c_void_p]
+    lib.mcsd_commit_latent.restype = c_int
+    lib.mcsd_commit_latent.argtypes = [c_void_p] * 2 + [c_int] + [c_void_p] * 4 + [c_int] * 6 + [c_void_p]
+    lib.mcsd_sample_candidates.restype = c_int
+    lib.mcsd_sample_candidates.argtypes = [c_void_p, ctypes.c_longlong, c_int, c_int, c_int] + [c_void_p] * 5 + [c_int] + [c_void_p] * 3
     return lib
 
 
@@ -656,6 +668,123 @@ def mcsd_tree_attention_kv4(q, cache, k_tree, v_tree, seq_lens, n_active, mask: 
                     _same(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel())
     _check(st, "mcsd_tree_attention_kv4")
     return out
+
+
+# ---------------------------------------------------------------- latent caches and candidates from logits
+
+def mcsd_latent_rows(latent_in, q_in, seq_lens, freqs, rows=None, q=None, row_start=None, depth=None, n_active=None, weight=None,
+                     eps: float = 1e-6, interleaved: bool = False):
+    """Rows of a latent cache and the rotated part of the queries from a layer's projections (see mcsd.h).
+
+    ``latent_in`` [B][N][rank + rot] and ``q_in`` [B][N][H][rot] may be views of larger projections (any strides but the last).
+    ``rows`` [B][L_rows][rank + rot] and ``q`` [B][H][N][rank + rot] are written in place, q from column rank on; either, with
+    its input, may be None.  ``freqs``: float64 [rot / 2] or None when rot is 0.  ``row_start``: int32 [B], row of token 0."""
+    if rows is None and q is None:
+        raise ValueError("rows or q must be given")
+    ref = rows if rows is not None else q
+    dt, dev = ref.dtype, ref.get_device()
+    code = _dtype_code(ref)
+    width, rot = ref.shape[-1], 0 if freqs is None else 2 * freqs.numel()
+    B, N = (latent_in if rows is not None else q_in).shape[:2]
+    lat, H, qp, L_rows, strides = None, 1, None, 1, [0] * 5
+    if rows is not None:
+        lat, strides[0], strides[1] = _projection(latent_in.unsqueeze(2), dt, dev, "latent_in")
+        if latent_in.shape != (B, N, width) or rows.dim() != 3:
+            raise ValueError("latent_in %s does not fit rows %s" % (tuple(latent_in.shape), tuple(rows.shape)))
+        L_rows = rows.shape[1]
+    if q is not None:
+        H = q.shape[1]
+        if q_in.shape != (B, N, H, rot):
+            raise ValueError("q_in has shape %s, expected %s" % (tuple(q_in.shape), (B, N, H, rot)))
+        if q_in.dtype is not dt or q_in.get_device() != dev or (q_in.stride(3) != 1 and rot > 1):
+            raise ValueError("q_in must be a CUDA tensor of dtype %s on device %d, its last axis dense" % (dt, dev))
+        qp, strides[2:] = q_in.data_ptr(), q_in.stride()[:3]
+    st = _on_device(dev, lib.mcsd_latent_rows, lat, qp, (ctypes.c_int64 * 5)(*strides), _maybe(weight, dt, (width - rot,), dev, "weight"), eps,
+                    _maybe(freqs, torch.float64, (rot // 2,), dev, "freqs"), int(interleaved), _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
+                    _maybe(depth, torch.int32, (N,), dev, "depth"), _maybe(n_active, torch.int32, (B,), dev, "n_active"),
+                    _maybe(row_start, torch.int32, (B,), dev, "row_start"), _maybe(rows, dt, (B, L_rows, width), dev, "rows"), L_rows,
+                    _maybe(q, dt, (B, H, N, width), dev, "q"), B, H, N, width - rot, rot, code)
+    _check(st, "mcsd_latent_rows")
+    return rows, q
+
+
+def mcsd_tree_attention_latent_workspace_bytes(B, H, N, rank, rot, L_max, dtype_code) -> int:
+    return int(lib.mcsd_tree_attention_latent_workspace_bytes(B, H, N, rank, rot, L_max, dtype_code))
+
+
+def mcsd_tree_attention_latent(q, cache, tree, seq_lens, n_active, mask: TreeMask, softmax_scale: float, rank: Optional[int] = None,
+                               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tree attention over a latent cache, absorbed form (see mcsd.h): q [B][H][N][rank + rot], cache [B][L_max][rank + rot],
+    tree [B][N][rank + rot], out [B][H][N][rank].  ``rank`` is taken from ``out`` where that is given.  The scale has no
+    default: it belongs to the width the heads had before they were multiplied into the latent space."""
+    dt, dev = q.dtype, q.get_device()
+    code = _dtype_code(q)
+    B, H, N, W = q.shape
+    if mask.n_nodes != N:
+        raise ValueError("mask was built for %d nodes, q has %d" % (mask.n_nodes, N))
+    if out is None:
+        if rank is None:
+            raise ValueError("rank or out must be given")
+        out = torch.empty((B, H, N, rank), dtype=dt, device=q.device)
+    elif rank is None:
+        rank = out.shape[-1]
+    L_max = cache.shape[1] if cache.dim() == 3 else -1
+    if workspace is None:
+        workspace = new_workspace(mcsd_tree_attention_latent_workspace_bytes(B, H, N, rank, W - rank, L_max, code), q.device)
+    st = _on_device(dev, lib.mcsd_tree_attention_latent, _same(q, dt, (B, H, N, W), dev, "q"), _same(cache, dt, (B, L_max, W), dev, "cache"),
+                    _same(tree, dt, (B, N, W), dev, "tree"), _same(out, dt, (B, H, N, rank), dev, "out"),
+                    _same(seq_lens, torch.int32, (B,), dev, "seq_lens"), _maybe(n_active, torch.int32, (B,), dev, "n_active"),
+                    _same(mask.anc, torch.int64, (N, mask.words), dev, "mask.anc"), mask.words, B, H, N, rank, W - rank, L_max,
+                    softmax_scale, code, _same(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel())
+    _check(st, "mcsd_tree_attention_latent")
+    return out
+
+
+def mcsd_commit_latent(cache_ptrs, tree_ptrs, seq_lens, verify_out, mask: TreeMask, B: int, width: int, L_max: int,
+                       dtype: torch.dtype) -> None:
+    """Append the accepted tokens' rows to every layer's latent cache and grow seq_lens (see mcsd.h; pointer tables and
+    ``verify_out`` as for mcsd_commit_kv)."""
+    dev, n_layers = seq_lens.get_device(), cache_ptrs.numel()
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("rows are bf16 or fp32")
+    st = _on_device(dev, lib.mcsd_commit_latent, _same(cache_ptrs, torch.int64, (n_layers,), dev, "cache_ptrs"),
+                    _same(tree_ptrs, torch.int64, (n_layers,), dev, "tree_ptrs"), n_layers, _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
+                    _same(verify_out["accept_len"], torch.int32, (B,), dev, "accept_len"),
+                    _same(verify_out["out_nodes"], torch.int32, (B, mask.n_levels), dev, "out_nodes"),
+                    _same(verify_out["best_root"], torch.int32, (B,), dev, "best_root"), mask.n_levels, B, mask.n_nodes, width, L_max,
+                    MCSD_BF16 if dtype == torch.bfloat16 else MCSD_F32)
+    _check(st, "mcsd_commit_latent")
+
+
+def mcsd_sample_candidates(logits, u=None, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, tokens=None):
+    """Draws from filtered next-token logits, and the probabilities they are drawn from (see mcsd.h).
+
+    ``logits`` [rows][V], rows any stride apart; ``u`` float32 [rows][K] uniforms, or None for no draws.  ``temperature``,
+    ``top_p``, ``min_p`` float32 [rows] and ``top_k`` int32 [rows] on the device, or None.  ``probs`` float32 [rows][V] to write
+    into, True for a new tensor, None for none; ``tokens`` int32 [rows][K] to write into.  Returns those of (tokens, probs)
+    that there are, as a tuple."""
+    dt, dev = logits.dtype, logits.get_device()
+    if dt not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be float32 or bfloat16")
+    rows, V = logits.shape
+    if dev < 0 or (V > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a CUDA tensor whose last axis is dense")
+    K = 0
+    if u is not None:
+        K = u.shape[1]
+        if tokens is None:
+            tokens = torch.empty((rows, K), dtype=torch.int32, device=logits.device)
+    elif tokens is not None:
+        raise ValueError("tokens need uniforms")
+    if probs is True:
+        probs = torch.empty((rows, V), dtype=torch.float32, device=logits.device)
+    f32 = torch.float32
+    st = _on_device(dev, lib.mcsd_sample_candidates, logits.data_ptr(), logits.stride(0) if rows > 1 else V, MCSD_BF16 if dt == torch.bfloat16 else MCSD_F32,
+                    rows, V, _maybe(temperature, f32, (rows,), dev, "temperature"), _maybe(top_k, torch.int32, (rows,), dev, "top_k"),
+                    _maybe(top_p, f32, (rows,), dev, "top_p"), _maybe(min_p, f32, (rows,), dev, "min_p"), _maybe(u, f32, (rows, K), dev, "u"), K,
+                    _maybe(tokens, torch.int32, (rows, K), dev, "tokens"), _maybe(probs, f32, (rows, V), dev, "probs"))
+    _check(st, "mcsd_sample_candidates")
+    return tuple(t for t in (tokens, probs) if t is not None)
 
 
 def mcsd_verify_shard_workspace_bytes(B, N) -> int:

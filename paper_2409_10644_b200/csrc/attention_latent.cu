@@ -1,0 +1,30 @@
+// C ABI entry point of tree attention over a latent cache: argument checks and the choice of kernel.
+#include "latent.cuh"
+
+static int check_latent(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
+    if (dtype != MCSD_BF16 && dtype != MCSD_F32) return MCSD_ERR_BAD_DTYPE;
+    if (B < 1 || H < 1 || N < 1 || N > MCSD_MAX_NODES || L_max < 0 || L_max > (1 << 30) || (long long)B * H > 65535) return MCSD_ERR_BAD_SHAPE;
+    return mcsd::latent_widths_ok(rank, rot) ? MCSD_OK : MCSD_ERR_BAD_SHAPE;
+}
+
+extern "C" size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
+    if (check_latent(B, H, N, rank, rot, L_max, dtype) != MCSD_OK) return 0;
+    const size_t scratch = mcsd::latent_simt_workspace_bytes(B, H, N, rank, L_max);
+    return sizeof(mcsd::AttentionWorkspace) + mcsd::align_up(scratch, 256);
+}
+
+extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, const void* tree, void* out, const int32_t* seq_lens,
+                                          const int32_t* n_active, const uint64_t* anc, int words, int B, int H, int N, int rank,
+                                          int rot, int L_max, float softmax_scale, int dtype, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+    if (!q || !tree || !out || !seq_lens || !anc || !workspace) return MCSD_ERR_NULL;
+    const int st = check_latent(B, H, N, rank, rot, L_max, dtype);
+    if (st != MCSD_OK) return st;
+    if (L_max > 0 && !cache) return MCSD_ERR_NULL;
+    if (words < (N + 63) / 64 || words > MCSD_MAX_WORDS) return MCSD_ERR_BAD_SHAPE;
+    if (workspace_bytes < mcsd_tree_attention_latent_workspace_bytes(B, H, N, rank, rot, L_max, dtype)) return MCSD_ERR_WORKSPACE_TOO_SMALL;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MCSD_ERR_BAD_SHAPE;
+    const mcsd::LatentArgs a{q, cache, tree, out, seq_lens, n_active, anc, words, B, H, N, rank, rot, L_max, softmax_scale, dtype};
+    auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
+    return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
+}

@@ -1,0 +1,33 @@
+// Internal interface of the operators over a latent cache (one shared row of `rank` + `rot` values a token): the row and
+// commit kernels (latent_rows.cu), the entry point of tree attention (attention_latent.cu) and its two kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "attention.cuh"
+
+namespace mcsd {
+
+constexpr int kLatentMaxRank = 512, kLatentMaxRot = 128;
+
+// ranks and rotated parts that every latent operator takes (rows are then whole 16-byte vectors in both types)
+inline bool latent_widths_ok(int rank, int rot) {
+    return rank >= 32 && rank <= kLatentMaxRank && rank % 32 == 0 && rot >= 0 && rot <= kLatentMaxRot && rot % 16 == 0;
+}
+
+struct LatentArgs {
+    const void *q, *cache, *tree;
+    void* out;
+    const int32_t *seq_lens, *n_active;
+    const uint64_t* anc;
+    int words;
+    int B, H, N, rank, rot, L_max;
+    float scale;
+    int dtype;
+};
+
+// CUDA-core kernel: fp32, and bf16 shapes or alignments that the tensor-core kernel does not take
+size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max);
+int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t stream);
+
+}  // namespace mcsd
