@@ -1,5 +1,9 @@
 // C ABI entry point of tree attention over a latent cache: argument checks and the choice of kernel.
+#include <algorithm>
+
 #include "latent.cuh"
+
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 static int check_latent(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
     if (dtype != MCSD_BF16 && dtype != MCSD_F32) return MCSD_ERR_BAD_DTYPE;
@@ -9,7 +13,8 @@ static int check_latent(int B, int H, int N, int rank, int rot, int L_max, int d
 
 extern "C" size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
     if (check_latent(B, H, N, rank, rot, L_max, dtype) != MCSD_OK) return 0;
-    const size_t scratch = mcsd::latent_simt_workspace_bytes(B, H, N, rank, L_max);
+    size_t scratch = mcsd::latent_simt_workspace_bytes(B, H, N, rank, L_max);      // bf16 tensors off a 16-byte boundary
+    if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype)) scratch = std::max(scratch, mcsd::latent_tc_workspace_bytes());
     return sizeof(mcsd::AttentionWorkspace) + mcsd::align_up(scratch, 256);
 }
 
@@ -26,5 +31,7 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MCSD_ERR_BAD_SHAPE;
     const mcsd::LatentArgs a{q, cache, tree, out, seq_lens, n_active, anc, words, B, H, N, rank, rot, L_max, softmax_scale, dtype};
     auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
+    if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned16(q) && aligned16(cache) && aligned16(tree) && aligned16(out))
+        return mcsd::tree_attention_latent_tc(a, &ws->header, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
 }

@@ -1,0 +1,685 @@
+// Tree attention over a latent cache on the fifth-generation tensor cores of sm_100a: bf16, rank 512, rotated part 64.
+//
+//   S = Q K^T,  P = exp2(scale S - ref),  O += P V,   Q: 128 query rows of 576, K: keys of 576, V: their first 512 values
+//
+// All heads and nodes of a sequence share the keys, so its H * n_active query rows are one matrix; a work item is 128 of
+// them.  Their 128 x 512 fp32 accumulators fill the tensor memory of one multiprocessor and leave no room for S, so a pair
+// of blocks (a cluster of two) takes an item together: tcgen05.mma.cta_group::2 with M = 128 gives each 64 rows, whose
+// accumulators take 256 columns there, rows in lanes 0..63 and the upper half of N in lanes 64..127.  The products of this
+// shape run at the full rate with N = 256 (64 cycles each, measured; 50 with N = 128), so a tile has 256 keys: S is 128
+// columns, twice, and tensor memory is full.
+//
+// A block loads its half of what a product needs: for S its half of the keys, 64 channels at a time, for O its half of the
+// channels, 64 keys at a time; both are 16 KB, and pass through one ring of seven slots in the order in which the products
+// take them: S of tile t + 1, then O of tile t, so that the softmax of a tile overlaps products of its neighbours.
+//
+// A tile always ends at the last key of its range and starts a multiple of 32 keys before: a ragged tile overlaps the tile
+// before it (or starts before the first row, where TMA gives zeros) and masks what it has no claim to, so that no row behind a
+// sequence's end ever meets a product.
+//
+// The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
+// inside an item, the pieces write unnormalised rows, and a second kernel joins them.  Tiles are 256 keys, or 128 or 64
+// where there would be fewer tiles than pairs.
+//
+// Warps of a block: 0 loads, 1 issues products (first block of the pair), 2 and 3 fetch queries, 4 to 7 do the softmax and
+// the output.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
+// blocks exit.
+#include <cuda.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "attention_tc_common.cuh"
+#include "latent.cuh"
+
+namespace mcsd {
+
+constexpr int kLtRank = 512, kLtRot = 64, kLtWidth = kLtRank + kLtRot;
+constexpr int kLtChunks = kLtWidth / 64;             // 64-channel chunks of a row
+constexpr int kLtThreads = 256;
+constexpr int kLtSlots = 7, kLtSlotBytes = 16384;
+constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;
+constexpr int kLtMaxBatch = 256;
+constexpr int kLtMaxPairs = kTcMaxBlocks / 2;
+constexpr int kLtColO = 0, kLtColS = 256;            // tensor memory: O 256 columns, S 128 twice
+
+struct LtPieces {                                    // an item cut over several pairs, by the pair that starts it
+    int count, b, rb, pad;
+};
+
+struct LtParams {
+    LatentArgs a;
+    float scale_log2;
+    float* part_o;                                   // [2 * pairs][128][512]
+    float2* part_ml;                                 // [2 * pairs][128]  reference (log2), sum
+    LtPieces* pieces;                                // [pairs]
+    WorkspaceHeader* header;
+};
+struct LtMaps {
+    CUtensorMap m[8];                                // boxes of 16, 32, 64, 128 rows: cache, then tree
+};
+
+struct LtSmall {
+    unsigned long long full[kLtSlots], empty[kLtSlots];
+    unsigned long long s_full[2], p_full, pv_done, q_full, q_free;
+    uint32_t tmem_base;
+    int abort_flag;
+    int tile_keys, pairs;                            // keys of a tile, pairs with work
+    int total;                                       // units of the launch
+    int sums[3];                                     // tiles of the launch with 256, 128, 64 keys a tile
+    int scan[8];
+    int cum[kLtMaxBatch + 1];                        // units before a sequence
+    float red[2][2][64];                             // row maxima of a tile's halves, by tile parity
+    float lsum[2][64];
+};
+constexpr int kLtSmem = 1024 + kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes + (int)sizeof(LtSmall);
+static_assert(kLtSmem <= kSmemLimit, "a block's shared memory");
+
+// ------------------------------------------------------------------ PTX of a pair of blocks
+__device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {      // the same shared variable in the pair's first block
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_cluster(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void pair_commit(void* bar) {              // the barrier of both blocks
+    const uint16_t both = 3;
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(smem_u32(bar)), "h"(both) : "memory");
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// 32 consecutive fp32 columns of this thread's lane; the caller waits with tc_wait_ld()
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
+        "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+
+// ------------------------------------------------------------------ the cut of a launch
+__host__ __device__ __forceinline__ int lt_tiles(int L, int Nb, int tk) { return (L + tk - 1) / tk + (Nb + tk - 1) / tk; }
+__host__ __device__ __forceinline__ int lt_row_blocks(int H, int Nb) { return (H * Nb + 127) / 128; }
+__device__ __forceinline__ int lt_len(const LatentArgs& a, int b) { return min(max(a.seq_lens[b], 0), a.L_max); }
+__device__ __forceinline__ int lt_nodes(const LatentArgs& a, int b) { return a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N; }
+// Unit 0 of an item stands for its fixed cost (queries, output), unit 1 + t for tile t.  First unit of pair c:
+__device__ __forceinline__ int lt_first(int c, int total, int pairs) { return (int)((long long)c * total / pairs); }
+__device__ __forceinline__ int lt_pair_of(int unit, int total, int pairs) { return (int)((((long long)unit + 1) * pairs - 1) / total); }
+
+struct LtItem {
+    int b, rb, L, Nb, nP, nt;      // sequence, row block; prefix length, nodes; prefix tiles, tiles
+    int t0, t1;                    // this pair's tiles
+    int unit0;                     // the item's first unit
+};
+// Walks the items of a pair's range; every role of both blocks walks alike.
+struct LtWalk {
+    int u, end, b;
+    __device__ __forceinline__ void start(const LtSmall* sm, int pair) {
+        b = 0;
+        u = end = 0;
+        if (pair < sm->pairs) {
+            u = lt_first(pair, sm->total, sm->pairs);
+            end = lt_first(pair + 1, sm->total, sm->pairs);
+        }
+    }
+    __device__ __forceinline__ bool next(const LtSmall* sm, const LatentArgs& a, LtItem& it) {
+        while (u < end) {
+            while (sm->cum[b + 1] <= u) ++b;
+            it.b = b;
+            it.L = lt_len(a, b);
+            it.Nb = lt_nodes(a, b);
+            it.nP = (it.L + sm->tile_keys - 1) / sm->tile_keys;
+            it.nt = it.nP + (it.Nb + sm->tile_keys - 1) / sm->tile_keys;
+            const int off = u - sm->cum[b];
+            it.rb = off / (it.nt + 1);
+            const int rem = off - it.rb * (it.nt + 1);
+            it.unit0 = u - rem;
+            const int stop = min(end, it.unit0 + it.nt + 1);
+            it.t0 = max(rem - 1, 0);
+            it.t1 = stop - it.unit0 - 1;
+            u = stop;
+            if (it.t1 > it.t0) return true;
+        }
+        return false;
+    }
+};
+struct LtTile {
+    int lo, start, kpc;            // first key it has a claim to, first key that is loaded, keys of a block (16 .. 128)
+    bool tree;
+};
+__device__ __forceinline__ LtTile lt_tile(const LtItem& it, int t, int tk) {
+    LtTile x;
+    x.tree = t >= it.nP;
+    x.lo = (x.tree ? t - it.nP : t) * tk;
+    const int stop = min(x.lo + tk, x.tree ? it.Nb : it.L);
+    x.kpc = (stop - x.lo + 31) / 32 * 16;
+    x.start = stop - 2 * x.kpc;
+    return x;
+}
+
+__device__ __forceinline__ uint64_t anc_word(const uint64_t* w, int words, int i) { return i >= 0 && i < words ? w[i] : 0; }
+// 32 bits of a mask row from bit `pos` on (which may lie before the first bit: zeros)
+__device__ __forceinline__ uint32_t anc_bits(const uint64_t* w, int words, int pos) {
+    const int i = pos >> 6, s = pos & 63;
+    uint64_t v = anc_word(w, words, i) >> s;
+    if (s) v |= anc_word(w, words, i + 1) << (64 - s);
+    return (uint32_t)v;
+}
+
+#define LT_WAIT(bar, parity, where) mbar_wait(bar, parity, &sm->abort_flag, p.header, where)
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtThreads, 1)
+tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_constant__ LtParams p) {
+    extern __shared__ uint8_t raw[];
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t q_a = smem_u32(base), p_a = q_a + kLtQBytes, ring_a = p_a + kLtPBytes;
+    LtSmall* sm = reinterpret_cast<LtSmall*>(base + kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes);
+    const LatentArgs& a = p.a;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int pair = blockIdx.x >> 1, rank = blockIdx.x & 1;
+
+    if (tid == 0) {
+        for (int i = 0; i < kLtSlots; ++i) { mbar_init(&sm->full[i], 2); mbar_init(&sm->empty[i], 1); }
+        mbar_init(&sm->s_full[0], 1);
+        mbar_init(&sm->s_full[1], 1);
+        mbar_init(&sm->p_full, 8);
+        mbar_init(&sm->pv_done, 1);
+        mbar_init(&sm->q_full, 4);
+        mbar_init(&sm->q_free, 1);
+        sm->abort_flag = 0;
+        sm->sums[0] = sm->sums[1] = sm->sums[2] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm->tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __syncthreads();
+    {   // tiles of the launch for each tile size, then the units of every sequence with the size that is taken
+        int t[3] = {0, 0, 0}, L = 0, Nb = 0, rbs = 0;
+        if (tid < a.B) {
+            L = lt_len(a, tid);
+            Nb = lt_nodes(a, tid);
+            rbs = lt_row_blocks(a.H, Nb);
+            if (Nb > 0)
+                for (int i = 0; i < 3; ++i) t[i] = rbs * lt_tiles(L, Nb, 256 >> i);
+        }
+        for (int i = 0; i < 3; ++i) {
+            const int s = __reduce_add_sync(0xffffffffu, t[i]);
+            if (lane == 0) atomicAdd(&sm->sums[i], s);
+        }
+        __syncthreads();
+        const int max_pairs = gridDim.x >> 1;
+        const int pick = sm->sums[0] >= max_pairs ? 0 : sm->sums[1] >= max_pairs ? 1 : 2;
+        int units = Nb > 0 ? t[pick] + rbs : 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, units, o);
+            if (lane >= o) units += x;
+        }
+        if (lane == 31) sm->scan[warp] = units;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) units += sm->scan[w];
+        sm->cum[tid + 1] = units;                       // sequences from B on: the total
+        if (tid == 0) { sm->cum[0] = 0; sm->tile_keys = 256 >> pick; }
+        if (tid == kLtThreads - 1) { sm->total = units; sm->pairs = min(max_pairs, units); }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                 // barriers and tensor memory of both blocks are ready
+    tc_fence_after();
+    const uint32_t tmem = sm->tmem_base;
+    const int tk = sm->tile_keys;
+    LtWalk walk;
+    walk.start(sm, pair);
+    LtItem it;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- loads
+        if (lane == 0) {
+            uint32_t slot = 0, phase = 0, issued = 0;
+            bool ok = true;
+            auto acquire = [&]() -> bool {
+                ok = ok && LT_WAIT(&sm->empty[slot], phase ^ 1, 1);
+                return ok;
+            };
+            auto advance = [&]() {
+                ++issued;
+                if (++slot == kLtSlots) { slot = 0; phase ^= 1; }
+            };
+            auto keys = [&](const LtTile& x, int b) {   // this block's keys, 64 channels a slot
+                const int size = x.kpc > 64 ? 3 : x.kpc > 32 ? 2 : x.kpc > 16 ? 1 : 0;
+                const CUtensorMap* map = &maps.m[(x.tree ? 4 : 0) + size];
+                for (int c = 0; c < kLtChunks; ++c) {
+                    if (!acquire()) return;
+                    const uint32_t bar = leader_addr(smem_u32(&sm->full[slot]));
+                    expect_cluster(bar, (16u << size) * 128u);
+                    pair_load(ring_a + slot * kLtSlotBytes, map, bar, 64 * c, x.start + rank * x.kpc, b);
+                    advance();
+                }
+            };
+            auto values = [&](const LtTile& x, int b) { // 64 keys and 128 of this block's channels a slot
+                for (int k0 = 0; k0 < 2 * x.kpc; k0 += 64) {
+                    const int size = 2 * x.kpc - k0 > 32 ? 2 : 1;
+                    const CUtensorMap* map = &maps.m[(x.tree ? 4 : 0) + size];
+                    for (int j = 0; j < 2; ++j) {
+                        if (!acquire()) return;
+                        const uint32_t bar = leader_addr(smem_u32(&sm->full[slot])), dst = ring_a + slot * kLtSlotBytes;
+                        expect_cluster(bar, (16u << size) * 256u);
+                        pair_load(dst, map, bar, 256 * j + 128 * rank, x.start + k0, b);
+                        pair_load(dst + 8192, map, bar, 256 * j + 128 * rank + 64, x.start + k0, b);
+                        advance();
+                    }
+                }
+            };
+            while (ok && walk.next(sm, a, it)) {
+                keys(lt_tile(it, it.t0, tk), it.b);
+                for (int t = it.t0; ok && t < it.t1; ++t) {
+                    if (t + 1 < it.t1) keys(lt_tile(it, t + 1, tk), it.b);
+                    if (ok) values(lt_tile(it, t, tk), it.b);
+                }
+            }
+            // every load has been taken by its products before the block may leave
+            const uint32_t left = issued < (uint32_t)kLtSlots ? issued : (uint32_t)kLtSlots;
+            for (uint32_t i = 0; i < left; ++i) {
+                if (slot == 0) { slot = kLtSlots; phase ^= 1; }
+                --slot;
+                mbar_wait_slow(&sm->empty[slot], phase, &sm->abort_flag, p.header, 2);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- products
+        if (rank == 0 && lane == 0) {
+            const uint64_t dq = smem_desc(q_a, 16, 1024, 2), dk = smem_desc(ring_a, 16, 1024, 2);
+            const uint64_t dp = smem_desc(p_a, 16, 1024, 2), dv = smem_desc(ring_a, 8192, 1024, 2);
+            const uint32_t idesc_v = instr_desc(256, 0, 1);
+            uint32_t slot = 0, phase = 0, g = 0, item = 0;
+            bool ok = true;
+            auto advance = [&]() {
+                pair_commit(&sm->empty[slot]);
+                if (++slot == kLtSlots) { slot = 0; phase ^= 1; }
+            };
+            auto scores = [&](const LtTile& x, uint32_t n, bool last) {
+                const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (n & 1) * 128;
+                for (int c = 0; c < kLtChunks; ++c) {
+                    ok = ok && LT_WAIT(&sm->full[slot], phase, 3);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint64_t qa = dq + c * 512, kb = dk + slot * 1024;
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) pair_mma(d, qa + 2 * s, kb + 2 * s, idesc, c > 0 || s > 0);
+                    advance();
+                }
+                pair_commit(&sm->s_full[n & 1]);
+                if (last) pair_commit(&sm->q_free);
+            };
+            auto product = [&](const LtTile& x, bool first) {
+                for (int k0 = 0; k0 < 2 * x.kpc; k0 += 64) {
+                    const bool whole = 2 * x.kpc - k0 > 32;
+                    for (int j = 0; j < 2; ++j) {
+                        ok = ok && LT_WAIT(&sm->full[slot], phase, 4);
+                        if (!ok) return;
+                        tc_fence_after();
+                        const uint32_t d = tmem + kLtColO + j * 128;
+                        const uint64_t pa = dp + (k0 >> 6) * 512, vb = dv + slot * 1024;
+                        pair_mma(d, pa, vb, idesc_v, !(first && k0 == 0));
+                        pair_mma(d, pa + 2, vb + 128, idesc_v, 1);
+                        if (whole) {
+                            pair_mma(d, pa + 4, vb + 256, idesc_v, 1);
+                            pair_mma(d, pa + 6, vb + 384, idesc_v, 1);
+                        }
+                        advance();
+                    }
+                }
+                pair_commit(&sm->pv_done);
+            };
+            while (ok && walk.next(sm, a, it)) {
+                ok = LT_WAIT(&sm->q_full, item & 1, 5);
+                ++item;
+                if (!ok) break;
+                tc_fence_after();
+                scores(lt_tile(it, it.t0, tk), g, it.t0 + 1 == it.t1);
+                for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
+                    if (t + 1 < it.t1) scores(lt_tile(it, t + 1, tk), g + 1, t + 2 == it.t1);
+                    ok = ok && LT_WAIT(&sm->p_full, g & 1, 6);
+                    if (!ok) break;
+                    tc_fence_after();
+                    product(lt_tile(it, t, tk), t == it.t0);
+                }
+            }
+        }
+    } else if (warp < 4) {
+        // ---------------------------------------------------------------- queries
+        // (a wait that ran out skips the later ones; the loop itself goes on, so that a warp stays together)
+        uint32_t item = 0;
+        bool ok = true;
+        const uint32_t q_bar = leader_addr(smem_u32(&sm->q_full));
+        for (; walk.next(sm, a, it); ++item) {
+            if (item > 0) ok = ok && LT_WAIT(&sm->q_free, (item - 1) & 1, 7);   // the last item's scores are done
+            __syncwarp();
+            const int rows = a.H * it.Nb, r0 = it.rb * 128 + rank * 64 + (warp - 2) * 32;
+            int h = r0 / it.Nb, n = r0 - h * it.Nb;
+            for (int i = 0; i < 32; ++i) {
+                const bool in = r0 + i < rows;
+                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (in ? (((long long)it.b * a.H + h) * a.N + n) * kLtWidth : 0);
+                const int row = (warp - 2) * 32 + i;
+                for (int v = lane; v < kLtWidth / 8; v += 32) {
+                    const uint32_t dst = q_a + (v >> 3) * 8192 + row * 128 + (((v & 7) ^ (row & 7)) << 4);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src + v * 8), "r"(in ? 16 : 0) : "memory");
+                }
+                if (++n == it.Nb) { n = 0; ++h; }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(q_bar);
+        }
+    } else {
+        // ---------------------------------------------------------------- softmax and output
+        const int w = warp - 4, half = w >> 1, row = (w & 1) * 32 + lane;      // lane 32 w + lane: row, half of the keys / channels
+        const uint32_t lane_addr = tmem + ((uint32_t)(w * 32) << 16);
+        const uint32_t p_bar = leader_addr(smem_u32(&sm->p_full));
+        uint32_t g = 0;
+        bool ok = true;
+        while (walk.next(sm, a, it)) {               // goes on after a wait that ran out: the four warps share a barrier
+            const int r = it.rb * 128 + rank * 64 + row;
+            const bool in = r < a.H * it.Nb;
+            const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
+            float ref = -INFINITY, l = 0.0f;
+            for (int t = it.t0; t < it.t1; ++t, ++g) {
+                const LtTile x = lt_tile(it, t, tk);
+                ok = ok && LT_WAIT(&sm->s_full[g & 1], (g >> 1) & 1, 8);
+                __syncwarp();
+                tc_fence_after();
+                float s[128];
+                const uint32_t sa = lane_addr + kLtColS + (g & 1) * 128;
+                float mx = -INFINITY;
+                if (x.kpc == 128 && !x.tree && x.start == x.lo) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tc_ld32(sa + 32 * c, s + 32 * c);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) {
+                        s[i] *= p.scale_log2;
+                        mx = fmaxf(mx, s[i]);
+                    }
+                } else {
+                    const int key0 = x.start + half * x.kpc;                   // key of column 0
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (32 * c < x.kpc) tc_ld32(sa + 32 * c, s + 32 * c);
+                        tc_wait_ld();
+                        const int from = max(x.lo - key0 - 32 * c, 0), to = min(x.kpc - 32 * c, 32);
+                        uint32_t see = to <= from ? 0u : (0xffffffffu >> (32 - (to - from))) << from;
+                        if (see && x.tree) see &= anc_bits(a.anc + (size_t)n * a.words, a.words, key0 + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            s[32 * c + i] = (see >> i) & 1 ? s[32 * c + i] * p.scale_log2 : -INFINITY;
+                            mx = fmaxf(mx, s[32 * c + i]);
+                        }
+                    }
+                }
+                sm->red[g & 1][half][row] = mx;
+                softmax_sync();
+                mx = fmaxf(mx, sm->red[g & 1][half ^ 1][row]);
+                // the reference moves only when a score exceeds it by more than 2^8 (weights stay exact: a common factor)
+                float factor = 1.0f;
+                if (mx > ref + kLazyTau) {
+                    factor = ex2_approx(ref - mx);
+                    ref = mx;
+                }
+                const float sub = ref == -INFINITY ? 0.0f : ref;
+                const bool move = t > it.t0 && __any_sync(0xffffffffu, factor != 1.0f);
+                float sum0 = 0.0f, sum1 = 0.0f;
+                uint32_t packed[64];
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    const float e0 = ex2_approx(s[2 * i] - sub), e1 = ex2_approx(s[2 * i + 1] - sub);
+                    sum0 += e0;
+                    sum1 += e1;
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed[i]) : "f"(e1), "f"(e0));
+                }
+                l = l * factor + (sum0 + sum1);
+                if (g > 0) ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 9);   // P is free, O is current
+                __syncwarp();
+                tc_fence_after();
+                if (move) {
+                    for (int c = 0; c < 8; ++c) {
+                        float o[32];
+                        tc_ld32(lane_addr + kLtColO + 32 * c, o);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] *= factor;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) tc_st8(lane_addr + kLtColO + 32 * c + i, o + i);
+                    }
+                    tc_wait_st();
+                }
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    if (8 * u >= x.kpc) continue;
+                    const int k = half * x.kpc + 8 * u;
+                    const uint32_t dst = p_a + (k >> 6) * 8192 + row * 128 + ((((k >> 3) & 7) ^ (row & 7)) << 4);
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(packed[4 * u]), "r"(packed[4 * u + 1]),
+                                 "r"(packed[4 * u + 2]), "r"(packed[4 * u + 3]) : "memory");
+                }
+                fence_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_cluster(p_bar);
+            }
+            // ---- the item's rows, or this piece of them
+            sm->lsum[half][row] = l;
+            softmax_sync();
+            l = sm->lsum[0][row] + sm->lsum[1][row];
+            ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 10);
+            __syncwarp();
+            tc_fence_after();
+            const bool whole = it.t0 == 0 && it.t1 == it.nt;
+            const int slot = 2 * pair + (it.t0 == 0 ? 1 : 0);
+            if (!whole) {
+                if (half == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
+                if (it.t0 == 0 && rank == 0 && w == 0 && lane == 0) {
+                    const int last = lt_pair_of(it.unit0 + it.nt, sm->total, sm->pairs);
+                    p.pieces[pair] = LtPieces{last - pair + 1, it.b, it.rb, 0};
+                }
+            }
+            const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + half * 128;
+            float* part = p.part_o + ((long long)slot * 128 + rank * 64 + row) * kLtRank + half * 128;
+#pragma unroll 1
+            for (int c = 0; c < 8; ++c) {                                       // 32 channels at 256 (c / 4) + 32 (c % 4)
+                float o[32];
+                tc_ld32(lane_addr + kLtColO + 32 * c, o);
+                tc_wait_ld();
+                const int at = (c >> 2) * 256 + (c & 3) * 32;
+                if (in && whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint4 v;
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o[i + 1] * inv), "f"(o[i] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[i + 3] * inv), "f"(o[i + 2] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.z) : "f"(o[i + 5] * inv), "f"(o[i + 4] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.w) : "f"(o[i + 7] * inv), "f"(o[i + 6] * inv));
+                        *reinterpret_cast<uint4*>(out + at + i) = v;
+                    }
+                } else if (in) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + at + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+        }
+    }
+    // a pair that starts no cut item says so
+    if (rank == 0 && tid == 0) {
+        bool cut = false;
+        LtWalk again;
+        again.start(sm, pair);
+        while (again.next(sm, a, it)) cut = cut || (it.t0 == 0 && it.t1 < it.nt);
+        if (!cut) p.pieces[pair] = LtPieces{0, 0, 0, 0};
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                 // the other block's products, loads and arrivals are done too
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// Joins the pieces of the items that were cut.  grid: (pairs, 32), four rows a block, 128 threads a row
+__global__ void __launch_bounds__(512) latent_join_kernel(const __grid_constant__ LtParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const LatentArgs& a = p.a;
+    const LtPieces x = p.pieces[blockIdx.x];
+    if (x.count < 2) return;
+    const int Nb = lt_nodes(a, x.b), row = blockIdx.y * 4 + (threadIdx.x >> 7), r = x.rb * 128 + row, d = (threadIdx.x & 127) * 4;
+    if (r >= a.H * Nb) return;
+    const int pair = blockIdx.x;
+    // piece 0 lies in the pair's second slot, piece k in the first slot of pair + k
+    float m = -INFINITY;
+    for (int k = 0; k < x.count; ++k) m = fmaxf(m, p.part_ml[(2 * (pair + k) + (k == 0)) * 128 + row].x);
+    const float sub = m == -INFINITY ? 0.0f : m;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float l = 0.0f;
+#pragma unroll 8
+    for (int k = 0; k < x.count; ++k) {
+        const int slot = 2 * (pair + k) + (k == 0);
+        const float2 ml = p.part_ml[slot * 128 + row];
+        const float f = ex2_approx(ml.x - sub);
+        const float4 v = *reinterpret_cast<const float4*>(p.part_o + ((long long)slot * 128 + row) * kLtRank + d);
+        l += f * ml.y;
+        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    const int h = r / Nb, n = r - h * Nb;
+    uint2 v;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o.y * inv), "f"(o.x * inv));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o.w * inv), "f"(o.z * inv));
+    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (((long long)x.b * a.H + h) * a.N + n) * kLtRank + d) = v;
+}
+
+// ------------------------------------------------------------------ host side
+typedef CUresult (*LtEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static LtEncodeFn lt_encode_fn() {
+    static LtEncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult res;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &res) == cudaSuccess &&
+            res == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<LtEncodeFn>(sym);
+    });
+    return fn;
+}
+// [B][rows][576] bf16 in boxes of box_rows x 64 channels, 128-byte swizzle, zeros outside
+static bool lt_map(CUtensorMap* map, const void* base, int rows, int B, int box_rows) {
+    const cuuint64_t dims[3] = {kLtWidth, (cuuint64_t)rows, (cuuint64_t)B};
+    const cuuint64_t strides[2] = {kLtWidth * 2, (cuuint64_t)rows * kLtWidth * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    return lt_encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Shapes of this kernel.  The units of a launch are 32-bit: a sequence has at most (L_max / 64 + 5) units for each of its
+// H * N / 128 row blocks.
+bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
+    if (dtype != MCSD_BF16 || rank != kLtRank || rot != kLtRot) return false;
+    const long long per_seq = ((long long)H * N + 127) / 128 * ((long long)L_max / 64 + 6);
+    return per_seq * std::min(B, kLtMaxBatch) < (1LL << 30);
+}
+size_t latent_tc_workspace_bytes() {
+    return (size_t)2 * kLtMaxPairs * 128 * (kLtRank * sizeof(float) + sizeof(float2)) + align_up(kLtMaxPairs * sizeof(LtPieces), 256);
+}
+
+int tree_attention_latent_tc(const LatentArgs& whole, WorkspaceHeader* header, void* scratch, cudaStream_t stream) {
+    if (lt_encode_fn() == nullptr) { set_last_cuda_error(cudaErrorInvalidValue); return MCSD_ERR_CUDA; }
+    int dev = 0, sms = 0;
+    MCSD_CUDA_CHECK(cudaGetDevice(&dev));
+    MCSD_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    {   // the opt-in to large dynamic shared memory is per device
+        static std::mutex mu;
+        static bool done[64] = {};
+        std::lock_guard<std::mutex> lock(mu);
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            MCSD_CUDA_CHECK(cudaFuncSetAttribute(tree_attention_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLtSmem));
+            if (dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    const int pairs = std::max(1, std::min(sms / 2, kLtMaxPairs));
+    LtParams p{};
+    p.header = header;
+    p.scale_log2 = whole.scale * 1.4426950408889634f;
+    p.part_o = static_cast<float*>(scratch);
+    p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)2 * kLtMaxPairs * 128 * kLtRank);
+    p.pieces = reinterpret_cast<LtPieces*>(p.part_ml + (size_t)2 * kLtMaxPairs * 128);
+    for (int b0 = 0; b0 < whole.B; b0 += kLtMaxBatch) {                         // tables of a launch hold 256 sequences
+        LatentArgs& a = p.a;
+        a = whole;
+        a.B = std::min(kLtMaxBatch, whole.B - b0);
+        const size_t row = (size_t)kLtWidth * 2, o_row = (size_t)kLtRank * 2;
+        a.q = static_cast<const char*>(whole.q) + (size_t)b0 * whole.H * whole.N * row;
+        a.cache = whole.cache ? static_cast<const char*>(whole.cache) + (size_t)b0 * whole.L_max * row : nullptr;
+        a.tree = static_cast<const char*>(whole.tree) + (size_t)b0 * whole.N * row;
+        a.out = static_cast<char*>(whole.out) + (size_t)b0 * whole.H * whole.N * o_row;
+        a.seq_lens = whole.seq_lens + b0;
+        a.n_active = whole.n_active ? whole.n_active + b0 : nullptr;
+        LtMaps maps;
+        for (int i = 0; i < 4; ++i) {
+            const bool have = whole.L_max > 0;
+            if (!lt_map(&maps.m[i], have ? a.cache : a.tree, have ? whole.L_max : whole.N, a.B, 16 << i) ||
+                !lt_map(&maps.m[4 + i], a.tree, whole.N, a.B, 16 << i)) {
+                set_last_cuda_error(cudaErrorInvalidValue);
+                return MCSD_ERR_CUDA;
+            }
+        }
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)pairs * 2);
+        cfg.blockDim = dim3(kLtThreads);
+        cfg.dynamicSmemBytes = kLtSmem;
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, tree_attention_latent_kernel, maps, p));
+        cfg.gridDim = dim3((unsigned)pairs, 32);
+        cfg.blockDim = dim3(512);
+        cfg.dynamicSmemBytes = 0;
+        MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_join_kernel, p));
+        count_launches(2);
+    }
+    return MCSD_OK;
+}
+
+}  // namespace mcsd
