@@ -84,9 +84,6 @@ __device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {      // the sam
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void expect_cluster(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
     asm volatile(
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -203,7 +200,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
     const int pair = blockIdx.x >> 1, rank = blockIdx.x & 1;
 
     if (tid == 0) {
-        for (int i = 0; i < kLtSlots; ++i) { mbar_init(&sm->full[i], 2); mbar_init(&sm->empty[i], 1); }
+        for (int i = 0; i < kLtSlots; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 1); }
         mbar_init(&sm->s_full[0], 1);
         mbar_init(&sm->s_full[1], 1);
         mbar_init(&sm->p_full, 8);
@@ -278,7 +275,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 for (int c = 0; c < kLtChunks; ++c) {
                     if (!acquire()) return;
                     const uint32_t bar = leader_addr(smem_u32(&sm->full[slot]));
-                    expect_cluster(bar, (16u << size) * 128u);
+                    if (rank == 0) mbar_expect_tx(&sm->full[slot], (16u << size) * 256u);      // both blocks' halves
                     pair_load(ring_a + slot * kLtSlotBytes, map, bar, 64 * c, x.start + rank * x.kpc, b);
                     advance();
                 }
@@ -290,7 +287,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     for (int j = 0; j < 2; ++j) {
                         if (!acquire()) return;
                         const uint32_t bar = leader_addr(smem_u32(&sm->full[slot])), dst = ring_a + slot * kLtSlotBytes;
-                        expect_cluster(bar, (16u << size) * 256u);
+                        if (rank == 0) mbar_expect_tx(&sm->full[slot], (16u << size) * 512u);
                         pair_load(dst, map, bar, 256 * j + 128 * rank, x.start + k0, b);
                         pair_load(dst + 8192, map, bar, 256 * j + 128 * rank + 64, x.start + k0, b);
                         advance();
