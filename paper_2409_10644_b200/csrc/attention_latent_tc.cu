@@ -10,8 +10,11 @@
 // columns, twice, and tensor memory is full.
 //
 // A block loads its half of what a product needs: for S its half of the keys, 64 channels at a time, for O its half of the
-// channels, 64 keys at a time; both are 16 KB, and pass through one ring of seven slots in the order in which the products
-// take them: S of tile t + 1, then O of tile t, so that the softmax of a tile overlaps products of its neighbours.
+// channels, 64 keys at a time; both are 16 KB, and pass through two rings of four and three slots.  S and O are issued by two
+// warps, each from its own ring: four products, the wait for their slot and the commit that releases it take a warp 370 to
+// 470 cycles and the tensor cores 256 (measured), so that one warp issuing both would pace them; and S of a tile or item
+// runs into O of the last one by itself.  A warp issues convergently through one elected lane, its operands then lie in
+// uniform registers (128 cycles a product from a single thread's branch).
 //
 // A tile always ends at the last key of its range and starts a multiple of 32 keys before: a ragged tile overlaps the tile
 // before it (or starts before the first row, where TMA gives zeros) and masks what it has no claim to, so that no row behind a
@@ -21,8 +24,8 @@
 // inside an item, the pieces write unnormalised rows, and a second kernel joins them.  Tiles are 256 keys, or 128 or 64
 // where there would be fewer tiles than pairs.
 //
-// Warps of a block: 0 loads, 1 issues products (first block of the pair), 2 and 3 fetch queries, 4 to 7 do the softmax and
-// the output.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
+// Warps of a block: 0 loads for S, 1 issues it, 2 loads for O, 3 issues it (1 and 3 in the first block of the pair), 4 to 11
+// do the softmax and the output, 12 and 13 fetch queries.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
 // blocks exit.
 #include <cuda.h>
 
@@ -30,14 +33,15 @@
 #include <mutex>
 
 #include "attention_tc_common.cuh"
+#include "f32x2.cuh"
 #include "latent.cuh"
 
 namespace mcsd {
 
 constexpr int kLtRank = 512, kLtRot = 64, kLtWidth = kLtRank + kLtRot;
 constexpr int kLtChunks = kLtWidth / 64;             // 64-channel chunks of a row
-constexpr int kLtThreads = 256;
-constexpr int kLtSlots = 7, kLtSlotBytes = 16384;
+constexpr int kLtThreads = 448;
+constexpr int kLtKeySlots = 4, kLtValueSlots = 3, kLtSlots = kLtKeySlots + kLtValueSlots, kLtSlotBytes = 16384;
 constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;
 constexpr int kLtMaxBatch = 256;
 constexpr int kLtMaxPairs = kTcMaxBlocks / 2;
@@ -60,17 +64,17 @@ struct LtMaps {
 };
 
 struct LtSmall {
-    unsigned long long full[kLtSlots], empty[kLtSlots];
-    unsigned long long s_full[2], p_full, pv_done, q_full, q_free;
+    unsigned long long full[kLtSlots], empty[kLtSlots];          // slots of S, then of O
+    unsigned long long s_full[2], p_full[2], pv_done, q_full, q_free;
     uint32_t tmem_base;
     int abort_flag;
     int tile_keys, pairs;                            // keys of a tile, pairs with work
     int total;                                       // units of the launch
     int sums[3];                                     // tiles of the launch with 256, 128, 64 keys a tile
-    int scan[8];
+    int scan[kLtThreads / 32];
     int cum[kLtMaxBatch + 1];                        // units before a sequence
-    float red[2][2][64];                             // row maxima of a tile's halves, by tile parity
-    float lsum[2][64];
+    float red[2][4][64];                             // row maxima of a tile's quarters, by tile parity
+    float lsum[4][64];
 };
 constexpr int kLtSmem = 1024 + kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes + (int)sizeof(LtSmall);
 static_assert(kLtSmem <= kSmemLimit, "a block's shared memory");
@@ -89,22 +93,31 @@ __device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, 
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+// Both by a warp that is together, through the lane for which `one` is not 0 (the same lane for both).
+__device__ __forceinline__ uint32_t elect_lane() {
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e;
 }
-__device__ __forceinline__ void pair_commit(void* bar) {              // the barrier of both blocks
+__device__ __forceinline__ void pair_mma(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, e;\n\t"
+        "setp.ne.b32 e, %5, 0;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(one) : "memory");
+}
+__device__ __forceinline__ void pair_commit(uint32_t one, void* bar) {              // the barrier of both blocks
     const uint16_t both = 3;
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(smem_u32(bar)), "h"(both) : "memory");
+    asm volatile("{\n\t.reg .pred e;\n\t"
+                 "setp.ne.b32 e, %2, 0;\n\t"
+                 "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}"
+                 ::"r"(smem_u32(bar)), "h"(both), "r"(one) : "memory");
 }
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 // 32 consecutive fp32 columns of this thread's lane; the caller waits with tc_wait_ld()
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
     uint32_t* r = reinterpret_cast<uint32_t*>(v);
@@ -131,6 +144,13 @@ struct LtItem {
     int b, rb, L, Nb, nP, nt;      // sequence, row block; prefix length, nodes; prefix tiles, tiles
     int t0, t1;                    // this pair's tiles
     int unit0;                     // the item's first unit
+    __device__ __forceinline__ void uniform() {      // alike in all lanes: say so
+        L = __shfl_sync(0xffffffffu, L, 0);
+        Nb = __shfl_sync(0xffffffffu, Nb, 0);
+        nP = __shfl_sync(0xffffffffu, nP, 0);
+        t0 = __shfl_sync(0xffffffffu, t0, 0);
+        t1 = __shfl_sync(0xffffffffu, t1, 0);
+    }
 };
 // Walks the items of a pair's range; every role of both blocks walks alike.
 struct LtWalk {
@@ -203,7 +223,8 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         for (int i = 0; i < kLtSlots; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 1); }
         mbar_init(&sm->s_full[0], 1);
         mbar_init(&sm->s_full[1], 1);
-        mbar_init(&sm->p_full, 8);
+        mbar_init(&sm->p_full[0], 16);
+        mbar_init(&sm->p_full[1], 16);
         mbar_init(&sm->pv_done, 1);
         mbar_init(&sm->q_full, 4);
         mbar_init(&sm->q_free, 1);
@@ -242,149 +263,146 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         if (lane == 31) sm->scan[warp] = units;
         __syncthreads();
         for (int w = 0; w < warp; ++w) units += sm->scan[w];
-        sm->cum[tid + 1] = units;                       // sequences from B on: the total
+        if (tid < kLtMaxBatch) sm->cum[tid + 1] = units;   // sequences from B on: the total
         if (tid == 0) { sm->cum[0] = 0; sm->tile_keys = 256 >> pick; }
-        if (tid == kLtThreads - 1) { sm->total = units; sm->pairs = min(max_pairs, units); }
+        if (tid == kLtMaxBatch - 1) { sm->total = units; sm->pairs = min(max_pairs, units); }
     }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();                                 // barriers and tensor memory of both blocks are ready
     tc_fence_after();
-    const uint32_t tmem = sm->tmem_base;
-    const int tk = sm->tile_keys;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sm->tmem_base, 0);
+    const int tk = __shfl_sync(0xffffffffu, sm->tile_keys, 0);
     LtWalk walk;
     walk.start(sm, pair);
     LtItem it;
 
-    if (warp == 0) {
-        // ---------------------------------------------------------------- loads
+    if (warp == 0 || warp == 2) {
+        // ---------------------------------------------------------------- loads for S, for O
         if (lane == 0) {
+            const bool for_s = warp == 0;
+            const uint32_t first = for_s ? 0 : kLtKeySlots, count = for_s ? kLtKeySlots : kLtValueSlots;
             uint32_t slot = 0, phase = 0, issued = 0;
             bool ok = true;
-            auto acquire = [&]() -> bool {
-                ok = ok && LT_WAIT(&sm->empty[slot], phase ^ 1, 1);
+            auto acquire = [&](uint32_t bytes) -> bool {
+                ok = ok && LT_WAIT(&sm->empty[first + slot], phase ^ 1, for_s ? 1 : 2);
+                if (ok && rank == 0) mbar_expect_tx(&sm->full[first + slot], 2 * bytes);   // both blocks' halves
                 return ok;
             };
             auto advance = [&]() {
                 ++issued;
-                if (++slot == kLtSlots) { slot = 0; phase ^= 1; }
-            };
-            auto keys = [&](const LtTile& x, int b) {   // this block's keys, 64 channels a slot
-                const int size = x.kpc > 64 ? 3 : x.kpc > 32 ? 2 : x.kpc > 16 ? 1 : 0;
-                const CUtensorMap* map = &maps.m[(x.tree ? 4 : 0) + size];
-                for (int c = 0; c < kLtChunks; ++c) {
-                    if (!acquire()) return;
-                    const uint32_t bar = leader_addr(smem_u32(&sm->full[slot]));
-                    if (rank == 0) mbar_expect_tx(&sm->full[slot], (16u << size) * 256u);      // both blocks' halves
-                    pair_load(ring_a + slot * kLtSlotBytes, map, bar, 64 * c, x.start + rank * x.kpc, b);
-                    advance();
-                }
-            };
-            auto values = [&](const LtTile& x, int b) { // 64 keys and 128 of this block's channels a slot
-                for (int k0 = 0; k0 < 2 * x.kpc; k0 += 64) {
-                    const int size = 2 * x.kpc - k0 > 32 ? 2 : 1;
-                    const CUtensorMap* map = &maps.m[(x.tree ? 4 : 0) + size];
-                    for (int j = 0; j < 2; ++j) {
-                        if (!acquire()) return;
-                        const uint32_t bar = leader_addr(smem_u32(&sm->full[slot])), dst = ring_a + slot * kLtSlotBytes;
-                        if (rank == 0) mbar_expect_tx(&sm->full[slot], (16u << size) * 512u);
-                        pair_load(dst, map, bar, 256 * j + 128 * rank, x.start + k0, b);
-                        pair_load(dst + 8192, map, bar, 256 * j + 128 * rank + 64, x.start + k0, b);
-                        advance();
-                    }
-                }
+                if (++slot == count) { slot = 0; phase ^= 1; }
             };
             while (ok && walk.next(sm, a, it)) {
-                keys(lt_tile(it, it.t0, tk), it.b);
                 for (int t = it.t0; ok && t < it.t1; ++t) {
-                    if (t + 1 < it.t1) keys(lt_tile(it, t + 1, tk), it.b);
-                    if (ok) values(lt_tile(it, t, tk), it.b);
+                    const LtTile x = lt_tile(it, t, tk);
+                    const CUtensorMap* map = &maps.m[x.tree ? 4 : 0];
+                    if (for_s) {                             // this block's keys, 64 channels a slot
+                        const int size = x.kpc > 64 ? 3 : x.kpc > 32 ? 2 : x.kpc > 16 ? 1 : 0;
+                        for (int c = 0; c < kLtChunks && acquire((16u << size) * 128u); ++c) {
+                            pair_load(ring_a + slot * kLtSlotBytes, map + size, leader_addr(smem_u32(&sm->full[slot])), 64 * c,
+                                      x.start + rank * x.kpc, it.b);
+                            advance();
+                        }
+                    } else {                                 // 64 keys and 128 of this block's channels a slot
+                        for (int k = 0; k < (2 * x.kpc + 63) / 64 * 2; ++k) {
+                            const int k0 = (k >> 1) * 64, j = k & 1, size = 2 * x.kpc - k0 > 32 ? 2 : 1;
+                            if (!acquire((16u << size) * 256u)) break;
+                            const uint32_t dst = ring_a + (kLtKeySlots + slot) * kLtSlotBytes, bar = leader_addr(smem_u32(&sm->full[kLtKeySlots + slot]));
+                            pair_load(dst, map + size, bar, 256 * j + 128 * rank, x.start + k0, it.b);
+                            pair_load(dst + 8192, map + size, bar, 256 * j + 128 * rank + 64, x.start + k0, it.b);
+                            advance();
+                        }
+                    }
                 }
             }
             // every load has been taken by its products before the block may leave
-            const uint32_t left = issued < (uint32_t)kLtSlots ? issued : (uint32_t)kLtSlots;
-            for (uint32_t i = 0; i < left; ++i) {
-                if (slot == 0) { slot = kLtSlots; phase ^= 1; }
+            for (uint32_t left = issued < count ? issued : count; left > 0; --left) {
+                if (slot == 0) { slot = count; phase ^= 1; }
                 --slot;
-                mbar_wait_slow(&sm->empty[slot], phase, &sm->abort_flag, p.header, 2);
+                mbar_wait_slow(&sm->empty[first + slot], phase, &sm->abort_flag, p.header, 3);
             }
         }
-    } else if (warp == 1) {
-        // ---------------------------------------------------------------- products
-        if (rank == 0 && lane == 0) {
-            const uint64_t dq = smem_desc(q_a, 16, 1024, 2), dk = smem_desc(ring_a, 16, 1024, 2);
-            const uint64_t dp = smem_desc(p_a, 16, 1024, 2), dv = smem_desc(ring_a, 8192, 1024, 2);
-            const uint32_t idesc_v = instr_desc(256, 0, 1);
+    } else if (warp == 1 || warp == 3) {
+        // ---------------------------------------------------------------- products S, products O
+        if (rank == 0) {
+            const uint32_t one = elect_lane();
             uint32_t slot = 0, phase = 0, g = 0, item = 0;
-            bool ok = true;
-            auto advance = [&]() {
-                pair_commit(&sm->empty[slot]);
-                if (++slot == kLtSlots) { slot = 0; phase ^= 1; }
-            };
-            auto scores = [&](const LtTile& x, uint32_t n, bool last) {
-                const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (n & 1) * 128;
-                for (int c = 0; c < kLtChunks; ++c) {
-                    ok = ok && LT_WAIT(&sm->full[slot], phase, 3);
-                    if (!ok) return;
-                    tc_fence_after();
-                    const uint64_t qa = dq + c * 512, kb = dk + slot * 1024;
+            bool ok = true;                                  // alike in all lanes
+            if (warp == 1) {
+                const uint64_t dq = smem_desc(q_a, 16, 1024, 2), dk = smem_desc(ring_a, 16, 1024, 2);
+                while (ok && walk.next(sm, a, it)) {
+                    it.uniform();
+                    ok = __all_sync(0xffffffffu, LT_WAIT(&sm->q_full, item & 1, 4));
+                    ++item;
+                    for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
+                        const LtTile x = lt_tile(it, t, tk);
+                        const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (g & 1) * 128;
+                        // the softmax has read what this S replaces
+                        if (g > 1) ok = __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[g & 1], ((g >> 1) - 1) & 1, 5));
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) pair_mma(d, qa + 2 * s, kb + 2 * s, idesc, c > 0 || s > 0);
-                    advance();
-                }
-                pair_commit(&sm->s_full[n & 1]);
-                if (last) pair_commit(&sm->q_free);
-            };
-            auto product = [&](const LtTile& x, bool first) {
-                for (int k0 = 0; k0 < 2 * x.kpc; k0 += 64) {
-                    const bool whole = 2 * x.kpc - k0 > 32;
-                    for (int j = 0; j < 2; ++j) {
-                        ok = ok && LT_WAIT(&sm->full[slot], phase, 4);
-                        if (!ok) return;
-                        tc_fence_after();
-                        const uint32_t d = tmem + kLtColO + j * 128;
-                        const uint64_t pa = dp + (k0 >> 6) * 512, vb = dv + slot * 1024;
-                        pair_mma(d, pa, vb, idesc_v, !(first && k0 == 0));
-                        pair_mma(d, pa + 2, vb + 128, idesc_v, 1);
-                        if (whole) {
-                            pair_mma(d, pa + 4, vb + 256, idesc_v, 1);
-                            pair_mma(d, pa + 6, vb + 384, idesc_v, 1);
+                        for (int c = 0; c < kLtChunks; ++c) {
+                            ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->full[slot], phase, 6));
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint64_t kb = dk + slot * 1024;
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) pair_mma(one, d, dq + c * 512 + 2 * s, kb + 2 * s, idesc, c > 0 || s > 0);
+                            pair_commit(one, &sm->empty[slot]);
+                            if (++slot == kLtKeySlots) { slot = 0; phase ^= 1; }
                         }
-                        advance();
+                        pair_commit(one, &sm->s_full[g & 1]);
+                    }
+                    pair_commit(one, &sm->q_free);
+                }
+            } else {
+                const uint64_t dp = smem_desc(p_a, 16, 1024, 2), dv = smem_desc(ring_a + kLtKeySlots * kLtSlotBytes, 8192, 1024, 2);
+                const uint32_t idesc = instr_desc(256, 0, 1);
+                while (ok && walk.next(sm, a, it)) {
+                    it.uniform();
+                    for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
+                        const LtTile x = lt_tile(it, t, tk);
+                        ok = __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[g & 1], (g >> 1) & 1, 7));
+                        for (int k0 = 0; ok && k0 < 2 * x.kpc; k0 += 64) {
+                            const uint64_t pa = dp + (k0 >> 6) * 512;
+                            const uint32_t more = t > it.t0 || k0 > 0;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->full[kLtKeySlots + slot], phase, 8));
+                                if (!ok) break;
+                                tc_fence_after();
+                                const uint32_t d = tmem + kLtColO + j * 128;
+                                const uint64_t vb = dv + slot * 1024;
+                                pair_mma(one, d, pa, vb, idesc, more);
+                                pair_mma(one, d, pa + 2, vb + 128, idesc, 1);
+                                if (2 * x.kpc - k0 > 32) {
+                                    pair_mma(one, d, pa + 4, vb + 256, idesc, 1);
+                                    pair_mma(one, d, pa + 6, vb + 384, idesc, 1);
+                                }
+                                pair_commit(one, &sm->empty[kLtKeySlots + slot]);
+                                if (++slot == kLtValueSlots) { slot = 0; phase ^= 1; }
+                            }
+                        }
+                        pair_commit(one, &sm->pv_done);
                     }
                 }
-                pair_commit(&sm->pv_done);
-            };
-            while (ok && walk.next(sm, a, it)) {
-                ok = LT_WAIT(&sm->q_full, item & 1, 5);
-                ++item;
-                if (!ok) break;
-                tc_fence_after();
-                scores(lt_tile(it, it.t0, tk), g, it.t0 + 1 == it.t1);
-                for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
-                    if (t + 1 < it.t1) scores(lt_tile(it, t + 1, tk), g + 1, t + 2 == it.t1);
-                    ok = ok && LT_WAIT(&sm->p_full, g & 1, 6);
-                    if (!ok) break;
-                    tc_fence_after();
-                    product(lt_tile(it, t, tk), t == it.t0);
-                }
             }
         }
-    } else if (warp < 4) {
+    } else if (warp >= 12) {
         // ---------------------------------------------------------------- queries
         // (a wait that ran out skips the later ones; the loop itself goes on, so that a warp stays together)
         uint32_t item = 0;
         bool ok = true;
         const uint32_t q_bar = leader_addr(smem_u32(&sm->q_full));
         for (; walk.next(sm, a, it); ++item) {
-            if (item > 0) ok = ok && LT_WAIT(&sm->q_free, (item - 1) & 1, 7);   // the last item's scores are done
+            if (item > 0) ok = ok && LT_WAIT(&sm->q_free, (item - 1) & 1, 9);   // the last item's scores are done
             __syncwarp();
-            const int rows = a.H * it.Nb, r0 = it.rb * 128 + rank * 64 + (warp - 2) * 32;
+            const int rows = a.H * it.Nb, r0 = it.rb * 128 + rank * 64 + (warp - 12) * 32;
             int h = r0 / it.Nb, n = r0 - h * it.Nb;
             for (int i = 0; i < 32; ++i) {
                 const bool in = r0 + i < rows;
                 const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (in ? (((long long)it.b * a.H + h) * a.N + n) * kLtWidth : 0);
-                const int row = (warp - 2) * 32 + i;
+                const int row = (warp - 12) * 32 + i;
                 for (int v = lane; v < kLtWidth / 8; v += 32) {
                     const uint32_t dst = q_a + (v >> 3) * 8192 + row * 128 + (((v & 7) ^ (row & 7)) << 4);
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src + v * 8), "r"(in ? 16 : 0) : "memory");
@@ -398,52 +416,60 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         }
     } else {
         // ---------------------------------------------------------------- softmax and output
-        const int w = warp - 4, half = w >> 1, row = (w & 1) * 32 + lane;      // lane 32 w + lane: row, half of the keys / channels
-        const uint32_t lane_addr = tmem + ((uint32_t)(w * 32) << 16);
-        const uint32_t p_bar = leader_addr(smem_u32(&sm->p_full));
+        // lane 32 (w % 4) + lane of tensor memory: a row, and half of the keys (of the channels); the two groups of four
+        // warps share its columns
+        const int w = warp - 4, group = w >> 2, half = (w >> 1) & 1, row = (w & 1) * 32 + lane;
+        const uint32_t lane_addr = tmem + ((uint32_t)((w & 3) * 32) << 16);
+        const uint32_t p_bar = leader_addr(smem_u32(&sm->p_full[0]));
         uint32_t g = 0;
         bool ok = true;
-        while (walk.next(sm, a, it)) {               // goes on after a wait that ran out: the four warps share a barrier
+        while (walk.next(sm, a, it)) {               // goes on after a wait that ran out: the eight warps share a barrier
             const int r = it.rb * 128 + rank * 64 + row;
-            const bool in = r < a.H * it.Nb;
-            const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
             float ref = -INFINITY, l = 0.0f;
             for (int t = it.t0; t < it.t1; ++t, ++g) {
                 const LtTile x = lt_tile(it, t, tk);
-                ok = ok && LT_WAIT(&sm->s_full[g & 1], (g >> 1) & 1, 8);
+                const int cols = min(max(x.kpc - 64 * group, 0), 64);          // this thread's columns, from 64 * group on
+                uint64_t see = ~0ull;                                          // keys that the row sees
+                const bool plain = x.kpc == 128 && !x.tree && x.start == x.lo;
+                if (!plain) {
+                    const int key0 = x.start + half * x.kpc + 64 * group;      // key of this thread's first column
+                    const int from = max(x.lo - key0, 0);
+                    see = cols <= from ? 0 : (~0ull >> (64 - (cols - from))) << from;
+                    if (see && x.tree) {
+                        const uint64_t* bits = a.anc + (size_t)(r % it.Nb) * a.words;
+                        see &= anc_bits(bits, a.words, key0) | (uint64_t)anc_bits(bits, a.words, key0 + 32) << 32;
+                    }
+                }
+                ok = ok && LT_WAIT(&sm->s_full[g & 1], (g >> 1) & 1, 10);
                 __syncwarp();
                 tc_fence_after();
-                float s[128];
-                const uint32_t sa = lane_addr + kLtColS + (g & 1) * 128;
-                float mx = -INFINITY;
-                if (x.kpc == 128 && !x.tree && x.start == x.lo) {
+                // The scores are read twice, 32 at a time, for their maximum and for the weights: tensor memory is near, and
+                // this block's cache is shared memory, so that a spilled register would come back from L2.
+                const uint32_t sa = lane_addr + kLtColS + (g & 1) * 128 + 64 * group;
+                float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tc_ld32(sa + 32 * c, s + 32 * c);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) {
-                        s[i] *= p.scale_log2;
-                        mx = fmaxf(mx, s[i]);
-                    }
-                } else {
-                    const int key0 = x.start + half * x.kpc;                   // key of column 0
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (32 * c < x.kpc) tc_ld32(sa + 32 * c, s + 32 * c);
+                for (int c = 0; c < 2; ++c) {
+                    if (cols > 32 * c) {
+                        float s[32];
+                        tc_ld32(sa + 32 * c, s);
                         tc_wait_ld();
-                        const int from = max(x.lo - key0 - 32 * c, 0), to = min(x.kpc - 32 * c, 32);
-                        uint32_t see = to <= from ? 0u : (0xffffffffu >> (32 - (to - from))) << from;
-                        if (see && x.tree) see &= anc_bits(a.anc + (size_t)n * a.words, a.words, key0 + 32 * c);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            s[32 * c + i] = (see >> i) & 1 ? s[32 * c + i] * p.scale_log2 : -INFINITY;
-                            mx = fmaxf(mx, s[32 * c + i]);
+                        for (int i = 0; i < 32; ++i) s[i] *= p.scale_log2;
+                        if (!plain) {
+                            const uint32_t bits = (uint32_t)(see >> (32 * c));
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) s[i] = (bits >> i) & 1 ? s[i] : -INFINITY;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            m0 = fmaxf(m0, s[i]);
+                            m1 = fmaxf(m1, s[i + 1]);
                         }
                     }
                 }
-                sm->red[g & 1][half][row] = mx;
+                sm->red[g & 1][2 * half + group][row] = fmaxf(m0, m1);
                 softmax_sync();
-                mx = fmaxf(mx, sm->red[g & 1][half ^ 1][row]);
+                const float mx = fmaxf(fmaxf(sm->red[g & 1][0][row], sm->red[g & 1][1][row]), fmaxf(sm->red[g & 1][2][row], sm->red[g & 1][3][row]));
                 // the reference moves only when a score exceeds it by more than 2^8 (weights stay exact: a common factor)
                 float factor = 1.0f;
                 if (mx > ref + kLazyTau) {
@@ -452,69 +478,87 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 }
                 const float sub = ref == -INFINITY ? 0.0f : ref;
                 const bool move = t > it.t0 && __any_sync(0xffffffffu, factor != 1.0f);
-                float sum0 = 0.0f, sum1 = 0.0f;
-                uint32_t packed[64];
+                float2 sum = make_float2(0.0f, 0.0f);
+                const float2 neg = make_float2(-sub, -sub), scale2 = make_float2(p.scale_log2, p.scale_log2);
+                uint32_t packed[32];
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    const float e0 = ex2_approx(s[2 * i] - sub), e1 = ex2_approx(s[2 * i + 1] - sub);
-                    sum0 += e0;
-                    sum1 += e1;
-                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed[i]) : "f"(e1), "f"(e0));
+                for (int c = 0; c < 2; ++c) {
+                    if (cols > 32 * c) {
+                        float s[32];
+                        tc_ld32(sa + 32 * c, s);
+                        tc_wait_ld();
+                        const uint32_t bits = plain ? ~0u : (uint32_t)(see >> (32 * c));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 d = fma_f32x2(make_float2(s[2 * i], s[2 * i + 1]), scale2, neg);
+                            float2 e = make_float2(ex2_approx(d.x), ex2_approx(d.y));
+                            if (!plain) {
+                                e.x = (bits >> (2 * i)) & 1 ? e.x : 0.0f;
+                                e.y = (bits >> (2 * i + 1)) & 1 ? e.y : 0.0f;
+                            }
+                            sum = add_f32x2(sum, e);
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed[16 * c + i]) : "f"(e.y), "f"(e.x));
+                        }
+                    }
                 }
-                l = l * factor + (sum0 + sum1);
-                if (g > 0) ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 9);   // P is free, O is current
+                l = l * factor + (sum.x + sum.y);
+                if (g > 0) ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 11);  // P is free, O is current
                 __syncwarp();
                 tc_fence_after();
                 if (move) {
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < 4; ++c) {
                         float o[32];
-                        tc_ld32(lane_addr + kLtColO + 32 * c, o);
+                        const uint32_t oa = lane_addr + kLtColO + 128 * group + 32 * c;
+                        tc_ld32(oa, o);
                         tc_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] *= factor;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) tc_st8(lane_addr + kLtColO + 32 * c + i, o + i);
+                        for (int i = 0; i < 32; i += 8) tc_st8(oa + i, o + i);
                     }
                     tc_wait_st();
                 }
 #pragma unroll
-                for (int u = 0; u < 16; ++u) {
-                    if (8 * u >= x.kpc) continue;
-                    const int k = half * x.kpc + 8 * u;
-                    const uint32_t dst = p_a + (k >> 6) * 8192 + row * 128 + ((((k >> 3) & 7) ^ (row & 7)) << 4);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(packed[4 * u]), "r"(packed[4 * u + 1]),
-                                 "r"(packed[4 * u + 2]), "r"(packed[4 * u + 3]) : "memory");
+                for (int u = 0; u < 8; ++u) {
+                    if (8 * u < cols) {
+                        const int k = half * x.kpc + 64 * group + 8 * u;
+                        const uint32_t dst = p_a + (k >> 6) * 8192 + row * 128 + ((((k >> 3) & 7) ^ (row & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(packed[4 * u]), "r"(packed[4 * u + 1]),
+                                     "r"(packed[4 * u + 2]), "r"(packed[4 * u + 3]) : "memory");
+                    }
                 }
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_cluster(p_bar);
+                if (lane == 0) arrive_cluster(p_bar + (g & 1) * 8);
             }
             // ---- the item's rows, or this piece of them
-            sm->lsum[half][row] = l;
+            sm->lsum[2 * half + group][row] = l;
             softmax_sync();
-            l = sm->lsum[0][row] + sm->lsum[1][row];
-            ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 10);
+            l = (sm->lsum[0][row] + sm->lsum[1][row]) + (sm->lsum[2][row] + sm->lsum[3][row]);
+            ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 12);
             __syncwarp();
             tc_fence_after();
             const bool whole = it.t0 == 0 && it.t1 == it.nt;
             const int slot = 2 * pair + (it.t0 == 0 ? 1 : 0);
             if (!whole) {
-                if (half == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
+                if (half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
                 if (it.t0 == 0 && rank == 0 && w == 0 && lane == 0) {
                     const int last = lt_pair_of(it.unit0 + it.nt, sm->total, sm->pairs);
                     p.pieces[pair] = LtPieces{last - pair + 1, it.b, it.rb, 0};
                 }
             }
+            const bool in = r < a.H * it.Nb;
+            const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
             const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + half * 128;
-            float* part = p.part_o + ((long long)slot * 128 + rank * 64 + row) * kLtRank + half * 128;
+            // columns 128 group .. of tensor memory are channels 256 group + 128 half ..
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * group + 128 * half;
+            float* part = p.part_o + ((long long)slot * 128 + rank * 64 + row) * kLtRank + 256 * group + 128 * half;
 #pragma unroll 1
-            for (int c = 0; c < 8; ++c) {                                       // 32 channels at 256 (c / 4) + 32 (c % 4)
+            for (int c = 0; c < 4; ++c) {
                 float o[32];
-                tc_ld32(lane_addr + kLtColO + 32 * c, o);
+                tc_ld32(lane_addr + kLtColO + 128 * group + 32 * c, o);
                 tc_wait_ld();
-                const int at = (c >> 2) * 256 + (c & 3) * 32;
                 if (in && whole) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
@@ -523,11 +567,11 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[i + 3] * inv), "f"(o[i + 2] * inv));
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.z) : "f"(o[i + 5] * inv), "f"(o[i + 4] * inv));
                         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.w) : "f"(o[i + 7] * inv), "f"(o[i + 6] * inv));
-                        *reinterpret_cast<uint4*>(out + at + i) = v;
+                        *reinterpret_cast<uint4*>(out + 32 * c + i) = v;
                     }
                 } else if (in) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + at + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + 32 * c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
                 }
                 __syncwarp();
             }
