@@ -32,6 +32,6 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
     const mcsd::LatentArgs a{q, cache, tree, out, seq_lens, n_active, anc, words, B, H, N, rank, rot, L_max, softmax_scale, dtype};
     auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
     if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned16(q) && aligned16(cache) && aligned16(tree) && aligned16(out))
-        return mcsd::tree_attention_latent_tc(a, &ws->header, ws + 1, static_cast<cudaStream_t>(stream));
+        return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
 }

@@ -21,11 +21,12 @@
 // sequence's end ever meets a product.
 //
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
-// inside an item, the pieces write unnormalised rows, and a second kernel joins them.  Tiles are 256 keys, or 128 or 64
-// where there would be fewer tiles than pairs.
+// inside an item, the pieces write unnormalised rows and count themselves in.  At the end of its range a pair waits for the
+// other pieces of such an item and joins a share of its rows.  (All blocks run at a time: one a multiprocessor, no more
+// pairs than fit.)  Tiles are 256 keys, or 128 or 64 where there would be fewer tiles than pairs.
 //
 // Warps of a block: 0 loads for S, 1 issues it, 2 loads for O, 3 issues it (1 and 3 in the first block of the pair), 4 to 11
-// do the softmax and the output, 12 and 13 fetch queries.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
+// fetch queries, do the softmax and the output.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
 // blocks exit.
 #include <cuda.h>
 
@@ -40,23 +41,19 @@ namespace mcsd {
 
 constexpr int kLtRank = 512, kLtRot = 64, kLtWidth = kLtRank + kLtRot;
 constexpr int kLtChunks = kLtWidth / 64;             // 64-channel chunks of a row
-constexpr int kLtThreads = 448;
+constexpr int kLtThreads = 384;
 constexpr int kLtKeySlots = 4, kLtValueSlots = 3, kLtSlots = kLtKeySlots + kLtValueSlots, kLtSlotBytes = 16384;
-constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;
+constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;      // queries, weights of a tile
 constexpr int kLtMaxBatch = 256;
 constexpr int kLtMaxPairs = kTcMaxBlocks / 2;
 constexpr int kLtColO = 0, kLtColS = 256;            // tensor memory: O 256 columns, S 128 twice
-
-struct LtPieces {                                    // an item cut over several pairs, by the pair that starts it
-    int count, b, rb, pad;
-};
 
 struct LtParams {
     LatentArgs a;
     float scale_log2;
     float* part_o;                                   // [2 * pairs][128][512]
     float2* part_ml;                                 // [2 * pairs][128]  reference (log2), sum
-    LtPieces* pieces;                                // [pairs]
+    int* counters;                                   // [2 * pairs][kCountersPerBlock]: pieces of the item that a block starts, shares joined
     WorkspaceHeader* header;
 };
 struct LtMaps {
@@ -65,10 +62,11 @@ struct LtMaps {
 
 struct LtSmall {
     unsigned long long full[kLtSlots], empty[kLtSlots];          // slots of S, then of O
-    unsigned long long s_full[2], p_full[2], pv_done, q_full, q_free;
+    unsigned long long s_full[2], s_free[2], p_full[4], p_free[4], pv_done, q_full;
     uint32_t tmem_base;
     int abort_flag;
     int tile_keys, pairs;                            // keys of a tile, pairs with work
+    int join_ready;
     int total;                                       // units of the launch
     int sums[3];                                     // tiles of the launch with 256, 128, 64 keys a tile
     int scan[kLtThreads / 32];
@@ -85,8 +83,11 @@ __device__ __forceinline__ uint32_t leader_addr(uint32_t addr) {      // the sam
     asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
     return r;
 }
-__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Arrival at a barrier of the pair's first block.  What is handed over with it lies in this block's own shared or tensor memory
+// and is read by products alone: the writer has made it visible to them before (fence.proxy.async, tcgen05.fence), so the
+// arrival needs no release at cluster scope, which costs a memory barrier (1300 cycles a tile, measured).
+__device__ __forceinline__ void arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
     asm volatile(
@@ -198,6 +199,12 @@ __device__ __forceinline__ LtTile lt_tile(const LtItem& it, int t, int tk) {
     return x;
 }
 
+// A tile's keys in quarters: up to 64 keys of the first block's half, the rest of that half, and the same of the second's.
+// Quarters pass from the softmax to the products one by one, so that weights are written while the products of the tile
+// before still read theirs.
+__device__ __forceinline__ int lt_quarter(int kpc, int q) { return min(max(kpc - 64 * (q & 1), 0), 64); }
+__device__ __forceinline__ int lt_quarter_start(int kpc, int q) { return (q >> 1) * kpc + 64 * (q & 1); }
+
 __device__ __forceinline__ uint64_t anc_word(const uint64_t* w, int words, int i) { return i >= 0 && i < words ? w[i] : 0; }
 // 32 bits of a mask row from bit `pos` on (which may lie before the first bit: zeros)
 __device__ __forceinline__ uint32_t anc_bits(const uint64_t* w, int words, int pos) {
@@ -207,12 +214,101 @@ __device__ __forceinline__ uint32_t anc_bits(const uint64_t* w, int words, int p
     return (uint32_t)v;
 }
 
+// The rows of a cut item that this block joins: a share of its 64, by the 256 threads of the softmax warps.
+__device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, const LtItem& it, int pair, int rank, int tid, bool ok) {
+    const LatentArgs& a = p.a;
+    const int first = lt_pair_of(it.unit0 + 1, sm->total, sm->pairs), last = lt_pair_of(it.unit0 + it.nt, sm->total, sm->pairs);
+    const int count = last - first + 1;
+    int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
+    if (tid == 0) {
+        const long long t0 = clock64();
+        int seen = 0;
+        while (ok) {
+            asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+            if (seen >= count || *(volatile int*)&sm->abort_flag) break;
+            if (clock64() - t0 > kSpinCycles) {
+                *(volatile int*)&sm->abort_flag = 1;
+                p.header->detail = 20;
+                p.header->status = MCSD_ERR_TIMEOUT;
+                __threadfence();
+                break;
+            }
+        }
+        sm->join_ready = seen >= count;
+    }
+    softmax_sync();
+    if (sm->join_ready) {
+        const int k0 = pair - first, lo = 64 * k0 / count, hi = 64 * (k0 + 1) / count;
+        const int d = (tid & 127) * 4;
+        constexpr int kRows = 4;                                   // rows in flight
+        for (int row0 = lo + (tid >> 7) * kRows; row0 < hi; row0 += 2 * kRows) {
+            float m[kRows], l[kRows];
+            float4 o[kRows];
+            int at[kRows];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                at[i] = rank * 64 + min(row0 + i, hi - 1);
+                m[i] = -INFINITY;
+                l[i] = 0.0f;
+                o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+            // piece 0 lies in its pair's second slot, the others in the first
+#pragma unroll 2
+            for (int k = 0; k < count; ++k) {
+                const int slot = 2 * (first + k) + (k == 0);
+                float2 ml[kRows];
+                float4 v[kRows];
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    ml[i] = __ldcg(p.part_ml + slot * 128 + at[i]);
+                    v[i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((long long)slot * 128 + at[i]) * kLtRank + d));
+                }
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const float top = fmaxf(m[i], ml[i].x), sub = top == -INFINITY ? 0.0f : top;
+                    const float f = ex2_approx(m[i] - sub), e = ex2_approx(ml[i].x - sub);
+                    m[i] = top;
+                    l[i] = l[i] * f + ml[i].y * e;
+                    o[i].x = o[i].x * f + v[i].x * e;
+                    o[i].y = o[i].y * f + v[i].y * e;
+                    o[i].z = o[i].z * f + v[i].z * e;
+                    o[i].w = o[i].w * f + v[i].w * e;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int r = it.rb * 128 + rank * 64 + row0 + i;
+                if (row0 + i >= hi || r >= a.H * it.Nb) continue;
+                const float inv = l[i] > 0.0f ? 1.0f / l[i] : l[i];
+                const int h = r / it.Nb, n = r - h * it.Nb;
+                uint2 v;
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o[i].y * inv), "f"(o[i].x * inv));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[i].w * inv), "f"(o[i].z * inv));
+                *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + d) = v;
+            }
+        }
+    }
+    softmax_sync();
+    if (tid == 0 && atomicAdd(counter + 1, 1) == count - 1) {      // the last share: counters are zero between launches
+        counter[0] = 0;
+        counter[1] = 0;
+    }
+}
+// The items of this pair's range that other pairs have pieces of: the first, the last, or one that is both.
+__device__ __forceinline__ void lt_join(LtSmall* sm, const LtParams& p, int pair, int rank, int tid, bool ok) {
+    LtWalk walk;
+    walk.start(sm, pair);
+    LtItem it;
+    while (walk.next(sm, p.a, it))
+        if (it.t0 > 0 || it.t1 < it.nt) lt_join_item(sm, p, it, pair, rank, tid, ok);
+}
+
 #define LT_WAIT(bar, parity, where) mbar_wait(bar, parity, &sm->abort_flag, p.header, where)
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtThreads, 1)
 tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_constant__ LtParams p) {
     extern __shared__ uint8_t raw[];
-    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* base = raw + (-(int)smem_u32(raw) & 1023);   // an offset, so that accesses stay shared-memory ones
     const uint32_t q_a = smem_u32(base), p_a = q_a + kLtQBytes, ring_a = p_a + kLtPBytes;
     LtSmall* sm = reinterpret_cast<LtSmall*>(base + kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes);
     const LatentArgs& a = p.a;
@@ -223,11 +319,11 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         for (int i = 0; i < kLtSlots; ++i) { mbar_init(&sm->full[i], 1); mbar_init(&sm->empty[i], 1); }
         mbar_init(&sm->s_full[0], 1);
         mbar_init(&sm->s_full[1], 1);
-        mbar_init(&sm->p_full[0], 16);
-        mbar_init(&sm->p_full[1], 16);
+        mbar_init(&sm->s_free[0], 16);
+        mbar_init(&sm->s_free[1], 16);
+        for (int i = 0; i < 4; ++i) { mbar_init(&sm->p_full[i], 4); mbar_init(&sm->p_free[i], 1); }
         mbar_init(&sm->pv_done, 1);
-        mbar_init(&sm->q_full, 4);
-        mbar_init(&sm->q_free, 1);
+        mbar_init(&sm->q_full, 16);
         sm->abort_flag = 0;
         sm->sums[0] = sm->sums[1] = sm->sums[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -304,9 +400,11 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                                       x.start + rank * x.kpc, it.b);
                             advance();
                         }
-                    } else {                                 // 64 keys and 128 of this block's channels a slot
-                        for (int k = 0; k < (2 * x.kpc + 63) / 64 * 2; ++k) {
-                            const int k0 = (k >> 1) * 64, j = k & 1, size = 2 * x.kpc - k0 > 32 ? 2 : 1;
+                    } else {                                 // a quarter of the keys and 128 of this block's channels a slot
+                        for (int k = 0; k < 8; ++k) {
+                            const int q = k >> 1, j = k & 1, n = lt_quarter(x.kpc, q), k0 = lt_quarter_start(x.kpc, q);
+                            if (n == 0) continue;
+                            const int size = n > 32 ? 2 : n > 16 ? 1 : 0;
                             if (!acquire((16u << size) * 256u)) break;
                             const uint32_t dst = ring_a + (kLtKeySlots + slot) * kLtSlotBytes, bar = leader_addr(smem_u32(&sm->full[kLtKeySlots + slot]));
                             pair_load(dst, map + size, bar, 256 * j + 128 * rank, x.start + k0, it.b);
@@ -339,7 +437,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         const LtTile x = lt_tile(it, t, tk);
                         const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (g & 1) * 128;
                         // the softmax has read what this S replaces
-                        if (g > 1) ok = __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[g & 1], ((g >> 1) - 1) & 1, 5));
+                        if (g > 1) ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], ((g >> 1) - 1) & 1, 5));
 #pragma unroll
                         for (int c = 0; c < kLtChunks; ++c) {
                             ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->full[slot], phase, 6));
@@ -353,7 +451,6 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         }
                         pair_commit(one, &sm->s_full[g & 1]);
                     }
-                    pair_commit(one, &sm->q_free);
                 }
             } else {
                 const uint64_t dp = smem_desc(p_a, 16, 1024, 2), dv = smem_desc(ring_a + kLtKeySlots * kLtSlotBytes, 8192, 1024, 2);
@@ -362,57 +459,34 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     it.uniform();
                     for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
                         const LtTile x = lt_tile(it, t, tk);
-                        ok = __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[g & 1], (g >> 1) & 1, 7));
-                        for (int k0 = 0; ok && k0 < 2 * x.kpc; k0 += 64) {
-                            const uint64_t pa = dp + (k0 >> 6) * 512;
-                            const uint32_t more = t > it.t0 || k0 > 0;
+                        ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], (g >> 1) & 1, 14));     // O has its reference
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int n = lt_quarter(x.kpc, q);
+                            ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[q], g & 1, 7));
+                            const uint64_t pa = dp + q * 512;
+                            const uint32_t more = t > it.t0 || q > 0;
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
+                                if (n == 0) continue;
                                 ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->full[kLtKeySlots + slot], phase, 8));
                                 if (!ok) break;
                                 tc_fence_after();
                                 const uint32_t d = tmem + kLtColO + j * 128;
                                 const uint64_t vb = dv + slot * 1024;
                                 pair_mma(one, d, pa, vb, idesc, more);
-                                pair_mma(one, d, pa + 2, vb + 128, idesc, 1);
-                                if (2 * x.kpc - k0 > 32) {
-                                    pair_mma(one, d, pa + 4, vb + 256, idesc, 1);
-                                    pair_mma(one, d, pa + 6, vb + 384, idesc, 1);
-                                }
+                                if (n > 16) pair_mma(one, d, pa + 2, vb + 128, idesc, 1);
+                                if (n > 32) pair_mma(one, d, pa + 4, vb + 256, idesc, 1);
+                                if (n > 48) pair_mma(one, d, pa + 6, vb + 384, idesc, 1);
                                 pair_commit(one, &sm->empty[kLtKeySlots + slot]);
                                 if (++slot == kLtValueSlots) { slot = 0; phase ^= 1; }
                             }
+                            pair_commit(one, &sm->p_free[q]);
                         }
                         pair_commit(one, &sm->pv_done);
                     }
                 }
             }
-        }
-    } else if (warp >= 12) {
-        // ---------------------------------------------------------------- queries
-        // (a wait that ran out skips the later ones; the loop itself goes on, so that a warp stays together)
-        uint32_t item = 0;
-        bool ok = true;
-        const uint32_t q_bar = leader_addr(smem_u32(&sm->q_full));
-        for (; walk.next(sm, a, it); ++item) {
-            if (item > 0) ok = ok && LT_WAIT(&sm->q_free, (item - 1) & 1, 9);   // the last item's scores are done
-            __syncwarp();
-            const int rows = a.H * it.Nb, r0 = it.rb * 128 + rank * 64 + (warp - 12) * 32;
-            int h = r0 / it.Nb, n = r0 - h * it.Nb;
-            for (int i = 0; i < 32; ++i) {
-                const bool in = r0 + i < rows;
-                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (in ? (((long long)it.b * a.H + h) * a.N + n) * kLtWidth : 0);
-                const int row = (warp - 12) * 32 + i;
-                for (int v = lane; v < kLtWidth / 8; v += 32) {
-                    const uint32_t dst = q_a + (v >> 3) * 8192 + row * 128 + (((v & 7) ^ (row & 7)) << 4);
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src + v * 8), "r"(in ? 16 : 0) : "memory");
-                }
-                if (++n == it.Nb) { n = 0; ++h; }
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) arrive_cluster(q_bar);
         }
     } else {
         // ---------------------------------------------------------------- softmax and output
@@ -420,15 +494,41 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         // warps share its columns
         const int w = warp - 4, group = w >> 2, half = (w >> 1) & 1, row = (w & 1) * 32 + lane;
         const uint32_t lane_addr = tmem + ((uint32_t)((w & 3) * 32) << 16);
-        const uint32_t p_bar = leader_addr(smem_u32(&sm->p_full[0]));
+        const uint32_t q_bar = leader_addr(smem_u32(&sm->q_full)), p_bar = leader_addr(smem_u32(&sm->p_full[0])), s_bar = leader_addr(smem_u32(&sm->s_free[0]));
         uint32_t g = 0;
-        bool ok = true;
-        while (walk.next(sm, a, it)) {               // goes on after a wait that ran out: the eight warps share a barrier
+        bool ok = true, more;
+        // a warp fetches eight rows of an item's queries, eight lanes a row, each one vector of every chunk
+        auto fetch = [&](const LtItem& x) {
+            const int rows = a.H * x.Nb, v = lane & 7;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int qr = w * 8 + i * 4 + (lane >> 3), r = x.rb * 128 + rank * 64 + qr;
+                const bool in = r < rows;
+                const int h = in ? r / x.Nb : 0, n = in ? r - h * x.Nb : 0;
+                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (((long long)x.b * a.H + h) * a.N + n) * kLtWidth + v * 8;
+                const uint32_t dst = q_a + qr * 128 + ((v ^ (qr & 7)) << 4);
+#pragma unroll
+                for (int c = 0; c < kLtChunks; ++c)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + c * 8192), "l"(src + c * 64), "r"(in ? 16 : 0) : "memory");
+            }
+        };
+        auto fetched = [&]() {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive_pair(q_bar);
+        };
+        more = walk.next(sm, a, it);
+        if (more) {
+            fetch(it);
+            fetched();
+        }
+        while (more) {                               // goes on after a wait that ran out: the eight warps share a barrier
             const int r = it.rb * 128 + rank * 64 + row;
             float ref = -INFINITY, l = 0.0f;
             for (int t = it.t0; t < it.t1; ++t, ++g) {
                 const LtTile x = lt_tile(it, t, tk);
-                const int cols = min(max(x.kpc - 64 * group, 0), 64);          // this thread's columns, from 64 * group on
+                const int cols = lt_quarter(x.kpc, group);                     // this thread's columns, from 64 * group on
                 uint64_t see = ~0ull;                                          // keys that the row sees
                 const bool plain = x.kpc == 128 && !x.tree && x.start == x.lo;
                 if (!plain) {
@@ -478,6 +578,22 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 }
                 const float sub = ref == -INFINITY ? 0.0f : ref;
                 const bool move = t > it.t0 && __any_sync(0xffffffffu, factor != 1.0f);
+                if (move) {
+                    ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 13);         // O is current
+                    __syncwarp();
+                    tc_fence_after();
+                    for (int c = 0; c < 4; ++c) {
+                        float o[32];
+                        const uint32_t oa = lane_addr + kLtColO + 128 * group + 32 * c;
+                        tc_ld32(oa, o);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] *= factor;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) tc_st8(oa + i, o + i);
+                    }
+                    tc_wait_st();
+                }
                 float2 sum = make_float2(0.0f, 0.0f);
                 const float2 neg = make_float2(-sub, -sub), scale2 = make_float2(p.scale_log2, p.scale_log2);
                 uint32_t packed[32];
@@ -501,28 +617,16 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         }
                     }
                 }
-                l = l * factor + (sum.x + sum.y);
-                if (g > 0) ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 11);  // P is free, O is current
+                tc_fence_before();
                 __syncwarp();
-                tc_fence_after();
-                if (move) {
-                    for (int c = 0; c < 4; ++c) {
-                        float o[32];
-                        const uint32_t oa = lane_addr + kLtColO + 128 * group + 32 * c;
-                        tc_ld32(oa, o);
-                        tc_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] *= factor;
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) tc_st8(oa + i, o + i);
-                    }
-                    tc_wait_st();
-                }
+                if (lane == 0) arrive_pair(s_bar + (g & 1) * 8);               // these scores have been read, O has its reference
+                l = l * factor + (sum.x + sum.y);
+                if (g > 0) ok = ok && LT_WAIT(&sm->p_free[2 * half + group], (g - 1) & 1, 11);   // this quarter of P is free
+                __syncwarp();
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     if (8 * u < cols) {
-                        const int k = half * x.kpc + 64 * group + 8 * u;
-                        const uint32_t dst = p_a + (k >> 6) * 8192 + row * 128 + ((((k >> 3) & 7) ^ (row & 7)) << 4);
+                        const uint32_t dst = p_a + (2 * half + group) * 8192 + row * 128 + ((u ^ (row & 7)) << 4);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(packed[4 * u]), "r"(packed[4 * u + 1]),
                                      "r"(packed[4 * u + 2]), "r"(packed[4 * u + 3]) : "memory");
                     }
@@ -530,24 +634,23 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 fence_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_cluster(p_bar + (g & 1) * 8);
+                if (lane == 0) arrive_pair(p_bar + (2 * half + group) * 8);
             }
+            // ---- the next item's queries: this one's scores are done
+            LtItem next;
+            more = walk.next(sm, a, next);
+            if (more) fetch(next);
             // ---- the item's rows, or this piece of them
             sm->lsum[2 * half + group][row] = l;
             softmax_sync();
             l = (sm->lsum[0][row] + sm->lsum[1][row]) + (sm->lsum[2][row] + sm->lsum[3][row]);
+            if (more) fetched();
             ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 12);
             __syncwarp();
             tc_fence_after();
             const bool whole = it.t0 == 0 && it.t1 == it.nt;
             const int slot = 2 * pair + (it.t0 == 0 ? 1 : 0);
-            if (!whole) {
-                if (half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
-                if (it.t0 == 0 && rank == 0 && w == 0 && lane == 0) {
-                    const int last = lt_pair_of(it.unit0 + it.nt, sm->total, sm->pairs);
-                    p.pieces[pair] = LtPieces{last - pair + 1, it.b, it.rb, 0};
-                }
-            }
+            if (!whole && half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
             const bool in = r < a.H * it.Nb;
             const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
             const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
@@ -576,53 +679,21 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 __syncwarp();
             }
             tc_fence_before();
+            if (!whole) {                                                       // this piece of a cut item is there
+                const int first = lt_pair_of(it.unit0 + 1, sm->total, sm->pairs);
+                __threadfence();
+                softmax_sync();
+                if (w == 0 && lane == 0) atomicAdd(&p.counters[(2 * first + rank) * kCountersPerBlock], 1);
+            }
+            it = next;
         }
-    }
-    // a pair that starts no cut item says so
-    if (rank == 0 && tid == 0) {
-        bool cut = false;
-        LtWalk again;
-        again.start(sm, pair);
-        while (again.next(sm, a, it)) cut = cut || (it.t0 == 0 && it.t1 < it.nt);
-        if (!cut) p.pieces[pair] = LtPieces{0, 0, 0, 0};
+        lt_join(sm, p, pair, rank, tid - 128, ok);
     }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();                                 // the other block's products, loads and arrivals are done too
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-}
-
-// Joins the pieces of the items that were cut.  grid: (pairs, 32), four rows a block, 128 threads a row
-__global__ void __launch_bounds__(512) latent_join_kernel(const __grid_constant__ LtParams p) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const LatentArgs& a = p.a;
-    const LtPieces x = p.pieces[blockIdx.x];
-    if (x.count < 2) return;
-    const int Nb = lt_nodes(a, x.b), row = blockIdx.y * 4 + (threadIdx.x >> 7), r = x.rb * 128 + row, d = (threadIdx.x & 127) * 4;
-    if (r >= a.H * Nb) return;
-    const int pair = blockIdx.x;
-    // piece 0 lies in the pair's second slot, piece k in the first slot of pair + k
-    float m = -INFINITY;
-    for (int k = 0; k < x.count; ++k) m = fmaxf(m, p.part_ml[(2 * (pair + k) + (k == 0)) * 128 + row].x);
-    const float sub = m == -INFINITY ? 0.0f : m;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    float l = 0.0f;
-#pragma unroll 8
-    for (int k = 0; k < x.count; ++k) {
-        const int slot = 2 * (pair + k) + (k == 0);
-        const float2 ml = p.part_ml[slot * 128 + row];
-        const float f = ex2_approx(ml.x - sub);
-        const float4 v = *reinterpret_cast<const float4*>(p.part_o + ((long long)slot * 128 + row) * kLtRank + d);
-        l += f * ml.y;
-        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
-    }
-    const float inv = l > 0.0f ? 1.0f / l : l;
-    const int h = r / Nb, n = r - h * Nb;
-    uint2 v;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o.y * inv), "f"(o.x * inv));
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o.w * inv), "f"(o.z * inv));
-    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (((long long)x.b * a.H + h) * a.N + n) * kLtRank + d) = v;
 }
 
 // ------------------------------------------------------------------ host side
@@ -659,30 +730,45 @@ bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtyp
     return per_seq * std::min(B, kLtMaxBatch) < (1LL << 30);
 }
 size_t latent_tc_workspace_bytes() {
-    return (size_t)2 * kLtMaxPairs * 128 * (kLtRank * sizeof(float) + sizeof(float2)) + align_up(kLtMaxPairs * sizeof(LtPieces), 256);
+    return (size_t)2 * kLtMaxPairs * 128 * (kLtRank * sizeof(float) + sizeof(float2));
 }
 
-int tree_attention_latent_tc(const LatentArgs& whole, WorkspaceHeader* header, void* scratch, cudaStream_t stream) {
+int tree_attention_latent_tc(const LatentArgs& whole, AttentionWorkspace* workspace, void* scratch, cudaStream_t stream) {
     if (lt_encode_fn() == nullptr) { set_last_cuda_error(cudaErrorInvalidValue); return MCSD_ERR_CUDA; }
     int dev = 0, sms = 0;
     MCSD_CUDA_CHECK(cudaGetDevice(&dev));
     MCSD_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    {   // the opt-in to large dynamic shared memory is per device
-        static std::mutex mu;
-        static bool done[64] = {};
+    // as many pairs as run at a time: a pair waits for others at its end
+    static std::mutex mu;
+    static int fit[64] = {};
+    int pairs = 0;
+    {
         std::lock_guard<std::mutex> lock(mu);
-        if (dev < 0 || dev >= 64 || !done[dev]) {
+        if (dev >= 0 && dev < 64) pairs = fit[dev];
+        if (pairs == 0) {
+            // the opt-in to large dynamic shared memory is per device
             MCSD_CUDA_CHECK(cudaFuncSetAttribute(tree_attention_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLtSmem));
-            if (dev >= 0 && dev < 64) done[dev] = true;
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+            cfg.gridDim = dim3((unsigned)sms / 2 * 2);
+            cfg.blockDim = dim3(kLtThreads);
+            cfg.dynamicSmemBytes = kLtSmem;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            MCSD_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&pairs, tree_attention_latent_kernel, &cfg));
+            pairs = std::min(pairs, std::min(sms / 2, kLtMaxPairs));
+            if (pairs < 1) { set_last_cuda_error(cudaErrorInvalidConfiguration); return MCSD_ERR_CUDA; }
+            if (dev >= 0 && dev < 64) fit[dev] = pairs;
         }
     }
-    const int pairs = std::max(1, std::min(sms / 2, kLtMaxPairs));
     LtParams p{};
-    p.header = header;
+    p.header = &workspace->header;
     p.scale_log2 = whole.scale * 1.4426950408889634f;
     p.part_o = static_cast<float*>(scratch);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)2 * kLtMaxPairs * 128 * kLtRank);
-    p.pieces = reinterpret_cast<LtPieces*>(p.part_ml + (size_t)2 * kLtMaxPairs * 128);
+    p.counters = workspace->counters;
     for (int b0 = 0; b0 < whole.B; b0 += kLtMaxBatch) {                         // tables of a launch hold 256 sequences
         LatentArgs& a = p.a;
         a = whole;
@@ -714,11 +800,7 @@ int tree_attention_latent_tc(const LatentArgs& whole, WorkspaceHeader* header, v
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, tree_attention_latent_kernel, maps, p));
-        cfg.gridDim = dim3((unsigned)pairs, 32);
-        cfg.blockDim = dim3(512);
-        cfg.dynamicSmemBytes = 0;
-        MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_join_kernel, p));
-        count_launches(2);
+        count_launches(1);
     }
     return MCSD_OK;
 }

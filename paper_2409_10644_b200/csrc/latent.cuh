@@ -33,6 +33,6 @@ int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t 
 // tcgen05 kernel: bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 size_t latent_tc_workspace_bytes();
-int tree_attention_latent_tc(const LatentArgs& a, WorkspaceHeader* header, void* scratch, cudaStream_t stream);
+int tree_attention_latent_tc(const LatentArgs& a, AttentionWorkspace* workspace, void* scratch, cudaStream_t stream);
 
 }  // namespace mcsd
