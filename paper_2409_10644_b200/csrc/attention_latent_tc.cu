@@ -22,7 +22,7 @@
 //
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
 // inside an item, the pieces write unnormalised rows and count themselves in.  At the end of its range a pair waits for the
-// other pieces of such an item and joins a share of its rows.  (All blocks run at a time: one a multiprocessor, no more
+// other pieces of such an item and joins a share of its channels.  (All blocks run at a time: one a multiprocessor, no more
 // pairs than fit.)  Tiles are 256 keys, or 128 or 64 where there would be fewer tiles than pairs.
 //
 // Warps of a block: 0 loads for S, 1 issues it, 2 loads for O, 3 issues it (1 and 3 in the first block of the pair), 4 to 11
@@ -51,7 +51,7 @@ constexpr int kLtColO = 0, kLtColS = 256;            // tensor memory: O 256 col
 struct LtParams {
     LatentArgs a;
     float scale_log2;
-    float* part_o;                                   // [2 * pairs][128][512]
+    float* part_o;                                   // unnormalised rows of pieces, two slots a pair (see lt_part)
     float2* part_ml;                                 // [2 * pairs][128]  reference (log2), sum
     int* counters;                                   // [2 * pairs][kCountersPerBlock]: pieces of the item that a block starts, shares joined
     WorkspaceHeader* header;
@@ -133,11 +133,43 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
 }
 
 // ------------------------------------------------------------------ the cut of a launch
-__host__ __device__ __forceinline__ int lt_tiles(int L, int Nb, int tk) { return (L + tk - 1) / tk + (Nb + tk - 1) / tk; }
+// Cost of an item's parts in units of 0.4 us (measured): a tile has a fixed part (its waits) and one by its keys (its
+// products), an item starts with its queries and ends with its output.  A pair takes the tiles that start in its range of the
+// launch's units.
+constexpr int kLtItemCost = 14;
+__host__ __device__ __forceinline__ int lt_tile_cost(int keys) { return 3 + (7 * keys + 255) / 256; }
 __host__ __device__ __forceinline__ int lt_row_blocks(int H, int Nb) { return (H * Nb + 127) / 128; }
 __device__ __forceinline__ int lt_len(const LatentArgs& a, int b) { return min(max(a.seq_lens[b], 0), a.L_max); }
 __device__ __forceinline__ int lt_nodes(const LatentArgs& a, int b) { return a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N; }
-// Unit 0 of an item stands for its fixed cost (queries, output), unit 1 + t for tile t.  First unit of pair c:
+
+// The tiles of an item: full prefix tiles, a shorter one, full tree tiles, a shorter one.
+struct LtShape {
+    int full, rest_cost, tree_full, tree_rest_cost, cost;      // cost of a full tile
+    __host__ __device__ __forceinline__ LtShape(int L, int Nb, int tk) {
+        full = L / tk;
+        rest_cost = L % tk ? lt_tile_cost(L % tk) : 0;
+        tree_full = Nb / tk;
+        tree_rest_cost = Nb % tk ? lt_tile_cost(Nb % tk) : 0;
+        cost = lt_tile_cost(tk);
+    }
+    __host__ __device__ __forceinline__ int prefix_tiles() const { return full + (rest_cost > 0); }
+    __host__ __device__ __forceinline__ int tiles() const { return prefix_tiles() + tree_full + (tree_rest_cost > 0); }
+    __host__ __device__ __forceinline__ int total() const { return kLtItemCost + full * cost + rest_cost + tree_full * cost + tree_rest_cost; }
+    // where tile t starts, in units from the item's start
+    __host__ __device__ __forceinline__ int start(int t) const {
+        return kLtItemCost + (t <= full ? t * cost : full * cost + rest_cost + (t - prefix_tiles()) * cost);
+    }
+    // the first tile that starts at x or later (tiles() where there is none)
+    __host__ __device__ __forceinline__ int tile_from(int x) const {
+        const int y = x - kLtItemCost, z = y - full * cost;
+        if (y <= 0) return 0;
+        if (z <= 0) return (y + cost - 1) / cost;
+        const int after = z - rest_cost;                       // past the shorter prefix tile
+        const int t = prefix_tiles() + (after > 0 ? (after + cost - 1) / cost : 0);
+        return t < tiles() ? t : tiles();
+    }
+};
+// first unit of pair c
 __device__ __forceinline__ int lt_first(int c, int total, int pairs) { return (int)((long long)c * total / pairs); }
 __device__ __forceinline__ int lt_pair_of(int unit, int total, int pairs) { return (int)((((long long)unit + 1) * pairs - 1) / total); }
 
@@ -170,21 +202,28 @@ struct LtWalk {
             it.b = b;
             it.L = lt_len(a, b);
             it.Nb = lt_nodes(a, b);
-            it.nP = (it.L + sm->tile_keys - 1) / sm->tile_keys;
-            it.nt = it.nP + (it.Nb + sm->tile_keys - 1) / sm->tile_keys;
-            const int off = u - sm->cum[b];
-            it.rb = off / (it.nt + 1);
-            const int rem = off - it.rb * (it.nt + 1);
+            const LtShape x(it.L, it.Nb, sm->tile_keys);
+            it.nP = x.prefix_tiles();
+            it.nt = x.tiles();
+            const int off = u - sm->cum[b], total = x.total();
+            it.rb = off / total;
+            const int rem = off - it.rb * total;
             it.unit0 = u - rem;
-            const int stop = min(end, it.unit0 + it.nt + 1);
-            it.t0 = max(rem - 1, 0);
-            it.t1 = stop - it.unit0 - 1;
+            const int stop = min(end, it.unit0 + total);
+            it.t0 = x.tile_from(rem);
+            it.t1 = x.tile_from(stop - it.unit0);
             u = stop;
             if (it.t1 > it.t0) return true;
         }
         return false;
     }
 };
+// The pairs that have tiles of an item: a range of units is no shorter than a tile, so that none between them is without.
+__device__ __forceinline__ void lt_owners(const LtSmall* sm, const LtItem& it, int& first, int& last) {
+    const LtShape x(it.L, it.Nb, sm->tile_keys);
+    first = lt_pair_of(it.unit0 + x.start(0), sm->total, sm->pairs);
+    last = lt_pair_of(it.unit0 + x.start(it.nt - 1), sm->total, sm->pairs);
+}
 struct LtTile {
     int lo, start, kpc;            // first key it has a claim to, first key that is loaded, keys of a block (16 .. 128)
     bool tree;
@@ -214,10 +253,69 @@ __device__ __forceinline__ uint32_t anc_bits(const uint64_t* w, int words, int p
     return (uint32_t)v;
 }
 
-// The rows of a cut item that this block joins: a share of its 64, by the 256 threads of the softmax warps.
+// Pieces lie as tensor memory does, four columns of its 128 lanes (a row and half of the channels each) side by side, so that a
+// warp writes and reads 512 bytes at a time: [slot][block of the pair][64 quads of columns][128 lanes][4].
+__device__ __forceinline__ float4* lt_part(const LtParams& p, int slot, int rank, int quad, int tlane) {
+    return reinterpret_cast<float4*>(p.part_o) + (((long long)slot * 2 + rank) * 64 + quad) * 128 + tlane;
+}
+// QUADS quads of one lane's columns, from quad0 on: all pieces joined, in their order, PIECES of them in flight.
+template <int QUADS, int PIECES>
+__device__ __forceinline__ void lt_join_quads(const LtParams& p, const LtItem& it, int first, int count, int rank, int tlane, int quad0) {
+    const LatentArgs& a = p.a;
+    const int row = tlane & 63, half = tlane >> 6, r = it.rb * 128 + rank * 64 + row;
+    if (r >= a.H * it.Nb) return;
+    float m = -INFINITY, l = 0.0f;
+    float4 o[QUADS];
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < count; k += PIECES) {
+        float2 ml[PIECES];
+        float4 v[PIECES][QUADS];
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            // piece 0 lies in its pair's second slot, the others in the first; past the last one: that one, without weight
+            const int kk = min(k + j, count - 1), slot = 2 * (first + kk) + (kk == 0);
+            ml[j] = __ldcg(p.part_ml + slot * 128 + rank * 64 + row);
+#pragma unroll
+            for (int i = 0; i < QUADS; ++i) v[j][i] = __ldcg(lt_part(p, slot, rank, quad0 + i, tlane));
+        }
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+            if (k + j >= count) continue;
+            const float top = fmaxf(m, ml[j].x), sub = top == -INFINITY ? 0.0f : top;
+            const float f = ex2_approx(m - sub), e = ex2_approx(ml[j].x - sub);
+            m = top;
+            l = l * f + ml[j].y * e;
+#pragma unroll
+            for (int i = 0; i < QUADS; ++i) {
+                o[i].x = o[i].x * f + v[j][i].x * e;
+                o[i].y = o[i].y * f + v[j][i].y * e;
+                o[i].z = o[i].z * f + v[j][i].z * e;
+                o[i].w = o[i].w * f + v[j][i].w * e;
+            }
+        }
+    }
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    const int h = r / it.Nb, n = r - h * it.Nb, c = 4 * quad0;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * (c >> 7) + 128 * half + (c & 127);
+    uint2 v[QUADS];
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i].x) : "f"(o[i].y * inv), "f"(o[i].x * inv));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i].y) : "f"(o[i].w * inv), "f"(o[i].z * inv));
+    }
+    if constexpr (QUADS == 1) {
+        *reinterpret_cast<uint2*>(out) = v[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < QUADS; i += 2) *reinterpret_cast<uint4*>(out + 4 * i) = make_uint4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
+    }
+}
+// This block's share of a cut item's columns, by the 256 threads of the softmax warps.
 __device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, const LtItem& it, int pair, int rank, int tid, bool ok) {
     const LatentArgs& a = p.a;
-    const int first = lt_pair_of(it.unit0 + 1, sm->total, sm->pairs), last = lt_pair_of(it.unit0 + it.nt, sm->total, sm->pairs);
+    int first, last;
+    lt_owners(sm, it, first, last);
     const int count = last - first + 1;
     int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
     if (tid == 0) {
@@ -238,54 +336,11 @@ __device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, const 
     }
     softmax_sync();
     if (sm->join_ready) {
-        const int k0 = pair - first, lo = 64 * k0 / count, hi = 64 * (k0 + 1) / count;
-        const int d = (tid & 127) * 4;
-        constexpr int kRows = 4;                                   // rows in flight
-        for (int row0 = lo + (tid >> 7) * kRows; row0 < hi; row0 += 2 * kRows) {
-            float m[kRows], l[kRows];
-            float4 o[kRows];
-            int at[kRows];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                at[i] = rank * 64 + min(row0 + i, hi - 1);
-                m[i] = -INFINITY;
-                l[i] = 0.0f;
-                o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
-            // piece 0 lies in its pair's second slot, the others in the first
-#pragma unroll 2
-            for (int k = 0; k < count; ++k) {
-                const int slot = 2 * (first + k) + (k == 0);
-                float2 ml[kRows];
-                float4 v[kRows];
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    ml[i] = __ldcg(p.part_ml + slot * 128 + at[i]);
-                    v[i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((long long)slot * 128 + at[i]) * kLtRank + d));
-                }
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    const float top = fmaxf(m[i], ml[i].x), sub = top == -INFINITY ? 0.0f : top;
-                    const float f = ex2_approx(m[i] - sub), e = ex2_approx(ml[i].x - sub);
-                    m[i] = top;
-                    l[i] = l[i] * f + ml[i].y * e;
-                    o[i].x = o[i].x * f + v[i].x * e;
-                    o[i].y = o[i].y * f + v[i].y * e;
-                    o[i].z = o[i].z * f + v[i].z * e;
-                    o[i].w = o[i].w * f + v[i].w * e;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int r = it.rb * 128 + rank * 64 + row0 + i;
-                if (row0 + i >= hi || r >= a.H * it.Nb) continue;
-                const float inv = l[i] > 0.0f ? 1.0f / l[i] : l[i];
-                const int h = r / it.Nb, n = r - h * it.Nb;
-                uint2 v;
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o[i].y * inv), "f"(o[i].x * inv));
-                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[i].w * inv), "f"(o[i].z * inv));
-                *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + d) = v;
-            }
+        const int k0 = pair - first, tlane = tid & 127;
+        if (count <= 4) {                                // few pieces: 16 channels a thread, whole sectors of the output
+            for (int u = 16 * k0 / count + (tid >> 7); u < 16 * (k0 + 1) / count; u += 2) lt_join_quads<4, 4>(p, it, first, count, rank, tlane, 4 * u);
+        } else {                                         // many: one quad, eight pieces in flight
+            for (int u = 64 * k0 / count + (tid >> 7); u < 64 * (k0 + 1) / count; u += 2) lt_join_quads<1, 8>(p, it, first, count, rank, tlane, u);
         }
     }
     softmax_sync();
@@ -304,7 +359,6 @@ __device__ __forceinline__ void lt_join(LtSmall* sm, const LtParams& p, int pair
 }
 
 #define LT_WAIT(bar, parity, where) mbar_wait(bar, parity, &sm->abort_flag, p.header, where)
-
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtThreads, 1)
 tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_constant__ LtParams p) {
     extern __shared__ uint8_t raw[];
@@ -342,7 +396,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             Nb = lt_nodes(a, tid);
             rbs = lt_row_blocks(a.H, Nb);
             if (Nb > 0)
-                for (int i = 0; i < 3; ++i) t[i] = rbs * lt_tiles(L, Nb, 256 >> i);
+                for (int i = 0; i < 3; ++i) t[i] = rbs * LtShape(L, Nb, 256 >> i).tiles();
         }
         for (int i = 0; i < 3; ++i) {
             const int s = __reduce_add_sync(0xffffffffu, t[i]);
@@ -351,7 +405,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         __syncthreads();
         const int max_pairs = gridDim.x >> 1;
         const int pick = sm->sums[0] >= max_pairs ? 0 : sm->sums[1] >= max_pairs ? 1 : 2;
-        int units = Nb > 0 ? t[pick] + rbs : 0;
+        int units = Nb > 0 ? rbs * LtShape(L, Nb, 256 >> pick).total() : 0;
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, units, o);
             if (lane >= o) units += x;
@@ -361,7 +415,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         for (int w = 0; w < warp; ++w) units += sm->scan[w];
         if (tid < kLtMaxBatch) sm->cum[tid + 1] = units;   // sequences from B on: the total
         if (tid == 0) { sm->cum[0] = 0; sm->tile_keys = 256 >> pick; }
-        if (tid == kLtMaxBatch - 1) { sm->total = units; sm->pairs = min(max_pairs, units); }
+        if (tid == kLtMaxBatch - 1) { sm->total = units; sm->pairs = max(min(max_pairs, units / lt_tile_cost(256 >> pick)), units > 0); }
     }
     tc_fence_before();
     __syncthreads();
@@ -656,7 +710,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
             // columns 128 group .. of tensor memory are channels 256 group + 128 half ..
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * group + 128 * half;
-            float* part = p.part_o + ((long long)slot * 128 + rank * 64 + row) * kLtRank + 256 * group + 128 * half;
+            float4* part = lt_part(p, slot, rank, 32 * group, 64 * half + row);
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 float o[32];
@@ -674,19 +728,22 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     }
                 } else if (in) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(part + 32 * c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    for (int i = 0; i < 8; ++i) part[(8 * c + i) * 128] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
                 __syncwarp();
             }
             tc_fence_before();
             if (!whole) {                                                       // this piece of a cut item is there
-                const int first = lt_pair_of(it.unit0 + 1, sm->total, sm->pairs);
+                int first, last;
+                lt_owners(sm, it, first, last);
                 __threadfence();
                 softmax_sync();
                 if (w == 0 && lane == 0) atomicAdd(&p.counters[(2 * first + rank) * kCountersPerBlock], 1);
             }
             it = next;
         }
+        if (g > 0) ok = ok && LT_WAIT(&sm->p_free[2 * half + group], (g - 1) & 1, 15);   // the last arrival here, before the block may leave
+        __syncwarp();
         lt_join(sm, p, pair, rank, tid - 128, ok);
     }
     tc_fence_before();
@@ -722,11 +779,11 @@ static bool lt_map(CUtensorMap* map, const void* base, int rows, int B, int box_
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Shapes of this kernel.  The units of a launch are 32-bit: a sequence has at most (L_max / 64 + 5) units for each of its
-// H * N / 128 row blocks.
+// Shapes of this kernel.  The units of a launch are 32-bit: a tile of 64 keys costs five, so a sequence has at most
+// 5 (L_max / 64 + 8) for each of its H * N / 128 row blocks.
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
     if (dtype != MCSD_BF16 || rank != kLtRank || rot != kLtRot) return false;
-    const long long per_seq = ((long long)H * N + 127) / 128 * ((long long)L_max / 64 + 6);
+    const long long per_seq = ((long long)H * N + 127) / 128 * 5 * ((long long)L_max / 64 + 8);
     return per_seq * std::min(B, kLtMaxBatch) < (1LL << 30);
 }
 size_t latent_tc_workspace_bytes() {
