@@ -10,16 +10,27 @@
 // largest weight is 1: a sum over V tokens is off by at most V 2^-32 of it (3e-5 for 131072 tokens whose weights all round
 // alike, 2e-8 where they do not).
 //
-// A row is read once and lies in shared memory from then on, split by columns over a cluster of blocks: one block as long as
-// it fits, more where there are fewer rows than multiprocessors.  A cut is found from a histogram over 1024 steps of
-// (max - l), linear over the part that carries mass; the tokens of the step where the sum crosses (some hundred) are
-// collected and placed by counting, every one against every other.  Steps that hold more tokens than that (equal logits,
-// masked ones, steep rows) are split again, in the order of (logit, id), 1024 ways a pass.
+// A row is read from memory once; what looks at it again finds it in L2, so that shared memory holds only what was found, and two
+// blocks share a multiprocessor: one row's chain of short steps runs under the other's.  (With the row in shared memory and one
+// block a multiprocessor 720 rows of 32000 took 103 us, with a row over two blocks 114.)  A block takes a row; where there are fewer
+// rows than multiprocessors a cluster of up to eight takes it, split by columns (a meeting of a cluster costs a microsecond, ten
+// times one of a block).  The first pass finds the largest logit; the second, a comparison a token, picks the few that can decide
+// anything, and all later work is on those:
+//   * top-k: the k-th largest of the threads' own maxima bounds the k-th largest logit from below; the tokens down to that
+//     bound are hardly more than k;
+//   * top-p alone: the tokens from 2^-14 of the largest on; the weights of the others are only added up.  (Where the cut turns
+//     out to be among those, the pass is made again for all tokens.)
+// Tokens that may hold the cut are collected in the cluster's first block: all of them under top-k, under top-p alone those of the
+// step of a histogram (1024 steps of (max - l), linear over the part that carries mass) in which the sum crosses.  On that list
+// the cut is found by dividing its range of places 1024 ways until 32 tokens are left, which a warp compares.  A list that
+// overflows (equal logits, masked ones, a large k) is divided in the same way by passes over the row.
+// Probabilities are zeros and a value for each token that is kept.  They are written last, behind all meetings of the cluster
+// but one that orders nothing: a meeting waits for the writes before it (1 us each).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include <algorithm>
-#include <mutex>
+#include <cstddef>
 
 #include "common.cuh"
 
@@ -27,13 +38,15 @@ namespace cg = cooperative_groups;
 
 namespace mcsd {
 
-constexpr int kSampleThreads = 1024, kSampleWarps = kSampleThreads / 32;
-constexpr int kSampleMaxSegment = 32768;      // tokens of a block
-constexpr int kSampleMaxVocab = 8 * kSampleMaxSegment;
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr int kSampleMaxVocab = 262144;
 constexpr int kChunk = 128;                   // tokens of a partial sum
-constexpr int kBins = 1024;
-constexpr int kListMax = 1024;                // tokens that are placed by counting
+constexpr int kBins = 2 * kSampleThreads;
+constexpr int kListMax = 3000;                // tokens of the first block's list
+constexpr int kPickMax = 4096;                // tokens that a block lists as picked; with more it goes through the row each time
+constexpr int kListK = 2560;                  // top-k that is tried on a list
 constexpr float kBinSpan = 20.0f;             // the first histogram reaches down to exp(-20) of the largest weight
+constexpr float kTail = 14.0f;                // tokens below 2^-14 of the largest are added up without a step of their own
 
 typedef unsigned long long u64;
 
@@ -49,23 +62,32 @@ struct SampleArgs {
 };
 
 struct alignas(16) SampleShared {
-    uint32_t lo[kBins], hi[kBins];            // sums of a step, low and high words
+    u64 list[kListMax];                       // places
+    u64 few[32];
+    alignas(16) uint32_t lo[kBins], hi[kBins];   // sums of a step, low and high words
+    int few_n;
     u64 scan[kSampleWarps];
-    u64 chunk[kSampleMaxSegment / kChunk + 1];
+    u64 chunk[kSampleMaxVocab / kChunk + 1];
     float red[kSampleWarps];
-    u64 total;                                // this block's kept mass
+    int red_live[kSampleWarps];
     float block_max;
-    // decision of a pass
-    int bin;
+    int block_live;                           // tokens that are not -infinity
+    u64 total;                                // this block's kept mass
+    u64 tail;                                 // mass below the steps
+    int bin;                                  // the step that was found, or kBins
     u64 before;                               // mass or count before that step
+    u64 target;
+    float c_hi, c_lo, bin_scale, scale;       // of the row, worked out by one thread: 64-bit arithmetic by all takes microseconds
     u64 range_lo, range_hi;                   // smallest and largest place among the step's tokens (this block's part)
     int list_n;                               // tokens collected (first block of the cluster)
     u64 cut;                                  // place of the last token kept
-    u64 cut_sum;                              // sum up to and with it
-    u64 list_place[kListMax];
-    uint32_t list_f[kListMax];
+    u64 cut_sum;                              // sum of the list's weights up to and with it
+    int picked;                               // tokens picked (more than kPickMax: none are listed)
+    int pick[kPickMax];
+    float pick_l[kPickMax];                   // their logits, later their weights
 };
-static_assert(sizeof(SampleShared) % 16 == 0, "the logits behind it are read as 16-byte vectors");
+static_assert(offsetof(SampleShared, lo) % 8 == 0 && offsetof(SampleShared, hi) % 8 == 0, "steps are read in pairs");
+static_assert(2 * (sizeof(SampleShared) + 1024) <= 228 * 1024, "two blocks a multiprocessor");
 
 // a token's place: smaller is earlier in the order (larger logit, lower id)
 __device__ __forceinline__ u64 place_of(float l, uint32_t id) {
@@ -74,17 +96,45 @@ __device__ __forceinline__ u64 place_of(float l, uint32_t id) {
     return ((u64)(~up) << 32) | id;
 }
 
-struct Row {
-    const float* data;        // this block's logits
-    int n, first;             // how many, id of the first
+template <typename T> __device__ __forceinline__ float logit_of(T x);
+template <> __device__ __forceinline__ float logit_of(float x) { return x; }
+template <> __device__ __forceinline__ float logit_of(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float no_nan(float x) { return isnan(x) ? -INFINITY : x; }
+
+struct Scale {
     float top;                // largest logit of the row
     float c_hi, c_lo;         // log2(e) / T
     float bin_scale;
 };
+template <typename T>
+struct Row : Scale {
+    const T* data;            // this block's logits
+    int n, first;             // how many, id of the first
+    bool vec;                 // four at a time
+    __device__ __forceinline__ float at(int i) const { return no_nan(logit_of<T>(data[i])); }
+    // tokens i .. i + 3, -infinity past the end; i a multiple of four
+    __device__ __forceinline__ float4 four(int i) const {
+        float4 v;
+        if (vec && i + 4 <= n) {
+            if constexpr (sizeof(T) == 4) {
+                v = *reinterpret_cast<const float4*>(data + i);
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(data + i);
+                v = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+            }
+            return make_float4(no_nan(v.x), no_nan(v.y), no_nan(v.z), no_nan(v.w));
+        }
+        v.x = i < n ? at(i) : -INFINITY;
+        v.y = i + 1 < n ? at(i + 1) : -INFINITY;
+        v.z = i + 2 < n ? at(i + 2) : -INFINITY;
+        v.w = i + 3 < n ? at(i + 3) : -INFINITY;
+        return v;
+    }
+};
 
-__device__ __forceinline__ float below_top(const Row& r, float l) { return l == r.top ? 0.0f : r.top - l; }
+__device__ __forceinline__ float below_top(const Scale& r, float l) { return l == r.top ? 0.0f : r.top - l; }
 // exp((l - top) / T) to about two units in the last place: the exponent's rounding is carried along
-__device__ __forceinline__ float weight(const Row& r, float l) {
+__device__ __forceinline__ float weight(const Scale& r, float l) {
     const float d = below_top(r, l), e = d * r.c_hi;
     if (!(e < 140.0f)) return 0.0f;
     const float rest = fmaf(d, r.c_hi, -e) + d * r.c_lo;
@@ -98,11 +148,22 @@ __device__ __forceinline__ uint32_t fixed31(float w) {
     const float t2 = fmaf(rest, 2048.0f, big);
     return (uint32_t)(__float_as_int(t) - 0x4B400000) * 2048u + (uint32_t)(__float_as_int(t2) - 0x4B400000);
 }
-__device__ __forceinline__ int bin_of(const Row& r, float l) {
+__device__ __forceinline__ int bin_of(const Scale& r, float l) {
     const float x = fminf(below_top(r, l) * r.bin_scale, (float)(kBins - 1));  // NaN cannot occur: top is finite or l == top
     return (int)x;
 }
 
+// a logit that lies below all of a step's, by little
+__device__ __forceinline__ float step_floor(const Scale& r, int bin) {
+    if (bin >= kBins - 1) return -INFINITY;
+    const float d = (float)(bin + 1) / r.bin_scale;
+    const float l = r.top - d * 1.00001f;
+    return l - fabsf(l) * 1e-6f > -INFINITY ? l - fabsf(l) * 1e-6f : -INFINITY;    // also where it is no number
+}
+__device__ __forceinline__ float logit_at(u64 place) {                        // the inverse of place_of
+    const uint32_t up = ~(uint32_t)(place >> 32);
+    return __uint_as_float((up & 0x80000000u) ? up ^ 0x80000000u : ~up);
+}
 __device__ __forceinline__ u64 warp_scan(u64 v, int lane) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -123,272 +184,490 @@ __device__ __forceinline__ void hist_add(SampleShared* sh, int bin, uint32_t f) 
     }
 }
 
-__device__ __forceinline__ void clear_hist(SampleShared* sh) {
-    for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { sh->lo[i] = 0; sh->hi[i] = 0; }
-}
-
-// The step in which the sum over steps passes `target`, over all blocks' histograms; every block finds the same.
-// Written to sh->bin and sh->before (sh->before starts as the sum before the first step).
-__device__ void find_bin(SampleShared* sh, cg::cluster_group& cluster, int ranks, u64 start, u64 target) {
-    cluster.sync();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    u64 v = 0;
-    for (int r = 0; r < ranks; ++r) {
-        const SampleShared* o = ranks == 1 ? sh : cluster.map_shared_rank(sh, r);
-        v += ((u64)o->hi[tid] << 32) + o->lo[tid];
-    }
-    if (tid == 0) sh->bin = kBins;                                            // no step: the target is beyond the sum
-    u64 in = warp_scan(v, lane);
-    if (lane == 31) sh->scan[warp] = in;
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) in += sh->scan[w];
-    in += start;
-    if (in - v < target && target <= in) { sh->bin = tid; sh->before = in - v; }
-    cluster.sync();                                                           // histograms have been read, decision is there
-}
-
-// The cut: the token at which the sum of f (MASS) or the count over the order passes `target` (1 .. sum).  `limit` is a cut
-// found before: tokens behind it do not take part.
-template <bool MASS>
-__device__ void select_cut(SampleShared* sh, cg::cluster_group& cluster, int ranks, const Row& r, u64 target, u64 limit) {
+// Picks the tokens whose logit is at least `least`; with TAILS, returns this thread's sum of the others' weights, which are
+// below 2^-10 at most (in steps of 2^-31 below 2^21: added to 1.5 * 2^23 a weight stands in the last places).
+template <bool TAILS, typename T>
+__device__ __forceinline__ u64 pick_tokens(SampleShared* sh, const Row<T>& r, float least) {
     const int tid = threadIdx.x;
-    clear_hist(sh);
-    if (tid == 0) { sh->list_n = 0; sh->range_lo = ~0ull; sh->range_hi = 0; }
     __syncthreads();
-    for (int i = tid; i < r.n; i += kSampleThreads) {
-        const float l = r.data[i];
-        if (l == -INFINITY || place_of(l, r.first + i) > limit) continue;
-        hist_add<MASS>(sh, bin_of(r, l), MASS ? fixed31(weight(r, l)) : 0u);
-    }
-    find_bin(sh, cluster, ranks, 0, target);
-    const int bin = sh->bin;
-    u64 before = sh->before, lo = 0, hi = ~0ull;
-    SampleShared* first = ranks == 1 ? sh : cluster.map_shared_rank(sh, 0);
-    for (;;) {
-        // collect the tokens of the step [lo, hi]; the first block holds the list
-        u64 mn = ~0ull, mx = 0;
-        for (int i = tid; i < r.n; i += kSampleThreads) {
-            const float l = r.data[i];
-            if (l == -INFINITY || bin_of(r, l) != bin) continue;
-            const u64 p = place_of(l, r.first + i);
-            if (p > limit || p < lo || p > hi) continue;
-            mn = min(mn, p);
-            mx = max(mx, p);
-            const int at = atomicAdd(&first->list_n, 1);
-            if (at < kListMax) {
-                first->list_place[at] = p;
-                first->list_f[at] = MASS ? fixed31(weight(r, l)) : 1u;
-            }
-        }
-        if (mn != ~0ull) { atomicMin(&sh->range_lo, mn); atomicMax(&sh->range_hi, mx); }
-        cluster.sync();
-        const int n = first->list_n;
-        if (n <= kListMax) {
-            // place by counting, in the first block: a few threads a token, each a part of the list
-            if (ranks == 1 || cluster.block_rank() == 0) {
-                const int per = max(1, min(32, kSampleThreads / max(n, 1)));
-                int width = 1;
-                while (width * 2 <= per) width *= 2;                          // threads a token: a power of two, inside a warp
-                for (int i0 = 0; i0 < n; i0 += kSampleThreads / width) {
-                    const int i = i0 + tid / width, part = tid % width;
-                    u64 sum = 0;
-                    const u64 p = i < n ? sh->list_place[i] : 0;
-                    if (i < n)
-                        for (int j = part; j < n; j += width)
-                            if (sh->list_place[j] < p) sum += sh->list_f[j];
-                    for (int o = width / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (i < n && part == 0) {
-                        const u64 b = before + sum;
-                        if (b < target && target <= b + sh->list_f[i]) { sh->cut = p; sh->cut_sum = b + sh->list_f[i]; }
-                    }
+    if (tid == 0) sh->picked = 0;
+    __syncthreads();
+    u64 tail = 0;
+    for (int base0 = 4 * tid; base0 < r.n; base0 += 32 * kSampleThreads) {        // a bit a token, 32 tokens of a thread at a time
+        uint32_t picks = 0;
+        float4 v4[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) v4[it] = r.four(base0 + it * 4 * kSampleThreads);
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const float v[4] = {v4[it].x, v4[it].y, v4[it].z, v4[it].w};
+            uint32_t bits = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool take = v[j] >= least && v[j] != -INFINITY;
+                picks |= take ? 1u << (4 * it + j) : 0u;
+                if (TAILS) {
+                    float w;
+                    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"((v[j] - r.top) * r.c_hi));
+                    const uint32_t f = (uint32_t)__float_as_int(fmaf(w, 2147483648.0f, 12582912.0f)) - 0x4B400000u;
+                    bits += take || v[j] == -INFINITY ? 0u : f;
                 }
             }
-            cluster.sync();
-            if (ranks > 1 && cluster.block_rank() != 0 && tid == 0) { sh->cut = first->cut; sh->cut_sum = first->cut_sum; }
-            cluster.sync();
+            if (TAILS) tail += bits;
+        }
+        if (picks) {
+            int at = atomicAdd(&sh->picked, __popc(picks));
+            for (; picks; picks &= picks - 1, ++at) {
+                const int bit = __ffs(picks) - 1, i = base0 + (bit >> 2) * 4 * kSampleThreads + (bit & 3);
+                if (at < kPickMax) sh->pick[at] = i;
+            }
+        }
+    }
+    __syncthreads();
+    const int n = min(sh->picked, kPickMax);
+    for (int j = tid; j < n; j += kSampleThreads) sh->pick_l[j] = r.at(sh->pick[j]);      // (each thread reads its own later)
+    return tail;
+}
+// f(token, its logit) for the picked tokens
+template <typename T, typename F>
+__device__ __forceinline__ void for_picked(SampleShared* sh, const Row<T>& r, float least, F f) {
+    const int n = sh->picked;
+    if (n <= kPickMax) {
+        for (int j = threadIdx.x; j < n; j += kSampleThreads) f(sh->pick[j], sh->pick_l[j]);
+    } else {
+        for (int i = threadIdx.x; i < r.n; i += kSampleThreads) {
+            const float l = r.at(i);
+            if (l >= least && l != -INFINITY) f(i, l);
+        }
+    }
+}
+
+__device__ __forceinline__ u64 share_of(u64 whole, double share) { return min(whole, max((u64)1, (u64)ceil((double)whole * share))); }
+// Sums of the block's warps before this one, from `sums` (a warp each), and of all.
+__device__ __forceinline__ u64 warps_before(const u64* sums, u64& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const u64 own = lane < kSampleWarps ? sums[lane] : 0, in = warp_scan(own, lane);
+    total = __shfl_sync(0xffffffffu, in, 31);
+    return __shfl_sync(0xffffffffu, in - own, warp);
+}
+
+// Blocks of a row: all meet, shared memory of any of them.
+struct Blocks {
+    int n, rank;
+    __device__ __forceinline__ void sync() const {
+        if (n == 1) __syncthreads();
+        else cg::this_cluster().sync();
+    }
+    __device__ __forceinline__ void leave() const {
+        if (n > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    }
+    __device__ __forceinline__ SampleShared* at(SampleShared* sh, int r) const { return n == 1 ? sh : cg::this_cluster().map_shared_rank(sh, r); }
+};
+
+__device__ __forceinline__ void clear_steps(SampleShared* sh) {
+    for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { sh->lo[i] = 0; sh->hi[i] = 0; }
+    if (threadIdx.x == 0) sh->tail = 0;
+    __syncthreads();
+}
+// (other blocks read the steps and the list's length: not before they have met)
+__device__ __forceinline__ void clear_pass(SampleShared* sh) {
+    if (threadIdx.x == 0) { sh->list_n = 0; sh->range_lo = ~0ull; sh->range_hi = 0; }
+    clear_steps(sh);
+}
+
+// The step in which the sum over steps passes the target, over all blocks' histograms; every block finds the same.  The target
+// is `target`, or with share >= 0 that part of the whole sum.  Written to sh->bin (kBins: beyond the steps), sh->before, sh->target.
+__device__ void find_bin(SampleShared* sh, const Blocks& blocks, u64 start, u64 target, double share) {
+    blocks.sync();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    u64 v0 = 0, v1 = 0, tail = 0;
+    for (int r = 0; r < blocks.n; ++r) {
+        const SampleShared* o = blocks.at(sh, r);
+        const uint2 lo = *reinterpret_cast<const uint2*>(&o->lo[2 * tid]), hi = *reinterpret_cast<const uint2*>(&o->hi[2 * tid]);
+        v0 += ((u64)hi.x << 32) + lo.x;
+        v1 += ((u64)hi.y << 32) + lo.y;
+        tail += o->tail;
+    }
+    u64 in = warp_scan(v0 + v1, lane);
+    if (lane == 31) sh->scan[warp] = in;
+    __syncthreads();
+    u64 total;
+    in += start + warps_before(sh->scan, total);
+    if (tid == 0) {
+        sh->bin = kBins;
+        sh->target = share >= 0.0 ? share_of(start + total + tail, share) : target;
+    }
+    __syncthreads();
+    target = sh->target;
+    const u64 mid = in - v1;
+    if (mid - v0 < target && target <= mid) { sh->bin = 2 * tid; sh->before = mid - v0; }
+    if (mid < target && target <= in) { sh->bin = 2 * tid + 1; sh->before = mid; }
+    __syncthreads();      // (other blocks may still read this block's histogram: its next change comes behind another meeting)
+}
+
+// On a short list (n at most kShort, by its block alone) every token is compared with every other: the first `count` of them in the
+// order are kept, and of those the ones before which the sum, `before` included, is below the target: `target`, or with share >= 0
+// that part of their sum.  Written to sh->cut and sh->cut_sum.
+constexpr int kShort = 256;
+__device__ void short_list(SampleShared* sh, const Scale& r, int n, u64 before, u64 target, u64 count, double share) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __syncthreads();
+    const u64 p = tid < n ? sh->list[tid] : ~0ull;
+    const uint32_t f = tid < n ? fixed31(weight(r, logit_at(p))) : 0u;
+    if (tid < n) sh->lo[tid] = f;
+    __syncthreads();
+    u64 sum = 0;
+    uint32_t rank = 0;
+    if (tid < n) {
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const bool earlier = sh->list[j] < p;
+            rank += earlier;
+            sum += earlier ? sh->lo[j] : 0u;
+        }
+    }
+    const bool keep = tid < n && (u64)rank < count;
+    if (share >= 0.0) {
+        u64 all = keep ? f : 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        if (lane == 0) sh->scan[warp] = all;
+        __syncthreads();
+        warps_before(sh->scan, all);
+        if (tid == 0) sh->target = share_of(before + all, share);
+        __syncthreads();
+        target = sh->target;
+    }
+    sum += before;
+    // the last token kept: nothing kept behind it
+    const bool in = keep && sum < target;
+    if (in && ((u64)rank + 1 == min((u64)n, count) || sum + f >= target)) { sh->cut = p; sh->cut_sum = sum + f; }
+    __syncthreads();
+}
+
+// The cut of the first block's list of n places (by that block alone): the place at which the sum of f (MASS) or the count, over
+// places up to `limit` and from `before` on, reaches the target.  Written to sh->cut, the sum up to and with it to sh->cut_sum.
+template <bool MASS>
+__device__ void list_cut(SampleShared* sh, const Scale& r, int n, u64 before, u64 target, u64 limit) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    const Blocks alone{1, 0};
+    if (MASS && n <= kShort && limit == ~0ull) {
+        short_list(sh, r, n, before, target, ~0ull, -1.0);
+        return;
+    }
+    u64 lo = ~0ull, hi = 0;
+    __syncthreads();
+    if (tid == 0) { sh->range_lo = ~0ull; sh->range_hi = 0; sh->few_n = 0; }
+    __syncthreads();
+    for (int i = tid; i < n; i += kSampleThreads) {
+        const u64 p = sh->list[i];
+        if (p <= limit) { lo = min(lo, p); hi = max(hi, p); }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+        hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    if (lane == 0) { atomicMin(&sh->range_lo, lo); atomicMax(&sh->range_hi, hi); }
+    __syncthreads();
+    lo = sh->range_lo;
+    hi = sh->range_hi;
+    for (;;) {
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const u64 p = sh->list[i];
+            if (p < lo || p > hi) continue;
+            const int at = atomicAdd(&sh->few_n, 1);
+            if (at < 32) sh->few[at] = p;
+        }
+        __syncthreads();
+        const int m = sh->few_n;
+        if (m <= 32) {
+            if (tid < 32) {
+                const u64 p = lane < m ? sh->few[lane] : ~0ull;
+                const uint32_t f = lane < m ? (MASS ? fixed31(weight(r, logit_at(p))) : 1u) : 0u;
+                u64 sum = before;
+                for (int j = 0; j < m; ++j) {
+                    const u64 pj = __shfl_sync(0xffffffffu, p, j);
+                    const uint32_t fj = __shfl_sync(0xffffffffu, f, j);
+                    if (pj < p) sum += fj;
+                }
+                if (lane < m && sum < target && target <= sum + f) { sh->cut = p; sh->cut_sum = sum + f; }
+            }
+            __syncthreads();
+            return;
+        }
+        int shift = 0;
+        while (((hi - lo) >> shift) >= (u64)kBins) ++shift;
+        clear_steps(sh);
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const u64 p = sh->list[i];
+            if (p >= lo && p <= hi) hist_add<MASS>(sh, (int)((p - lo) >> shift), MASS ? fixed31(weight(r, logit_at(p))) : 0u);
+        }
+        find_bin(sh, alone, before, target, -1.0);
+        before = sh->before;
+        lo += (u64)sh->bin << shift;
+        hi = min(hi, lo + (((u64)1 << shift) - 1));
+        if (tid == 0) sh->few_n = 0;
+        __syncthreads();
+    }
+}
+// Both filters on a list that holds every token they keep: the first `count` of it, then, with share >= 0, that part of their mass.
+__device__ void list_filters(SampleShared* sh, const Scale& r, int n, u64 count, double share) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (n <= kShort) {
+        short_list(sh, r, n, 0, ~0ull, count, share);
+        return;
+    }
+    list_cut<false>(sh, r, n, 0, count, ~0ull);
+    const u64 limit = sh->cut;
+    u64 sum = 0;
+    for (int i = tid; i < n; i += kSampleThreads) {
+        const u64 p = sh->list[i];
+        if (p <= limit) sum += fixed31(weight(r, logit_at(p)));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    __syncthreads();
+    if (lane == 0) sh->scan[warp] = sum;
+    __syncthreads();
+    u64 total;
+    warps_before(sh->scan, total);
+    if (share >= 0.0) {
+        if (tid == 0) sh->target = share_of(total, share);
+        __syncthreads();
+        list_cut<true>(sh, r, n, 0, sh->target, limit);
+    } else {
+        __syncthreads();
+        if (tid == 0) { sh->cut = limit; sh->cut_sum = total; }
+    }
+}
+
+// Collects the picked tokens for which `take` says so in the first block's list; returns how many there are (the list holds
+// kListMax).
+template <typename T, typename F>
+__device__ __forceinline__ int collect(SampleShared* sh, const Blocks& blocks, const Row<T>& r, float least, F take) {
+    SampleShared* first = blocks.at(sh, 0);
+    u64 mn = ~0ull, mx = 0;
+    for_picked(sh, r, least, [&](int i, float l) {
+        if (!take(l, i)) return;
+        const u64 p = place_of(l, r.first + i);
+        mn = min(mn, p);
+        mx = max(mx, p);
+        const int at = atomicAdd(&first->list_n, 1);
+        if (at < kListMax) first->list[at] = p;
+    });
+    if (mn != ~0ull) { atomicMin(&sh->range_lo, mn); atomicMax(&sh->range_hi, mx); }
+    blocks.sync();
+    return first->list_n;
+}
+
+// The cut: the token at which the sum of weights (MASS) or the count over the order passes the target: `target`, or with
+// share >= 0 that part of the whole.  `limit` is a cut found before: tokens behind it do not take part.  The picked tokens (those
+// from `least` on) hold the cut; with `tails` that is not known yet, and `least` may be lowered.  The first block has the result,
+// before the next meeting.
+template <bool MASS, typename T>
+__device__ void select_cut(SampleShared* sh, const Blocks& blocks, const Row<T>& r, u64 target, double share, u64 limit, bool tails,
+                           float& least) {
+    const int lane = threadIdx.x & 31;
+    for (;;) {
+        clear_pass(sh);
+        if (tails) {
+            u64 tail = pick_tokens<true, T>(sh, r, least);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) tail += __shfl_xor_sync(0xffffffffu, tail, o);
+            if (lane == 0 && tail) atomicAdd(&sh->tail, tail);
+        }
+        for_picked(sh, r, least, [&](int i, float l) {
+            if (limit != ~0ull && place_of(l, r.first + i) > limit) return;
+            hist_add<MASS>(sh, bin_of(r, l), MASS ? fixed31(weight(r, l)) : 0u);
+        });
+        find_bin(sh, blocks, 0, target, share);
+        if (sh->bin < kBins || !tails) break;
+        least = -INFINITY;                               // among the small ones: all tokens, exactly
+        tails = false;
+        pick_tokens<false, T>(sh, r, least);
+        blocks.sync();
+    }
+    target = sh->target;
+    const int bin = sh->bin;
+    u64 before = sh->before, lo = 0, hi = ~0ull;
+    for (;;) {
+        const int n = collect(sh, blocks, r, least, [&](float l, int i) {
+            if (bin_of(r, l) != bin) return false;
+            const u64 p = place_of(l, r.first + i);
+            return p <= limit && p >= lo && p <= hi;
+        });
+        if (n <= kListMax) {
+            if (blocks.rank == 0) list_cut<MASS>(sh, r, n, before, target, ~0ull);
             return;
         }
         // too many: split the range of places
         u64 a = ~0ull, z = 0;
-        for (int k = 0; k < ranks; ++k) {
-            const SampleShared* o = ranks == 1 ? sh : cluster.map_shared_rank(sh, k);
+        for (int k = 0; k < blocks.n; ++k) {
+            const SampleShared* o = blocks.at(sh, k);
             a = min(a, o->range_lo);
             z = max(z, o->range_hi);
         }
-        cluster.sync();
+        blocks.sync();
         int shift = 0;
         while (((z - a) >> shift) >= (u64)kBins) ++shift;
-        clear_hist(sh);
-        if (tid == 0) { sh->list_n = 0; sh->range_lo = ~0ull; sh->range_hi = 0; }
-        __syncthreads();
-        for (int i = tid; i < r.n; i += kSampleThreads) {
-            const float l = r.data[i];
-            if (l == -INFINITY || bin_of(r, l) != bin) continue;
+        clear_pass(sh);
+        for_picked(sh, r, least, [&](int i, float l) {
+            if (bin_of(r, l) != bin) return;
             const u64 p = place_of(l, r.first + i);
-            if (p > limit || p < a || p > z) continue;
+            if (p > limit || p < a || p > z) return;
             hist_add<MASS>(sh, (int)((p - a) >> shift), MASS ? fixed31(weight(r, l)) : 0u);
-        }
-        find_bin(sh, cluster, ranks, before, target);
+        });
+        find_bin(sh, blocks, before, target, -1.0);
         before = sh->before;
         lo = a + ((u64)sh->bin << shift);
         hi = min(z, lo + (((u64)1 << shift) - 1));
-        __syncthreads();
+        blocks.sync();
+        clear_pass(sh);                                                       // the list starts anew
+        blocks.sync();
     }
 }
-
-// sum of f over the cluster's tokens up to `limit`
-__device__ u64 mass_up_to(SampleShared* sh, cg::cluster_group& cluster, int ranks, const Row& r, u64 limit) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    u64 sum = 0;
-    for (int i = tid; i < r.n; i += kSampleThreads) {
-        const float l = r.data[i];
-        if (l != -INFINITY && place_of(l, r.first + i) <= limit) sum += fixed31(weight(r, l));
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) sh->scan[warp] = sum;
-    __syncthreads();
-    if (warp == 0) {
-        u64 v = sh->scan[lane];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) sh->total = v;
-    }
-    cluster.sync();
-    u64 all = 0;
-    for (int k = 0; k < ranks; ++k) all += (ranks == 1 ? sh : cluster.map_shared_rank(sh, k))->total;
-    cluster.sync();
-    return all;
-}
-
-template <typename T> __device__ __forceinline__ float logit_of(T x);
-template <> __device__ __forceinline__ float logit_of(float x) { return x; }
-template <> __device__ __forceinline__ float logit_of(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // grid: rows * cluster size
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads, 1) sample_kernel(const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a) {
     extern __shared__ float4 raw4[];
     SampleShared* sh = reinterpret_cast<SampleShared*>(raw4);
-    float* data = reinterpret_cast<float*>(sh + 1);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const long long row = blockIdx.x / ranks;
+    Blocks blocks;
+    blocks.n = (int)cg::this_cluster().num_blocks();
+    blocks.rank = (int)cg::this_cluster().block_rank();
+    const int rank = blocks.rank;
+    const long long row = blockIdx.x / blocks.n;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int first = rank * a.segment, n = max(0, min(a.segment, a.V - first));
     const T* src = static_cast<const T*>(a.logits) + row * a.row_stride + first;
 
-    // ---- the row into shared memory, NaN as -infinity, and its largest logit
-    float mx = -INFINITY;
-    constexpr int kVec = 16 / sizeof(T);
-    int done = 0;
-    if (a.vec_in) {
-        done = n / kVec * kVec;
-#pragma unroll 4
-        for (int i = tid * kVec; i < done; i += kSampleThreads * kVec) {
-            alignas(16) T t[kVec];
-            *reinterpret_cast<uint4*>(t) = __ldcs(reinterpret_cast<const uint4*>(src + i));
-            float v[kVec];
-#pragma unroll
-            for (int j = 0; j < kVec; ++j) {
-                v[j] = logit_of<T>(t[j]);
-                if (isnan(v[j])) v[j] = -INFINITY;
-                mx = fmaxf(mx, v[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < kVec; j += 4) *reinterpret_cast<float4*>(data + i + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-        }
-    }
-#pragma unroll 8
-    for (int i = done + tid; i < n; i += kSampleThreads) {
-        float v = logit_of<T>(src[i]);
-        if (isnan(v)) v = -INFINITY;
-        mx = fmaxf(mx, v);
-        data[i] = v;
-    }
-    const int padded = (n + kChunk - 1) / kChunk * kChunk;
-    for (int i = n + tid; i < padded; i += kSampleThreads) data[i] = -INFINITY;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    if (lane == 0) sh->red[warp] = mx;
-    __syncthreads();
-    if (warp == 0) {
-        float v = sh->red[lane];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-        if (lane == 0) sh->block_max = v;
-    }
-    cluster.sync();
-    float top = -INFINITY;
-    for (int k = 0; k < ranks; ++k) top = fmaxf(top, (ranks == 1 ? sh : cluster.map_shared_rank(sh, k))->block_max);
-
-    // ---- the filters of this row
     const float T_in = a.temperature ? a.temperature[row] : 1.0f;
     const bool greedy = !(T_in > 0.0f);
-    const double inv = 1.4426950408889634 / (greedy ? 1.0 : (double)T_in);
-    Row r;
-    r.data = data; r.n = n; r.first = first; r.top = top;
-    r.c_hi = (float)fmin(inv, 1e38);                     // a temperature near zero: finite, so that the top keeps weight 1
-    r.c_lo = inv < 1e38 ? (float)(inv - (double)r.c_hi) : 0.0f;
-    r.bin_scale = fminf((float)((double)kBins / (kBinSpan * (greedy ? 1.0 : (double)T_in))), 1e30f);
-    int k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-    const float tp = greedy || !a.top_p ? 1.0f : a.top_p[row], mp = greedy || !a.min_p ? 0.0f : a.min_p[row];
-    u64 cut = ~0ull;
-    if (top > -INFINITY) {
-        if (k > 0 && k < a.V) {
-            // fewer than k tokens may be left of a masked row: find_bin then reports no step
-            clear_hist(sh);
-            __syncthreads();
-            int mine = 0;
-            for (int i = tid; i < n; i += kSampleThreads) mine += data[i] != -INFINITY;
-            mine = __reduce_add_sync(0xffffffffu, mine);
-            if (lane == 0) atomicAdd(&sh->lo[0], (uint32_t)mine);
-            cluster.sync();
-            u64 live = 0;
-            for (int q = 0; q < ranks; ++q) live += (ranks == 1 ? sh : cluster.map_shared_rank(sh, q))->lo[0];
-            cluster.sync();
-            if ((u64)k < live) {
-                select_cut<false>(sh, cluster, ranks, r, (u64)k, ~0ull);
-                cut = sh->cut;
-            }
+    if (tid == kSampleThreads - 1) {
+        const double t = greedy ? 1.0 : (double)T_in, inv = 1.4426950408889634 / t;
+        sh->c_hi = (float)fmin(inv, 1e38);               // a temperature near zero: finite, so that the top keeps weight 1
+        sh->c_lo = inv < 1e38 ? (float)(inv - (double)sh->c_hi) : 0.0f;
+        sh->bin_scale = fminf((float)((double)kBins / (kBinSpan * t)), 1e30f);
+    }
+    // ---- the row's largest logit, and how many are not -infinity (NaN counts as that)
+    Row<T> r;
+    r.data = src; r.n = n; r.first = first; r.vec = a.vec_in;
+    const float u_first = a.tokens && warp < a.K ? a.u[row * a.K + warp] : 0.0f;      // the warp's first draw
+    float mine = -INFINITY;
+    int live = 0;
+    for (int base = 4 * tid; base < n; base += 32 * kSampleThreads) {
+        float4 v[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) v[it] = r.four(base + it * 4 * kSampleThreads);
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            mine = fmaxf(mine, fmaxf(fmaxf(v[it].x, v[it].y), fmaxf(v[it].z, v[it].w)));
+            live += (v[it].x != -INFINITY) + (v[it].y != -INFINITY) + (v[it].z != -INFINITY) + (v[it].w != -INFINITY);
         }
-        if (tp < 1.0f) {
-            const u64 total = mass_up_to(sh, cluster, ranks, r, cut);
-            const double want = ceil((double)total * (double)fmaxf(tp, 0.0f));
-            const u64 target = min(total, max((u64)1, (u64)want));
-            select_cut<true>(sh, cluster, ranks, r, target, cut);
-            cut = sh->cut;
-        }
+    }
+    const int padded = (n + kChunk - 1) / kChunk * kChunk;
+    float mx = mine;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    live = __reduce_add_sync(0xffffffffu, live);
+    if (lane == 0) { sh->red[warp] = mx; sh->red_live[warp] = live; }
+    __syncthreads();
+    if (warp == 0) {
+        float v = lane < kSampleWarps ? sh->red[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+        const int c = __reduce_add_sync(0xffffffffu, lane < kSampleWarps ? sh->red_live[lane] : 0);
+        if (lane == 0) { sh->block_max = v; sh->block_live = c; }
+    }
+    blocks.sync();
+    float top = -INFINITY;
+    live = 0;
+    for (int k = 0; k < blocks.n; ++k) {
+        const SampleShared* o = blocks.at(sh, k);
+        top = fmaxf(top, o->block_max);
+        live += o->block_live;
     }
 
-    // ---- weights of what is kept, their sums by chunks of 128
-    __syncthreads();
+    // ---- the filters of this row
+    r.top = top;
+    r.c_hi = sh->c_hi; r.c_lo = sh->c_lo; r.bin_scale = sh->bin_scale;
+    int k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+    if (k >= live) k = 0;                                // off
+    const float tp = greedy || !a.top_p ? 1.0f : a.top_p[row], mp = greedy || !a.min_p ? 0.0f : a.min_p[row];
+    const double share = tp < 1.0f ? (double)fmaxf(tp, 0.0f) : -1.0;
+    float* dst = a.probs ? a.probs + row * a.V + first : nullptr;
+    const bool sparse = top > -INFINITY && (k > 0 || share >= 0.0);      // what is kept are some of the picked tokens
+    u64 cut = ~0ull;
+    float least = -INFINITY;
+    if (sparse) {
+        bool found = false;
+        if (k > 0) {
+            clear_pass(sh);
+            if (mine != -INFINITY) atomicAdd(&sh->lo[bin_of(r, mine)], 1u);
+            find_bin(sh, blocks, 0, (u64)k, -1.0);
+            const int step = sh->bin;                    // kBins where fewer than k threads have a token
+            least = step_floor(r, step);
+            pick_tokens<false, T>(sh, r, least);
+            if (k <= kListK && step < kBins) {
+                const int got = collect(sh, blocks, r, least, [&](float l, int) { return bin_of(r, l) <= step; });
+                found = got <= kListMax;
+                if (found && rank == 0) list_filters(sh, r, got, (u64)k, share);
+            }
+            if (!found) {
+                blocks.sync();                           // all have seen it: the list may start anew
+                select_cut<false>(sh, blocks, r, (u64)k, -1.0, ~0ull, false, least);
+                blocks.sync();
+                cut = blocks.at(sh, 0)->cut;
+            }
+        }
+        if (!found && share >= 0.0) {
+            blocks.sync();
+            if (k == 0) {
+                least = r.top - kTail / r.c_hi;
+                if (!(least > -INFINITY)) least = -INFINITY;
+                if (top == INFINITY) least = INFINITY;   // nothing else carries mass
+            }
+            select_cut<true>(sh, blocks, r, 0, share, cut, k == 0, least);
+        }
+        blocks.sync();
+        cut = blocks.at(sh, 0)->cut;
+    }
+
+    // ---- weights of what is kept, and their sums by chunks of 128
     const float floor_w = mp > 0.0f ? fminf(mp, 1.0f) : 0.0f;
     const int chunks = padded / kChunk;
-    for (int c = warp; c < chunks; c += kSampleWarps) {
-        float4 v = *reinterpret_cast<const float4*>(data + c * kChunk + lane * 4);
-        float* e = reinterpret_cast<float*>(&v);
-        uint32_t hi = 0, lo = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float l = e[j];
-            float w = 0.0f;
-            if (l != -INFINITY && place_of(l, first + c * kChunk + lane * 4 + j) <= cut) {
-                w = weight(r, l);
-                if (w < floor_w) w = 0.0f;
-            }
-            e[j] = w;
-            const uint32_t f = fixed31(w);
-            hi += f >> 16;
-            lo += f & 0xffffu;
+    const bool listed = sparse && sh->picked <= kPickMax;
+    auto kept_weight = [&](float l, int i) -> float {
+        if (l == -INFINITY || (cut != ~0ull && place_of(l, first + i) > cut)) return 0.0f;
+        const float w = weight(r, l);
+        return w < floor_w ? 0.0f : w;
+    };
+    auto four_weights = [&](int i) -> float4 {
+        const float4 v = r.four(i);
+        return make_float4(kept_weight(v.x, i), kept_weight(v.y, i + 1), kept_weight(v.z, i + 2), kept_weight(v.w, i + 3));
+    };
+    if (listed) {
+        for (int i = tid; i <= chunks; i += kSampleThreads) sh->chunk[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < sh->picked; j += kSampleThreads) {
+            const int i = sh->pick[j];
+            const float w = kept_weight(sh->pick_l[j], i);
+            sh->pick_l[j] = w;
+            if (w > 0.0f) atomicAdd(&sh->chunk[i / kChunk + 1], (u64)fixed31(w));
         }
-        *reinterpret_cast<float4*>(data + c * kChunk + lane * 4) = v;
-        hi = __reduce_add_sync(0xffffffffu, hi);
-        lo = __reduce_add_sync(0xffffffffu, lo);
-        if (lane == 0) sh->chunk[c + 1] = ((u64)hi << 16) + lo;
+    } else {
+        __syncthreads();
+        for (int c = warp; c < chunks; c += kSampleWarps) {
+            const float4 v = four_weights(c * kChunk + lane * 4);
+            const uint32_t f0 = fixed31(v.x), f1 = fixed31(v.y), f2 = fixed31(v.z), f3 = fixed31(v.w);
+            const uint32_t hi = __reduce_add_sync(0xffffffffu, (f0 >> 16) + (f1 >> 16) + (f2 >> 16) + (f3 >> 16));
+            const uint32_t lo = __reduce_add_sync(0xffffffffu, (f0 & 0xffffu) + (f1 & 0xffffu) + (f2 & 0xffffu) + (f3 & 0xffffu));
+            if (lane == 0) sh->chunk[c + 1] = ((u64)hi << 16) + lo;
+        }
     }
     __syncthreads();
-    if (warp == 0) {                                     // running sums of at most 256 chunks
+    if (warp == 0) {                                     // running sums of the chunks
         u64 base = 0;
         if (lane == 0) sh->chunk[0] = 0;
         for (int c0 = 0; c0 < chunks; c0 += 32) {
@@ -399,14 +678,16 @@ __global__ void __launch_bounds__(kSampleThreads, 1) sample_kernel(const __grid_
         }
         if (lane == 0) sh->total = base;
     }
-    cluster.sync();
+    blocks.sync();
     u64 all = 0, mine0 = 0;
-    for (int q = 0; q < ranks; ++q) {
-        const u64 t = (ranks == 1 ? sh : cluster.map_shared_rank(sh, q))->total;
+    for (int q = 0; q < blocks.n; ++q) {
+        const u64 t = blocks.at(sh, q)->total;
         if (q < rank) mine0 += t;
         all += t;
     }
     const u64 mine1 = mine0 + sh->total;
+    if (tid == kSampleThreads - 1) sh->scale = all ? (float)(2147483648.0 / (double)all) : 0.0f;
+    __syncthreads();
 
     // ---- draws: the first token at which the running sum passes u * sum
     if (a.tokens) {
@@ -416,8 +697,12 @@ __global__ void __launch_bounds__(kSampleThreads, 1) sample_kernel(const __grid_
                 if (rank == 0 && lane == 0) *out = -1;
                 continue;
             }
-            const double x = (double)a.u[row * a.K + j] * (double)all;
-            const u64 t = x > 0.0 ? min(all - 1, (u64)x) : 0;
+            u64 t = 0;
+            if (lane == 0) {
+                const double x = (double)(j < kSampleWarps ? u_first : a.u[row * a.K + j]) * (double)all;
+                if (x > 0.0) t = min(all - 1, (u64)x);
+            }
+            t = __shfl_sync(0xffffffffu, t, 0);
             if (t < mine0 || t >= mine1) continue;       // another block's
             const u64 at = t - mine0;
             int lo = 0, hi = chunks;                     // chunk[lo] <= at < chunk[hi]
@@ -425,7 +710,7 @@ __global__ void __launch_bounds__(kSampleThreads, 1) sample_kernel(const __grid_
                 const int mid = (lo + hi) >> 1;
                 if (sh->chunk[mid] <= at) lo = mid; else hi = mid;
             }
-            const float4 v = *reinterpret_cast<const float4*>(data + lo * kChunk + lane * 4);
+            const float4 v = four_weights(lo * kChunk + lane * 4);
             const float e[4] = {v.x, v.y, v.z, v.w};
             u64 own = 0;
 #pragma unroll
@@ -445,20 +730,28 @@ __global__ void __launch_bounds__(kSampleThreads, 1) sample_kernel(const __grid_
         }
     }
     // ---- probabilities
-    if (a.probs) {
-        const float scale = all ? (float)(2147483648.0 / (double)all) : 0.0f;
-        float* dst = a.probs + row * a.V + first;
-        if (a.vec_out) {
+    if (dst) {
+        const float scale = sh->scale;
+        if (listed) {                                    // zeros, and the few values between them
+            if (a.vec_out) {
+                for (int i = tid * 4; i < n; i += kSampleThreads * 4) __stcs(reinterpret_cast<float4*>(dst + i), make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+            } else {
+                for (int i = tid; i < n; i += kSampleThreads) __stcs(dst + i, 0.0f);
+            }
+            __syncthreads();
+            for (int j = tid; j < sh->picked; j += kSampleThreads)
+                if (sh->pick_l[j] > 0.0f) __stcs(dst + sh->pick[j], sh->pick_l[j] * scale);
+        } else if (a.vec_out) {
             for (int i = tid * 4; i < n; i += kSampleThreads * 4) {
-                float4 v = *reinterpret_cast<const float4*>(data + i);
+                float4 v = four_weights(i);
                 v.x *= scale; v.y *= scale; v.z *= scale; v.w *= scale;
                 __stcs(reinterpret_cast<float4*>(dst + i), v);
             }
         } else {
-            for (int i = tid; i < n; i += kSampleThreads) __stcs(dst + i, data[i] * scale);
+            for (int i = tid; i < n; i += kSampleThreads) __stcs(dst + i, kept_weight(r.at(i), i) * scale);
         }
     }
-    cluster.sync();                                      // no block leaves while another may read its shared memory
+    blocks.leave();                                      // no block leaves while another may read its shared memory
 }
 
 }  // namespace mcsd
@@ -473,9 +766,8 @@ extern "C" int mcsd_sample_candidates(const void* logits, long long row_stride, 
     int dev = 0, sms = 0;
     MCSD_CUDA_CHECK(cudaGetDevice(&dev));
     MCSD_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    // blocks a row: enough for the row to fit, then more while there are multiprocessors without a row
+    // blocks a row: more while there are multiprocessors without a row
     int c = 1;
-    while ((long long)c * mcsd::kSampleMaxSegment < V) c *= 2;
     while (c < 8 && (long long)rows * c * 2 <= sms && V / (c * 2) >= 1024) c *= 2;
     mcsd::SampleArgs a{};
     a.logits = logits; a.row_stride = row_stride;
@@ -486,7 +778,7 @@ extern "C" int mcsd_sample_candidates(const void* logits, long long row_stride, 
     const int elt = dtype == MCSD_F32 ? 4 : 2;
     a.vec_in = (reinterpret_cast<uintptr_t>(logits) & 15u) == 0 && (row_stride * elt) % 16 == 0;
     a.vec_out = probs && (reinterpret_cast<uintptr_t>(probs) & 15u) == 0 && V % 4 == 0;
-    const int smem = (int)sizeof(mcsd::SampleShared) + a.segment * (int)sizeof(float);
+    const int smem = (int)sizeof(mcsd::SampleShared);
     auto kernel = dtype == MCSD_F32 ? mcsd::sample_kernel<float> : mcsd::sample_kernel<__nv_bfloat16>;
     MCSD_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     cudaLaunchConfig_t cfg = {};
