@@ -21,9 +21,13 @@
 // sequence's end ever meets a product.
 //
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
-// inside an item, the pieces write unnormalised rows and count themselves in.  At the end of its range a pair waits for the
-// other pieces of such an item and joins a share of its channels.  (All blocks run at a time: one a multiprocessor, no more
+// inside an item, the pieces write unnormalised rows and count themselves in.  An item of two or three pieces is joined by the
+// pair that starts it, from tensor memory: the others wrote theirs early, as the first of their ranges.  Where there are more, a
+// pair at the end of its range waits for the other pieces of such an item and joins a share of its channels.  (All blocks run at a time: one a multiprocessor, no more
 // pairs than fit.)  Tiles are 256 keys, or 128 or 64 where there would be fewer tiles than pairs.
+//
+// The five roles run side by side, each its own loop: unrolled, they did not fit the instruction caches, and a tile took 4.9 us
+// instead of 3.4 (the loops of S over nine chunks and of O over four quarters are rolled for that alone).
 //
 // Warps of a block: 0 loads for S, 1 issues it, 2 loads for O, 3 issues it (1 and 3 in the first block of the pair), 4 to 11
 // fetch queries, do the softmax and the output.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
@@ -46,6 +50,7 @@ constexpr int kLtKeySlots = 4, kLtValueSlots = 3, kLtSlots = kLtKeySlots + kLtVa
 constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;      // queries, weights of a tile
 constexpr int kLtMaxBatch = 256;
 constexpr int kLtMaxPairs = kTcMaxBlocks / 2;
+constexpr int kLtFew = 3;                            // pieces of an item that are joined by the pair that starts it
 constexpr int kLtColO = 0, kLtColS = 256;            // tensor memory: O 256 columns, S 128 twice
 
 struct LtParams {
@@ -65,7 +70,7 @@ struct LtSmall {
     unsigned long long s_full[2], s_free[2], p_full[4], p_free[4], pv_done, q_full;
     uint32_t tmem_base;
     int abort_flag;
-    int tile_keys, pairs;                            // keys of a tile, pairs with work
+    int tile_shift, pairs;                           // keys of a tile (their logarithm), pairs with work
     int join_ready;
     int total;                                       // units of the launch
     int sums[3];                                     // tiles of the launch with 256, 128, 64 keys a tile
@@ -145,12 +150,13 @@ __device__ __forceinline__ int lt_nodes(const LatentArgs& a, int b) { return a.n
 // The tiles of an item: full prefix tiles, a shorter one, full tree tiles, a shorter one.
 struct LtShape {
     int full, rest_cost, tree_full, tree_rest_cost, cost;      // cost of a full tile
-    __host__ __device__ __forceinline__ LtShape(int L, int Nb, int tk) {
-        full = L / tk;
-        rest_cost = L % tk ? lt_tile_cost(L % tk) : 0;
-        tree_full = Nb / tk;
-        tree_rest_cost = Nb % tk ? lt_tile_cost(Nb % tk) : 0;
-        cost = lt_tile_cost(tk);
+    __host__ __device__ __forceinline__ LtShape(int L, int Nb, int shift) {     // tiles of 1 << shift keys
+        const int rest = L & ((1 << shift) - 1), tree_rest = Nb & ((1 << shift) - 1);
+        full = L >> shift;
+        rest_cost = rest ? lt_tile_cost(rest) : 0;
+        tree_full = Nb >> shift;
+        tree_rest_cost = tree_rest ? lt_tile_cost(tree_rest) : 0;
+        cost = lt_tile_cost(1 << shift);
     }
     __host__ __device__ __forceinline__ int prefix_tiles() const { return full + (rest_cost > 0); }
     __host__ __device__ __forceinline__ int tiles() const { return prefix_tiles() + tree_full + (tree_rest_cost > 0); }
@@ -202,7 +208,7 @@ struct LtWalk {
             it.b = b;
             it.L = lt_len(a, b);
             it.Nb = lt_nodes(a, b);
-            const LtShape x(it.L, it.Nb, sm->tile_keys);
+            const LtShape x(it.L, it.Nb, sm->tile_shift);
             it.nP = x.prefix_tiles();
             it.nt = x.tiles();
             const int off = u - sm->cum[b], total = x.total();
@@ -220,7 +226,7 @@ struct LtWalk {
 };
 // The pairs that have tiles of an item: a range of units is no shorter than a tile, so that none between them is without.
 __device__ __forceinline__ void lt_owners(const LtSmall* sm, const LtItem& it, int& first, int& last) {
-    const LtShape x(it.L, it.Nb, sm->tile_keys);
+    const LtShape x(it.L, it.Nb, sm->tile_shift);
     first = lt_pair_of(it.unit0 + x.start(0), sm->total, sm->pairs);
     last = lt_pair_of(it.unit0 + x.start(it.nt - 1), sm->total, sm->pairs);
 }
@@ -311,34 +317,38 @@ __device__ __forceinline__ void lt_join_quads(const LtParams& p, const LtItem& i
         for (int i = 0; i < QUADS; i += 2) *reinterpret_cast<uint4*>(out + 4 * i) = make_uint4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
     }
 }
+// Waits (one thread; bounded) until `count` pieces have been counted in; sm->join_ready says whether they have.
+__device__ __noinline__ void lt_await(LtSmall* sm, const LtParams& p, const int* counter, int count, bool ok) {
+    const long long t0 = clock64();
+    int seen = 0;
+    while (ok) {
+        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
+        if (seen >= count || *(volatile int*)&sm->abort_flag) break;
+        if (clock64() - t0 > kSpinCycles) {
+            *(volatile int*)&sm->abort_flag = 1;
+            p.header->detail = 20;
+            p.header->status = MCSD_ERR_TIMEOUT;
+            __threadfence();
+            break;
+        }
+    }
+    sm->join_ready = seen >= count;
+}
 // This block's share of a cut item's columns, by the 256 threads of the softmax warps.
 __device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, const LtItem& it, int pair, int rank, int tid, bool ok) {
-    const LatentArgs& a = p.a;
     int first, last;
     lt_owners(sm, it, first, last);
     const int count = last - first + 1;
+    if (count <= kLtFew) return;                               // joined where it started
     int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
-    if (tid == 0) {
-        const long long t0 = clock64();
-        int seen = 0;
-        while (ok) {
-            asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
-            if (seen >= count || *(volatile int*)&sm->abort_flag) break;
-            if (clock64() - t0 > kSpinCycles) {
-                *(volatile int*)&sm->abort_flag = 1;
-                p.header->detail = 20;
-                p.header->status = MCSD_ERR_TIMEOUT;
-                __threadfence();
-                break;
-            }
-        }
-        sm->join_ready = seen >= count;
-    }
+    if (tid == 0) lt_await(sm, p, counter, count, ok);
     softmax_sync();
     if (sm->join_ready) {
         const int k0 = pair - first, tlane = tid & 127;
         if (count <= 4) {                                // few pieces: 16 channels a thread, whole sectors of the output
             for (int u = 16 * k0 / count + (tid >> 7); u < 16 * (k0 + 1) / count; u += 2) lt_join_quads<4, 4>(p, it, first, count, rank, tlane, 4 * u);
+        } else if (count <= 16) {
+            for (int u = 32 * k0 / count + (tid >> 7); u < 32 * (k0 + 1) / count; u += 2) lt_join_quads<2, 8>(p, it, first, count, rank, tlane, 2 * u);
         } else {                                         // many: one quad, eight pieces in flight
             for (int u = 64 * k0 / count + (tid >> 7); u < 64 * (k0 + 1) / count; u += 2) lt_join_quads<1, 8>(p, it, first, count, rank, tlane, u);
         }
@@ -396,7 +406,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             Nb = lt_nodes(a, tid);
             rbs = lt_row_blocks(a.H, Nb);
             if (Nb > 0)
-                for (int i = 0; i < 3; ++i) t[i] = rbs * LtShape(L, Nb, 256 >> i).tiles();
+                for (int i = 0; i < 3; ++i) t[i] = rbs * LtShape(L, Nb, 8 - i).tiles();
         }
         for (int i = 0; i < 3; ++i) {
             const int s = __reduce_add_sync(0xffffffffu, t[i]);
@@ -405,7 +415,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         __syncthreads();
         const int max_pairs = gridDim.x >> 1;
         const int pick = sm->sums[0] >= max_pairs ? 0 : sm->sums[1] >= max_pairs ? 1 : 2;
-        int units = Nb > 0 ? rbs * LtShape(L, Nb, 256 >> pick).total() : 0;
+        int units = Nb > 0 ? rbs * LtShape(L, Nb, 8 - pick).total() : 0;
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, units, o);
             if (lane >= o) units += x;
@@ -414,7 +424,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         __syncthreads();
         for (int w = 0; w < warp; ++w) units += sm->scan[w];
         if (tid < kLtMaxBatch) sm->cum[tid + 1] = units;   // sequences from B on: the total
-        if (tid == 0) { sm->cum[0] = 0; sm->tile_keys = 256 >> pick; }
+        if (tid == 0) { sm->cum[0] = 0; sm->tile_shift = 8 - pick; }
         if (tid == kLtMaxBatch - 1) { sm->total = units; sm->pairs = max(min(max_pairs, units / lt_tile_cost(256 >> pick)), units > 0); }
     }
     tc_fence_before();
@@ -422,7 +432,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
     cluster_sync_all();                                 // barriers and tensor memory of both blocks are ready
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm->tmem_base, 0);
-    const int tk = __shfl_sync(0xffffffffu, sm->tile_keys, 0);
+    const int tk = 1 << __shfl_sync(0xffffffffu, sm->tile_shift, 0);
     LtWalk walk;
     walk.start(sm, pair);
     LtItem it;
@@ -492,7 +502,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (g & 1) * 128;
                         // the softmax has read what this S replaces
                         if (g > 1) ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], ((g >> 1) - 1) & 1, 5));
-#pragma unroll
+#pragma unroll 1                                          // (small loops: see above)
                         for (int c = 0; c < kLtChunks; ++c) {
                             ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->full[slot], phase, 6));
                             if (!ok) break;
@@ -514,7 +524,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
                         const LtTile x = lt_tile(it, t, tk);
                         ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], (g >> 1) & 1, 14));     // O has its reference
-#pragma unroll
+#pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
                             const int n = lt_quarter(x.kpc, q);
                             ok = ok && __all_sync(0xffffffffu, LT_WAIT(&sm->p_full[q], g & 1, 7));
@@ -704,7 +714,33 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             tc_fence_after();
             const bool whole = it.t0 == 0 && it.t1 == it.nt;
             const int slot = 2 * pair + (it.t0 == 0 ? 1 : 0);
-            if (!whole && half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
+            int first = pair, last = pair;
+            if (!whole) lt_owners(sm, it, first, last);
+            const int pieces = last - first + 1;
+            const bool finish = whole || (it.t0 == 0 && pieces <= kLtFew);        // the rows leave from here
+            // the other pieces' references and sums, and what this one counts for
+            float2 others[kLtFew - 1];
+            float own = 1.0f;
+            int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
+            if (finish && !whole) {
+                if (w == 0 && lane == 0) lt_await(sm, p, counter, pieces - 1, ok);
+                softmax_sync();
+                float top = ref;
+#pragma unroll
+                for (int k = 0; k < kLtFew - 1; ++k) {
+                    others[k] = k + 1 < pieces ? __ldcg(p.part_ml + 2 * (first + 1 + k) * 128 + rank * 64 + row) : make_float2(-INFINITY, 0.0f);
+                    top = fmaxf(top, others[k].x);
+                }
+                const float sub = top == -INFINITY ? 0.0f : top;
+                own = ex2_approx(ref - sub);
+                l *= own;
+#pragma unroll
+                for (int k = 0; k < kLtFew - 1; ++k) {
+                    others[k].x = ex2_approx(others[k].x - sub);
+                    l += others[k].x * others[k].y;
+                }
+            }
+            if (!finish && half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
             const bool in = r < a.H * it.Nb;
             const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
             const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
@@ -714,9 +750,32 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 float o[32];
+                float4 v[kLtFew - 1][8];
+                const bool join = in && finish && !whole;
                 tc_ld32(lane_addr + kLtColO + 128 * group + 32 * c, o);
+#pragma unroll
+                for (int k = 0; k < kLtFew - 1; ++k)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        v[k][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (join && k + 1 < pieces) v[k][i] = __ldcg(lt_part(p, 2 * (first + 1 + k), rank, 32 * group + 8 * c + i, 64 * half + row));
+                    }
+                __syncwarp();
                 tc_wait_ld();
-                if (in && whole) {
+                if (join) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        o[4 * i] *= own; o[4 * i + 1] *= own; o[4 * i + 2] *= own; o[4 * i + 3] *= own;
+#pragma unroll
+                        for (int k = 0; k < kLtFew - 1; ++k) {
+                            o[4 * i] += others[k].x * v[k][i].x;
+                            o[4 * i + 1] += others[k].x * v[k][i].y;
+                            o[4 * i + 2] += others[k].x * v[k][i].z;
+                            o[4 * i + 3] += others[k].x * v[k][i].w;
+                        }
+                    }
+                }
+                if (in && finish) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
                         uint4 v;
@@ -733,12 +792,13 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 __syncwarp();
             }
             tc_fence_before();
-            if (!whole) {                                                       // this piece of a cut item is there
-                int first, last;
-                lt_owners(sm, it, first, last);
+            if (!finish) {                                                      // this piece of a cut item is there
                 __threadfence();
                 softmax_sync();
-                if (w == 0 && lane == 0) atomicAdd(&p.counters[(2 * first + rank) * kCountersPerBlock], 1);
+                if (w == 0 && lane == 0) atomicAdd(counter, 1);
+            } else if (!whole) {
+                softmax_sync();                                                 // all have read: zero between launches
+                if (w == 0 && lane == 0) *counter = 0;
             }
             it = next;
         }
