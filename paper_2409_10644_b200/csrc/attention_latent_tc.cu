@@ -23,8 +23,11 @@
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
 // inside an item, the pieces write unnormalised rows and count themselves in.  An item of two or three pieces is joined by the
 // pair that starts it, from tensor memory: the others wrote theirs early, as the first of their ranges.  Where there are more, a
-// pair at the end of its range waits for the other pieces of such an item and joins a share of its channels.  (All blocks run at a time: one a multiprocessor, no more
-// pairs than fit.)  Tiles are 256 keys, or 128 or 64 where there would be fewer tiles than pairs.
+// pair at the end of its range waits for the other pieces of such an item and joins a share of its channels (only as many pairs
+// get work as keeps items in three pieces, where that is sooner done).  All blocks usually run at a time, one a multiprocessor;
+// where others hold multiprocessors (a kernel of another stream), a pair must not wait for one that cannot start before it
+// leaves.  So it waits for a millisecond at most, then notes that it is gone, and the pair that brings the last piece joins the
+// shares of those that are: no result depends on which blocks run together.
 //
 // The five roles run side by side, each its own loop: unrolled, they did not fit the instruction caches, and a tile took 4.9 us
 // instead of 3.4 (the loops of S over nine chunks and of O over four quarters are rolled for that alone).
@@ -46,11 +49,16 @@ namespace mcsd {
 constexpr int kLtRank = 512, kLtRot = 64, kLtWidth = kLtRank + kLtRot;
 constexpr int kLtChunks = kLtWidth / 64;             // 64-channel chunks of a row
 constexpr int kLtThreads = 384;
+constexpr int kLtTile = 256;                         // keys of a tile
 constexpr int kLtKeySlots = 4, kLtValueSlots = 3, kLtSlots = kLtKeySlots + kLtValueSlots, kLtSlotBytes = 16384;
 constexpr int kLtQBytes = kLtChunks * 8192, kLtPBytes = 4 * 8192;      // queries, weights of a tile
 constexpr int kLtMaxBatch = 256;
 constexpr int kLtMaxPairs = kTcMaxBlocks / 2;
 constexpr int kLtFew = 3;                            // pieces of an item that are joined by the pair that starts it
+constexpr int kLtGone = 1 << 8, kLtLeft = 1 << 16;   // an item's counter: pieces that are in, pairs that wait no more, pairs done with it
+constexpr int kLtGoneWords = kCountersPerBlock - 1;  // and the pairs that wait no more, a bit each
+static_assert(kLtMaxPairs <= 32 * kLtGoneWords && kLtMaxPairs < 256, "an item's counters");
+constexpr long long kLtPatience = 1 << 21;           // cycles, about a millisecond
 constexpr int kLtColO = 0, kLtColS = 256;            // tensor memory: O 256 columns, S 128 twice
 
 struct LtParams {
@@ -58,22 +66,38 @@ struct LtParams {
     float scale_log2;
     float* part_o;                                   // unnormalised rows of pieces, two slots a pair (see lt_part)
     float2* part_ml;                                 // [2 * pairs][128]  reference (log2), sum
-    int* counters;                                   // [2 * pairs][kCountersPerBlock]: pieces of the item that a block starts, shares joined
+    int* counters;                                   // [2 * pairs][kCountersPerBlock] of the item that a block starts
     WorkspaceHeader* header;
 };
 struct LtMaps {
     CUtensorMap m[8];                                // boxes of 16, 32, 64, 128 rows: cache, then tree
 };
 
+struct LtItem {
+    int b, rb, L, Nb, nP, nt;      // sequence, row block; prefix length, nodes; prefix tiles, tiles
+    int t0, t1;                    // this pair's tiles
+    int unit0;                     // the item's first unit
+    __device__ __forceinline__ void uniform() {      // alike in all lanes: say so
+        L = __shfl_sync(0xffffffffu, L, 0);
+        Nb = __shfl_sync(0xffffffffu, Nb, 0);
+        nP = __shfl_sync(0xffffffffu, nP, 0);
+        t0 = __shfl_sync(0xffffffffu, t0, 0);
+        t1 = __shfl_sync(0xffffffffu, t1, 0);
+    }
+};
 struct LtSmall {
     unsigned long long full[kLtSlots], empty[kLtSlots];          // slots of S, then of O
     unsigned long long s_full[2], s_free[2], p_full[4], p_free[4], pv_done, q_full;
     uint32_t tmem_base;
     int abort_flag;
-    int tile_shift, pairs;                           // keys of a tile (their logarithm), pairs with work
-    int join_ready;
+    int pairs;                                       // pairs with work
+    int joins;                                       // items to join at the end of the range (the first and the last at most)
+    LtItem join[2];
+    int join_in[2];                                  // their counter as this pair's piece found it
+    int all_in;                                      // what a wait for pieces found
+    uint32_t shares[kLtGoneWords];                   // shares of an item that this pair joins
     int total;                                       // units of the launch
-    int sums[3];                                     // tiles of the launch with 256, 128, 64 keys a tile
+    int items;                                       // work items of the launch
     int scan[kLtThreads / 32];
     int cum[kLtMaxBatch + 1];                        // units before a sequence
     float red[2][4][64];                             // row maxima of a tile's quarters, by tile parity
@@ -138,25 +162,25 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
 }
 
 // ------------------------------------------------------------------ the cut of a launch
-// Cost of an item's parts in units of 0.4 us (measured): a tile has a fixed part (its waits) and one by its keys (its
-// products), an item starts with its queries and ends with its output.  A pair takes the tiles that start in its range of the
-// launch's units.
-constexpr int kLtItemCost = 14;
-__host__ __device__ __forceinline__ int lt_tile_cost(int keys) { return 3 + (7 * keys + 255) / 256; }
+// Cost of an item's parts in units of 525 cycles (a least-squares fit of when pairs finished, over launches of few and many, long
+// and short items): a tile has a fixed part (its waits) and one by its keys (its products), an item starts with its queries and
+// ends with its output.  A pair takes the tiles that start in its range of the launch's units.
+constexpr int kLtItemCost = 14, kLtJoinCost = 25;      // the latter: an item in more than kLtFew pieces
+__host__ __device__ __forceinline__ int lt_tile_cost(int keys) { return 6 + (4 * keys + 255) / 256; }
 __host__ __device__ __forceinline__ int lt_row_blocks(int H, int Nb) { return (H * Nb + 127) / 128; }
 __device__ __forceinline__ int lt_len(const LatentArgs& a, int b) { return min(max(a.seq_lens[b], 0), a.L_max); }
 __device__ __forceinline__ int lt_nodes(const LatentArgs& a, int b) { return a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N; }
 
 // The tiles of an item: full prefix tiles, a shorter one, full tree tiles, a shorter one.
 struct LtShape {
-    int full, rest_cost, tree_full, tree_rest_cost, cost;      // cost of a full tile
-    __host__ __device__ __forceinline__ LtShape(int L, int Nb, int shift) {     // tiles of 1 << shift keys
-        const int rest = L & ((1 << shift) - 1), tree_rest = Nb & ((1 << shift) - 1);
-        full = L >> shift;
+    static constexpr int cost = 10;                            // of a full tile
+    int full, rest_cost, tree_full, tree_rest_cost;
+    __host__ __device__ __forceinline__ LtShape(int L, int Nb) {
+        const int rest = L % kLtTile, tree_rest = Nb % kLtTile;
+        full = L / kLtTile;
         rest_cost = rest ? lt_tile_cost(rest) : 0;
-        tree_full = Nb >> shift;
+        tree_full = Nb / kLtTile;
         tree_rest_cost = tree_rest ? lt_tile_cost(tree_rest) : 0;
-        cost = lt_tile_cost(1 << shift);
     }
     __host__ __device__ __forceinline__ int prefix_tiles() const { return full + (rest_cost > 0); }
     __host__ __device__ __forceinline__ int tiles() const { return prefix_tiles() + tree_full + (tree_rest_cost > 0); }
@@ -179,18 +203,6 @@ struct LtShape {
 __device__ __forceinline__ int lt_first(int c, int total, int pairs) { return (int)((long long)c * total / pairs); }
 __device__ __forceinline__ int lt_pair_of(int unit, int total, int pairs) { return (int)((((long long)unit + 1) * pairs - 1) / total); }
 
-struct LtItem {
-    int b, rb, L, Nb, nP, nt;      // sequence, row block; prefix length, nodes; prefix tiles, tiles
-    int t0, t1;                    // this pair's tiles
-    int unit0;                     // the item's first unit
-    __device__ __forceinline__ void uniform() {      // alike in all lanes: say so
-        L = __shfl_sync(0xffffffffu, L, 0);
-        Nb = __shfl_sync(0xffffffffu, Nb, 0);
-        nP = __shfl_sync(0xffffffffu, nP, 0);
-        t0 = __shfl_sync(0xffffffffu, t0, 0);
-        t1 = __shfl_sync(0xffffffffu, t1, 0);
-    }
-};
 // Walks the items of a pair's range; every role of both blocks walks alike.
 struct LtWalk {
     int u, end, b;
@@ -208,7 +220,7 @@ struct LtWalk {
             it.b = b;
             it.L = lt_len(a, b);
             it.Nb = lt_nodes(a, b);
-            const LtShape x(it.L, it.Nb, sm->tile_shift);
+            const LtShape x(it.L, it.Nb);
             it.nP = x.prefix_tiles();
             it.nt = x.tiles();
             const int off = u - sm->cum[b], total = x.total();
@@ -226,7 +238,7 @@ struct LtWalk {
 };
 // The pairs that have tiles of an item: a range of units is no shorter than a tile, so that none between them is without.
 __device__ __forceinline__ void lt_owners(const LtSmall* sm, const LtItem& it, int& first, int& last) {
-    const LtShape x(it.L, it.Nb, sm->tile_shift);
+    const LtShape x(it.L, it.Nb);
     first = lt_pair_of(it.unit0 + x.start(0), sm->total, sm->pairs);
     last = lt_pair_of(it.unit0 + x.start(it.nt - 1), sm->total, sm->pairs);
 }
@@ -234,11 +246,11 @@ struct LtTile {
     int lo, start, kpc;            // first key it has a claim to, first key that is loaded, keys of a block (16 .. 128)
     bool tree;
 };
-__device__ __forceinline__ LtTile lt_tile(const LtItem& it, int t, int tk) {
+__device__ __forceinline__ LtTile lt_tile(const LtItem& it, int t) {
     LtTile x;
     x.tree = t >= it.nP;
-    x.lo = (x.tree ? t - it.nP : t) * tk;
-    const int stop = min(x.lo + tk, x.tree ? it.Nb : it.L);
+    x.lo = (x.tree ? t - it.nP : t) * kLtTile;
+    const int stop = min(x.lo + kLtTile, x.tree ? it.Nb : it.L);
     x.kpc = (stop - x.lo + 31) / 32 * 16;
     x.start = stop - 2 * x.kpc;
     return x;
@@ -317,57 +329,64 @@ __device__ __forceinline__ void lt_join_quads(const LtParams& p, const LtItem& i
         for (int i = 0; i < QUADS; i += 2) *reinterpret_cast<uint4*>(out + 4 * i) = make_uint4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
     }
 }
-// Waits (one thread; bounded) until `count` pieces have been counted in; sm->join_ready says whether they have.
-__device__ __noinline__ void lt_await(LtSmall* sm, const LtParams& p, const int* counter, int count, bool ok) {
+// Waits (one thread) until `count` pieces are in or patience runs out; then this pair is counted as gone, unless they came in
+// just before.  Returns whether they are in.  `bit` of `word` goes before the count: who sees the count finds it.
+__device__ __noinline__ bool lt_await(LtSmall* sm, int* counter, int count, bool ok, int* word, int bit) {
     const long long t0 = clock64();
-    int seen = 0;
-    while (ok) {
+    while (ok && clock64() - t0 < kLtPatience && !*(volatile int*)&sm->abort_flag) {
+        int seen;
         asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
-        if (seen >= count || *(volatile int*)&sm->abort_flag) break;
-        if (clock64() - t0 > kSpinCycles) {
-            *(volatile int*)&sm->abort_flag = 1;
-            p.header->detail = 20;
-            p.header->status = MCSD_ERR_TIMEOUT;
-            __threadfence();
-            break;
-        }
+        if ((seen & (kLtGone - 1)) >= count) return true;
     }
-    sm->join_ready = seen >= count;
+    if (bit) atomicOr(word, bit);
+    __threadfence();
+    const bool in = (atomicAdd(counter, kLtGone) & (kLtGone - 1)) >= count;
+    __threadfence();
+    return in;
 }
-// This block's share of a cut item's columns, by the 256 threads of the softmax warps.
-__device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, const LtItem& it, int pair, int rank, int tid, bool ok) {
+// Share k of `count` of a cut item's columns, by the 256 threads of the softmax warps.
+__device__ __noinline__ void lt_join_share(const LtParams& p, const LtItem& it, int first, int count, int k, int rank, int tid) {
+    const int tlane = tid & 127;
+    if (count <= 6) {                                    // few pieces: 16 channels a thread, whole sectors of the output
+        for (int u = 16 * k / count + (tid >> 7); u < 16 * (k + 1) / count; u += 2) lt_join_quads<4, 6>(p, it, first, count, rank, tlane, 4 * u);
+    } else if (count <= 16) {
+        for (int u = 32 * k / count + (tid >> 7); u < 32 * (k + 1) / count; u += 2) lt_join_quads<2, 12>(p, it, first, count, rank, tlane, 2 * u);
+    } else {                                             // many: one quad, sixteen pieces in flight
+        for (int u = 64 * k / count + (tid >> 7); u < 64 * (k + 1) / count; u += 2) lt_join_quads<1, 16>(p, it, first, count, rank, tlane, u);
+    }
+}
+// At the end of a range: this pair's share of an item in more than kLtFew pieces, and where its piece was the last one to come
+// in, the shares of the pairs that are gone (of an item in fewer pieces, which the pair that starts it did not wait for: all).
+__device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, int i, int pair, int rank, int tid, bool ok) {
+    const LtItem& it = sm->join[i];
     int first, last;
     lt_owners(sm, it, first, last);
-    const int count = last - first + 1;
-    if (count <= kLtFew) return;                               // joined where it started
+    const int count = last - first + 1, own = pair - first;
     int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
-    if (tid == 0) lt_await(sm, p, counter, count, ok);
-    softmax_sync();
-    if (sm->join_ready) {
-        const int k0 = pair - first, tlane = tid & 127;
-        if (count <= 4) {                                // few pieces: 16 channels a thread, whole sectors of the output
-            for (int u = 16 * k0 / count + (tid >> 7); u < 16 * (k0 + 1) / count; u += 2) lt_join_quads<4, 4>(p, it, first, count, rank, tlane, 4 * u);
-        } else if (count <= 16) {
-            for (int u = 32 * k0 / count + (tid >> 7); u < 32 * (k0 + 1) / count; u += 2) lt_join_quads<2, 8>(p, it, first, count, rank, tlane, 2 * u);
-        } else {                                         // many: one quad, eight pieces in flight
-            for (int u = 64 * k0 / count + (tid >> 7); u < 64 * (k0 + 1) / count; u += 2) lt_join_quads<1, 8>(p, it, first, count, rank, tlane, u);
+    if (tid == 0) {
+        const int in = sm->join_in[i];
+        const bool last_in = (in & (kLtGone - 1)) == count - 1, gone = in / kLtGone > 0;
+        const uint32_t bit = 1u << (own & 31);
+        if (!last_in) {
+            const bool mine = lt_await(sm, counter, count, ok, counter + 1 + (own >> 5), (int)bit);
+            for (int k = 0; k < kLtGoneWords; ++k) sm->shares[k] = mine && k == own >> 5 ? bit : 0;
+        } else {
+            __threadfence();
+            for (int k = 0; k < kLtGoneWords; ++k)
+                sm->shares[k] = count <= kLtFew ? ~0u : (gone ? (uint32_t)__ldcg(counter + 1 + k) : 0) | (k == own >> 5 ? bit : 0);
         }
     }
     softmax_sync();
-    if (tid == 0 && atomicAdd(counter + 1, 1) == count - 1) {      // the last share: counters are zero between launches
-        counter[0] = 0;
-        counter[1] = 0;
+    for (int k = 0; k < count; ++k)
+        if (sm->shares[k >> 5] >> (k & 31) & 1) lt_join_share(p, it, first, count, k, rank, tid);
+    softmax_sync();
+    if (tid == 0) {                                      // counters are zero between launches: the last one to leave
+        bool reset = count <= kLtFew;
+        if (!reset) reset = atomicAdd(counter, kLtLeft) / kLtLeft == count - 1;
+        if (reset)
+            for (int k = 0; k < kCountersPerBlock; ++k) counter[k] = 0;
     }
 }
-// The items of this pair's range that other pairs have pieces of: the first, the last, or one that is both.
-__device__ __forceinline__ void lt_join(LtSmall* sm, const LtParams& p, int pair, int rank, int tid, bool ok) {
-    LtWalk walk;
-    walk.start(sm, pair);
-    LtItem it;
-    while (walk.next(sm, p.a, it))
-        if (it.t0 > 0 || it.t1 < it.nt) lt_join_item(sm, p, it, pair, rank, tid, ok);
-}
-
 #define LT_WAIT(bar, parity, where) mbar_wait(bar, parity, &sm->abort_flag, p.header, where)
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtThreads, 1)
 tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_constant__ LtParams p) {
@@ -389,7 +408,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         mbar_init(&sm->pv_done, 1);
         mbar_init(&sm->q_full, 16);
         sm->abort_flag = 0;
-        sm->sums[0] = sm->sums[1] = sm->sums[2] = 0;
+        sm->items = sm->joins = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -399,40 +418,40 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __syncthreads();
-    {   // tiles of the launch for each tile size, then the units of every sequence with the size that is taken
-        int t[3] = {0, 0, 0}, L = 0, Nb = 0, rbs = 0;
+    {   // units of every sequence, and how many pairs get work
+        int units = 0, items = 0;
         if (tid < a.B) {
-            L = lt_len(a, tid);
-            Nb = lt_nodes(a, tid);
-            rbs = lt_row_blocks(a.H, Nb);
-            if (Nb > 0)
-                for (int i = 0; i < 3; ++i) t[i] = rbs * LtShape(L, Nb, 8 - i).tiles();
+            const int Nb = lt_nodes(a, tid);
+            if (Nb > 0) {
+                items = lt_row_blocks(a.H, Nb);
+                units = items * LtShape(lt_len(a, tid), Nb).total();
+            }
         }
-        for (int i = 0; i < 3; ++i) {
-            const int s = __reduce_add_sync(0xffffffffu, t[i]);
-            if (lane == 0) atomicAdd(&sm->sums[i], s);
-        }
-        __syncthreads();
-        const int max_pairs = gridDim.x >> 1;
-        const int pick = sm->sums[0] >= max_pairs ? 0 : sm->sums[1] >= max_pairs ? 1 : 2;
-        int units = Nb > 0 ? rbs * LtShape(L, Nb, 8 - pick).total() : 0;
+        items = __reduce_add_sync(0xffffffffu, items);
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, units, o);
             if (lane >= o) units += x;
         }
         if (lane == 31) sm->scan[warp] = units;
+        if (lane == 0 && items) atomicAdd(&sm->items, items);
         __syncthreads();
         for (int w = 0; w < warp; ++w) units += sm->scan[w];
         if (tid < kLtMaxBatch) sm->cum[tid + 1] = units;   // sequences from B on: the total
-        if (tid == 0) { sm->cum[0] = 0; sm->tile_shift = 8 - pick; }
-        if (tid == kLtMaxBatch - 1) { sm->total = units; sm->pairs = max(min(max_pairs, units / lt_tile_cost(256 >> pick)), units > 0); }
+        if (tid == kLtMaxBatch - 1) {
+            // a range is no shorter than a tile; and no item in more than kLtFew pieces where that is sooner done
+            int pairs = max(min((int)(gridDim.x >> 1), units / LtShape::cost), units > 0);
+            const long long few = min((long long)kLtFew * sm->items, (long long)pairs);
+            if (pairs > few && units / (int)few <= units / pairs + kLtJoinCost) pairs = (int)few;
+            sm->cum[0] = 0;
+            sm->total = units;
+            sm->pairs = pairs;
+        }
     }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();                                 // barriers and tensor memory of both blocks are ready
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm->tmem_base, 0);
-    const int tk = 1 << __shfl_sync(0xffffffffu, sm->tile_shift, 0);
     LtWalk walk;
     walk.start(sm, pair);
     LtItem it;
@@ -455,7 +474,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             };
             while (ok && walk.next(sm, a, it)) {
                 for (int t = it.t0; ok && t < it.t1; ++t) {
-                    const LtTile x = lt_tile(it, t, tk);
+                    const LtTile x = lt_tile(it, t);
                     const CUtensorMap* map = &maps.m[x.tree ? 4 : 0];
                     if (for_s) {                             // this block's keys, 64 channels a slot
                         const int size = x.kpc > 64 ? 3 : x.kpc > 32 ? 2 : x.kpc > 16 ? 1 : 0;
@@ -498,7 +517,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     ok = __all_sync(0xffffffffu, LT_WAIT(&sm->q_full, item & 1, 4));
                     ++item;
                     for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
-                        const LtTile x = lt_tile(it, t, tk);
+                        const LtTile x = lt_tile(it, t);
                         const uint32_t idesc = instr_desc(2 * x.kpc, 0, 0), d = tmem + kLtColS + (g & 1) * 128;
                         // the softmax has read what this S replaces
                         if (g > 1) ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], ((g >> 1) - 1) & 1, 5));
@@ -522,7 +541,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 while (ok && walk.next(sm, a, it)) {
                     it.uniform();
                     for (int t = it.t0; ok && t < it.t1; ++t, ++g) {
-                        const LtTile x = lt_tile(it, t, tk);
+                        const LtTile x = lt_tile(it, t);
                         ok = __all_sync(0xffffffffu, LT_WAIT(&sm->s_free[g & 1], (g >> 1) & 1, 14));     // O has its reference
 #pragma unroll 1
                         for (int q = 0; q < 4; ++q) {
@@ -591,7 +610,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             const int r = it.rb * 128 + rank * 64 + row;
             float ref = -INFINITY, l = 0.0f;
             for (int t = it.t0; t < it.t1; ++t, ++g) {
-                const LtTile x = lt_tile(it, t, tk);
+                const LtTile x = lt_tile(it, t);
                 const int cols = lt_quarter(x.kpc, group);                     // this thread's columns, from 64 * group on
                 uint64_t see = ~0ull;                                          // keys that the row sees
                 const bool plain = x.kpc == 128 && !x.tree && x.start == x.lo;
@@ -717,14 +736,17 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             int first = pair, last = pair;
             if (!whole) lt_owners(sm, it, first, last);
             const int pieces = last - first + 1;
-            const bool finish = whole || (it.t0 == 0 && pieces <= kLtFew);        // the rows leave from here
+            bool finish = whole || (it.t0 == 0 && pieces <= kLtFew);              // the rows leave from here
             // the other pieces' references and sums, and what this one counts for
             float2 others[kLtFew - 1];
             float own = 1.0f;
             int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
             if (finish && !whole) {
-                if (w == 0 && lane == 0) lt_await(sm, p, counter, pieces - 1, ok);
+                if (w == 0 && lane == 0) sm->all_in = lt_await(sm, counter, pieces - 1, ok, nullptr, 0);
                 softmax_sync();
+                finish = sm->all_in;                                            // or the last piece's pair joins them
+            }
+            if (finish && !whole) {
                 float top = ref;
 #pragma unroll
                 for (int k = 0; k < kLtFew - 1; ++k) {
@@ -745,7 +767,8 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             const int h = in ? r / it.Nb : 0, n = in ? r - h * it.Nb : 0;
             const float inv = l > 0.0f ? 1.0f / l : l;                          // no key seen: zeros
             // columns 128 group .. of tensor memory are channels 256 group + 128 half ..
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * group + 128 * half;
+            __nv_bfloat16* out = in ? static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * group + 128 * half : nullptr;
+            const uint32_t stage = p_a + (2 * half + group) * 8192;
             float4* part = lt_part(p, slot, rank, 32 * group, 64 * half + row);
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
@@ -775,15 +798,30 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                         }
                     }
                 }
-                if (in && finish) {
+                if (finish) {
+                    // through this warp's rows of P (free by now), so that a row's 128 bytes leave together
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
-                        uint4 v;
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.x) : "f"(o[i + 1] * inv), "f"(o[i] * inv));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.y) : "f"(o[i + 3] * inv), "f"(o[i + 2] * inv));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.z) : "f"(o[i + 5] * inv), "f"(o[i + 4] * inv));
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v.w) : "f"(o[i + 7] * inv), "f"(o[i + 6] * inv));
-                        *reinterpret_cast<uint4*>(out + 32 * c + i) = v;
+                        uint4 x;
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.x) : "f"(o[i + 1] * inv), "f"(o[i] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.y) : "f"(o[i + 3] * inv), "f"(o[i + 2] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.z) : "f"(o[i + 5] * inv), "f"(o[i + 4] * inv));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.w) : "f"(o[i + 7] * inv), "f"(o[i + 6] * inv));
+                        const uint32_t at = stage + row * 128 + ((((c & 1) * 4 + i / 8) ^ (row & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+                    }
+                    if (c & 1) {
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int from = 4 * i + (lane >> 3), u = lane & 7, r2 = (w & 1) * 32 + from;
+                            uint4 x;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w)
+                                         : "r"(stage + r2 * 128 + ((u ^ (r2 & 7)) << 4)) : "memory");
+                            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), from));
+                            if (to) *reinterpret_cast<uint4*>(to + 32 * (c - 1) + 8 * u) = x;
+                        }
+                        __syncwarp();
                     }
                 } else if (in) {
 #pragma unroll
@@ -795,7 +833,13 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             if (!finish) {                                                      // this piece of a cut item is there
                 __threadfence();
                 softmax_sync();
-                if (w == 0 && lane == 0) atomicAdd(counter, 1);
+                if (w == 0 && lane == 0) {
+                    const int in = atomicAdd(counter, 1);
+                    if (pieces > kLtFew || (in & (kLtGone - 1)) == pieces - 1) {
+                        sm->join_in[sm->joins] = in;
+                        sm->join[sm->joins++] = it;
+                    }
+                }
             } else if (!whole) {
                 softmax_sync();                                                 // all have read: zero between launches
                 if (w == 0 && lane == 0) *counter = 0;
@@ -803,12 +847,14 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             it = next;
         }
         if (g > 0) ok = ok && LT_WAIT(&sm->p_free[2 * half + group], (g - 1) & 1, 15);   // the last arrival here, before the block may leave
-        __syncwarp();
-        lt_join(sm, p, pair, rank, tid - 128, ok);
+        softmax_sync();
+        for (int i = 0; i < sm->joins; ++i) lt_join_item(sm, p, i, pair, rank, tid - 128, ok);
     }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();                                 // the other block's products, loads and arrivals are done too
+    // the other block's products, loads and arrivals are done too (all waited for: a meeting that orders no writes, since one
+    // that does waits for those of the output)
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
@@ -839,11 +885,11 @@ static bool lt_map(CUtensorMap* map, const void* base, int rows, int B, int box_
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Shapes of this kernel.  The units of a launch are 32-bit: a tile of 64 keys costs five, so a sequence has at most
-// 5 (L_max / 64 + 8) for each of its H * N / 128 row blocks.
+// Shapes of this kernel.  The units of a launch are 32-bit: a sequence has at most 10 (L_max / 256 + 2) + 14 for each of its
+// H * N / 128 row blocks (a tree is one tile).
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
     if (dtype != MCSD_BF16 || rank != kLtRank || rot != kLtRot) return false;
-    const long long per_seq = ((long long)H * N + 127) / 128 * 5 * ((long long)L_max / 64 + 8);
+    const long long per_seq = ((long long)H * N + 127) / 128 * (10 * ((long long)L_max / kLtTile + 2) + kLtItemCost);
     return per_seq * std::min(B, kLtMaxBatch) < (1LL << 30);
 }
 size_t latent_tc_workspace_bytes() {
