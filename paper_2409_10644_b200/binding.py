@@ -672,6 +672,9 @@ def mcsd_tree_attention_kv4(q, cache, k_tree, v_tree, seq_lens, n_active, mask: 
 
 # ---------------------------------------------------------------- latent caches and candidates from logits
 
+_Strides5 = ctypes.c_int64 * 5
+
+
 def mcsd_latent_rows(latent_in, q_in, seq_lens, freqs, rows=None, q=None, row_start=None, depth=None, n_active=None, weight=None,
                      eps: float = 1e-6, interleaved: bool = False):
     """Rows of a latent cache and the rotated part of the queries from a layer's projections (see mcsd.h).
@@ -685,21 +688,24 @@ def mcsd_latent_rows(latent_in, q_in, seq_lens, freqs, rows=None, q=None, row_st
     dt, dev = ref.dtype, ref.get_device()
     code = _dtype_code(ref)
     width, rot = ref.shape[-1], 0 if freqs is None else 2 * freqs.numel()
-    B, N = (latent_in if rows is not None else q_in).shape[:2]
-    lat, H, qp, L_rows, strides = None, 1, None, 1, [0] * 5
+    src = latent_in if rows is not None else q_in
+    B, N = src.size(0), src.size(1)
+    lat, H, qp, L_rows, strides = None, 1, None, 1, _Strides5()
     if rows is not None:
-        lat, strides[0], strides[1] = _projection(latent_in.unsqueeze(2), dt, dev, "latent_in")
         if latent_in.shape != (B, N, width) or rows.dim() != 3:
             raise ValueError("latent_in %s does not fit rows %s" % (tuple(latent_in.shape), tuple(rows.shape)))
-        L_rows = rows.shape[1]
+        if latent_in.dtype is not dt or latent_in.get_device() != dev or (latent_in.stride(2) != 1 and width > 1):
+            raise ValueError("latent_in must be a CUDA tensor of dtype %s on device %d, its last axis dense" % (dt, dev))
+        lat, strides[0], strides[1] = latent_in.data_ptr(), latent_in.stride(0), latent_in.stride(1)
+        L_rows = rows.size(1)
     if q is not None:
-        H = q.shape[1]
+        H = q.size(1)
         if q_in.shape != (B, N, H, rot):
             raise ValueError("q_in has shape %s, expected %s" % (tuple(q_in.shape), (B, N, H, rot)))
         if q_in.dtype is not dt or q_in.get_device() != dev or (q_in.stride(3) != 1 and rot > 1):
             raise ValueError("q_in must be a CUDA tensor of dtype %s on device %d, its last axis dense" % (dt, dev))
-        qp, strides[2:] = q_in.data_ptr(), q_in.stride()[:3]
-    st = _on_device(dev, lib.mcsd_latent_rows, lat, qp, (ctypes.c_int64 * 5)(*strides), _maybe(weight, dt, (width - rot,), dev, "weight"), eps,
+        qp, strides[2], strides[3], strides[4] = q_in.data_ptr(), q_in.stride(0), q_in.stride(1), q_in.stride(2)
+    st = _on_device(dev, lib.mcsd_latent_rows, lat, qp, strides, _maybe(weight, dt, (width - rot,), dev, "weight"), eps,
                     _maybe(freqs, torch.float64, (rot // 2,), dev, "freqs"), int(interleaved), _same(seq_lens, torch.int32, (B,), dev, "seq_lens"),
                     _maybe(depth, torch.int32, (N,), dev, "depth"), _maybe(n_active, torch.int32, (B,), dev, "n_active"),
                     _maybe(row_start, torch.int32, (B,), dev, "row_start"), _maybe(rows, dt, (B, L_rows, width), dev, "rows"), L_rows,

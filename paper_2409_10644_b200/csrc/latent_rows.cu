@@ -35,19 +35,19 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f(float x) { return __
 
 // eight consecutive elements
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* v, bool vec) {
-    if (vec) {
-        constexpr int n = sizeof(T) * 8 / 16;
-        alignas(16) T t[8];
+struct alignas(16) Eight {
+    T t[8];
+    __device__ __forceinline__ void load(const T* p, bool vec) {
+        if (vec) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f<T>(t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_f<T>(p[i]);
+            for (int i = 0; i < 8; ++i) t[i] = p[i];
+        }
     }
-}
+    __device__ __forceinline__ float operator[](int i) const { return to_f<T>(t[i]); }
+};
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* v, bool vec) {
     alignas(16) T t[8];
@@ -63,37 +63,37 @@ __device__ __forceinline__ void store8(T* p, const float* v, bool vec) {
     }
 }
 
-// Pairs 8 v .. 8 v + 7 of a rotated part: read from src, turned, stored to dst.  cs holds (cos, sin) of every pair.
+// Pairs 8 v .. 8 v + 7 of a rotated part: read, then turned and stored.  cs holds (cos, sin) of every pair.
 template <typename T>
-__device__ __forceinline__ void turn8(const T* src, T* dst, const float2* cs, int rot, int v, bool interleaved, bool vin, bool vout) {
-    float a[8], b[8], x[8], y[8];
-    const int half = rot / 2, p0 = 8 * v;
-    if (interleaved) {
-        load8(src + 2 * p0, a, vin);
-        load8(src + 2 * p0 + 8, b, vin);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 c = cs[p0 + i], d = cs[p0 + 4 + i];
-            x[2 * i] = a[2 * i] * c.x - a[2 * i + 1] * c.y;
-            x[2 * i + 1] = a[2 * i + 1] * c.x + a[2 * i] * c.y;
-            y[2 * i] = b[2 * i] * d.x - b[2 * i + 1] * d.y;
-            y[2 * i + 1] = b[2 * i + 1] * d.x + b[2 * i] * d.y;
-        }
-        store8(dst + 2 * p0, x, vout);
-        store8(dst + 2 * p0 + 8, y, vout);
-    } else {
-        load8(src + p0, a, vin);
-        load8(src + half + p0, b, vin);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 c = cs[p0 + i];
-            x[i] = a[i] * c.x - b[i] * c.y;
-            y[i] = b[i] * c.x + a[i] * c.y;
-        }
-        store8(dst + p0, x, vout);
-        store8(dst + half + p0, y, vout);
+struct Turn8 {
+    Eight<T> a, b;
+    __device__ __forceinline__ void load(const T* src, int rot, int v, bool interleaved, bool vec) {
+        a.load(src + (interleaved ? 16 * v : 8 * v), vec);
+        b.load(src + (interleaved ? 16 * v + 8 : rot / 2 + 8 * v), vec);
     }
-}
+    __device__ __forceinline__ void store(T* dst, const float2* cs, int rot, int v, bool interleaved, bool vec) const {
+        float x[8], y[8];
+        if (interleaved) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 c = cs[8 * v + i], d = cs[8 * v + 4 + i];
+                x[2 * i] = a[2 * i] * c.x - a[2 * i + 1] * c.y;
+                x[2 * i + 1] = a[2 * i + 1] * c.x + a[2 * i] * c.y;
+                y[2 * i] = b[2 * i] * d.x - b[2 * i + 1] * d.y;
+                y[2 * i + 1] = b[2 * i + 1] * d.x + b[2 * i] * d.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float2 c = cs[8 * v + i];
+                x[i] = a[i] * c.x - b[i] * c.y;
+                y[i] = b[i] * c.x + a[i] * c.y;
+            }
+        }
+        store8(dst + (interleaved ? 16 * v : 8 * v), x, vec);
+        store8(dst + (interleaved ? 16 * v + 8 : rot / 2 + 8 * v), y, vec);
+    }
+};
 
 // grid: (ceil(N / tokens), B)
 template <typename T>
@@ -105,6 +105,30 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
     if (nt <= 0) return;
     const int half = a.rot / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int W = a.rank + a.rot;
+    // the heads' parts are on their way while the angles are reduced and the latent part is normalised
+    constexpr int kAhead = 4 / sizeof(T);
+    const int per_head = half / 8, per_token = a.H * per_head, parts = a.q ? nt * per_token : 0;
+    auto part = [&](int i, int& t, int& h, int& v) {
+        t = i / per_token;
+        const int k = i - t * per_token;
+        h = k / per_head;
+        v = k - h * per_head;
+    };
+    auto fetch = [&](Turn8<T>& x, int i) {
+        int t, h, v;
+        part(i, t, h, v);
+        x.load(static_cast<const T*>(a.q_in) + b * a.q_batch + (n0 + t) * a.q_token + h * a.q_head, a.rot, v, a.interleaved, a.vec_q);
+    };
+    auto put = [&](const Turn8<T>& x, int i) {
+        int t, h, v;
+        part(i, t, h, v);
+        T* o = static_cast<T*>(a.q) + (((long long)b * a.H + h) * a.N + n0 + t) * W + a.rank;
+        x.store(o, cs[t], a.rot, v, a.interleaved, a.vec_qout);
+    };
+    Turn8<T> ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if ((int)threadIdx.x + j * kRowThreads < parts) fetch(ahead[j], threadIdx.x + j * kRowThreads);
     for (int i = threadIdx.x; i < nt * half; i += kRowThreads) {
         const int t = i / half, j = i - t * half, n = n0 + t;
         const double pos = (double)a.seq_lens[b] + (double)(a.depth ? a.depth[n] : n);
@@ -123,12 +147,13 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
         x = static_cast<const T*>(a.latent) + b * a.latent_batch + n * a.latent_token;
         if (row >= 0 && row < a.L_rows) dst = static_cast<T*>(a.rows) + ((long long)b * a.L_rows + row) * W;
         if (dst) {
-            float v[kLatentMaxRank / 256][8], sum = 0.0f;
+            Eight<T> v[kLatentMaxRank / 256];
+            float sum = 0.0f;
 #pragma unroll
             for (int k = 0; k < kLatentMaxRank / 256; ++k) {
                 const int e = (k * 32 + lane) * 8;
                 if (e < a.rank) {
-                    load8(x + e, v[k], a.vec_latent);
+                    v[k].load(x + e, a.vec_latent);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sum += v[k][i] * v[k][i];
                 }
@@ -143,27 +168,29 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
             for (int k = 0; k < kLatentMaxRank / 256; ++k) {
                 const int e = (k * 32 + lane) * 8;
                 if (e < a.rank) {
-                    if (a.weight) {
-                        float w[8];
-                        load8(static_cast<const T*>(a.weight) + e, w, a.vec_w);
+                    float y[8];
+                    Eight<T> w;
+                    if (a.weight) w.load(static_cast<const T*>(a.weight) + e, a.vec_w);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) v[k][i] = v[k][i] * r * w[i];
-                    }
-                    store8(dst + e, v[k], a.vec_rows);
+                    for (int i = 0; i < 8; ++i) y[i] = a.weight ? v[k][i] * r * w[i] : v[k][i];
+                    store8(dst + e, y, a.vec_rows);
                 }
             }
         }
     }
     __syncthreads();
-    if (dst && lane < half / 8) turn8(x + a.rank, dst + a.rank, cs[warp], a.rot, lane, a.interleaved, a.vec_latent, a.vec_rows);
-    if (a.q) {
-        const int per_head = half / 8, per_token = a.H * per_head;
-        for (int i = threadIdx.x; i < nt * per_token; i += kRowThreads) {
-            const int t = i / per_token, k = i - t * per_token, h = k / per_head, v = k - h * per_head, n = n0 + t;
-            const T* src = static_cast<const T*>(a.q_in) + b * a.q_batch + n * a.q_token + h * a.q_head;
-            T* o = static_cast<T*>(a.q) + (((long long)b * a.H + h) * a.N + n) * W + a.rank;
-            turn8(src, o, cs[t], a.rot, v, a.interleaved, a.vec_q, a.vec_qout);
-        }
+    if (dst && lane < half / 8) {
+        Turn8<T> r;
+        r.load(x + a.rank, a.rot, lane, a.interleaved, a.vec_latent);
+        r.store(dst + a.rank, cs[warp], a.rot, lane, a.interleaved, a.vec_rows);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+        if ((int)threadIdx.x + j * kRowThreads < parts) put(ahead[j], threadIdx.x + j * kRowThreads);
+    for (int i = threadIdx.x + kAhead * kRowThreads; i < parts; i += kRowThreads) {
+        Turn8<T> x;
+        fetch(x, i);
+        put(x, i);
     }
 }
 
@@ -183,18 +210,33 @@ commit_latent_kernel(void* const* __restrict__ cache_layers, const void* const* 
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the length has been read
     const int vecs = row_bytes / 16, per_layer = count * vecs;
     const int layers = (n_layers - rank + kCommitCluster - 1) / kCommitCluster;
-    for (int i = threadIdx.x; i < layers * per_layer; i += kLatentCommitThreads) {
-        const int k = i / per_layer, rest = i - k * per_layer, layer = rank + k * kCommitCluster;
-        const int t = rest / vecs, v = rest - t * vecs;
-        const int node = t == 0 ? best_root[b] : out_nodes[(size_t)b * n_levels + (t - 1)];
-        if (node < 0 || node >= N) continue;                        // malformed verify output: leave the row alone
-        const char* src = static_cast<const char*>(tree_layers[layer]) + ((size_t)b * N + node) * row_bytes + v * 16;
-        char* dst = static_cast<char*>(cache_layers[layer]) + ((size_t)b * L_max + L + t) * row_bytes + v * 16;
-        if (((reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst)) & 15u) == 0) {
-            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-        } else {
-            for (int j = 0; j < 16; j += 2) *reinterpret_cast<uint16_t*>(dst + j) = *reinterpret_cast<const uint16_t*>(src + j);
+    constexpr int kFlight = 4;                          // vectors of a thread on their way at a time
+    for (int i = threadIdx.x; i < layers * per_layer; i += kFlight * kLatentCommitThreads) {
+        const char* src[kFlight];
+        char* dst[kFlight];
+        uint4 x[kFlight];
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j) {
+            src[j] = nullptr;
+            const int at = i + j * kLatentCommitThreads;
+            if (at >= layers * per_layer) continue;
+            const int k = at / per_layer, rest = at - k * per_layer, layer = rank + k * kCommitCluster;
+            const int t = rest / vecs, v = rest - t * vecs;
+            const int node = t == 0 ? best_root[b] : out_nodes[(size_t)b * n_levels + (t - 1)];
+            if (node < 0 || node >= N) continue;                    // malformed verify output: leave the row alone
+            src[j] = static_cast<const char*>(tree_layers[layer]) + ((size_t)b * N + node) * row_bytes + v * 16;
+            dst[j] = static_cast<char*>(cache_layers[layer]) + ((size_t)b * L_max + L + t) * row_bytes + v * 16;
         }
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j)
+            if (src[j] && (reinterpret_cast<uintptr_t>(src[j]) & 15u) == 0) x[j] = *reinterpret_cast<const uint4*>(src[j]);
+            else if (src[j])
+                for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(&x[j])[e] = reinterpret_cast<const uint16_t*>(src[j])[e];
+#pragma unroll
+        for (int j = 0; j < kFlight; ++j)
+            if (src[j] && (reinterpret_cast<uintptr_t>(dst[j]) & 15u) == 0) *reinterpret_cast<uint4*>(dst[j]) = x[j];
+            else if (src[j])
+                for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(dst[j])[e] = reinterpret_cast<const uint16_t*>(&x[j])[e];
     }
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (rank == 0 && threadIdx.x == 0) seq_lens[b] = min(L_max, L + 1 + acc);
