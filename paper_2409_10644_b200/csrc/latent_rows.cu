@@ -13,7 +13,7 @@
 namespace mcsd {
 
 constexpr int kRowThreads = 256;
-constexpr int kRowTokens = 4;          // tokens of a block at most
+constexpr int kRowTokens = 8;          // tokens of a block at most
 
 struct LatentRowArgs {
     const void *latent, *q_in, *weight;
@@ -51,8 +51,13 @@ struct alignas(16) Eight {
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* v, bool vec) {
     alignas(16) T t[8];
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = from_f<T>(v[i]);
+        for (int i = 0; i < 4; ++i) reinterpret_cast<__nv_bfloat162*>(t)[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = from_f<T>(v[i]);
+    }
     if (vec) {
         constexpr int n = sizeof(T) * 8 / 16;
 #pragma unroll
@@ -73,10 +78,17 @@ struct Turn8 {
     }
     __device__ __forceinline__ void store(T* dst, const float2* cs, int rot, int v, bool interleaved, bool vec) const {
         float x[8], y[8];
+        float2 w[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 c = reinterpret_cast<const float4*>(cs + 8 * v)[i];
+            w[2 * i] = make_float2(c.x, c.y);
+            w[2 * i + 1] = make_float2(c.z, c.w);
+        }
         if (interleaved) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 c = cs[8 * v + i], d = cs[8 * v + 4 + i];
+                const float2 c = w[i], d = w[4 + i];
                 x[2 * i] = a[2 * i] * c.x - a[2 * i + 1] * c.y;
                 x[2 * i + 1] = a[2 * i + 1] * c.x + a[2 * i] * c.y;
                 y[2 * i] = b[2 * i] * d.x - b[2 * i + 1] * d.y;
@@ -85,7 +97,7 @@ struct Turn8 {
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float2 c = cs[8 * v + i];
+                const float2 c = w[i];
                 x[i] = a[i] * c.x - b[i] * c.y;
                 y[i] = b[i] * c.x + a[i] * c.y;
             }
@@ -95,41 +107,47 @@ struct Turn8 {
     }
 };
 
-// grid: (ceil(N / tokens), B)
-template <typename T>
+// grid: (ceil(N / tokens), B).  VEC: all accesses are 16-byte ones
+template <typename T, bool VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_constant__ LatentRowArgs a) {
-    __shared__ float2 cs[kRowTokens][kLatentMaxRot / 2];
+    __shared__ __align__(16) float2 cs[kRowTokens][kLatentMaxRot / 2];      // (a row: 16-byte aligned)
     const int b = blockIdx.y, n0 = blockIdx.x * a.tokens;
     const int Nb = a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N;
     const int nt = min(a.tokens, Nb - n0);
     if (nt <= 0) return;
     const int half = a.rot / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int W = a.rank + a.rot;
-    // the heads' parts are on their way while the angles are reduced and the latent part is normalised
+    // the heads' parts are on their way while the angles are reduced and the latent part is normalised: a thread takes the
+    // same vector of every G-th head, counted through the block's tokens (without a division: the kernel is bound by its
+    // instructions before it is by memory)
     constexpr int kAhead = 4 / sizeof(T);
-    const int per_head = half / 8, per_token = a.H * per_head, parts = a.q ? nt * per_token : 0;
-    auto part = [&](int i, int& t, int& h, int& v) {
-        t = i / per_token;
-        const int k = i - t * per_token;
-        h = k / per_head;
-        v = k - h * per_head;
+    const int per_head = half / 8, G = per_head > 0 ? kRowThreads / per_head : 1;
+    const int g = per_head > 0 ? threadIdx.x / per_head : 0, v8 = threadIdx.x - g * per_head;
+    const bool heads = a.q && g < G;
+    const T* const q_src = static_cast<const T*>(a.q_in) + b * a.q_batch + n0 * a.q_token;
+    T* const q_dst = static_cast<T*>(a.q) + ((long long)b * a.H * a.N + n0) * W + a.rank;
+    const long long head_step = (long long)a.N * W;
+    auto next = [&](int& t, int& h) {
+        h += G;
+        while (h >= a.H && t < nt) { h -= a.H; ++t; }
     };
-    auto fetch = [&](Turn8<T>& x, int i) {
-        int t, h, v;
-        part(i, t, h, v);
-        x.load(static_cast<const T*>(a.q_in) + b * a.q_batch + (n0 + t) * a.q_token + h * a.q_head, a.rot, v, a.interleaved, a.vec_q);
+    int ft = 0, fh = g - G, pt = 0, ph = g - G;        // token and head that are fetched, and put
+    next(ft, fh);
+    next(pt, ph);
+    auto fetch = [&](Turn8<T>& x) {
+        if (ft < nt) x.load(q_src + ft * a.q_token + fh * a.q_head, a.rot, v8, INTERLEAVED, VEC || a.vec_q);
+        next(ft, fh);
     };
-    auto put = [&](const Turn8<T>& x, int i) {
-        int t, h, v;
-        part(i, t, h, v);
-        T* o = static_cast<T*>(a.q) + (((long long)b * a.H + h) * a.N + n0 + t) * W + a.rank;
-        x.store(o, cs[t], a.rot, v, a.interleaved, a.vec_qout);
+    auto put = [&](const Turn8<T>& x) {
+        if (pt < nt) x.store(q_dst + ph * head_step + pt * W, cs[pt], a.rot, v8, INTERLEAVED, VEC || a.vec_qout);
+        next(pt, ph);
     };
     Turn8<T> ahead[kAhead];
+    if (heads) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-        if ((int)threadIdx.x + j * kRowThreads < parts) fetch(ahead[j], threadIdx.x + j * kRowThreads);
-    for (int i = threadIdx.x; i < nt * half; i += kRowThreads) {
+        for (int j = 0; j < kAhead; ++j) fetch(ahead[j]);
+    }
+    for (int i = threadIdx.x ^ (kRowThreads / 2); i < nt * half; i += kRowThreads) {   // by the warps without a latent part first
         const int t = i / half, j = i - t * half, n = n0 + t;
         const double pos = (double)a.seq_lens[b] + (double)(a.depth ? a.depth[n] : n);
         double turns = pos * a.freqs[j] * 0.15915494309189535;      // 1 / 2 pi
@@ -153,7 +171,7 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
             for (int k = 0; k < kLatentMaxRank / 256; ++k) {
                 const int e = (k * 32 + lane) * 8;
                 if (e < a.rank) {
-                    v[k].load(x + e, a.vec_latent);
+                    v[k].load(x + e, VEC || a.vec_latent);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sum += v[k][i] * v[k][i];
                 }
@@ -170,10 +188,10 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
                 if (e < a.rank) {
                     float y[8];
                     Eight<T> w;
-                    if (a.weight) w.load(static_cast<const T*>(a.weight) + e, a.vec_w);
+                    if (a.weight) w.load(static_cast<const T*>(a.weight) + e, VEC || a.vec_w);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) y[i] = a.weight ? v[k][i] * r * w[i] : v[k][i];
-                    store8(dst + e, y, a.vec_rows);
+                    store8(dst + e, y, VEC || a.vec_rows);
                 }
             }
         }
@@ -181,16 +199,17 @@ __global__ void __launch_bounds__(kRowThreads) latent_rows_kernel(const __grid_c
     __syncthreads();
     if (dst && lane < half / 8) {
         Turn8<T> r;
-        r.load(x + a.rank, a.rot, lane, a.interleaved, a.vec_latent);
-        r.store(dst + a.rank, cs[warp], a.rot, lane, a.interleaved, a.vec_rows);
+        r.load(x + a.rank, a.rot, lane, INTERLEAVED, VEC || a.vec_latent);
+        r.store(dst + a.rank, cs[warp], a.rot, lane, INTERLEAVED, VEC || a.vec_rows);
     }
+    if (heads) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-        if ((int)threadIdx.x + j * kRowThreads < parts) put(ahead[j], threadIdx.x + j * kRowThreads);
-    for (int i = threadIdx.x + kAhead * kRowThreads; i < parts; i += kRowThreads) {
-        Turn8<T> x;
-        fetch(x, i);
-        put(x, i);
+        for (int j = 0; j < kAhead; ++j) put(ahead[j]);
+        while (pt < nt) {
+            Turn8<T> x;
+            fetch(x);
+            put(x);
+        }
     }
 }
 
@@ -242,6 +261,14 @@ commit_latent_kernel(void* const* __restrict__ cache_layers, const void* const* 
     if (rank == 0 && threadIdx.x == 0) seq_lens[b] = min(L_max, L + 1 + acc);
 }
 
+template <typename T>
+static void launch_latent_rows(const LatentRowArgs& a, dim3 grid, cudaStream_t s) {
+    const bool vec = (a.vec_latent && a.vec_rows && (a.vec_w || !a.weight) || !a.rows) && (a.vec_q && a.vec_qout || !a.q);
+    if (vec && a.interleaved) latent_rows_kernel<T, true, true><<<grid, kRowThreads, 0, s>>>(a);
+    else if (vec) latent_rows_kernel<T, true, false><<<grid, kRowThreads, 0, s>>>(a);
+    else if (a.interleaved) latent_rows_kernel<T, false, true><<<grid, kRowThreads, 0, s>>>(a);
+    else latent_rows_kernel<T, false, false><<<grid, kRowThreads, 0, s>>>(a);
+}
 static bool vec_ok(const void* p, std::initializer_list<long long> strides, int elt) {
     if (reinterpret_cast<uintptr_t>(p) & 15u) return false;
     for (long long s : strides)
@@ -281,8 +308,8 @@ extern "C" int mcsd_latent_rows(const void* latent_in, const void* q_in, const i
     a.tokens = (long long)B * N >= 4096 ? mcsd::kRowTokens : 1;
     const dim3 grid((N + a.tokens - 1) / a.tokens, B);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (dtype == MCSD_F32) mcsd::latent_rows_kernel<float><<<grid, mcsd::kRowThreads, 0, s>>>(a);
-    else mcsd::latent_rows_kernel<__nv_bfloat16><<<grid, mcsd::kRowThreads, 0, s>>>(a);
+    if (dtype == MCSD_F32) mcsd::launch_latent_rows<float>(a, grid, s);
+    else mcsd::launch_latent_rows<__nv_bfloat16>(a, grid, s);
     MCSD_CUDA_CHECK(cudaGetLastError());
     mcsd::count_launches(1);
     return MCSD_OK;
