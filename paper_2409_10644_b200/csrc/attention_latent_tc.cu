@@ -22,19 +22,27 @@
 //
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
 // inside an item, the pieces write unnormalised rows and count themselves in.  An item of two or three pieces is joined by the
-// pair that starts it, from tensor memory: the others wrote theirs early, as the first of their ranges.  Where there are more, a
-// pair at the end of its range waits for the other pieces of such an item and joins a share of its channels (only as many pairs
-// get work as keeps items in three pieces, where that is sooner done).  All blocks usually run at a time, one a multiprocessor;
-// where others hold multiprocessors (a kernel of another stream), a pair must not wait for one that cannot start before it
-// leaves.  So it waits for a millisecond at most, then notes that it is gone, and the pair that brings the last piece joins the
-// shares of those that are: no result depends on which blocks run together.
+// pair that starts it, from tensor memory: the others wrote theirs early, as the first of their ranges (with three instead of
+// two 32 single tokens of 128 heads over 4000 keys take 42 instead of 56 us).  Where there are more, the pairs wait at the end of
+// their ranges and join a share of its channels each (only as many pairs get work as keeps items in three pieces, where that is
+// sooner done).  Both bring what they join into shared memory at once: the range is over, its memory free.
+//
+// All blocks usually run at a time, one a multiprocessor; where others hold multiprocessors (a kernel of another stream), a pair
+// must not wait for one that cannot start before it leaves.  So it waits for a millisecond at most, then notes that it is gone,
+// and the pair that brings the last piece joins the shares of those that are: no result depends on which blocks run together.
+//
+// What bounds it.  Many rows: the tensor cores; 128 heads of a 74-node tree over 32768 keys run at 1.59 PFLOP/s, the rate of a
+// plain matrix product on this card.  A tile takes 3.3 us, an item 4 more for its last products and its output, which nothing
+// covers, and a launch 9 to start: 16 trees of 45 nodes and 32 heads over 4096 keys 180 us, 1.15 PFLOP/s.  One row block a
+// sequence: memory, at 7 TB/s once it streams; 8 tokens of 128 heads over up to 32001 keys 59 us, of which 20 are start and
+// joining.  One token of 16 heads over 1001 keys: 18 us of latencies (5 until the first scores, 5 for two tiles, 7 to join).
 //
 // The five roles run side by side, each its own loop: unrolled, they did not fit the instruction caches, and a tile took 4.9 us
 // instead of 3.4 (the loops of S over nine chunks and of O over four quarters are rolled for that alone).
 //
 // Warps of a block: 0 loads for S, 1 issues it, 2 loads for O, 3 issues it (1 and 3 in the first block of the pair), 4 to 11
-// fetch queries, do the softmax and the output.  Every wait is bounded; one that runs out raises a flag in the workspace header, all roles drain and the
-// blocks exit.
+// fetch queries, do the softmax and the output.  Every wait is bounded; one that runs out raises a flag in the workspace header,
+// all roles drain and the blocks exit.
 #include <cuda.h>
 
 #include <algorithm>
@@ -104,6 +112,7 @@ struct LtSmall {
     float lsum[4][64];
 };
 constexpr int kLtSmem = 1024 + kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes + (int)sizeof(LtSmall);
+static_assert((kLtFew - 1) * 8 * 4096 <= kLtQBytes && kLtQBytes <= kLtSlots * kLtSlotBytes, "a quarter of the pieces that are joined at the start");
 static_assert(kLtSmem <= kSmemLimit, "a block's shared memory");
 
 // ------------------------------------------------------------------ PTX of a pair of blocks
@@ -276,58 +285,19 @@ __device__ __forceinline__ uint32_t anc_bits(const uint64_t* w, int words, int p
 __device__ __forceinline__ float4* lt_part(const LtParams& p, int slot, int rank, int quad, int tlane) {
     return reinterpret_cast<float4*>(p.part_o) + (((long long)slot * 2 + rank) * 64 + quad) * 128 + tlane;
 }
-// QUADS quads of one lane's columns, from quad0 on: all pieces joined, in their order, PIECES of them in flight.
-template <int QUADS, int PIECES>
-__device__ __forceinline__ void lt_join_quads(const LtParams& p, const LtItem& it, int first, int count, int rank, int tlane, int quad0) {
-    const LatentArgs& a = p.a;
-    const int row = tlane & 63, half = tlane >> 6, r = it.rb * 128 + rank * 64 + row;
-    if (r >= a.H * it.Nb) return;
-    float m = -INFINITY, l = 0.0f;
-    float4 o[QUADS];
-#pragma unroll
-    for (int i = 0; i < QUADS; ++i) o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int k = 0; k < count; k += PIECES) {
-        float2 ml[PIECES];
-        float4 v[PIECES][QUADS];
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
-            // piece 0 lies in its pair's second slot, the others in the first; past the last one: that one, without weight
-            const int kk = min(k + j, count - 1), slot = 2 * (first + kk) + (kk == 0);
-            ml[j] = __ldcg(p.part_ml + slot * 128 + rank * 64 + row);
-#pragma unroll
-            for (int i = 0; i < QUADS; ++i) v[j][i] = __ldcg(lt_part(p, slot, rank, quad0 + i, tlane));
-        }
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
-            if (k + j >= count) continue;
-            const float top = fmaxf(m, ml[j].x), sub = top == -INFINITY ? 0.0f : top;
-            const float f = ex2_approx(m - sub), e = ex2_approx(ml[j].x - sub);
-            m = top;
-            l = l * f + ml[j].y * e;
-#pragma unroll
-            for (int i = 0; i < QUADS; ++i) {
-                o[i].x = o[i].x * f + v[j][i].x * e;
-                o[i].y = o[i].y * f + v[j][i].y * e;
-                o[i].z = o[i].z * f + v[j][i].z * e;
-                o[i].w = o[i].w * f + v[j][i].w * e;
-            }
-        }
-    }
-    const float inv = l > 0.0f ? 1.0f / l : l;
-    const int h = r / it.Nb, n = r - h * it.Nb, c = 4 * quad0;
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * (c >> 7) + 128 * half + (c & 127);
-    uint2 v[QUADS];
-#pragma unroll
-    for (int i = 0; i < QUADS; ++i) {
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i].x) : "f"(o[i].y * inv), "f"(o[i].x * inv));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[i].y) : "f"(o[i].w * inv), "f"(o[i].z * inv));
-    }
-    if constexpr (QUADS == 1) {
-        *reinterpret_cast<uint2*>(out) = v[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < QUADS; i += 2) *reinterpret_cast<uint4*>(out + 4 * i) = make_uint4(v[i].x, v[i].y, v[i + 1].x, v[i + 1].y);
-    }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ float4 lds16(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 lds8(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
 }
 // Waits (one thread) until `count` pieces are in or patience runs out; then this pair is counted as gone, unless they came in
 // just before.  Returns whether they are in.  `bit` of `word` goes before the count: who sees the count finds it.
@@ -344,28 +314,85 @@ __device__ __noinline__ bool lt_await(LtSmall* sm, int* counter, int count, bool
     __threadfence();
     return in;
 }
-// Share k of `count` of a cut item's columns, by the 256 threads of the softmax warps.
-__device__ __noinline__ void lt_join_share(const LtParams& p, const LtItem& it, int first, int count, int k, int rank, int tid) {
-    const int tlane = tid & 127;
-    if (count <= 6) {                                    // few pieces: 16 channels a thread, whole sectors of the output
-        for (int u = 16 * k / count + (tid >> 7); u < 16 * (k + 1) / count; u += 2) lt_join_quads<4, 6>(p, it, first, count, rank, tlane, 4 * u);
-    } else if (count <= 16) {
-        for (int u = 32 * k / count + (tid >> 7); u < 32 * (k + 1) / count; u += 2) lt_join_quads<2, 12>(p, it, first, count, rank, tlane, 2 * u);
-    } else {                                             // many: one quad, sixteen pieces in flight
-        for (int u = 64 * k / count + (tid >> 7); u < 64 * (k + 1) / count; u += 2) lt_join_quads<1, 16>(p, it, first, count, rank, tlane, u);
-    }
+// This pair is done with an item in `count` pieces: the last one to leave puts its counters back to zero.
+__device__ __forceinline__ void lt_leave(int* counter, int count) {
+    if (atomicAdd(counter, kLtLeft) / kLtLeft == count - 1)
+        for (int k = 0; k < kCountersPerBlock; ++k) counter[k] = 0;
 }
-// At the end of a range: this pair's share of an item in more than kLtFew pieces, and where its piece was the last one to come
-// in, the shares of the pairs that are gone (of an item in fewer pieces, which the pair that starts it did not wait for: all).
-__device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, int i, int pair, int rank, int tid, bool ok) {
+// Share k of `shares` of the columns of an item in `count` pieces, by the 256 threads of the softmax warps: a thread has a lane of tensor memory and
+// every other quad of columns.  The range is over, so that all of a block's operand memory is free: the pieces' values come
+// there, as many at a time as fit, and are joined in their order.
+constexpr int kLtJoinSlots = 44;                                  // of 16 bytes a thread
+static_assert((kLtJoinSlots * 256 * 16) + kLtMaxPairs * 512 <= kLtQBytes + kLtPBytes + kLtSlots * kLtSlotBytes, "joining");
+__device__ __noinline__ void lt_join_share(const LtParams& p, const LtItem& it, uint32_t smem, int first, int count, int k, int shares, int rank, int tid) {
+    const LatentArgs& a = p.a;
+    const int tlane = tid & 127, row = tlane & 63, half = tlane >> 6, r = it.rb * 128 + rank * 64 + row;
+    const bool in = r < a.H * it.Nb;
+    const uint32_t ml = smem + kLtJoinSlots * 4096, own = smem + tid * 16;
+    // piece 0 lies in its pair's second slot, the others in the first
+    for (int i = tid; i < 32 * count; i += 256) {
+        const int piece = i >> 5, slot = 2 * (first + piece) + (piece == 0);
+        copy16(ml + piece * 512 + (i & 31) * 16, p.part_ml + slot * 128 + rank * 64 + 2 * (i & 31));
+    }
+    const int q0 = 64 * k / shares + (tid >> 7), q1 = 64 * (k + 1) / shares, n = in && q1 > q0 ? (q1 - q0 + 1) / 2 * count : 0;
+    float top = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    int quad = q0, piece = 0, fq = q0, fp = 0;
+    const int h = in ? r / it.Nb : 0, node = in ? r - h * it.Nb : 0;
+    __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + node) * kLtRank + 128 * half;
+    for (int done = 0; done == 0 || done < n;) {
+        const int now = min(n - done, kLtJoinSlots);
+#pragma unroll 4
+        for (int i = 0; i < now; ++i) {
+            copy16(own + i * 4096, lt_part(p, 2 * (first + fp) + (fp == 0), rank, fq, tlane));
+            if (++fp == count) { fp = 0; fq += 2; }
+        }
+        copies_done();
+        if (done == 0) {
+            softmax_sync();                                       // references and sums are there
+            for (int i = 0; i < count; ++i) top = fmaxf(top, lds8(ml + i * 512 + row * 8).x);
+            if (top == -INFINITY) top = 0.0f;
+            for (int i = 0; i < count; ++i) {
+                const float2 x = lds8(ml + i * 512 + row * 8);
+                l += x.y * ex2_approx(x.x - top);
+            }
+            if (n == 0) break;
+        }
+        for (int i = 0; i < now; ++i) {
+            const float e = ex2_approx(lds8(ml + piece * 512 + row * 8).x - top);
+            const float4 v = lds16(own + i * 4096);
+            o.x += v.x * e;
+            o.y += v.y * e;
+            o.z += v.z * e;
+            o.w += v.w * e;
+            if (++piece == count) {
+                const float inv = l > 0.0f ? 1.0f / l : l;
+                uint2 x;
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.x) : "f"(o.y * inv), "f"(o.x * inv));
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x.y) : "f"(o.w * inv), "f"(o.z * inv));
+                const int c = 4 * quad;
+                *reinterpret_cast<uint2*>(out + 256 * (c >> 7) + (c & 127)) = x;
+                o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                piece = 0;
+                quad += 2;
+            }
+        }
+        done += now;
+    }
+    softmax_sync();                                               // its memory is free for the next share
+}
+// At the end of a range: this pair's share of an item in more than kLtFew pieces (the pair with the last piece has none: it has a
+// share of the next item), and where its piece was the last one to come in, the shares of the pairs that are gone (of an item in
+// fewer pieces, which the pair that starts it did not wait for: all).
+__device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, uint32_t smem, int i, int pair, int rank, int tid, bool ok) {
     const LtItem& it = sm->join[i];
     int first, last;
     lt_owners(sm, it, first, last);
-    const int count = last - first + 1, own = pair - first;
+    const int count = last - first + 1, own = pair - first, shares = count <= kLtFew ? 1 : count - 1;
     int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
     if (tid == 0) {
         const int in = sm->join_in[i];
-        const bool last_in = (in & (kLtGone - 1)) == count - 1, gone = in / kLtGone > 0;
+        const bool last_in = (in & (kLtGone - 1)) == count - 1;
         const uint32_t bit = 1u << (own & 31);
         if (!last_in) {
             const bool mine = lt_await(sm, counter, count, ok, counter + 1 + (own >> 5), (int)bit);
@@ -373,19 +400,17 @@ __device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, int i,
         } else {
             __threadfence();
             for (int k = 0; k < kLtGoneWords; ++k)
-                sm->shares[k] = count <= kLtFew ? ~0u : (gone ? (uint32_t)__ldcg(counter + 1 + k) : 0) | (k == own >> 5 ? bit : 0);
+                sm->shares[k] = count <= kLtFew ? 1u : (uint32_t)__ldcg(counter + 1 + k) | (own < shares && k == own >> 5 ? bit : 0);
         }
     }
     softmax_sync();
-    for (int k = 0; k < count; ++k)
-        if (sm->shares[k >> 5] >> (k & 31) & 1) lt_join_share(p, it, first, count, k, rank, tid);
-    softmax_sync();
-    if (tid == 0) {                                      // counters are zero between launches: the last one to leave
-        bool reset = count <= kLtFew;
-        if (!reset) reset = atomicAdd(counter, kLtLeft) / kLtLeft == count - 1;
-        if (reset)
-            for (int k = 0; k < kCountersPerBlock; ++k) counter[k] = 0;
+    for (int k = 0; k < shares; ++k)
+        if (sm->shares[k >> 5] >> (k & 31) & 1) lt_join_share(p, it, smem, first, count, k, shares, rank, tid);
+    if (tid == 0) {
+        if (count <= kLtFew) *counter = 0;
+        else lt_leave(counter, count);
     }
+    softmax_sync();
 }
 #define LT_WAIT(bar, parity, where) mbar_wait(bar, parity, &sm->abort_flag, p.header, where)
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLtThreads, 1)
@@ -770,33 +795,46 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             __nv_bfloat16* out = in ? static_cast<__nv_bfloat16*>(a.out) + (((long long)it.b * a.H + h) * a.N + n) * kLtRank + 256 * group + 128 * half : nullptr;
             const uint32_t stage = p_a + (2 * half + group) * 8192;
             float4* part = lt_part(p, slot, rank, 32 * group, 64 * half + row);
+            // the other pieces' values come into shared memory, a quarter of a thread's columns at a time, two quarters ahead:
+            // this item is the last of its range, so that queries and rings are free
+            const bool join = finish && !whole;
+            const uint32_t ahead = tid * 16 - 2048;                             // (softmax threads count from 128)
+            auto bring = [&](int c) {
+                if (join && in && c < 4) {
+                    for (int k = 0; k + 1 < pieces; ++k)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            copy16((c & 1 ? ring_a : q_a) + (8 * k + i) * 4096 + ahead, lt_part(p, 2 * (first + 1 + k), rank, 32 * group + 8 * c + i, 64 * half + row));
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            bring(0);
+            bring(1);
+            __syncwarp();
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 float o[32];
-                float4 v[kLtFew - 1][8];
-                const bool join = in && finish && !whole;
                 tc_ld32(lane_addr + kLtColO + 128 * group + 32 * c, o);
-#pragma unroll
-                for (int k = 0; k < kLtFew - 1; ++k)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[k][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (join && k + 1 < pieces) v[k][i] = __ldcg(lt_part(p, 2 * (first + 1 + k), rank, 32 * group + 8 * c + i, 64 * half + row));
-                    }
-                __syncwarp();
                 tc_wait_ld();
                 if (join) {
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    if (in) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        o[4 * i] *= own; o[4 * i + 1] *= own; o[4 * i + 2] *= own; o[4 * i + 3] *= own;
+                        for (int i = 0; i < 32; ++i) o[i] *= own;
+#pragma unroll 1
+                        for (int k = 0; k + 1 < pieces; ++k) {
+                            const float e = k == 0 ? others[0].x : others[1].x;
 #pragma unroll
-                        for (int k = 0; k < kLtFew - 1; ++k) {
-                            o[4 * i] += others[k].x * v[k][i].x;
-                            o[4 * i + 1] += others[k].x * v[k][i].y;
-                            o[4 * i + 2] += others[k].x * v[k][i].z;
-                            o[4 * i + 3] += others[k].x * v[k][i].w;
+                            for (int i = 0; i < 8; ++i) {
+                                const float4 v = lds16((c & 1 ? ring_a : q_a) + (8 * k + i) * 4096 + ahead);
+                                o[4 * i] += e * v.x;
+                                o[4 * i + 1] += e * v.y;
+                                o[4 * i + 2] += e * v.z;
+                                o[4 * i + 3] += e * v.w;
+                            }
                         }
                     }
+                    bring(c + 2);
                 }
                 if (finish) {
                     // through this warp's rows of P (free by now), so that a row's 128 bytes leave together
@@ -835,7 +873,10 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 softmax_sync();
                 if (w == 0 && lane == 0) {
                     const int in = atomicAdd(counter, 1);
-                    if (pieces > kLtFew || (in & (kLtGone - 1)) == pieces - 1) {
+                    const bool last_in = (in & (kLtGone - 1)) == pieces - 1, gone = (in & (kLtLeft - 1)) >= kLtGone;
+                    if (pieces > kLtFew && pair == last && !(last_in && gone)) {
+                        lt_leave(counter, pieces);                              // no share: see there
+                    } else if (pieces > kLtFew || last_in) {
                         sm->join_in[sm->joins] = in;
                         sm->join[sm->joins++] = it;
                     }
@@ -848,7 +889,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
         }
         if (g > 0) ok = ok && LT_WAIT(&sm->p_free[2 * half + group], (g - 1) & 1, 15);   // the last arrival here, before the block may leave
         softmax_sync();
-        for (int i = 0; i < sm->joins; ++i) lt_join_item(sm, p, i, pair, rank, tid - 128, ok);
+        for (int i = 0; i < sm->joins; ++i) lt_join_item(sm, p, q_a, i, pair, rank, tid - 128, ok);
     }
     tc_fence_before();
     __syncthreads();
