@@ -354,17 +354,17 @@ __device__ __noinline__ void lt_join_share(const LtParams& p, const LtItem& it, 
             if (top == -INFINITY) top = 0.0f;
             for (int i = 0; i < count; ++i) {
                 const float2 x = lds8(ml + i * 512 + row * 8);
-                l += x.y * ex2_approx(x.x - top);
+                l = __fmaf_rn(x.y, ex2_approx(x.x - top), l);      // (spelt out: alike wherever an item is joined)
             }
             if (n == 0) break;
         }
         for (int i = 0; i < now; ++i) {
             const float e = ex2_approx(lds8(ml + piece * 512 + row * 8).x - top);
             const float4 v = lds16(own + i * 4096);
-            o.x += v.x * e;
-            o.y += v.y * e;
-            o.z += v.z * e;
-            o.w += v.w * e;
+            o.x = __fmaf_rn(v.x, e, o.x);
+            o.y = __fmaf_rn(v.y, e, o.y);
+            o.z = __fmaf_rn(v.z, e, o.z);
+            o.w = __fmaf_rn(v.w, e, o.w);
             if (++piece == count) {
                 const float inv = l > 0.0f ? 1.0f / l : l;
                 uint2 x;
@@ -780,11 +780,11 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                 }
                 const float sub = top == -INFINITY ? 0.0f : top;
                 own = ex2_approx(ref - sub);
-                l *= own;
+                l = __fmul_rn(l, own);
 #pragma unroll
                 for (int k = 0; k < kLtFew - 1; ++k) {
                     others[k].x = ex2_approx(others[k].x - sub);
-                    l += others[k].x * others[k].y;
+                    l = __fmaf_rn(others[k].y, others[k].x, l);
                 }
             }
             if (!finish && half == 0 && group == 0) p.part_ml[slot * 128 + rank * 64 + row] = make_float2(ref, l);
@@ -820,17 +820,17 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     if (in) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] *= own;
+                        for (int i = 0; i < 32; ++i) o[i] = __fmul_rn(o[i], own);
 #pragma unroll 1
                         for (int k = 0; k + 1 < pieces; ++k) {
                             const float e = k == 0 ? others[0].x : others[1].x;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const float4 v = lds16((c & 1 ? ring_a : q_a) + (8 * k + i) * 4096 + ahead);
-                                o[4 * i] += e * v.x;
-                                o[4 * i + 1] += e * v.y;
-                                o[4 * i + 2] += e * v.z;
-                                o[4 * i + 3] += e * v.w;
+                                o[4 * i] = __fmaf_rn(v.x, e, o[4 * i]);
+                                o[4 * i + 1] = __fmaf_rn(v.y, e, o[4 * i + 1]);
+                                o[4 * i + 2] = __fmaf_rn(v.z, e, o[4 * i + 2]);
+                                o[4 * i + 3] = __fmaf_rn(v.w, e, o[4 * i + 3]);
                             }
                         }
                     }

@@ -397,6 +397,60 @@ def test_captured_with_lengths_that_change(m):  # noqa: F811
 
 
 @pytest.mark.gpu
+def test_two_calls_at_once(m):  # noqa: F811
+    """Calls of two streams, each with its own workspace: items in few pieces and in many, whichever blocks run first."""
+    cases = []
+    for seed, (B, H, tree, lens) in enumerate([(2, 32, "static", [6000, 300]), (1, 16, "token", [30000]), (3, 64, "token", [9000, 20, 4000])]):
+        parent = parent_array(*TREES[tree])
+        q, cache, rows = _problem(30 + seed, "bf16", B, H, 512, 64, parent, lens)
+        cases.append((q, cache, rows, _i32(lens), m.mcsd_build_mask(parent)))
+    size = max(m.mcsd_tree_attention_latent_workspace_bytes(*c[0].shape[:3], 512, 64, c[1].shape[1], m.MCSD_BF16) for c in cases)
+    spaces = [m.new_workspace(size, "cuda") for _ in range(2)]
+    call = lambda c, ws, out: m.mcsd_tree_attention_latent(*c[:4], None, c[4], 0.07, out=out, workspace=ws)  # noqa: E731
+    want = [call(c, spaces[0], torch.empty(*c[0].shape[:3], 512, dtype=torch.bfloat16, device="cuda")) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream(priority=-1)]
+    outs = [[], []]
+    for i in range(30):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                out = torch.full_like(want[(i + k) % 3], NAN)
+                call(cases[(i + k) % 3], spaces[k], out)
+                outs[k].append(out)
+    torch.cuda.synchronize()
+    assert [m.mcsd_workspace_status(ws) for ws in spaces] == [0, 0]
+    for k in range(2):
+        for i, out in enumerate(outs[k]):
+            assert torch.equal(out, want[(i + k) % 3]), (k, i)
+
+
+@pytest.mark.gpu
+def test_two_graphs_share_a_workspace(m):  # noqa: F811
+    """Replayed in turn; counters are zero between launches."""
+    parent = parent_array(*TREES["static"])
+    tm, ws = m.mcsd_build_mask(parent), torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    graphs, s = [], torch.cuda.Stream()
+    for seed, (H, dtype, lens) in enumerate([(16, "bf16", [20000, 10]), (2, "f32", [3000, 3001]), (32, "bf16", [7, 900])]):
+        q, cache, rows = _problem(40 + seed, dtype, 2, H, 512, 64, parent, lens)
+        ln, out = _i32(lens), torch.zeros(2, H, len(parent), 512, dtype=DT[dtype], device="cuda")
+        call = lambda: m.mcsd_tree_attention_latent(q, cache, rows, ln, None, tm, 0.07, out=out, workspace=ws)  # noqa: E731, B023
+        call()
+        torch.cuda.synchronize()
+        want, graph = out.clone(), torch.cuda.CUDAGraph()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=s):
+            call()
+        graphs.append((graph, out, want, (q, cache, rows, ln)))
+    for i in (0, 1, 2, 2, 0, 0, 1, 0, 2, 1):
+        graph, out, want, _ = graphs[i]
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert m.mcsd_workspace_status(ws) == 0
+
+
+@pytest.mark.gpu
 def test_lengths_out_of_range_are_clamped(m):  # noqa: F811
     parent = parent_array(*TREES["binary"])
     tm = m.mcsd_build_mask(parent)
