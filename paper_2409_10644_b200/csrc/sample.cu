@@ -12,7 +12,7 @@
 //
 // A row is read from memory once; what looks at it again finds it in L2, so that shared memory holds only what was found, and two
 // blocks share a multiprocessor: one row's chain of short steps runs under the other's.  (With the row in shared memory and one
-// block a multiprocessor 720 rows of 32000 took 103 us, with a row over two blocks 114.)  A block takes a row; where there are fewer
+// block a multiprocessor 720 rows of 32000 took 103 us, with a row over two blocks 114; with three blocks of 40 registers 139.)  A block takes a row; where there are fewer
 // rows than multiprocessors a cluster of up to eight takes it, split by columns (a meeting of a cluster costs a microsecond, ten
 // times one of a block).  The first pass finds the largest logit; the second, a comparison a token, picks the few that can decide
 // anything, and all later work is on those:
@@ -24,6 +24,9 @@
 // step of a histogram (1024 steps of (max - l), linear over the part that carries mass) in which the sum crosses.  On that list
 // the cut is found by dividing its range of places 1024 ways until 32 tokens are left, which a warp compares.  A list that
 // overflows (equal logits, masked ones, a large k) is divided in the same way by passes over the row.
+// What bounds it: latency.  720 rows of 32000 take 86 us (184 MB in and out, 2.1 TB/s; 39 % of the issue slots, the two blocks of a
+// multiprocessor waiting half of their time for memory or for one another), one row 16 us, 16 rows of 131071 30 us (of which
+// six meetings, two readings and the cut).
 // Probabilities are zeros and a value for each token that is kept.  They are written last, behind all meetings of the cluster
 // but one that orders nothing: a meeting waits for the writes before it (1 us each).
 #include <cooperative_groups.h>
@@ -124,6 +127,7 @@ struct Row : Scale {
             }
             return make_float4(no_nan(v.x), no_nan(v.y), no_nan(v.z), no_nan(v.w));
         }
+        if (i >= n) return make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         v.x = i < n ? at(i) : -INFINITY;
         v.y = i + 1 < n ? at(i + 1) : -INFINITY;
         v.z = i + 2 < n ? at(i + 2) : -INFINITY;
