@@ -500,11 +500,15 @@ int mcsd_latent_rows(const void* latent_in, const void* q_in, const int64_t* str
  *
  *   q [dev] dtype[B][H][N][rank + rot];  cache [dev] dtype[B][L_max][rank + rot] (NULL allowed when L_max is 0);
  *   tree [dev] dtype[B][N][rank + rot];  out [dev] dtype[B][H][N][rank]
+ *               `out` must not overlap the inputs
  *   seq_lens, n_active, anc, words   as for mcsd_tree_attention;   L_max <= 2^30;  B * H <= 65535
+ *   dtype       MCSD_BF16 runs on the tensor cores with rank 512 and rot 64 when q, cache, tree and out are 16-byte aligned;
+ *               everything else on the CUDA cores in fp32
  *   workspace   [dev] >= mcsd_tree_attention_latent_workspace_bytes(...) bytes, 256-byte aligned, zero-filled once; may be the
  *               workspace of the other attention calls; calls that may overlap on the device need distinct ones
  *
- * Errors: as mcsd_tree_attention.
+ * One launch on `stream` for up to 256 sequences on the tensor cores; one on the CUDA cores, two where the keys are cut into more
+ * than eight pieces.  Equal inputs give equal outputs, to the bit.  Errors: as mcsd_tree_attention.
  */
 size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 
@@ -544,7 +548,7 @@ int mcsd_commit_latent(void* const* cache_layers, const void* const* tree_layers
  *   logits       [dev] dtype, row r at r * row_stride elements, V each (MCSD_F32, or MCSD_BF16 widened exactly)
  *   temperature, top_p, min_p  [dev] float[rows], top_k  [dev] int32[rows]: a value a row; NULL = 1, or that filter off
  *   u            [dev] float[rows][K] uniforms in [0, 1);   tokens  [dev] int32[rows][K] out, or NULL (u is then not read)
- *   probs        [dev] float[rows][V] out, or NULL;  not both NULL
+ *   probs        [dev] float[rows][V] out, or NULL;  not both NULL;  outputs must not overlap the logits
  *   V            1 .. 262144;  K  1 .. 1024 (any, when tokens is NULL);  rows  1 .. 2^24
  *
  * Weights are fp32 and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of

@@ -241,3 +241,45 @@ def test_captured_and_on_another_stream(m):  # noqa: F811
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(tokens, want[0]) and torch.equal(probs, want[1])
+
+
+# more tokens above 2^-14 of the largest than a block lists: a higher bound is found (1.0), or not (1.3); large k by finer maxima
+MANY = [(160, 32000, 1.0, None, 0.95), (160, 32000, 1.0, None, 0.6), (150, 20000, 1.3, None, 0.95), (150, 20000, 1.3, None, 0.3),
+        (149, 16001, 3.0, None, 0.9), (160, 9000, 1.0, 2000, 0.9), (150, 9000, 1.5, 3500, 0.8), (150, 4001, 1.0, 300, None)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,V,temperature,top_k,top_p", MANY)
+def test_flat_rows_of_many(m, rows, V, temperature, top_k, top_p):  # noqa: F811
+    """Rows that take a block each, a few of them against the definition, and all as when they are split over several blocks.
+
+    A token at the cut of such a row weighs less than the sum's error bound (twice REL for the weights, half a step of 2^-31 for
+    each of its tokens, on either side of a comparison), so no seed is clear of it: what is kept has to be a beginning of the
+    order whose mass reaches top_p by that bound, and without its last token does not exceed it by more."""
+    g = torch.Generator("cuda").manual_seed(0)
+    x = 3 * torch.randn(rows, V, generator=g, device="cuda")
+    u = torch.rand(rows, 5, generator=g, device="cuda")
+    kw = lambda n: dict(temperature=_per_row(temperature, n, torch.float32), top_k=_per_row(top_k, n, torch.int32), top_p=_per_row(top_p, n, torch.float32))  # noqa: E731
+    tokens, probs = m.mcsd_sample_candidates(x, u, probs=True, **kw(rows))
+    T = float(np.float32(temperature))
+    for r in (0, 1, rows // 2, rows - 1):
+        host, got = x[r].double().cpu().numpy(), probs[r].double().cpu().numpy()
+        order = np.lexsort((np.arange(V), -host))[: top_k or V]
+        w = np.exp((host[order] - host[order[0]]) / T)
+        mass = np.cumsum(w) / w.sum()
+        n = int((got > 0).sum())
+        assert (got[order[:n]] > 0).all()
+        if top_p is None:
+            assert n == len(order)
+        else:
+            p, slack = float(np.float32(top_p)), 2 * REL + len(order) * 2.0 ** -31
+            assert mass[n - 1] >= p - slack and (n == 1 or mass[n - 2] < p + slack), (n, mass[n - 1] - p)
+        want = np.zeros(V)
+        want[order[:n]] = w[:n] / w[:n].sum()
+        assert (np.abs(got - want) <= (REL + n * 2.0 ** -31) * want + 1e-36).all()
+        run, slack = np.cumsum(want), 2 * REL + n * 2.0 ** -31
+        for t, z in zip(tokens[r].tolist(), u[r].tolist()):
+            assert want[t] > 0 and run[t] > z - slack and run[t] - want[t] <= z + slack
+    for lo, n in ((0, 1), (rows // 2, 2), (rows - 20, 20), (3, 70)):
+        t, p = m.mcsd_sample_candidates(x[lo:lo + n], u[lo:lo + n], probs=True, **kw(n))
+        assert torch.equal(tokens[lo:lo + n], t) and torch.equal(probs[lo:lo + n], p)
