@@ -22,12 +22,13 @@
 //     out to be among those, the pass is made again for all tokens.)  Where they are more than the list holds, a pass adds up
 //     what lies below 2^-10 .. 2^-13, and a higher bound is taken if that allows it;
 //   * once the cut is known, a list that overflowed is made again of what is kept (at temperature 1 and top_p 0.95 of normal
-//     logits three units wide, 720 rows: 192 us; 278 with passes over the row from there on).
+//     logits three units wide, 720 rows of 32000: 180 us; 278 with passes over the row from there on; 329 at temperature 1.3,
+//     where no bound is high enough and the cut is found by passes over the row).
 // Tokens that may hold the cut are collected in the cluster's first block: all of them under top-k, under top-p alone those of the
 // step of a histogram (1024 steps of (max - l), linear over the part that carries mass) in which the sum crosses.  On that list
 // the cut is found by dividing its range of places 1024 ways until 32 tokens are left, which a warp compares.  A list that
 // overflows (equal logits, masked ones, a large k) is divided in the same way by passes over the row.
-// What bounds it: latency.  720 rows of 32000 take 89 us (184 MB in and out, 2.1 TB/s; 39 % of the issue slots, the two blocks of a
+// What bounds it: latency.  720 rows of 32000 take 90 us (184 MB in and out, 2.0 TB/s; 39 % of the issue slots, the two blocks of a
 // multiprocessor waiting half of their time for memory or for one another), one row 17 us, 16 rows of 131071 32 us (of which
 // six meetings, two readings and the cut).
 // Probabilities are zeros and a value for each token that is kept.  They are written last, behind all meetings of the cluster
@@ -257,9 +258,22 @@ __device__ __forceinline__ void for_picked(SampleShared* sh, const Row<T>& r, fl
     if (n <= kPickMax) {
         for (int j = threadIdx.x; j < n; j += kSampleThreads) f(sh->pick[j], sh->pick_l[j]);
     } else {
-        for (int i = threadIdx.x; i < r.n; i += kSampleThreads) {
-            const float l = r.at(i);
-            if (l >= least && l != -INFINITY) f(i, l);
+        constexpr int kFlight = 2;                       // vectors of a thread on their way
+        for (int base = 4 * threadIdx.x; base < r.n; base += 4 * kFlight * kSampleThreads) {
+            float4 x[kFlight];
+#pragma unroll
+            for (int it = 0; it < kFlight; ++it) x[it] = r.four(base + it * 4 * kSampleThreads);
+#pragma unroll 1
+            for (int it = 0; it < kFlight; ++it) {
+                const float4 v = x[0];
+#pragma unroll
+                for (int k = 0; k + 1 < kFlight; ++k) x[k] = x[k + 1];
+                const int i = base + it * 4 * kSampleThreads;
+                if (v.x >= least && v.x != -INFINITY) f(i, v.x);
+                if (v.y >= least && v.y != -INFINITY) f(i + 1, v.y);
+                if (v.z >= least && v.z != -INFINITY) f(i + 2, v.z);
+                if (v.w >= least && v.w != -INFINITY) f(i + 3, v.w);
+            }
         }
     }
 }
