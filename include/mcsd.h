@@ -502,8 +502,8 @@ int mcsd_latent_rows(const void* latent_in, const void* q_in, const int64_t* str
  *   tree [dev] dtype[B][N][rank + rot];  out [dev] dtype[B][H][N][rank]
  *               `out` must not overlap the inputs
  *   seq_lens, n_active, anc, words   as for mcsd_tree_attention;   L_max <= 2^30;  B * H <= 65535
- *   dtype       MCSD_BF16 runs on the tensor cores with rank 512 and rot 64 when q, cache, tree and out are 16-byte aligned;
- *               everything else on the CUDA cores in fp32
+ *   dtype       MCSD_BF16 runs on the tensor cores with rank 512 and rot 64 when q, cache, tree and out are 16-byte aligned
+ *               (a kernel of its own where H * N <= 16 and the keys are few); everything else on the CUDA cores in fp32
  *   workspace   [dev] >= mcsd_tree_attention_latent_workspace_bytes(...) bytes, 256-byte aligned, zero-filled once; may be the
  *               workspace of the other attention calls; calls that may overlap on the device need distinct ones
  *

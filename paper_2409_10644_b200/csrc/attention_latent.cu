@@ -31,7 +31,12 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
     if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MCSD_ERR_BAD_SHAPE;
     const mcsd::LatentArgs a{q, cache, tree, out, seq_lens, n_active, anc, words, B, H, N, rank, rot, L_max, softmax_scale, dtype};
     auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
-    if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned16(q) && aligned16(cache) && aligned16(tree) && aligned16(out))
+    const bool aligned = aligned16(q) && aligned16(cache) && aligned16(tree) && aligned16(out);
+    int few = 0;
+    const int fs = aligned ? mcsd::latent_few_splits(B, H, N, rank, rot, L_max, dtype, &few) : MCSD_OK;
+    if (fs != MCSD_OK) return fs;
+    if (few > 0) return mcsd::tree_attention_latent_few(a, few, static_cast<cudaStream_t>(stream));
+    if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned)
         return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
 }

@@ -16,7 +16,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "latent.cuh"
+#include "latent_pieces.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -24,23 +24,11 @@ namespace mcsd {
 
 constexpr int kLsRows = 32, kLsKeys = 32, kLsThreads = 256;
 constexpr int kLsBlocks = 296;             // blocks that a launch is cut into, about
-constexpr int kLsCluster = 8;               // pieces that a cluster joins
 constexpr int kLsScores = 36;              // floats of a key's weights
-
-struct LatentSimt {
-    LatentArgs a;
-    int row_blocks, splits, keys_per_split;
-    bool vec;                              // 16-byte loads
-    float* part;                           // [splits][B][H * N][rank + 2], unused where a cluster joins
-};
 
 template <typename T> __device__ __forceinline__ float ls_load(const T* p);
 template <> __device__ __forceinline__ float ls_load(const float* p) { return __ldg(p); }
 template <> __device__ __forceinline__ float ls_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-template <typename T> __device__ __forceinline__ void ls_store(T* p, float v);
-template <> __device__ __forceinline__ void ls_store(float* p, float v) { *p = v; }
-template <> __device__ __forceinline__ void ls_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
 // One row of W values to shared memory, by a warp; four vectors of a lane are on their way at a time.
 template <typename T>
 __device__ __forceinline__ void ls_row(float* dst, const T* src, int W, int lane, bool vec) {
@@ -68,7 +56,7 @@ __device__ __forceinline__ void ls_row(float* dst, const T* src, int W, int lane
 
 // grid: (row blocks, splits, B), splits a cluster where JOIN.  ROWS: rows of a warp's products, 32 columns of 64 for 8 warps
 template <typename T, int ROWS, bool JOIN>
-__global__ void __launch_bounds__(kLsThreads) latent_simt_kernel(const __grid_constant__ LatentSimt g) {
+__global__ void __launch_bounds__(kLsThreads) latent_simt_kernel(const __grid_constant__ LatentPieces g) {
     extern __shared__ float4 raw4[];
     const LatentArgs& a = g.a;
     const int W = a.rank + a.rot;
@@ -201,35 +189,7 @@ __global__ void __launch_bounds__(kLsThreads) latent_simt_kernel(const __grid_co
         }
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
-        const int vecs = a.rank / 4, mine = (nr - (int)blockIdx.y + g.splits - 1) / g.splits;
-        for (int i = tid; i < mine * vecs; i += kLsThreads) {
-            const int r = (int)blockIdx.y + i / vecs * g.splits, d = 4 * (i % vecs);
-            float pm[kLsCluster], pl[kLsCluster], top = -INFINITY, sum = 0.0f;
-            float4 v[kLsCluster], o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int k = 0; k < kLsCluster; ++k) {
-                if (k >= g.splits) continue;
-                const float* peer = cluster.map_shared_rank(ps, k);
-                pm[k] = peer[r];
-                pl[k] = peer[kLsRows + r];
-                v[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(os, k) + r * a.rank + d);
-            }
-#pragma unroll
-            for (int k = 0; k < kLsCluster; ++k)
-                if (k < g.splits) top = fmaxf(top, pm[k]);
-#pragma unroll
-            for (int k = 0; k < kLsCluster; ++k) {
-                if (k >= g.splits || pm[k] == -INFINITY) continue;
-                const float f = expf(pm[k] - top);
-                sum += pl[k] * f;
-                o.x += v[k].x * f; o.y += v[k].y * f; o.z += v[k].z * f; o.w += v[k].w * f;
-            }
-            const int rr = r0 + r, h = rr / Nb, n = rr - h * Nb;
-            T* out = static_cast<T*>(a.out) + (((long long)b * a.H + h) * a.N + n) * a.rank + d;
-            const float y[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ls_store(out + j, sum > 0.0f ? y[j] / sum : y[j]);
-        }
+        latent_join_cluster<T, kLatentCluster>(g, os, ps, kLsRows, b, Nb, r0, nr, tid, kLsThreads);
         cluster.sync();                                  // others may still read this block's rows
     } else {
         __syncthreads();
@@ -247,37 +207,53 @@ __global__ void __launch_bounds__(kLsThreads) latent_simt_kernel(const __grid_co
     }
 }
 
-// grid: (H * N, B); joins the pieces of a row in their order
+// grid: (H * N, B, 128 channels each); joins the pieces of a row in their order
 template <typename T>
-__global__ void __launch_bounds__(128) latent_simt_join_kernel(const __grid_constant__ LatentSimt g) {
+__global__ void __launch_bounds__(128) latent_join_kernel(const __grid_constant__ LatentPieces g) {
+    __shared__ float weight[kLsBlocks];
+    __shared__ float red[4];
     const LatentArgs& a = g.a;
-    const int b = blockIdx.y, n = blockIdx.x % a.N;
+    const int b = blockIdx.y, n = blockIdx.x % a.N, tid = threadIdx.x;
     const int Nb = a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N;
     if (n >= Nb) return;
     const long long row = (long long)b * a.H * a.N + blockIdx.x, stride = (long long)a.B * a.H * a.N * (a.rank + 2);
     const float* p = g.part + row * (a.rank + 2);
     float m = -INFINITY;
-    for (int s = 0; s < g.splits; ++s) m = fmaxf(m, p[s * stride + a.rank]);
-    float l = 0.0f;
+    for (int s = tid; s < g.splits; s += 128) {
+        weight[s] = p[s * stride + a.rank];
+        m = fmaxf(m, weight[s]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((tid & 31) == 0) red[tid >> 5] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int s = tid; s < g.splits; s += 128) weight[s] = weight[s] == -INFINITY ? 0.0f : expf(weight[s] - m);
+    __syncthreads();
+    const int d = blockIdx.z * 128 + tid;
+    if (d >= a.rank) return;
+    float l = 0.0f, o = 0.0f;
+#pragma unroll 8
     for (int s = 0; s < g.splits; ++s) {
-        const float ms = p[s * stride + a.rank];
-        if (ms != -INFINITY) l += p[s * stride + a.rank + 1] * expf(ms - m);
+        const float x = p[s * stride + d], y = p[s * stride + a.rank + 1];
+        l += y * weight[s];
+        o += x * weight[s];
     }
-    for (int d = threadIdx.x; d < a.rank; d += 128) {
-        float o = 0.0f;
-        for (int s = 0; s < g.splits; ++s) {
-            const float ms = p[s * stride + a.rank];
-            if (ms != -INFINITY) o += p[s * stride + d] * expf(ms - m);
-        }
-        ls_store(static_cast<T*>(a.out) + row * a.rank + d, l > 0.0f ? o / l : o);
-    }
+    latent_store(static_cast<T*>(a.out) + row * a.rank + d, l > 0.0f ? o / l : o);
+}
+int latent_join_pieces(const LatentPieces& g, cudaStream_t stream) {
+    const dim3 grid(g.a.H * g.a.N, g.a.B, (g.a.rank + 127) / 128);
+    if (g.a.dtype == MCSD_F32) latent_join_kernel<float><<<grid, 128, 0, stream>>>(g);
+    else latent_join_kernel<__nv_bfloat16><<<grid, 128, 0, stream>>>(g);
+    MCSD_CUDA_CHECK(cudaGetLastError());
+    return MCSD_OK;
 }
 
 static int split_of(int B, int H, int N, int L_max, int* row_blocks, int* keys_per_split) {
     *row_blocks = (int)(((long long)H * N + kLsRows - 1) / kLsRows);
     const long long blocks = (long long)*row_blocks * B, total = (long long)L_max + N, tiles = (total + kLsKeys - 1) / kLsKeys;
     long long want = std::max(1LL, std::min(tiles, (kLsBlocks + blocks - 1) / blocks));
-    if (want <= 2 * kLsCluster) want = std::min(want, (long long)kLsCluster);   // one launch
+    if (want <= 2 * kLatentCluster) want = std::min(want, (long long)kLatentCluster);   // one launch
     const long long per = (tiles + want - 1) / want;
     *keys_per_split = (int)std::min(per * kLsKeys, 0x7fffffffLL - kLsKeys);
     return (int)((tiles + per - 1) / per);
@@ -286,11 +262,11 @@ static int split_of(int B, int H, int N, int L_max, int* row_blocks, int* keys_p
 size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max) {
     int rb, ks;
     const int splits = split_of(B, H, N, L_max, &rb, &ks);
-    return splits > kLsCluster ? (size_t)splits * B * H * N * (rank + 2) * sizeof(float) : 0;
+    return splits > kLatentCluster ? (size_t)splits * B * H * N * (rank + 2) * sizeof(float) : 0;
 }
 
 template <typename T, int ROWS, bool JOIN>
-static int run_simt(const LatentSimt& g, cudaStream_t stream) {
+static int run_simt(const LatentPieces& g, cudaStream_t stream) {
     const int smem = ((kLsRows + kLsKeys) * (g.a.rank + g.a.rot) + kLsKeys * kLsScores + kLsRows) * (int)sizeof(float);
     MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_simt_kernel<T, ROWS, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     cudaLaunchAttribute attr[1];
@@ -304,16 +280,12 @@ static int run_simt(const LatentSimt& g, cudaStream_t stream) {
     cfg.attrs = attr;
     cfg.numAttrs = JOIN ? 1 : 0;
     MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_simt_kernel<T, ROWS, JOIN>, g));
-    if (!JOIN) {
-        latent_simt_join_kernel<T><<<dim3(g.a.H * g.a.N, g.a.B), 128, 0, stream>>>(g);
-        MCSD_CUDA_CHECK(cudaGetLastError());
-    }
     count_launches(JOIN ? 1 : 2);
-    return MCSD_OK;
+    return JOIN ? MCSD_OK : latent_join_pieces(g, stream);
 }
 template <typename T>
-static int pick_simt(const LatentSimt& g, cudaStream_t stream) {
-    const bool join = g.splits <= kLsCluster;
+static int pick_simt(const LatentPieces& g, cudaStream_t stream) {
+    const bool join = g.splits <= kLatentCluster;
     if (g.a.rank > 256) return join ? run_simt<T, 32, true>(g, stream) : run_simt<T, 32, false>(g, stream);
     if (g.a.rank > 128) return join ? run_simt<T, 16, true>(g, stream) : run_simt<T, 16, false>(g, stream);
     if (g.a.rank > 64) return join ? run_simt<T, 8, true>(g, stream) : run_simt<T, 8, false>(g, stream);
@@ -321,7 +293,7 @@ static int pick_simt(const LatentSimt& g, cudaStream_t stream) {
 }
 
 int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t stream) {
-    LatentSimt g{};
+    LatentPieces g{};
     g.a = a;
     g.splits = split_of(a.B, a.H, a.N, a.L_max, &g.row_blocks, &g.keys_per_split);
     g.part = static_cast<float*>(scratch);

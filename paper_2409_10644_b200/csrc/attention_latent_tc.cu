@@ -35,7 +35,7 @@
 // plain matrix product on this card.  A tile takes 3.3 us, an item 4 more for its last products and its output, which nothing
 // covers, and a launch 9 to start: 16 trees of 45 nodes and 32 heads over 4096 keys 180 us, 1.15 PFLOP/s.  One row block a
 // sequence: memory, at 7 TB/s once it streams; 8 tokens of 128 heads over up to 32001 keys 59 us, of which 20 are start and
-// joining.  One token of 16 heads over 1001 keys: 18 us of latencies (5 until the first scores, 5 for two tiles, 7 to join).
+// joining.  One token over 1001 keys: 18 us of latencies (5 until the first scores, 5 for two tiles, 7 to join).
 //
 // The five roles run side by side, each its own loop: unrolled, they did not fit the instruction caches, and a tile took 4.9 us
 // instead of 3.4 (the loops of S over nine chunks and of O over four quarters are rolled for that alone).

@@ -30,6 +30,11 @@ struct LatentArgs {
 size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max);
 int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t stream);
 
+// warp-level matrix instructions: up to 16 query rows a sequence, bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
+// (blocks a sequence, 0 where it is not taken)
+int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits);
+int tree_attention_latent_few(const LatentArgs& a, int splits, cudaStream_t stream);
+
 // tcgen05 kernel: bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 size_t latent_tc_workspace_bytes();

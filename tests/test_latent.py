@@ -568,3 +568,44 @@ def test_every_selected_path_is_documented(m):  # noqa: F811
     w = m.mcsd_tree_attention_latent_workspace_bytes
     assert w(1, 16, 1, 512, 64, 1001, 0) > 0 and w(32, 32, 45, 512, 64, 32768, 0) <= 96 << 20
     assert w(8, 128, 1, 512, 64, 32001, 0) <= 96 << 20
+
+
+# up to 16 query rows a sequence: every split of the keys, sequences of several waves, masks and inactive nodes
+FEW = [(1, 16, "token", [1], None), (1, 16, "token", [63], None), (2, 16, "token", [64, 1023], None), (1, 16, "token", [4000], None),
+       (3, 8, "two", [700, 0, 129], [2, 1, 2]), (5, 4, "fork3", [300, 64, 5, 0, 1000], [4, 3, 2, 1, 0]), (1, 1, "chain16", [900], None),
+       (130, 5, "token", [(37 * i) % 500 for i in range(130)], None), (40, 16, "token", [(97 * i) % 900 for i in range(40)], None)]
+FEW_TREES = {"token": [-1], "two": [-1, -1], "fork3": [-1, 0, 0, 0], "chain16": list(range(-1, 15))}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,H,tree,lens,act", FEW)
+def test_few_rows(m, B, H, tree, lens, act):  # noqa: F811
+    parent = np.array(FEW_TREES[tree], dtype=np.int32)
+    q, cache, rows = _problem(50 + B, "bf16", B, H, 512, 64, parent, lens)
+    for b, L in enumerate(lens):
+        cache[b, L:] = NAN
+        if act is not None:
+            rows[b, act[b]:] = NAN
+            q[b, :, act[b]:] = NAN
+    tm = m.mcsd_build_mask(parent)
+    out = _attend(m, q, cache, rows, lens, act, tm, 0.07, 512)
+    _compare(out, q, cache, rows, lens, act, orc.dense_mask(parent), 0.07, 512, None if B < 10 else [0, H - 1])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        again = _attend(m, q, cache, rows, lens, act, tm, 0.07, 512)
+    s.synchronize()
+    assert torch.equal(out.nan_to_num(7.0), again.nan_to_num(7.0))
+
+
+@pytest.mark.gpu
+def test_few_rows_that_see_nothing_and_growing_scores(m):  # noqa: F811
+    parent = np.array(FEW_TREES["fork3"], dtype=np.int32)
+    tm, see = m.mcsd_build_mask(parent), orc.dense_mask(parent).copy()
+    q, cache, rows = _problem(60, "bf16", 2, 4, 512, 64, parent, [0, 1500])
+    cache = (cache.float() * torch.linspace(0.01, 3.0, cache.shape[1], device="cuda")[None, :, None]).bfloat16()
+    tm.anc[2] = 0
+    see[2] = False
+    out = _attend(m, q, cache, rows, [0, 1500], None, tm, 0.07, 512)
+    assert (out[0, :, 2] == 0).all()
+    _compare(out, q, cache, rows, [0, 1500], None, see, 0.07, 512)
