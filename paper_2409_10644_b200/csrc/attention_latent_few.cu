@@ -10,9 +10,10 @@
 // weights pass through shared memory, two meetings of the block a tile.  The ranges of a sequence are a cluster, which joins them
 // through shared memory.
 //
-// What bounds it: the chain of a tile (scores, maximum, weights, products: 2 us with two warps a scheduler, three times what its
-// loads take), so that it is taken only where a block has few tiles.  One token of 16 heads over 1001 keys: 9.7 us in 16
-// blocks, 11.1 in eight, 17.8 on tensor memory.
+// What bounds it: the chain of a tile (scores, maximum, weights, products: 1.6 us with two warps a scheduler, two and a half times
+// what its loads take), so that it is taken where a block has few tiles, or where memory is the bound.  Rows come by bulk copies,
+// one a row: fetched by all threads in 16-byte pieces their issue alone took 0.9 us a tile.  One token of 16 heads over 1001
+// keys: 9.3 us in 16 blocks, 10.5 in eight, 17.8 on tensor memory.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -31,7 +32,7 @@ constexpr int kFewLd = kFewWidth + 8;      // elements of a row in shared memory
 constexpr int kFewPLd = kFewKeys + 8;
 constexpr int kFewVecs = kFewWidth / 8;    // 16-byte vectors of a row
 constexpr int kFewCluster = 16;            // blocks of a sequence, at most
-constexpr int kFewSmem = (kFewRows * kFewLd + 2 * kFewKeys * kFewLd + kFewRows * kFewPLd) * 2 + (2 * 8 * kFewRows + 2 * kFewRows) * 4;
+constexpr int kFewSmem = (kFewRows * kFewLd + 2 * kFewKeys * kFewLd + kFewRows * kFewPLd) * 2 + (2 * 8 * kFewRows + 2 * kFewRows) * 4 + 32;
 static_assert(kFewRows * kFewRank * 4 <= kFewKeys * kFewLd * 2, "results lie where keys were");
 static_assert(kFewSmem <= 227 * 1024, "a block's shared memory");
 
@@ -50,7 +51,7 @@ __device__ __forceinline__ void few_copy(uint32_t dst, const void* src) {
 }
 
 // grid: (1, splits, B), the splits of a sequence a cluster
-__global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid_constant__ LatentPieces g, float scale_log2) {
+__global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid_constant__ LatentPieces g, float scale_log2, WorkspaceHeader* header) {
     extern __shared__ float4 raw4[];
     const LatentArgs& a = g.a;
     __nv_bfloat16* qs = reinterpret_cast<__nv_bfloat16*>(raw4);          // [16][kFewLd]
@@ -58,6 +59,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
     __nv_bfloat16* ps = ks + 2 * kFewKeys * kFewLd;                      // [16][kFewPLd] weights of a tile
     float* red = reinterpret_cast<float*>(ps + kFewRows * kFewPLd);      // [2][warp][row]
     float* ml = red + 2 * 8 * kFewRows;                                  // [16] references, [16] sums
+    unsigned long long* full = reinterpret_cast<unsigned long long*>(ml + 2 * kFewRows);
+    int* abort_flag = reinterpret_cast<int*>(full + 2);
     const uint32_t q_a = smem_u32(qs), k_a = smem_u32(ks), p_a = smem_u32(ps);
     const int b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int Nb = a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N;
@@ -68,12 +71,20 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
     const int k0 = min((long long)blockIdx.y * per, (long long)total), k1 = (int)min((long long)total, (long long)k0 + per);
     const __nv_bfloat16 *cache = static_cast<const __nv_bfloat16*>(a.cache) + (long long)b * a.L_max * kFewWidth,
                         *tree = static_cast<const __nv_bfloat16*>(a.tree) + (long long)b * a.N * kFewWidth;
-    auto load_tile = [&](int buffer, int kb) {
-#pragma unroll 6
-        for (int i = tid; i < kFewKeys * kFewVecs; i += kFewThreads) {
-            const int r = i / kFewVecs, v = i - r * kFewVecs, key = min(kb + r, k1 - 1);
+    if (tid == 0) {
+        mbar_init(&full[0], 1);
+        mbar_init(&full[1], 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    auto load_tile = [&](int buffer, int kb) {           // a row a copy, eight of them a warp
+        if (tid == 0) mbar_expect_tx(&full[buffer], kFewKeys * kFewWidth * 2);
+        if (lane < 8) {
+            const int r = 8 * warp + lane, key = min(kb + r, k1 - 1);
             const __nv_bfloat16* src = key < L ? cache + (long long)key * kFewWidth : tree + (long long)(key - L) * kFewWidth;
-            few_copy(k_a + ((buffer * kFewKeys + r) * kFewLd + v * 8) * 2, src + v * 8);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(k_a + (buffer * kFewKeys + r) * kFewLd * 2), "l"(src), "r"(kFewWidth * 2), "r"(smem_u32(&full[buffer])) : "memory");
         }
     };
     if (k0 < k1) load_tile(0, k0);
@@ -92,8 +103,9 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
     uint32_t q[kFewWidth / 16][4];
     int t = 0;
     for (int kb = k0; kb < k1; kb += kFewKeys, ++t) {
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncthreads();
+        if (t == 0) asm volatile("cp.async.wait_all;" ::: "memory");                // the queries
+        mbar_wait(&full[t & 1], (t >> 1) & 1, abort_flag, header, 30);
+        __syncthreads();                                                            // and the other buffer has been read
         if (kb + kFewKeys < k1) load_tile((t + 1) & 1, kb + kFewKeys);
         if (t == 0) {
 #pragma unroll
@@ -249,10 +261,10 @@ static int few_fit(FewFit* out) {
 }
 
 // Blocks a sequence, or 0 where the kernel on tensor memory is sooner done.  In microseconds, from calls of 1 to 256 sequences of
-// 100 to 131072 keys: here 2.5 and, for every wave of clusters, 5.1 and 2.05 a tile of 64 keys (and some for a join by few); there 18 (less for one or two
-// tiles) and 0.004 for each unit of its cut (10 a tile of 256 keys, 21 a sequence).  Here and there, 16 heads: one token over
-// 100 keys 9 and 11, 1001: 9.7 and 17.8, 4000: 15.9 and 20.0, 8000: 24.3 and 24.5; 16 over 4000: 31.1 and 31.4, 128 over 1000:
-// 48.5 and 51.1, 256 over 4000: 289 and 265.
+// 100 to 131072 keys: here 2.5 and, for every wave of clusters, 5 and 1.63 a tile of 64 keys, and some for a join by few; there 18
+// (less for one or two tiles, up to 5 more for pieces of long items) and 0.004 for each unit of its cut (10 a tile of 256 keys, 21
+// a sequence), or the rows at 4.6 TB/s.  Here and there, 16 heads: one token over 100 keys 8.7 and 11, 1001: 9.3 and 17.8, 4000: 14.1
+// and 20.0, 8000: 20.8 and 24.5, 32000: 59 and 31; 16 over 4000: 26 and 31, 64 over 2000: 38 and 44, 256 over 4000: 232 and 256.
 int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits) {
     *splits = 0;
     if (dtype != MCSD_BF16 || rank != kFewRank || rot != kFewWidth - kFewRank || (long long)H * N > kFewRows) return MCSD_OK;
@@ -260,10 +272,11 @@ int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dty
     const int st = few_fit(&fit);
     if (st != MCSD_OK) return st;
     const double tiles = std::ceil(((double)L_max + N) / kFewKeys);
-    double best = std::min(18.0, 9.5 + B * (1.0 + std::ceil(L_max / 256.0))) + 0.004 * B * (21.0 + 10.0 * L_max / 256.0);
+    const double keys = L_max, there = std::min(18.0 + 0.0006 * std::min(keys, 8000.0), 9.5 + B * (1.0 + std::ceil(keys / 256.0)));
+    double best = std::max(there + 0.004 * B * (21.0 + 10.0 * keys / 256.0), B * keys * kFewWidth * 2 / 4.6e6);
     for (int s = 1; s <= kFewCluster; ++s) {
         if (fit.clusters[s] < 1) continue;
-        const double t = 2.5 + std::ceil((double)B / fit.clusters[s]) * (5.1 + 2.05 * std::ceil(tiles / s)) + 3.0 / s;
+        const double t = 2.5 + std::ceil((double)B / fit.clusters[s]) * (5.0 + 1.63 * std::ceil(tiles / s)) + 4.5 / s;
         if (t < best) {
             best = t;
             *splits = s;
@@ -271,13 +284,13 @@ int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dty
     }
     return MCSD_OK;
 }
-int tree_attention_latent_few(const LatentArgs& a, int splits, cudaStream_t stream) {
+int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* header, cudaStream_t stream) {
     LatentPieces g{};
     g.a = a;
     g.splits = splits;
     cudaLaunchAttribute attr[1];
     const cudaLaunchConfig_t cfg = few_config(splits, a.B, stream, attr);
-    MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_few_kernel, g, a.scale * 1.4426950408889634f));
+    MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_few_kernel, g, a.scale * 1.4426950408889634f, header));
     count_launches(1);
     return MCSD_OK;
 }
