@@ -609,3 +609,26 @@ def test_few_rows_that_see_nothing_and_growing_scores(m):  # noqa: F811
     out = _attend(m, q, cache, rows, [0, 1500], None, tm, 0.07, 512)
     assert (out[0, :, 2] == 0).all()
     _compare(out, q, cache, rows, [0, 1500], None, see, 0.07, 512)
+
+
+@pytest.mark.gpu
+def test_few_rows_captured(m):  # noqa: F811
+    """The choice of kernel goes by L_max, the split of the keys by the lengths a replay finds."""
+    tm = m.mcsd_build_mask(np.array(FEW_TREES["token"], dtype=np.int32))
+    q, cache, rows = _problem(70, "bf16", 3, 16, 512, 64, [-1], [1500] * 3)
+    lens, act = _i32([1500, 0, 3]), _i32([1, 1, 1])
+    out = torch.full((3, 16, 1, 512), NAN, dtype=torch.bfloat16, device="cuda")
+    ws = m.new_workspace(m.mcsd_tree_attention_latent_workspace_bytes(3, 16, 1, 512, 64, 1500, 0), "cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        m.mcsd_tree_attention_latent(q, cache, rows, lens, act, tm, 0.07, out=out, workspace=ws)
+    for L, a in (([1500, 0, 3], [1, 1, 1]), ([64, 1023, 1025], [1, 0, 1]), ([0, 0, 0], [0, 0, 0]), ([1, 1500, 700], [1, 1, 1])):
+        lens.copy_(_i32(L))
+        act.copy_(_i32(a))
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        _compare(out, q, cache, rows, L, a, np.ones((1, 1), bool), 0.07, 512)
+    assert m.mcsd_workspace_status(ws) == 0
