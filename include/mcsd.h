@@ -503,12 +503,12 @@ int mcsd_latent_rows(const void* latent_in, const void* q_in, const int64_t* str
  *               `out` must not overlap the inputs
  *   seq_lens, n_active, anc, words   as for mcsd_tree_attention;   L_max <= 2^30;  B * H <= 65535
  *   dtype       MCSD_BF16 runs on the tensor cores with rank 512 and rot 64 when q, cache, tree and out are 16-byte aligned
- *               (a kernel of its own where H * N <= 16 and the keys are few); everything else on the CUDA cores in fp32
+ *               (a kernel of its own for H * N <= 16 where that is sooner done); everything else on the CUDA cores in fp32
  *   workspace   [dev] >= mcsd_tree_attention_latent_workspace_bytes(...) bytes, 256-byte aligned, zero-filled once; may be the
  *               workspace of the other attention calls; calls that may overlap on the device need distinct ones
  *
- * One launch on `stream` for up to 256 sequences on the tensor cores; one on the CUDA cores, two where the keys are cut into more
- * than eight pieces.  Equal inputs give equal outputs, to the bit.  Errors: as mcsd_tree_attention.
+ * One launch on `stream` (one for every 256 sequences), two where the pieces of few rows or of the CUDA cores' kernel are too many
+ * for a cluster.  Equal inputs give equal outputs, to the bit.  Errors: as mcsd_tree_attention.
  */
 size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 

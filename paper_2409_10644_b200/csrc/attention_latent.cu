@@ -35,7 +35,7 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
     int few = 0;
     const int fs = aligned ? mcsd::latent_few_splits(B, H, N, rank, rot, L_max, dtype, &few) : MCSD_OK;
     if (fs != MCSD_OK) return fs;
-    if (few > 0) return mcsd::tree_attention_latent_few(a, few, &ws->header, static_cast<cudaStream_t>(stream));
+    if (few > 0) return mcsd::tree_attention_latent_few(a, few, &ws->header, ws + 1, static_cast<cudaStream_t>(stream));
     if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned)
         return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));

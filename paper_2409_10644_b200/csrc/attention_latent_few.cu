@@ -8,7 +8,7 @@
 // time, two tiles in shared memory: one is used, one on its way.  Queries stay in registers.  Scores: a warp has eight keys over
 // the whole row, in four independent sums; products with the values: 64 of the 512 channels.  The maximum of a tile and its
 // weights pass through shared memory, two meetings of the block a tile.  The ranges of a sequence are a cluster, which joins them
-// through shared memory.
+// through shared memory, or, where a sequence is long enough for more than 16, go through memory to a second kernel.
 //
 // What bounds it: the chain of a tile (scores, maximum, weights, products: 1.6 us with two warps a scheduler, two and a half times
 // what its loads take), so that it is taken where a block has few tiles, or where memory is the bound.  Rows come by bulk copies,
@@ -31,7 +31,8 @@ constexpr int kFewRows = 16, kFewKeys = 64, kFewThreads = 256, kFewRank = 512, k
 constexpr int kFewLd = kFewWidth + 8;      // elements of a row in shared memory: eight rows meet all banks
 constexpr int kFewPLd = kFewKeys + 8;
 constexpr int kFewVecs = kFewWidth / 8;    // 16-byte vectors of a row
-constexpr int kFewCluster = 16;            // blocks of a sequence, at most
+constexpr int kFewCluster = 16;            // blocks of a cluster, at most
+constexpr int kFewMost = 160;              // blocks of a sequence that are joined through memory, at most
 constexpr int kFewSmem = (kFewRows * kFewLd + 2 * kFewKeys * kFewLd + kFewRows * kFewPLd) * 2 + (2 * 8 * kFewRows + 2 * kFewRows) * 4 + 32;
 static_assert(kFewRows * kFewRank * 4 <= kFewKeys * kFewLd * 2, "results lie where keys were");
 static_assert(kFewSmem <= 227 * 1024, "a block's shared memory");
@@ -50,7 +51,8 @@ __device__ __forceinline__ void few_copy(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// grid: (1, splits, B), the splits of a sequence a cluster
+// grid: (1, splits, B), the splits of a sequence a cluster where JOIN
+template <bool JOIN>
 __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid_constant__ LatentPieces g, float scale_log2, WorkspaceHeader* header) {
     extern __shared__ float4 raw4[];
     const LatentArgs& a = g.a;
@@ -210,9 +212,19 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
         for (int i = 0; i < 8; ++i) l += red[i * kFewRows + tid];
         ml[kFewRows + tid] = l;
     }
-    cg::this_cluster().sync();
-    latent_join_cluster<__nv_bfloat16, kFewCluster>(g, os, ml, kFewRows, b, Nb, 0, nr, tid, kFewThreads);
-    cg::this_cluster().sync();                                          // others may still read this block's rows
+    if constexpr (JOIN) {
+        cg::this_cluster().sync();
+        latent_join_cluster<__nv_bfloat16, kFewCluster>(g, os, ml, kFewRows, b, Nb, 0, nr, tid, kFewThreads);
+        cg::this_cluster().sync();                                      // others may still read this block's rows
+    } else {
+        __syncthreads();
+        for (int i = tid; i < nr * (kFewRank / 2); i += kFewThreads) {
+            const int r = i / (kFewRank / 2), d = 2 * (i % (kFewRank / 2)), h = r / Nb, n = r - h * Nb;
+            float* p = g.part + ((long long)blockIdx.y * a.B * a.H * a.N + ((long long)b * a.H + h) * a.N + n) * (kFewRank + 2);
+            *reinterpret_cast<float2*>(p + d) = *reinterpret_cast<const float2*>(os + r * kFewRank + d);
+            if (d == 0) { p[kFewRank] = ml[r]; p[kFewRank + 1] = ml[kFewRows + r]; }
+        }
+    }
 }
 
 // Clusters of 1 .. kFewCluster blocks that run at a time.
@@ -228,7 +240,7 @@ static cudaLaunchConfig_t few_config(int splits, int B, cudaStream_t stream, cud
     cfg.dynamicSmemBytes = kFewSmem;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = splits <= kFewCluster ? 1 : 0;
     return cfg;
 }
 static int few_fit(FewFit* out) {
@@ -243,13 +255,14 @@ static int few_fit(FewFit* out) {
         return MCSD_OK;
     }
     // both attributes are per device; clusters of more than eight blocks are an option that a device may not have
-    MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
-    const bool large = cudaFuncSetAttribute(latent_few_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_few_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
+    MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_few_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
+    const bool large = cudaFuncSetAttribute(latent_few_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
     for (int s = 1; s <= kFewCluster; ++s) {
         cudaLaunchAttribute attr[1];
         const cudaLaunchConfig_t cfg = few_config(s, 1, nullptr, attr);
         int n = 0;
-        if ((s > 8 && !large) || cudaOccupancyMaxActiveClusters(&n, latent_few_kernel, &cfg) != cudaSuccess) n = 0;
+        if ((s > 8 && !large) || cudaOccupancyMaxActiveClusters(&n, latent_few_kernel<true>, &cfg) != cudaSuccess) n = 0;
         out->clusters[s] = n;
     }
     cudaGetLastError();                                                 // what was refused is not an error of this call
@@ -264,7 +277,8 @@ static int few_fit(FewFit* out) {
 // 100 to 131072 keys: here 2.5 and, for every wave of clusters, 5 and 1.63 a tile of 64 keys, and some for a join by few; there 18
 // (less for one or two tiles, up to 5 more for pieces of long items) and 0.004 for each unit of its cut (10 a tile of 256 keys, 21
 // a sequence), or the rows at 4.6 TB/s.  Here and there, 16 heads: one token over 100 keys 8.7 and 11, 1001: 9.3 and 17.8, 4000: 14.1
-// and 20.0, 8000: 20.8 and 24.5, 32000: 59 and 31; 16 over 4000: 26 and 31, 64 over 2000: 38 and 44, 256 over 4000: 232 and 256.
+// and 20.0, 8000: 20.8 and 24.5, 32000: 59 in a cluster, 24.7 through memory, and 31, 131072: 44.6 and 53.5; 8 over 8000: 22.4 through
+// memory and 31, 16 over 4000: 26 and 31, 64 over 2000: 38 and 44, 256 over 4000: 232 and 256.
 int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits) {
     *splits = 0;
     if (dtype != MCSD_BF16 || rank != kFewRank || rot != kFewWidth - kFewRank || (long long)H * N > kFewRows) return MCSD_OK;
@@ -282,17 +296,31 @@ int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dty
             *splits = s;
         }
     }
+    // more blocks a sequence, joined through memory by a second kernel: one wave, its scratch within the other kernel's
+    const int many = std::min(fit.clusters[1] / B, kFewMost);
+    if (many > kFewCluster && tiles >= many && latent_tc_shape(B, H, N, rank, rot, L_max, dtype) &&
+        (size_t)many * B * H * N * (kFewRank + 2) * sizeof(float) <= latent_tc_workspace_bytes()) {
+        const double t = 2.5 + 5.0 + 1.63 * std::ceil(tiles / many) + 8.0;
+        if (t < best) *splits = many;
+    }
     return MCSD_OK;
 }
-int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* header, cudaStream_t stream) {
+int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* header, void* scratch, cudaStream_t stream) {
     LatentPieces g{};
     g.a = a;
     g.splits = splits;
+    g.part = static_cast<float*>(scratch);
     cudaLaunchAttribute attr[1];
     const cudaLaunchConfig_t cfg = few_config(splits, a.B, stream, attr);
-    MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_few_kernel, g, a.scale * 1.4426950408889634f, header));
-    count_launches(1);
-    return MCSD_OK;
+    const float scale_log2 = a.scale * 1.4426950408889634f;
+    if (splits <= kFewCluster) {
+        MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_few_kernel<true>, g, scale_log2, header));
+        count_launches(1);
+        return MCSD_OK;
+    }
+    MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_few_kernel<false>, g, scale_log2, header));
+    count_launches(2);
+    return latent_join_pieces(g, stream);
 }
 
 }  // namespace mcsd

@@ -207,19 +207,22 @@ __global__ void __launch_bounds__(kLsThreads) latent_simt_kernel(const __grid_co
     }
 }
 
-// grid: (H * N, B, 128 channels each); joins the pieces of a row in their order
+// grid: (H * N, B, 128 channels each); joins the pieces of a row in their order, every fourth by a quarter of the threads
+constexpr int kJoinThreads = 512, kJoinParts = kJoinThreads / 128;
 template <typename T>
-__global__ void __launch_bounds__(128) latent_join_kernel(const __grid_constant__ LatentPieces g) {
+__global__ void __launch_bounds__(kJoinThreads) latent_join_kernel(const __grid_constant__ LatentPieces g) {
     __shared__ float weight[kLsBlocks];
-    __shared__ float red[4];
+    __shared__ float red[kJoinThreads / 32];
+    __shared__ float2 parts[kJoinParts][128];
     const LatentArgs& a = g.a;
-    const int b = blockIdx.y, n = blockIdx.x % a.N, tid = threadIdx.x;
+    const int b = blockIdx.y, n = blockIdx.x % a.N, tid = threadIdx.x, part = tid >> 7;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int Nb = a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N;
     if (n >= Nb) return;
     const long long row = (long long)b * a.H * a.N + blockIdx.x, stride = (long long)a.B * a.H * a.N * (a.rank + 2);
     const float* p = g.part + row * (a.rank + 2);
     float m = -INFINITY;
-    for (int s = tid; s < g.splits; s += 128) {
+    for (int s = tid; s < g.splits; s += kJoinThreads) {
         weight[s] = p[s * stride + a.rank];
         m = fmaxf(m, weight[s]);
     }
@@ -227,25 +230,40 @@ __global__ void __launch_bounds__(128) latent_join_kernel(const __grid_constant_
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if ((tid & 31) == 0) red[tid >> 5] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    for (int s = tid; s < g.splits; s += 128) weight[s] = weight[s] == -INFINITY ? 0.0f : expf(weight[s] - m);
+    for (int i = 0; i < kJoinThreads / 32; ++i) m = fmaxf(m, red[i]);
+    for (int s = tid; s < g.splits; s += kJoinThreads) weight[s] = weight[s] == -INFINITY ? 0.0f : expf(weight[s] - m);
     __syncthreads();
-    const int d = blockIdx.z * 128 + tid;
-    if (d >= a.rank) return;
+    const int d = blockIdx.z * 128 + (tid & 127);
     float l = 0.0f, o = 0.0f;
+    if (d < a.rank) {
 #pragma unroll 8
-    for (int s = 0; s < g.splits; ++s) {
-        const float x = p[s * stride + d], y = p[s * stride + a.rank + 1];
-        l += y * weight[s];
-        o += x * weight[s];
+        for (int s = part; s < g.splits; s += kJoinParts) {
+            const float x = p[s * stride + d], y = p[s * stride + a.rank + 1];
+            l += y * weight[s];
+            o += x * weight[s];
+        }
+    }
+    parts[part][tid & 127] = make_float2(l, o);
+    __syncthreads();
+    if (part > 0 || d >= a.rank) return;
+    for (int k = 1; k < kJoinParts; ++k) {
+        l += parts[k][tid].x;
+        o += parts[k][tid].y;
     }
     latent_store(static_cast<T*>(a.out) + row * a.rank + d, l > 0.0f ? o / l : o);
 }
 int latent_join_pieces(const LatentPieces& g, cudaStream_t stream) {
-    const dim3 grid(g.a.H * g.a.N, g.a.B, (g.a.rank + 127) / 128);
-    if (g.a.dtype == MCSD_F32) latent_join_kernel<float><<<grid, 128, 0, stream>>>(g);
-    else latent_join_kernel<__nv_bfloat16><<<grid, 128, 0, stream>>>(g);
-    MCSD_CUDA_CHECK(cudaGetLastError());
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(g.a.H * g.a.N, g.a.B, (g.a.rank + 127) / 128);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (g.a.dtype == MCSD_F32) MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_join_kernel<float>, g));
+    else MCSD_CUDA_CHECK(cudaLaunchKernelEx(&cfg, latent_join_kernel<__nv_bfloat16>, g));
     return MCSD_OK;
 }
 

@@ -33,7 +33,7 @@ int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t 
 // warp-level matrix instructions: up to 16 query rows a sequence, bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
 // (blocks a sequence, 0 where it is not taken)
 int latent_few_splits(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits);
-int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* header, cudaStream_t stream);
+int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* header, void* scratch, cudaStream_t stream);
 
 // tcgen05 kernel: bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype);

@@ -573,6 +573,7 @@ def test_every_selected_path_is_documented(m):  # noqa: F811
 # up to 16 query rows a sequence: every split of the keys, sequences of several waves, masks and inactive nodes
 FEW = [(1, 16, "token", [1], None), (1, 16, "token", [63], None), (2, 16, "token", [64, 1023], None), (1, 16, "token", [4000], None),
        (3, 8, "two", [700, 0, 129], [2, 1, 2]), (5, 4, "fork3", [300, 64, 5, 0, 1000], [4, 3, 2, 1, 0]), (1, 1, "chain16", [900], None),
+       (6, 16, "token", [9000, 0, 100, 5000, 1, 8999], [1, 1, 0, 1, 1, 1]), (1, 4, "fork3", [21000], [3]),
        (130, 5, "token", [(37 * i) % 500 for i in range(130)], None), (40, 16, "token", [(97 * i) % 900 for i in range(40)], None)]
 FEW_TREES = {"token": [-1], "two": [-1, -1], "fork3": [-1, 0, 0, 0], "chain16": list(range(-1, 15))}
 
