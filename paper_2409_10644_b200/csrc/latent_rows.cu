@@ -231,6 +231,7 @@ commit_latent_kernel(void* const* __restrict__ cache_layers, const void* const* 
     const int L = min(max(seq_lens[b], 0), L_max);
     const int acc = min(max(accept_len[b], 0), n_levels);
     const int count = min(1 + acc, L_max - L);
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the length has been read
     const int vecs = row_bytes / 16, per_layer = count * vecs;
     const int layers = (n_layers - rank + kCommitCluster - 1) / kCommitCluster;
@@ -262,6 +263,7 @@ commit_latent_kernel(void* const* __restrict__ cache_layers, const void* const* 
             else if (src[j])
                 for (int e = 0; e < 8; ++e) reinterpret_cast<uint16_t*>(dst[j])[e] = reinterpret_cast<const uint16_t*>(&x[j])[e];
     }
+    __syncwarp();                                       // lanes leave the loop after different trips; the wait is the warp's
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (rank == 0 && threadIdx.x == 0) seq_lens[b] = min(L_max, L + 1 + acc);
 }

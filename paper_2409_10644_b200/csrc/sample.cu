@@ -295,7 +295,9 @@ struct Blocks {
         else cg::this_cluster().sync();
     }
     __device__ __forceinline__ void leave() const {
-        if (n > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+        if (n == 1) return;
+        __syncwarp();                                     // lanes come from loops of different trips; the barrier is the warp's
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     }
     __device__ __forceinline__ SampleShared* at(SampleShared* sh, int r) const { return n == 1 ? sh : cg::this_cluster().map_shared_rank(sh, r); }
 };
