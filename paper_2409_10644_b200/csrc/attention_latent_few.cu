@@ -88,6 +88,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
             asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                          ::"r"(k_a + (buffer * kFewKeys + r) * kFewLd * 2), "l"(src), "r"(kFewWidth * 2), "r"(smem_u32(&full[buffer])) : "memory");
         }
+        __syncwarp();                                    // matrix instructions follow, which a warp executes together
     };
     if (k0 < k1) load_tile(0, k0);
     for (int i = tid; i < kFewRows * kFewVecs; i += kFewThreads) {

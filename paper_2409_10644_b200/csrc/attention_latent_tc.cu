@@ -154,9 +154,14 @@ __device__ __forceinline__ void pair_commit(uint32_t one, void* bar) {          
                  ::"r"(smem_u32(bar)), "h"(both), "r"(one) : "memory");
 }
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// Lanes come here from waits of one thread and from loops of different trips (rows behind the last one join nothing).
+__device__ __forceinline__ void softmax_sync() {
+    __syncwarp();
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+}
 // 32 consecutive fp32 columns of this thread's lane; the caller waits with tc_wait_ld()
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
     uint32_t* r = reinterpret_cast<uint32_t*>(v);
@@ -685,7 +690,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
                     ref = mx;
                 }
                 const float sub = ref == -INFINITY ? 0.0f : ref;
-                const bool move = t > it.t0 && __any_sync(0xffffffffu, factor != 1.0f);
+                const bool move = __any_sync(0xffffffffu, factor != 1.0f) && t > it.t0;   // (the lanes meet in either case)
                 if (move) {
                     ok = ok && LT_WAIT(&sm->pv_done, (g - 1) & 1, 13);         // O is current
                     __syncwarp();

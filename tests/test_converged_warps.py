@@ -33,7 +33,7 @@ def test_the_check_finds_what_it_looks_for():
     assert _unguarded('x();\n__syncwarp();  // y\n\nasm volatile("bar.sync 1, 256;" ::: "memory");') == []
 
 
-@pytest.mark.parametrize("name", ["latent_rows.cu", "sample.cu"])
+@pytest.mark.parametrize("name", ["latent_rows.cu", "sample.cu", "attention_latent_tc.cu"])
 def test_barriers_of_a_warp_follow_a_meeting_of_its_lanes(name):
     assert _unguarded(open(os.path.join(CSRC, name)).read()) == []
 
