@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
     float* red = reinterpret_cast<float*>(ps + kFewRows * kFewPLd);      // [2][warp][row]
     float* ml = red + 2 * 8 * kFewRows;                                  // [16] references, [16] sums
     unsigned long long* full = reinterpret_cast<unsigned long long*>(ml + 2 * kFewRows);
-    int* abort_flag = reinterpret_cast<int*>(full + 2);
+    int* abort_flag = reinterpret_cast<int*>(full + 2);                  // [2]
     const uint32_t q_a = smem_u32(qs), k_a = smem_u32(ks), p_a = smem_u32(ps);
     const int b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int Nb = a.n_active ? min(max(a.n_active[b], 0), a.N) : a.N;
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
     if (tid == 0) {
         mbar_init(&full[0], 1);
         mbar_init(&full[1], 1);
-        *abort_flag = 0;
+        abort_flag[0] = abort_flag[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -109,6 +109,12 @@ __global__ void __launch_bounds__(kFewThreads, 1) latent_few_kernel(const __grid
         if (t == 0) asm volatile("cp.async.wait_all;" ::: "memory");                // the queries
         mbar_wait(&full[t & 1], (t >> 1) & 1, abort_flag, header, 30);
         __syncthreads();                                                            // and the other buffer has been read
+        if (*(volatile int*)abort_flag) {              // (alike in all threads: whoever could set it next comes behind two meetings)
+            // A wait ran out: no more copies, and this tile's, the only ones on their way, have as long again to come in before the
+            // block leaves its memory.
+            if (tid == 0) mbar_wait_slow(&full[t & 1], (t >> 1) & 1, abort_flag + 1, header, 31);
+            break;
+        }
         if (kb + kFewKeys < k1) load_tile((t + 1) & 1, kb + kFewKeys);
         if (t == 0) {
 #pragma unroll
