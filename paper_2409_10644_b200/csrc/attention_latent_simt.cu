@@ -25,6 +25,9 @@ namespace mcsd {
 constexpr int kLsRows = 32, kLsKeys = 32, kLsThreads = 256;
 constexpr int kLsBlocks = 296;             // blocks that a launch is cut into, about
 constexpr int kLsScores = 36;              // floats of a key's weights
+constexpr int ls_smem(int width) { return ((kLsRows + kLsKeys) * width + kLsKeys * kLsScores + kLsRows) * (int)sizeof(float); }
+constexpr int kLsSmemMost = ls_smem(kLatentMaxRank + kLatentMaxRot);
+static_assert(kLsSmemMost <= 227 * 1024, "a block's shared memory");
 
 template <typename T> __device__ __forceinline__ float ls_load(const T* p);
 template <> __device__ __forceinline__ float ls_load(const float* p) { return __ldg(p); }
@@ -285,15 +288,16 @@ size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max) {
 
 template <typename T, int ROWS, bool JOIN>
 static int run_simt(const LatentPieces& g, cudaStream_t stream) {
-    const int smem = ((kLsRows + kLsKeys) * (g.a.rank + g.a.rot) + kLsKeys * kLsScores + kLsRows) * (int)sizeof(float);
-    MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_simt_kernel<T, ROWS, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // one instance serves many widths, and what it may take is the process's: the most that any of them takes, so that no host thread
+    // lowers it between another one's setting and launch
+    MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_simt_kernel<T, ROWS, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLsSmemMost));
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = (unsigned)g.splits; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(g.row_blocks, g.splits, g.a.B);
     cfg.blockDim = dim3(kLsThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = ls_smem(g.a.rank + g.a.rot);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = JOIN ? 1 : 0;
