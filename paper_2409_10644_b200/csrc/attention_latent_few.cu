@@ -265,14 +265,19 @@ static int few_fit(FewFit* out) {
     MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_few_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
     MCSD_CUDA_CHECK(cudaFuncSetAttribute(latent_few_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem));
     const bool large = cudaFuncSetAttribute(latent_few_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    bool refused = !large;
     for (int s = 1; s <= kFewCluster; ++s) {
         cudaLaunchAttribute attr[1];
         const cudaLaunchConfig_t cfg = few_config(s, 1, nullptr, attr);
         int n = 0;
-        if ((s > 8 && !large) || cudaOccupancyMaxActiveClusters(&n, latent_few_kernel<true>, &cfg) != cudaSuccess) n = 0;
+        if (s <= 8 || large) {
+            const bool fits = cudaOccupancyMaxActiveClusters(&n, latent_few_kernel<true>, &cfg) == cudaSuccess;
+            refused = refused || !fits;
+            if (!fits) n = 0;
+        }
         out->clusters[s] = n;
     }
-    cudaGetLastError();                                                 // what was refused is not an error of this call
+    if (refused) (void)cudaGetLastError();                              // what was refused here is not an error of this call
     if (dev >= 0 && dev < 64) {
         known[dev] = *out;
         have[dev] = true;

@@ -23,11 +23,14 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace mcsd
 
+// The runtime also keeps an error until it is asked for, and a launch is checked by asking: what is reported here is taken from
+// it, so that a later call does not report it again.
 #define MCSD_CUDA_CHECK(expr)                                  \
     do {                                                       \
         cudaError_t _e = (expr);                               \
         if (_e != cudaSuccess) {                               \
             ::mcsd::set_last_cuda_error(_e);                   \
+            (void)cudaGetLastError();                          \
             return MCSD_ERR_CUDA;                              \
         }                                                      \
     } while (0)
