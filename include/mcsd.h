@@ -549,7 +549,7 @@ int mcsd_commit_latent(void* const* cache_layers, const void* const* tree_layers
  *   temperature, top_p, min_p  [dev] float[rows], top_k  [dev] int32[rows]: a value a row; NULL = 1, or that filter off
  *   u            [dev] float[rows][K] uniforms in [0, 1);   tokens  [dev] int32[rows][K] out, or NULL (u is then not read)
  *   probs        [dev] float[rows][V] out, or NULL;  not both NULL;  outputs must not overlap the logits
- *   V            1 .. 262144;  K  1 .. 1024 (any, when tokens is NULL);  rows  1 .. 2^24
+ *   V            1 .. 262144;  K  1 .. 1024 (any that is not negative, when tokens is NULL);  rows  1 .. 2^24
  *
  * Weights are fp32 and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of
  * sums: equal inputs give equal outputs, to the bit.  One launch on `stream`, no workspace.

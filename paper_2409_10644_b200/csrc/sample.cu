@@ -905,7 +905,7 @@ extern "C" int mcsd_sample_candidates(const void* logits, long long row_stride, 
                                       int32_t* tokens, float* probs, void* stream) {
     if (!logits || (!tokens && !probs) || (tokens && !u)) return MCSD_ERR_NULL;
     if (dtype != MCSD_BF16 && dtype != MCSD_F32) return MCSD_ERR_BAD_DTYPE;
-    if (rows < 1 || rows > (1 << 24) || V < 1 || V > mcsd::kSampleMaxVocab || row_stride < V || K < 0 || (tokens && K < 1) || K > 1024)
+    if (rows < 1 || rows > (1 << 24) || V < 1 || V > mcsd::kSampleMaxVocab || row_stride < V || K < 0 || (tokens && (K < 1 || K > 1024)))
         return MCSD_ERR_BAD_SHAPE;
     int dev = 0, sms = 0;
     MCSD_CUDA_CHECK(cudaGetDevice(&dev));
