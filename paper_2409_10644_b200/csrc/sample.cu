@@ -90,7 +90,6 @@ struct alignas(16) SampleShared {
     u64 range_lo, range_hi;                   // smallest and largest place among the step's tokens (this block's part)
     int list_n;                               // tokens collected (first block of the cluster)
     u64 cut;                                  // place of the last token kept
-    u64 cut_sum;                              // sum of the list's weights up to and with it
     int picked;                               // tokens picked (more than kPickMax: none are listed)
     u64 below[kSteps + 1];                    // weight of all, and of what lies below some thresholds, in steps of 2^-20
     int pick[kPickMax];
@@ -345,7 +344,7 @@ __device__ void find_bin(SampleShared* sh, const Blocks& blocks, u64 start, u64 
 
 // On a short list (n at most kShort, by its block alone) every token is compared with every other: the first `count` of them in the
 // order are kept, and of those the ones before which the sum, `before` included, is below the target: `target`, or with share >= 0
-// that part of their sum.  Written to sh->cut and sh->cut_sum.
+// that part of their sum.  Written to sh->cut.
 constexpr int kShort = 256;
 __device__ void short_list(SampleShared* sh, const Scale& r, int n, u64 before, u64 target, u64 count, double share) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -379,12 +378,12 @@ __device__ void short_list(SampleShared* sh, const Scale& r, int n, u64 before, 
     sum += before;
     // the last token kept: nothing kept behind it
     const bool in = keep && sum < target;
-    if (in && ((u64)rank + 1 == min((u64)n, count) || sum + f >= target)) { sh->cut = p; sh->cut_sum = sum + f; }
+    if (in && ((u64)rank + 1 == min((u64)n, count) || sum + f >= target)) sh->cut = p;
     __syncthreads();
 }
 
 // The cut of the first block's list of n places (by that block alone): the place at which the sum of f (MASS) or the count, over
-// places up to `limit` and from `before` on, reaches the target.  Written to sh->cut, the sum up to and with it to sh->cut_sum.
+// places up to `limit` and from `before` on, reaches the target.  Written to sh->cut.
 template <bool MASS>
 __device__ void list_cut(SampleShared* sh, const Scale& r, int n, u64 before, u64 target, u64 limit) {
     const int tid = threadIdx.x, lane = tid & 31;
@@ -429,7 +428,7 @@ __device__ void list_cut(SampleShared* sh, const Scale& r, int n, u64 before, u6
                     const uint32_t fj = __shfl_sync(0xffffffffu, f, j);
                     if (pj < p) sum += fj;
                 }
-                if (lane < m && sum < target && target <= sum + f) { sh->cut = p; sh->cut_sum = sum + f; }
+                if (lane < m && sum < target && target <= sum + f) sh->cut = p;
             }
             __syncthreads();
             return;
@@ -457,6 +456,7 @@ __device__ void list_filters(SampleShared* sh, const Scale& r, int n, u64 count,
         return;
     }
     list_cut<false>(sh, r, n, 0, count, ~0ull);
+    if (share < 0.0) return;
     const u64 limit = sh->cut;
     u64 sum = 0;
     for (int i = tid; i < n; i += kSampleThreads) {
@@ -470,14 +470,9 @@ __device__ void list_filters(SampleShared* sh, const Scale& r, int n, u64 count,
     __syncthreads();
     u64 total;
     warps_before(sh->scan, total);
-    if (share >= 0.0) {
-        if (tid == 0) sh->target = share_of(total, share);
-        __syncthreads();
-        list_cut<true>(sh, r, n, 0, sh->target, limit);
-    } else {
-        __syncthreads();
-        if (tid == 0) { sh->cut = limit; sh->cut_sum = total; }
-    }
+    if (tid == 0) sh->target = share_of(total, share);
+    __syncthreads();
+    list_cut<true>(sh, r, n, 0, sh->target, limit);
 }
 
 // Collects the picked tokens for which `take` says so in the first block's list; returns how many there are (the list holds

@@ -30,3 +30,20 @@ def test_probabilities_alone_take_any_number_of_draws(m, K):  # noqa: F811
     assert st == 0
     (want,) = m.mcsd_sample_candidates(x, probs=True)
     assert torch.equal(probs, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,V", [(1, 9001), (150, 4001)])
+@pytest.mark.parametrize("k", [257, 600, 2560, 2561])
+@pytest.mark.parametrize("steps", [0.001, 0.25])
+def test_top_k_alone_beyond_the_short_list(m, rows, V, k, steps):  # noqa: F811
+    """The kept tokens, to the token: distinct logits, and logits of which many are equal at the cut."""
+    x = 2 * torch.randn(rows, V, generator=torch.Generator("cuda").manual_seed(k), device="cuda")
+    x = torch.round(x / steps) * steps
+    (probs,) = m.mcsd_sample_candidates(x, top_k=torch.full((rows,), k, dtype=torch.int32, device="cuda"), probs=True)
+    for r in range(0, rows, 29):
+        want, _ = orc.filtered(x[r].cpu().numpy(), 1.0, k)
+        got = probs[r].cpu().numpy()
+        assert ((got > 0) == (want > 0)).all() and (got > 0).sum() == k
+        # weights 2^-21, a sum of k of them in steps of 2^-31 of the largest, a scale and a product
+        assert (np.abs(got - want) <= (2.0 ** -20 + k * 2.0 ** -32) * want).all()
