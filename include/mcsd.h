@@ -517,6 +517,15 @@ int mcsd_tree_attention_latent(const void* q, const void* cache, const void* tre
                                int L_max, float softmax_scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Self-test of the joins in mcsd_tree_attention_latent (the paper has no counterpart).  On the tensor cores a long item is cut
+ * into pieces, and a pair of thread blocks that needs the others' pieces waits for them 2^21 cycles at most; then it leaves its share
+ * of the result to the pair whose piece comes last.  This sets how long the calls that follow wait, of all threads of the process:
+ * 0 .. 2^21 cycles, or the default with a negative number.  Results are the same, to the bit, whatever it is.  Host only.
+ * Errors: MCSD_ERR_BAD_SHAPE (beyond 2^21).
+ */
+int mcsd_selftest_latent_patience(long long cycles);
+
+/*
  * mcsd_commit_kv for latent caches (Fig. 1 step 6): the rows of the winning root and of the accepted nodes are copied to cache
  * rows seq_lens[b], seq_lens[b] + 1, ... of every layer, then seq_lens[b] grows by 1 + accept_len[b].  Rows that would fall
  * beyond L_max are dropped and the length saturates at L_max.

@@ -30,7 +30,7 @@ _EXPORTS = (
     "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
     "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
     "mcsd_latent_rows", "mcsd_tree_attention_latent_workspace_bytes", "mcsd_tree_attention_latent", "mcsd_commit_latent",
-    "mcsd_sample_candidates",
+    "mcsd_sample_candidates", "mcsd_selftest_latent_patience",
 )
 
 
@@ -116,6 +116,8 @@ def _load() -> ctypes.CDLL:
     lib.mcsd_tree_attention_latent_workspace_bytes.argtypes = [c_int] * 7
     lib.mcsd_tree_attention_latent.restype = c_int
     lib.mcsd_tree_attention_latent.argtypes = [c_void_p] * 7 + [c_int] * 7 + [c_float, c_int, c_void_p, c_size_t, c_void_p]
+    lib.mcsd_selftest_latent_patience.restype = c_int
+    lib.mcsd_selftest_latent_patience.argtypes = [ctypes.c_longlong]
     lib.mcsd_commit_latent.restype = c_int
     lib.mcsd_commit_latent.argtypes = [c_void_p] * 2 + [c_int] + [c_void_p] * 4 + [c_int] * 6 + [c_void_p]
     lib.mcsd_sample_candidates.restype = c_int
@@ -744,6 +746,11 @@ def mcsd_tree_attention_latent(q, cache, tree, seq_lens, n_active, mask: TreeMas
                     softmax_scale, code, _same(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel())
     _check(st, "mcsd_tree_attention_latent")
     return out
+
+
+def mcsd_selftest_latent_patience(cycles: int = -1) -> None:
+    """Sets how long pairs of thread blocks wait for one another's pieces in latent tree attention (see mcsd.h); -1: the default."""
+    _check(lib.mcsd_selftest_latent_patience(int(cycles)), "mcsd_selftest_latent_patience")
 
 
 def mcsd_commit_latent(cache_ptrs, tree_ptrs, seq_lens, verify_out, mask: TreeMask, B: int, width: int, L_max: int,

@@ -40,3 +40,7 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
         return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
 }
+
+extern "C" int mcsd_selftest_latent_patience(long long cycles) {
+    return mcsd::latent_tc_set_patience(cycles) ? MCSD_OK : MCSD_ERR_BAD_SHAPE;
+}

@@ -46,6 +46,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 
 #include "attention_tc_common.cuh"
@@ -76,6 +77,7 @@ struct LtParams {
     float2* part_ml;                                 // [2 * pairs][128]  reference (log2), sum
     int* counters;                                   // [2 * pairs][kCountersPerBlock] of the item that a block starts
     WorkspaceHeader* header;
+    long long patience;                              // cycles that a pair waits for pieces of others
 };
 struct LtMaps {
     CUtensorMap m[8];                                // boxes of 16, 32, 64, 128 rows: cache, then tree
@@ -306,9 +308,9 @@ __device__ __forceinline__ float2 lds8(uint32_t at) {
 }
 // Waits (one thread) until `count` pieces are in or patience runs out; then this pair is counted as gone, unless they came in
 // just before.  Returns whether they are in.  `bit` of `word` goes before the count: who sees the count finds it.
-__device__ __noinline__ bool lt_await(LtSmall* sm, int* counter, int count, bool ok, int* word, int bit) {
+__device__ __noinline__ bool lt_await(LtSmall* sm, long long patience, int* counter, int count, bool ok, int* word, int bit) {
     const long long t0 = clock64();
-    while (ok && clock64() - t0 < kLtPatience && !*(volatile int*)&sm->abort_flag) {
+    while (ok && clock64() - t0 < patience && !*(volatile int*)&sm->abort_flag) {
         int seen;
         asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(counter) : "memory");
         if ((seen & (kLtGone - 1)) >= count) return true;
@@ -400,7 +402,7 @@ __device__ __noinline__ void lt_join_item(LtSmall* sm, const LtParams& p, uint32
         const bool last_in = (in & (kLtGone - 1)) == count - 1;
         const uint32_t bit = 1u << (own & 31);
         if (!last_in) {
-            const bool mine = lt_await(sm, counter, count, ok, counter + 1 + (own >> 5), (int)bit);
+            const bool mine = lt_await(sm, p.patience, counter, count, ok, counter + 1 + (own >> 5), (int)bit);
             for (int k = 0; k < kLtGoneWords; ++k) sm->shares[k] = mine && k == own >> 5 ? bit : 0;
         } else {
             __threadfence();
@@ -772,7 +774,7 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
             float own = 1.0f;
             int* counter = p.counters + (2 * first + rank) * kCountersPerBlock;
             if (finish && !whole) {
-                if (w == 0 && lane == 0) sm->all_in = lt_await(sm, counter, pieces - 1, ok, nullptr, 0);
+                if (w == 0 && lane == 0) sm->all_in = lt_await(sm, p.patience, counter, pieces - 1, ok, nullptr, 0);
                 softmax_sync();
                 finish = sm->all_in;                                            // or the last piece's pair joins them
             }
@@ -906,6 +908,12 @@ tree_attention_latent_kernel(const __grid_constant__ LtMaps maps, const __grid_c
 }
 
 // ------------------------------------------------------------------ host side
+static std::atomic<long long> lt_patience{kLtPatience};
+bool latent_tc_set_patience(long long cycles) {
+    if (cycles > kLtPatience) return false;
+    lt_patience.store(cycles < 0 ? kLtPatience : cycles, std::memory_order_relaxed);
+    return true;
+}
 typedef CUresult (*LtEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -978,6 +986,7 @@ int tree_attention_latent_tc(const LatentArgs& whole, AttentionWorkspace* worksp
     p.part_o = static_cast<float*>(scratch);
     p.part_ml = reinterpret_cast<float2*>(p.part_o + (size_t)2 * kLtMaxPairs * 128 * kLtRank);
     p.counters = workspace->counters;
+    p.patience = lt_patience.load(std::memory_order_relaxed);
     for (int b0 = 0; b0 < whole.B; b0 += kLtMaxBatch) {                         // tables of a launch hold 256 sequences
         LatentArgs& a = p.a;
         a = whole;

@@ -38,6 +38,7 @@ int tree_attention_latent_few(const LatentArgs& a, int splits, WorkspaceHeader* 
 // tcgen05 kernel: bf16, rank 512, rotated part 64, tensors on 16-byte boundaries
 bool latent_tc_shape(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 size_t latent_tc_workspace_bytes();
+bool latent_tc_set_patience(long long cycles);       // negative: the default, which is the most
 int tree_attention_latent_tc(const LatentArgs& a, AttentionWorkspace* workspace, void* scratch, cudaStream_t stream);
 
 }  // namespace mcsd
