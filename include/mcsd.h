@@ -517,6 +517,16 @@ int mcsd_tree_attention_latent(const void* q, const void* cache, const void* tre
                                int L_max, float softmax_scale, int dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Which kernel mcsd_tree_attention_latent runs for a shape whose tensors lie on 16-byte boundaries (others take the CUDA cores):
+ * MCSD_PATH_TENSOR_CORE, MCSD_PATH_CUDA_CORE or MCSD_PATH_FEW_ROWS (warp-level matrix instructions), or a negative status for a shape
+ * that it rejects.  `splits` [host, or NULL] is set to the blocks that share the keys of a sequence (few rows: up to 16 are a cluster,
+ * more go through the workspace), or to the pieces that the CUDA-core kernel cuts L_max keys into (up to 8 are a cluster); 0 on the tensor cores.
+ * No launch; asks the current device how many clusters fit where few rows could be taken (MCSD_ERR_CUDA without one).
+ */
+#define MCSD_PATH_FEW_ROWS 2
+int mcsd_tree_attention_latent_path(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits);
+
+/*
  * Self-test of the joins in mcsd_tree_attention_latent (the paper has no counterpart).  On the tensor cores a long item is cut
  * into pieces, and a pair of thread blocks that needs the others' pieces waits for them 2^21 cycles at most; then it leaves its share
  * of the result to the pair whose piece comes last.  This sets how long the calls that follow wait, of all threads of the process:

@@ -13,7 +13,7 @@ _BINDING_NAMES = (
     "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "new_kv4_cache", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
     "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
     "mcsd_latent_rows", "mcsd_tree_attention_latent_workspace_bytes", "mcsd_tree_attention_latent", "mcsd_commit_latent",
-    "mcsd_sample_candidates", "mcsd_selftest_latent_patience",
+    "mcsd_sample_candidates", "mcsd_selftest_latent_patience", "mcsd_tree_attention_latent_path",
 )
 
 

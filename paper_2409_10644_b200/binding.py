@@ -30,7 +30,7 @@ _EXPORTS = (
     "mcsd_qk_norm_rope", "mcsd_kv4_cache_bytes", "mcsd_append_kv4", "mcsd_read_kv4", "mcsd_commit_kv4",
     "mcsd_tree_attention_kv4_workspace_bytes", "mcsd_tree_attention_kv4",
     "mcsd_latent_rows", "mcsd_tree_attention_latent_workspace_bytes", "mcsd_tree_attention_latent", "mcsd_commit_latent",
-    "mcsd_sample_candidates", "mcsd_selftest_latent_patience",
+    "mcsd_sample_candidates", "mcsd_selftest_latent_patience", "mcsd_tree_attention_latent_path",
 )
 
 
@@ -116,6 +116,8 @@ def _load() -> ctypes.CDLL:
     lib.mcsd_tree_attention_latent_workspace_bytes.argtypes = [c_int] * 7
     lib.mcsd_tree_attention_latent.restype = c_int
     lib.mcsd_tree_attention_latent.argtypes = [c_void_p] * 7 + [c_int] * 7 + [c_float, c_int, c_void_p, c_size_t, c_void_p]
+    lib.mcsd_tree_attention_latent_path.restype = c_int
+    lib.mcsd_tree_attention_latent_path.argtypes = [c_int] * 7 + [c_void_p]
     lib.mcsd_selftest_latent_patience.restype = c_int
     lib.mcsd_selftest_latent_patience.argtypes = [ctypes.c_longlong]
     lib.mcsd_commit_latent.restype = c_int
@@ -746,6 +748,16 @@ def mcsd_tree_attention_latent(q, cache, tree, seq_lens, n_active, mask: TreeMas
                     softmax_scale, code, _same(workspace, torch.uint8, workspace.shape, dev, "workspace"), workspace.numel())
     _check(st, "mcsd_tree_attention_latent")
     return out
+
+
+def mcsd_tree_attention_latent_path(B, H, N, rank, rot, L_max, dtype_code):
+    """(kernel, splits) of latent tree attention for this shape on the current device (see mcsd.h): kernel 0 CUDA cores, 1 tensor
+    cores, 2 few rows; raises on bad shapes."""
+    splits = ctypes.c_int(0)
+    path = int(lib.mcsd_tree_attention_latent_path(B, H, N, rank, rot, L_max, dtype_code, ctypes.byref(splits)))
+    if path < 0:
+        _check(path, "mcsd_tree_attention_latent_path")
+    return path, splits.value
 
 
 def mcsd_selftest_latent_patience(cycles: int = -1) -> None:

@@ -11,6 +11,28 @@ static int check_latent(int B, int H, int N, int rank, int rot, int L_max, int d
     return mcsd::latent_widths_ok(rank, rot) ? MCSD_OK : MCSD_ERR_BAD_SHAPE;
 }
 
+// The kernel of a call, or a status; *splits: blocks a sequence of the one for few rows, pieces of the keys of the one on the CUDA cores.
+static int choose(int B, int H, int N, int rank, int rot, int L_max, int dtype, bool aligned, int* splits) {
+    *splits = 0;
+    if (aligned) {
+        const int st = mcsd::latent_few_splits(B, H, N, rank, rot, L_max, dtype, splits);
+        if (st != MCSD_OK) return st;
+        if (*splits > 0) return MCSD_PATH_FEW_ROWS;
+        if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype)) return MCSD_PATH_TENSOR_CORE;
+    }
+    *splits = mcsd::latent_simt_splits(B, H, N, L_max);
+    return MCSD_PATH_CUDA_CORE;
+}
+
+extern "C" int mcsd_tree_attention_latent_path(int B, int H, int N, int rank, int rot, int L_max, int dtype, int* splits) {
+    const int st = check_latent(B, H, N, rank, rot, L_max, dtype);
+    if (st != MCSD_OK) return st;
+    int s = 0;
+    const int path = choose(B, H, N, rank, rot, L_max, dtype, true, &s);
+    if (splits) *splits = s;
+    return path;
+}
+
 extern "C" size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype) {
     if (check_latent(B, H, N, rank, rot, L_max, dtype) != MCSD_OK) return 0;
     size_t scratch = mcsd::latent_simt_workspace_bytes(B, H, N, rank, L_max);      // bf16 tensors off a 16-byte boundary
@@ -32,12 +54,11 @@ extern "C" int mcsd_tree_attention_latent(const void* q, const void* cache, cons
     const mcsd::LatentArgs a{q, cache, tree, out, seq_lens, n_active, anc, words, B, H, N, rank, rot, L_max, softmax_scale, dtype};
     auto* ws = static_cast<mcsd::AttentionWorkspace*>(workspace);
     const bool aligned = aligned16(q) && aligned16(cache) && aligned16(tree) && aligned16(out);
-    int few = 0;
-    const int fs = aligned ? mcsd::latent_few_splits(B, H, N, rank, rot, L_max, dtype, &few) : MCSD_OK;
-    if (fs != MCSD_OK) return fs;
-    if (few > 0) return mcsd::tree_attention_latent_few(a, few, &ws->header, ws + 1, static_cast<cudaStream_t>(stream));
-    if (mcsd::latent_tc_shape(B, H, N, rank, rot, L_max, dtype) && aligned)
-        return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
+    int splits = 0;
+    const int path = choose(B, H, N, rank, rot, L_max, dtype, aligned, &splits);
+    if (path < 0) return path;
+    if (path == MCSD_PATH_FEW_ROWS) return mcsd::tree_attention_latent_few(a, splits, &ws->header, ws + 1, static_cast<cudaStream_t>(stream));
+    if (path == MCSD_PATH_TENSOR_CORE) return mcsd::tree_attention_latent_tc(a, ws, ws + 1, static_cast<cudaStream_t>(stream));
     return mcsd::tree_attention_latent_simt(a, ws + 1, static_cast<cudaStream_t>(stream));
 }
 

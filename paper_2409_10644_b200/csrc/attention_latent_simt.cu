@@ -280,9 +280,12 @@ static int split_of(int B, int H, int N, int L_max, int* row_blocks, int* keys_p
     return (int)((tiles + per - 1) / per);
 }
 
-size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max) {
+int latent_simt_splits(int B, int H, int N, int L_max) {
     int rb, ks;
-    const int splits = split_of(B, H, N, L_max, &rb, &ks);
+    return split_of(B, H, N, L_max, &rb, &ks);
+}
+size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max) {
+    const int splits = latent_simt_splits(B, H, N, L_max);
     return splits > kLatentCluster ? (size_t)splits * B * H * N * (rank + 2) * sizeof(float) : 0;
 }
 

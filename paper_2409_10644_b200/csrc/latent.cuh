@@ -27,6 +27,7 @@ struct LatentArgs {
 };
 
 // CUDA-core kernel: fp32, and bf16 shapes or alignments that the tensor-core kernel does not take
+int latent_simt_splits(int B, int H, int N, int L_max);
 size_t latent_simt_workspace_bytes(int B, int H, int N, int rank, int L_max);
 int tree_attention_latent_simt(const LatentArgs& a, void* scratch, cudaStream_t stream);
 

@@ -137,3 +137,83 @@ def test_pieces_that_are_not_waited_for_next_to_another_stream(m):  # noqa: F811
     assert [m.mcsd_workspace_status(ws) for ws in spaces] == [0, 0] and not any(ws[COUNTERS].any() for ws in spaces)
     for j, out in outs:
         assert torch.equal(out, want[j])
+
+
+# ---------------------------------------------------------------------------------------------- kernels, lengths, workspaces
+
+def test_path_refusals_and_shapes_that_need_no_device(m):  # noqa: F811
+    path = m.lib.mcsd_tree_attention_latent_path
+    assert path(0, 4, 15, 512, 64, 100, 0, None) == -2
+    assert path(1, 4, 193, 512, 64, 100, 0, None) == -2
+    assert path(1, 4, 15, 500, 64, 100, 0, None) == -2
+    assert path(1, 4, 15, 512, 64, -1, 0, None) == -2
+    assert path(1, 4, 15, 512, 64, 100, 2, None) == -4
+    assert m.mcsd_tree_attention_latent_path(1, 4, 15, 512, 64, 100, m.MCSD_F32) == (0, 4)       # 115 keys: four tiles of 32
+    assert m.mcsd_tree_attention_latent_path(2, 32, 45, 512, 64, 4096, m.MCSD_BF16) == (1, 0)
+    assert m.mcsd_tree_attention_latent_path(1, 4, 15, 256, 64, 100, m.MCSD_BF16)[0] == 0
+    with pytest.raises(m.McsdError):
+        m.mcsd_tree_attention_latent_path(1, 0, 15, 512, 64, 100, m.MCSD_BF16)
+
+
+# dtype, B, H, rank, rot, tree, rows of the cache, lengths, kernel (0 CUDA cores, 1 tensor cores, 2 few rows), least and most splits
+KERNELS = {
+    "few_small": ("bf16", 100, 16, 512, 64, "token", 200, [(31 * i) % 201 for i in range(100)], 2, 1, 2),
+    "few_cluster": ("bf16", 1, 16, 512, 64, "token", 1000, [1000], 2, 9, 16),
+    "few_no_cache": ("bf16", 2, 4, 512, 64, "token", 0, [0, 0], 2, 1, 16),
+    "few_memory": ("bf16", 1, 16, 512, 64, "token", 20000, [20000], 2, 17, 160),
+    "few_memory_short": ("bf16", 1, 16, 512, 64, "token", 131072, [500], 2, 17, 160),
+    "few_memory_empty": ("bf16", 2, 8, 512, 64, "token", 131072, [0, 1], 2, 17, 160),
+    "tensor": ("bf16", 2, 32, 512, 64, "static", 1500, [1500, 200], 1, 0, 0),
+    "tensor_short": ("bf16", 2, 32, 512, 64, "static", 65536, [300, 0], 1, 0, 0),
+    "tensor_two_launches": ("bf16", 300, 20, 512, 64, "token", 270, [(83 * i) % 271 for i in range(300)], 1, 0, 0),
+    "cuda_cluster": ("f32", 2, 3, 128, 32, "binary", 131, [131, 30], 0, 2, 8),
+    "cuda_memory": ("f32", 1, 2, 512, 64, "token", 3000, [3000], 0, 9, 296),
+    "cuda_memory_short": ("f32", 1, 2, 128, 32, "token", 131072, [500], 0, 9, 296),
+    "cuda_memory_bf16": ("bf16", 1, 4, 256, 64, "binary", 131072, [33], 0, 9, 296),
+    "cuda_memory_empty": ("f32", 2, 2, 32, 16, "binary", 70000, [0, 70000], 0, 9, 296),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(KERNELS))
+def test_kernels_by_name_and_workspaces_to_the_byte(m, name):  # noqa: F811
+    """Each way that the keys are divided, lengths far below the cache's among them, in a workspace of the size that is asked for,
+    whose surroundings stay as they were."""
+    dtype, B, H, rank, rot, tree, L_max, lens, kernel, least, most = KERNELS[name]
+    parent = parent_array(*TREES[tree])
+    code = m.MCSD_BF16 if dtype == "bf16" else m.MCSD_F32
+    shape = (B, H, len(parent), rank, rot, L_max, code)
+    path, splits = m.mcsd_tree_attention_latent_path(*shape)
+    assert path == kernel and least <= splits <= most, (path, splits)
+    q, cache, rows = _problem(100 + B + L_max, dtype, B, H, rank, rot, parent, [max(L_max, 1)])
+    cache = cache[:, :L_max]
+    for b, L in enumerate(lens):
+        cache[b, L:] = NAN
+    tm, need = m.mcsd_build_mask(parent), m.mcsd_tree_attention_latent_workspace_bytes(*shape)
+    space = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    ws = space[:need]
+    ws.zero_()
+    out = _attend(m, q, cache, rows, lens, None, tm, 0.07, rank, ws)
+    _compare(out, q, cache, rows, lens, None, orc.dense_mask(parent), 0.07, rank, None if B * H <= 32 else [0, H - 1])
+    assert (space[need:] == 0xA5).all() and not ws[COUNTERS].any()
+    space[256 + 160 * 16:need] = 0xFF                                  # scratch may hold anything between launches
+    assert torch.equal(_attend(m, q, cache, rows, lens, None, tm, 0.07, rank, ws), out)
+    assert (space[need:] == 0xA5).all()
+
+
+@pytest.mark.gpu
+def test_every_number_of_blocks_that_few_rows_are_divided_among(m):  # noqa: F811
+    """Batches from one sequence up to more than there are multiprocessors: clusters small and large, with and without keys for all."""
+    tm, L_max, seen = m.mcsd_build_mask([-1]), 700, {}
+    for B in range(1, 301):
+        path, splits = m.mcsd_tree_attention_latent_path(B, 3, 1, 512, 64, L_max, m.MCSD_BF16)
+        if path == 2:
+            seen.setdefault(splits, B)
+    assert {1, 2, 3, 4, 16} <= set(seen) and any(5 <= s <= 8 for s in seen) and any(9 <= s <= 15 for s in seen), seen
+    for splits, B in seen.items():
+        lens = [(149 * i + 11 * splits) % (L_max + 1) for i in range(B)]
+        q, cache, rows = _problem(200 + splits, "bf16", B, 3, 512, 64, [-1], [L_max])
+        for b, L in enumerate(lens):
+            cache[b, L:] = NAN
+        out = _attend(m, q, cache, rows, lens, None, tm, 0.07, 512)
+        _compare(out, q, cache, rows, lens, None, np.ones((1, 1), bool), 0.07, 512, [0, 2])
