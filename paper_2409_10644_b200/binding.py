@@ -688,6 +688,8 @@ def mcsd_latent_rows(latent_in, q_in, seq_lens, freqs, rows=None, q=None, row_st
     its input, may be None.  ``freqs``: float64 [rot / 2] or None when rot is 0.  ``row_start``: int32 [B], row of token 0."""
     if rows is None and q is None:
         raise ValueError("rows or q must be given")
+    if rows is not None and latent_in is None or q is not None and q_in is None:
+        raise ValueError("rows are made from latent_in, q from q_in: both must be given")
     ref = rows if rows is not None else q
     dt, dev = ref.dtype, ref.get_device()
     code = _dtype_code(ref)

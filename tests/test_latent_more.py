@@ -217,3 +217,15 @@ def test_every_number_of_blocks_that_few_rows_are_divided_among(m):  # noqa: F81
             cache[b, L:] = NAN
         out = _attend(m, q, cache, rows, lens, None, tm, 0.07, 512)
         _compare(out, q, cache, rows, lens, None, np.ones((1, 1), bool), 0.07, 512, [0, 2])
+
+
+def test_an_output_without_its_input_is_refused(m):  # noqa: F811
+    rows, q, lens = torch.zeros(1, 3, 96), torch.zeros(1, 2, 3, 96), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="latent_in"):
+        m.mcsd_latent_rows(None, None, lens, None, rows=rows)
+    with pytest.raises(ValueError, match="q_in"):
+        m.mcsd_latent_rows(None, None, lens, None, q=q)
+    with pytest.raises(ValueError, match="q_in"):
+        m.mcsd_latent_rows(rows, None, lens, None, rows=rows.clone(), q=q)
+    with pytest.raises(ValueError, match="latent_in"):
+        m.mcsd_latent_rows(None, q[..., :32], lens, torch.zeros(16, dtype=torch.float64), rows=rows, q=q)
