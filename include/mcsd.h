@@ -508,7 +508,9 @@ int mcsd_latent_rows(const void* latent_in, const void* q_in, const int64_t* str
  *               workspace of the other attention calls; calls that may overlap on the device need distinct ones
  *
  * One launch on `stream` (one for every 256 sequences), two where the pieces of few rows or of the CUDA cores' kernel are too many
- * for a cluster.  Equal inputs give equal outputs, to the bit.  Errors: as mcsd_tree_attention.
+ * for a cluster.  Equal inputs give equal outputs, to the bit.  Lengths are known on the device alone, so that the kernel is chosen by
+ * L_max; the CUDA cores' kernel also cuts the keys by it, and sequences far shorter than L_max then take longer (fp32, one token of 16
+ * heads over 500 rows: 27 us in a cache of 500 or 4000, 66 of 32768, 171 of 131072).  Errors: as mcsd_tree_attention.
  */
 size_t mcsd_tree_attention_latent_workspace_bytes(int B, int H, int N, int rank, int rot, int L_max, int dtype);
 
@@ -564,14 +566,17 @@ int mcsd_commit_latent(void* const* cache_layers, const void* const* tree_layers
  * temperature <= 0 (or NaN) keeps the largest logit alone, the lowest id among equal ones.  Logits that are NaN or -infinity
  * are never kept; a row that holds nothing else gives tokens of -1 and probabilities of 0.
  *
- *   logits       [dev] dtype, row r at r * row_stride elements, V each (MCSD_F32, or MCSD_BF16 widened exactly)
+ *   logits       [dev] dtype, row r at r * row_stride elements (row_stride >= V), V each (MCSD_F32, or MCSD_BF16 widened exactly)
  *   temperature, top_p, min_p  [dev] float[rows], top_k  [dev] int32[rows]: a value a row; NULL = 1, or that filter off
  *   u            [dev] float[rows][K] uniforms in [0, 1);   tokens  [dev] int32[rows][K] out, or NULL (u is then not read)
  *   probs        [dev] float[rows][V] out, or NULL;  not both NULL;  outputs must not overlap the logits
  *   V            1 .. 262144;  K  1 .. 1024 (any that is not negative, when tokens is NULL);  rows  1 .. 2^24
  *
  * Weights are fp32 and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of
- * sums: equal inputs give equal outputs, to the bit.  One launch on `stream`, no workspace.
+ * sums: equal inputs give equal outputs, to the bit.  A kept token whose weight is 2^-32 of the largest or less therefore has its
+ * probability in `probs` and is never drawn; all such tokens of a row together have at most V * 2^-32 of the mass, and by so much
+ * can the distribution of `tokens` differ from `probs`.  (A min_p above 2^-32 keeps none of them.)
+ * One launch on `stream`, no workspace.
  * Errors: MCSD_ERR_NULL, MCSD_ERR_BAD_SHAPE, MCSD_ERR_BAD_DTYPE, MCSD_ERR_CUDA.
  */
 int mcsd_sample_candidates(const void* logits, long long row_stride, int dtype, int rows, int V, const float* temperature,

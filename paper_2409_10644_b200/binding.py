@@ -786,7 +786,7 @@ def mcsd_commit_latent(cache_ptrs, tree_ptrs, seq_lens, verify_out, mask: TreeMa
 def mcsd_sample_candidates(logits, u=None, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, tokens=None):
     """Draws from filtered next-token logits, and the probabilities they are drawn from (see mcsd.h).
 
-    ``logits`` [rows][V], rows any stride apart; ``u`` float32 [rows][K] uniforms, or None for no draws.  ``temperature``,
+    ``logits`` [rows][V], rows V elements apart or more; ``u`` float32 [rows][K] uniforms, or None for no draws.  ``temperature``,
     ``top_p``, ``min_p`` float32 [rows] and ``top_k`` int32 [rows] on the device, or None.  ``probs`` float32 [rows][V] to write
     into, True for a new tensor, None for none; ``tokens`` int32 [rows][K] to write into.  Returns those of (tokens, probs)
     that there are, as a tuple."""

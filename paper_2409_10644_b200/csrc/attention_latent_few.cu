@@ -7,8 +7,10 @@
 // are there and how short the way from the last ones to the result is.  A block takes all 16 rows and a range of keys, 64 at a
 // time, two tiles in shared memory: one is used, one on its way.  Queries stay in registers.  Scores: a warp has eight keys over
 // the whole row, in four independent sums; products with the values: 64 of the 512 channels.  The maximum of a tile and its
-// weights pass through shared memory, two meetings of the block a tile.  The ranges of a sequence are a cluster, which joins them
-// through shared memory, or, where a sequence is long enough for more than 16, go through memory to a second kernel.
+// weights pass through shared memory: three meetings of the block a tile (the tile is there, its maxima are, its weights are).  The
+// ranges of a sequence are a cluster, which joins them through shared memory, or, where a sequence is long enough for more than 16, go
+// through memory to a second kernel.  Weights are rounded to bf16, the type of the values that they multiply (half a step, 2^-8 of
+// each); their sum is taken before that, in fp32.
 //
 // What bounds it: the chain of a tile (scores, maximum, weights, products: 1.6 us with two warps a scheduler, two and a half times
 // what its loads take), so that it is taken where a block has few tiles, or where memory is the bound.  Rows come by bulk copies,

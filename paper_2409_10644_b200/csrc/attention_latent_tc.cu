@@ -20,6 +20,10 @@
 // before it (or starts before the first row, where TMA gives zeros) and masks what it has no claim to, so that no row behind a
 // sequence's end ever meets a product.
 //
+// Weights are rounded to bf16, since both operands of a product are of one type and the values are bf16: half a step, 2^-8 of each.
+// Their sum is taken before that, in fp32.  Against 64 bits the outputs of 45-node trees are off by 2.0e-3 of their size, where one
+// rounding of exact outputs leaves 1.7e-3.
+//
 // The launch's tiles are numbered (sequence, row block, tile) and cut into equal ranges, one a pair; where a cut falls
 // inside an item, the pieces write unnormalised rows and count themselves in.  An item of two or three pieces is joined by the
 // pair that starts it, from tensor memory: the others wrote theirs early, as the first of their ranges (with three instead of
@@ -29,7 +33,8 @@
 //
 // All blocks usually run at a time, one a multiprocessor; where others hold multiprocessors (a kernel of another stream), a pair
 // must not wait for one that cannot start before it leaves.  So it waits for a millisecond at most, then notes that it is gone,
-// and the pair that brings the last piece joins the shares of those that are: no result depends on which blocks run together.
+// and the pair that brings the last piece joins the shares of those that are: no result depends on which blocks run together.  (How
+// long it waits is a parameter of the launch, which tests set to nothing and to a few thousand cycles.)
 //
 // What bounds it.  Many rows: the tensor cores; 128 heads of a 74-node tree over 32768 keys run at 1.59 PFLOP/s, the rate of a
 // plain matrix product on this card.  A tile takes 3.3 us, an item 4 more for its last products and its output, which nothing

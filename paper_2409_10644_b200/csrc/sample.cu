@@ -8,7 +8,8 @@
 // Weights are summed as whole numbers of 2^-31, so that a sum does not depend on its order: filters, draws and
 // probabilities are the same whatever the number of blocks, and from run to run.  A rounding to 2^-31 is half a step, and the
 // largest weight is 1: a sum over V tokens is off by at most V 2^-32 of it (3e-5 for 131072 tokens whose weights all round
-// alike, 2e-8 where they do not).
+// alike, 2e-8 where they do not).  A kept token of half a step or less, 2^-32 of the largest, counts as nothing in a sum: it has
+// its probability and is never drawn.  All such tokens of a row together have at most V 2^-32 (6e-5 for 262144).
 //
 // A row is read from memory once; what looks at it again finds it in L2, so that shared memory holds only what was found, and two
 // blocks share a multiprocessor: one row's chain of short steps runs under the other's.  (With the row in shared memory and one
@@ -159,9 +160,9 @@ __device__ __forceinline__ uint32_t fixed31(float w) {
     return (uint32_t)(__float_as_int(t) - 0x4B400000) * 2048u + (uint32_t)(__float_as_int(t2) - 0x4B400000);
 }
 // The weight as filters add it up.  Small ones are added by the hundred of thousands while the row is read: an approximate
-// exponential (within 3e-6: the rounded exponent), in steps of 2^-31 by adding it to 1.5 * 2^23 (below 2^21.5 they stand in the
-// last places).  Wherever a token is
-// met its weight is the same.
+// exponential, in steps of 2^-31 by adding it to 1.5 * 2^23 (below 2^21.5 they stand in the last places).  Its exponent is
+// rounded three times (the difference, log2(e) / T and their product, 2^-24 each), which makes 3 * 2^-24 * ln 2 * 32 = 4e-6 where
+// the weight is 2^-32 and 1.2e-6 where it is 2^-9.5, and the instruction adds 2^-22.  Wherever a token is met its weight is the same.
 constexpr float kSmall = 9.5f;
 __device__ __forceinline__ uint32_t small31(float e) {                        // 2^e
     float w;
