@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) sample_kernel(const __grid_
     r.top = top;
     r.c_hi = sh->c_hi; r.c_lo = sh->c_lo; r.bin_scale = sh->bin_scale;
     int k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-    if (k >= live) k = 0;                                // off
+    if (k < 0 || k >= live) k = 0;                       // off
     const float tp = greedy || !a.top_p ? 1.0f : a.top_p[row], mp = greedy || !a.min_p ? 0.0f : a.min_p[row];
     const double share = tp < 1.0f ? (double)fmaxf(tp, 0.0f) : -1.0;
     float* dst = a.probs ? a.probs + row * a.V + first : nullptr;

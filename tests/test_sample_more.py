@@ -91,3 +91,18 @@ def test_a_cut_among_weights_that_are_added_up_approximately(m, rows, V, top_p):
         c = np.cumsum(np.exp(l[order] - l.max()))
         tol = 2 * 4.5e-6 + V * 2.0 ** -32 / c[-1]
         assert c[n - 1] >= (share - tol) * c[-1] and (c[n - 2] if n > 1 else 0.0) < (share + tol) * c[-1]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,V", [(1, 8), (3, 4093), (18, 32000), (160, 9000), (2, 131071)])
+@pytest.mark.parametrize("top_p", [None, -1.0, 0.1, 0.9])
+def test_a_negative_top_k_is_off(m, rows, V, top_p):  # noqa: F811
+    """With every other filter, as without one."""
+    g = torch.Generator("cuda").manual_seed(V)
+    x, u = 3 * torch.randn(rows, V, generator=g, device="cuda"), torch.rand(rows, 5, generator=g, device="cuda")
+    f32 = lambda v: None if v is None else torch.full((rows,), v, device="cuda")  # noqa: E731
+    for kw in (dict(), dict(min_p=f32(0.02)), dict(temperature=f32(1.3)), dict(temperature=f32(0.0))):
+        want = m.mcsd_sample_candidates(x, u, top_p=f32(top_p), probs=True, **kw)
+        for k in (-1, -3, -(1 << 31), 0):
+            got = m.mcsd_sample_candidates(x, u, top_k=torch.full((rows,), k, dtype=torch.int32, device="cuda"), top_p=f32(top_p), probs=True, **kw)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), k
