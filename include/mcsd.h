@@ -572,7 +572,8 @@ int mcsd_commit_latent(void* const* cache_layers, const void* const* tree_layers
  *   probs        [dev] float[rows][V] out, or NULL;  not both NULL;  outputs must not overlap the logits
  *   V            1 .. 262144;  K  1 .. 1024 (any that is not negative, when tokens is NULL);  rows  1 .. 2^24
  *
- * Weights are fp32 and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of
+ * Weights are fp32 (off by 2^-24 ln(1 / w) + 2^-22 of themselves at most, w relative to the largest; a little more where filters add up
+ * small ones) and are summed as whole numbers of 2^-31 of the largest, so that results do not depend on the order of
  * sums: equal inputs give equal outputs, to the bit.  A kept token whose weight is 2^-32 of the largest or less therefore has its
  * probability in `probs` and is never drawn; all such tokens of a row together have at most V * 2^-32 of the mass, and by so much
  * can the distribution of `tokens` differ from `probs`.  (A min_p above 2^-32 keeps none of them.)

@@ -144,7 +144,8 @@ struct Row : Scale {
 };
 
 __device__ __forceinline__ float below_top(const Scale& r, float l) { return l == r.top ? 0.0f : r.top - l; }
-// exp((l - top) / T) to about two units in the last place: the exponent's rounding is carried along
+// exp((l - top) / T).  The difference is rounded to 32 bits, which moves a weight by 2^-24 ln(1 / w) of itself (1.3e-6 at 2^-31, less
+// the heavier it is); behind it the exponent's rounding is carried along, so that about two units in the last place come on top.
 __device__ __forceinline__ float weight(const Scale& r, float l) {
     const float d = below_top(r, l), e = d * r.c_hi;
     if (!(e < 140.0f)) return 0.0f;
