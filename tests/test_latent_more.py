@@ -229,3 +229,31 @@ def test_an_output_without_its_input_is_refused(m):  # noqa: F811
         m.mcsd_latent_rows(rows, None, lens, None, rows=rows.clone(), q=q)
     with pytest.raises(ValueError, match="latent_in"):
         m.mcsd_latent_rows(None, q[..., :32], lens, torch.zeros(16, dtype=torch.float64), rows=rows, q=q)
+
+
+@pytest.mark.gpu
+def test_captured_where_pieces_go_through_memory(m):  # noqa: F811
+    """Two graphs that share a workspace, of few rows and of the CUDA cores' kernel, replayed in turn with lengths that change: the joining
+    kernel is launched early and has to find the pieces of its own replay."""
+    tm, ws, graphs, s = m.mcsd_build_mask([-1]), torch.zeros(64 << 20, dtype=torch.uint8, device="cuda"), [], torch.cuda.Stream()
+    for dtype, rank, rot, H, L_max in (("bf16", 512, 64, 16, 20000), ("f32", 128, 32, 2, 6000)):
+        path, splits = m.mcsd_tree_attention_latent_path(1, H, 1, rank, rot, L_max, m.MCSD_BF16 if dtype == "bf16" else m.MCSD_F32)
+        assert path == (2 if dtype == "bf16" else 0) and splits > 16
+        q, cache, rows = _problem(300 + H, dtype, 1, H, rank, rot, [-1], [L_max])
+        lens, out = _i32([L_max]), torch.zeros(1, H, 1, rank, dtype=q.dtype, device="cuda")
+        call = lambda: m.mcsd_tree_attention_latent(q, cache, rows, lens, None, tm, 0.07, out=out, workspace=ws)  # noqa: E731, B023
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=s):
+            for _ in range(3):
+                call()
+        graphs.append((graph, q, cache, rows, lens, out, rank))
+    for i, L in ((0, 20000), (1, 6000), (0, 1), (0, 777), (1, 0), (1, 5999), (0, 19999), (1, 64)):
+        graph, q, cache, rows, lens, out, rank = graphs[i]
+        lens.fill_(L)
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        _compare(out, q, cache, rows, [L], None, np.ones((1, 1), bool), 0.07, rank)
